@@ -9,7 +9,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspec.so")
-SOURCES = ["gemm.hip", "rowops.hip", "attention.hip", "hca.hip", "distill.hip", "select.hip", "noalloc.hip", "api.cpp"]
+SOURCES = ["gemm.hip", "rowops.hip", "attention.hip", "hca.hip", "distill.hip", "select.hip", "noalloc.hip", "gemm8.hip",
+           "attention8.hip", "rotary.hip", "api.cpp", "api_layer8.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed fp32 instructions stay off (device code only; the host pass ignores the feature)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -286,4 +286,47 @@ hipError_t launch_prefill_handoff(const void *feat, int row_bytes, const int *ro
 hipError_t launch_pending_rows(const AcceptResult *res, const int *n_committed, const int *pend_tok, int rows, int *token, int *src, int *pos, int *slot,
                                int *depth, int *base, hipStream_t st);
 
+// ---- gemm8.hip (8-bit matrices: layout in fp8.h) ------------------------------------------------
+struct Gemm8Args {
+  const unsigned char *x8, *w8;         // packed: [m, in] (set by launch_gemm8), [rows, in]
+  int m, in, rows;
+  void *y;  int64_t ldy;                // [m, rows] in the output type
+};
+hipError_t launch_pack_weight8(int dtype, const void *src, int rows, int in, void *dst, hipStream_t st);
+// x [m, in] in dtype, row stride ldx, is put into 8 bits in `scratch` (packed8_bytes of [m, in])
+hipError_t launch_gemm8(int dtype, const void *x, int64_t ldx, int out_dtype, Gemm8Args a, void *scratch, hipStream_t st);
+
+// ---- attention8.hip -------------------------------------------------------------------------------
+constexpr int kKv8Block = 64;           // tokens of a block
+// A block: per kv head its keys and its values, 64 * hd bytes each, in the order in which the matrix instructions take them (attention8.hip); then the
+// exponents + 127 of every head's keys and values, two bytes a head, padded to 256.
+__host__ __device__ inline size_t kv8_block_bytes(int hkv, int hd) { return (size_t)hkv * 2 * kKv8Block * hd + (2 * hkv + 255) / 256 * 256; }
+hipError_t launch_kv8_store(const void *k, const void *v, int64_t ld, int n_blocks, int hkv, int hd, void *cache8, int first_block, hipStream_t st);
+hipError_t launch_kv8_load(const void *cache8, int first_block, int n_blocks, int hkv, int hd, void *k, void *v, int64_t ld, hipStream_t st);
+struct Attn8Args {
+  const float *q;                       // [rows, hq * hd]
+  const unsigned char *cache8;  int n_blocks;
+  const void *kwin, *vwin;  int win_rows;   // bf16 [win_rows, hkv * hd]
+  int rows, hq, hkv, hd;
+  int base;                             // key position of the rows of depth 0
+  const int *depth, *anc;  int max_depth;   // as in AttnArgs
+  float scale;                          // 1 / sqrt(hd) in units of log2
+  float *part;                          // scratch
+  void *out;                            // bf16 [rows, hq * hd]
+};
+size_t attention8_scratch_floats(int rows, int hq, int hkv, int hd, int n_blocks, int win_rows);
+hipError_t launch_attention8(const Attn8Args &a, hipStream_t st);
+
+// ---- rotary.hip -----------------------------------------------------------------------------------
+struct RotaryPart { const void *x; void *out; int64_t ldx, hsx, ldo, hso; int heads, dtype, out_dtype, turn; };
+constexpr int kRotaryMaxPlanes = 128;
+struct RotaryArgs {
+  RotaryPart part[3];
+  int n_parts, hd, rows, rot, interleaved, adjoint, pos0;
+  const int *pos;
+  float mscale;
+  double turns[kRotaryMaxPlanes];       // of a plane per position
+};
+hipError_t launch_rotary(const RotaryArgs &a, hipStream_t st);
+
 }  // namespace spec
