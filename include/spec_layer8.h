@@ -79,7 +79,7 @@ int spec_k_kv8_load(const void *cache8, int32_t first_block, int32_t n_blocks, i
  * query in q[i] ([hq*hd], fp32), sits at position base + depth[i] (base >= n8) and
  * attends to positions 0 .. base + depth[i]: n8 <= p < base is window row p - n8,
  * p >= base is window row base - n8 + anc[i*16 + p - base] (anc NULL: p - n8, a
- * causal chain).  A position whose window row is negative or not below win_rows is left out; a row that sees nothing gets zeros.
+ * causal chain).  A position whose window row is negative or not below win_rows is left out; a row that sees nothing, or scores of -infinity only, gets zeros.
  * A row of negative depth is padding: its output is left as it was.  What a row
  * does not see does not touch its result, whatever is stored there (NaN included).
  * kwin, vwin: [win_rows, hkv*hd] bf16, win_rows >= 1 and 16-byte aligned, as are q, out and cache8 (256).

@@ -63,72 +63,555 @@ __global__ __launch_bounds__(256) void kv8_load_kernel(const unsigned char *cach
   }
 }
 
-// A workgroup owns one query of one row: 256 keys at a time, a thread's key each, one running maximum and sum; then a thread's dim over these keys.
-template <int HD>
-__global__ __launch_bounds__(256) void attention8_kernel(Attn8Args a) {
-  __shared__ float q[HD], w[256], sh[16], o_sh[256];
-  __shared__ int row_of[256];                                 // window row of a key, -1: in the blocks, -2: not seen
-  const int i = blockIdx.x, h = blockIdx.y, kvh = h / (a.hq / a.hkv), tid = threadIdx.x;
-  const int deep = min(a.depth[i], a.max_depth);
-  if (deep < 0) return;
-  const int n8 = a.n_blocks * kKv8Block, keys = a.base + deep + 1;
-  for (int d = tid; d < HD; d += 256) q[d] = a.q[(size_t)i * a.hq * HD + h * HD + d];
-  const size_t block_bytes = kv8_block_bytes(a.hkv, HD);
-  const unsigned char *exps = a.cache8 + (size_t)a.hkv * 2 * kKv8Block * HD + 2 * kvh;
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  constexpr int kShares = 256 / HD;                           // threads that share a dim
-  const int d = tid % HD, share = tid / HD;
-  for (int p0 = 0; p0 < keys; p0 += 256) {
-    __syncthreads();
-    const int p = p0 + tid;
-    int row = -2;
-    float s = -INFINITY;
-    if (p < keys) {
-      if (p < n8) row = -1;
-      else {
-        row = (p < a.base || !a.anc) ? p - n8 : a.base - n8 + a.anc[(size_t)i * kAncStride + p - a.base];
-        if (row < 0 || row >= a.win_rows) row = -2;
-      }
-      if (row != -2) {
-        s = 0.f;
-        if (row == -1) {
-          const unsigned char *block = a.cache8 + (size_t)(p / kKv8Block) * block_bytes;
-          const unsigned char *kc = block + (size_t)(2 * kvh) * kKv8Block * HD;
-          for (int e = 0; e < HD; e++) s = fmaf(q[e], code_to_f32(kc[key_at<HD>(p % kKv8Block, e)]), s);
-          s *= pow2((int)exps[(size_t)(p / kKv8Block) * block_bytes] - 127);
-        } else {
-          const bf16_t *kr = (const bf16_t *)a.kwin + (size_t)row * a.hkv * HD + kvh * HD;
-          for (int e = 0; e < HD; e++) s = fmaf(q[e], to_f32(kr[e]), s);
-        }
-        s *= a.scale;
-      }
-    }
-    row_of[tid] = row;
-    const float m_new = fmaxf(m, block_max(s, sh));           // (a NaN score: its weight is NaN below)
-    const float m_use = m_new == -INFINITY ? 0.f : m_new, turn = exp2_((m == -INFINITY ? m_use : m) - m_use);
-    const float weight = row == -2 ? 0.f : exp2_(s - m_use);
-    w[tid] = weight;
-    l = l * turn + block_sum(weight, sh);
+// ---- attention --------------------------------------------------------------------
+// The queries of a kv head are numbered row * G + head in group; a wavefront owns 32 of them as the columns of its products: lane (c = lane % 32, g = lane / 32)
+// holds query c, of a 32-key tile's scores the keys 8 i + 4 g + 0 .. 3 (i < 4), of the outputs the same dims of every 32.
+//
+// In the blocks the products are fp16: codes are exact there, a query row is divided by the power of two of its largest value and rounded once (2^-12), and
+// a weight is rounded once.  Weights are 2^(score - reference + kRefLift): up to 2^15 while the reference lags by kRefSlack, so that fp16 keeps its full precision for
+// weights down to 2^-29 of the largest.  A block's exponents go into the scores' factor and into the weights (relative to the largest of the
+// blocks so far, which the outputs are in units of); nothing is done per value for them.
+constexpr float kRefLift = 7.f;
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+__device__ __forceinline__ f32x16_t mul_f16(const u32x4_t &a, const u32x4_t &b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16_t mul_bf16(const u32x4_t &a, const u32x4_t &b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  typedef __attribute__((ext_vector_type(2))) float f2_t;
+  typedef __attribute__((ext_vector_type(2))) _Float16 h2_t;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2_t{lo, hi}, h2_t));   // to nearest even
+}
+// Sixteen codes as the fp16 operands of two products
+__device__ __forceinline__ void widen(const u32x4_t &w, u32x4_t &first, u32x4_t &second) {
+  first = u32x4_t{f16_of_codes<false>(w.x, 1.f), f16_of_codes<true>(w.x, 1.f), f16_of_codes<false>(w.y, 1.f), f16_of_codes<true>(w.y, 1.f)};
+  second = u32x4_t{f16_of_codes<false>(w.z, 1.f), f16_of_codes<true>(w.z, 1.f), f16_of_codes<false>(w.w, 1.f), f16_of_codes<true>(w.w, 1.f)};
+}
+
+// The work of a launch: parts 0 .. blocks - 1 are ranges of the cache's blocks, the others ranges of the window.
+struct Plan8 { int waves, query_blocks, block_parts, win_parts, win_part; };   // waves: of 32 queries each in a workgroup; 0: few queries
+__host__ __device__ inline int range_at(int n, int parts, int i) { return (int)((int64_t)n * i / parts); }
+
+// Running softmax of 32 queries (this lane's)
+template <int HD> struct Running {
+  f32x16_t o[HD / 32];
+  float m = -INFINITY, l = 0.f;                               // reference of the weights (lifted: m + kRefLift is the scores'), sum of this lane's weights
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) o[db][i] = 0.f;
+  }
+  __device__ __forceinline__ void turn_by(float t) {
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++) o[db] *= t;
+    l *= t;
+  }
+  // top: the largest score of this query's new keys.  The reference moves where it lags by more than kRefSlack.
+  __device__ __forceinline__ void raise(float top) {
+    const bool move = top - kRefLift > m + kRefSlack;          // (also the first keys; NaN moves nothing)
+    if (__builtin_amdgcn_ballot_w64(move) == 0) return;
+    const float m_new = move ? top - kRefLift : m;
+    turn_by(move ? exp2_(m - m_new) : 1.f);
     m = m_new;
-    o *= turn;
-    __syncthreads();
-    for (int t = share; t < 256 && p0 + t < keys; t += kShares) {
-      const int r = row_of[t], p2 = p0 + t;
-      if (r == -2) continue;
-      float v;
-      if (r == -1) {
-        const unsigned char *block = a.cache8 + (size_t)(p2 / kKv8Block) * block_bytes;
-        v = code_to_f32(block[(size_t)(2 * kvh + 1) * kKv8Block * HD + value_at<HD>(p2 % kKv8Block, d)]) *
-            pow2((int)exps[(size_t)(p2 / kKv8Block) * block_bytes + 1] - 127);
-      } else v = to_f32(((const bf16_t *)a.vwin)[(size_t)r * a.hkv * HD + kvh * HD + d]);
-      o = fmaf(w[t], v, o);
+  }
+};
+
+template <int HD> struct Query8 {
+  u32x4_t f[HD / 16];
+  float scale;                                                // of the scores, without a block's exponent
+};
+// Query `index` of the kv head (clamped by the caller); lane's dims: those of the keys' pieces, 32 u + 16 g + 0 .. 15
+template <int HD> __device__ __forceinline__ Query8<HD> load_query8(const float *q, int g, float scale) {
+  float x[HD / 2], amax = 0.f;
+#pragma unroll
+  for (int u = 0; u < HD / 32; u++) {
+    float v[16];
+    load16(q + 32 * u + 16 * g, v);
+#pragma unroll
+    for (int i = 0; i < 16; i++) { x[16 * u + i] = v[i]; amax = fmaxf(amax, finite_abs(v[i])); }
+  }
+  amax = max_halves(amax);
+  const int e = min(max((int)(__float_as_uint(amax) >> 23) - 127, -126), 126);
+  const float down = pow2(-e);
+  Query8<HD> r;
+#pragma unroll
+  for (int s = 0; s < HD / 16; s++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) r.f[s][i] = pack_f16x2(x[8 * s + 2 * i] * down, x[8 * s + 2 * i + 1] * down);
+  r.scale = scale * pow2(e);
+  return r;
+}
+
+// 64 keys of a block for 32 queries.  keys(kt, s), values(kt, db, a): the fp16 operands (s: 16 dims, a: 16 keys); exps: the block's exponents + 127 of keys and values;
+// top_exp: the largest value exponent so far, r.o is in units of 2^top_exp.
+template <int HD, typename K, typename V>
+__device__ __forceinline__ void block_step(Running<HD> &r, const Query8<HD> &q, uint32_t exps, int &top_exp, K keys, V values) {
+  f32x16_t s[2];
+#pragma unroll
+  for (int kt = 0; kt < 2; kt++) {
+#pragma unroll
+    for (int i = 0; i < 16; i++) s[kt][i] = 0.f;
+#pragma unroll
+    for (int t = 0; t < HD / 16; t++) s[kt] = mul_f16(keys(kt, t), q.f[t], s[kt]);
+  }
+  const int ek = (int)(exps & 0xFF) - 127, ev = (int)((exps >> 8) & 0xFF) - 127;
+  if (ev > top_exp) {
+    const float t = exp2_((float)(top_exp - ev));
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++) r.o[db] *= t;
+    top_exp = ev;
+  }
+  const float f = q.scale * pow2(ek);
+  float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+  for (int i = 1; i < 16; i++) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
+  r.raise(max_halves(top) * f);
+  const float minus = (float)(ev - top_exp) - r.m;             // (the reference of a query whose scores are all NaN stays -inf: its weights are NaN)
+  float sum = 0.f;
+#pragma unroll
+  for (int kt = 0; kt < 2; kt++) {
+#pragma unroll
+    for (int i = 0; i < 16; i++) { s[kt][i] = exp2_(fmaf(s[kt][i], f, minus)); sum += s[kt][i]; }
+#pragma unroll
+    for (int a = 0; a < 2; a++) {
+      u32x4_t p;
+#pragma unroll
+      for (int i = 0; i < 4; i++) p[i] = pack_f16x2(s[kt][8 * a + 2 * i], s[kt][8 * a + 2 * i + 1]);
+#pragma unroll
+      for (int db = 0; db < HD / 32; db++) r.o[db] = mul_f16(values(kt, db, a), p, r.o[db]);
     }
   }
-  o_sh[tid] = o;
+  r.l = fmaf(sum, pow2(min(top_exp - ev, 127)), r.l);
+}
+
+// ---- the window: a wavefront takes 32 of its rows at a time for its 32 queries ----
+// Queries and weights go through the bf16 products as two terms each (value and what its rounding left).  Values that are not finite are taken out of the products, where they
+// would reach every query, and added by hand to those that see them.
+template <int HD> struct QueryWin { u32x4_t hi[HD / 16], lo[HD / 16]; };
+template <int HD> __device__ __forceinline__ QueryWin<HD> load_query_win(const float *q, int g) {
+  QueryWin<HD> r;
+#pragma unroll
+  for (int s = 0; s < HD / 16; s++) {
+    const f32x4_t a = *(const f32x4_t *)(q + 16 * s + 8 * g), b = *(const f32x4_t *)(q + 16 * s + 8 * g + 4);
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const uint32_t h = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+      r.hi[s][i] = h;
+      r.lo[s][i] = pack_bf16x2(x[2 * i] - __uint_as_float(h << 16), x[2 * i + 1] - __uint_as_float(h & 0xFFFF0000u));
+    }
+  }
+  return r;
+}
+// What a query sees of the window: rows below `first`, and its path: rows path[0 .. deep] (anc), or first .. first + deep
+struct Sight { int deep, last; };                             // last: the highest row it sees
+__device__ __forceinline__ int path_row(const Attn8Args &a, int row, int d) {   // -1: outside the window
+  const int64_t r = (int64_t)a.base - a.n_blocks * kKv8Block + a.anc[(size_t)row * kAncStride + d];
+  return r >= 0 && r < a.win_rows ? (int)r : -1;
+}
+// Orders this wavefront's LDS accesses for the compiler (the hardware keeps their order)
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+__device__ __forceinline__ Sight sight_of(const Attn8Args &a, int row, bool any) {
+  Sight s{any ? min(a.depth[row], a.max_depth) : -1, -1};
+  if (s.deep < 0) return s;
+  const int first = a.base - a.n_blocks * kKv8Block;
+  if (!a.anc) s.last = first + s.deep;
+  else {
+    s.last = first - 1;
+    for (int d = 0; d <= s.deep; d++) s.last = max(s.last, path_row(a, row, d));
+  }
+  s.last = min(s.last, a.win_rows - 1);
+  return s;
+}
+
+template <int HD>
+__device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, const QueryWin<HD> &q, int kvh, int row, const Sight &see, int w0,
+                                            unsigned char *v_lds, uint32_t *count) {
+  const int lane = threadIdx.x & 63, c = lane & 31, g = lane >> 5;
+  const size_t ld = (size_t)a.hkv * HD;
+  const uint16_t *vw = (const uint16_t *)a.vwin + (size_t)kvh * HD;
+  wave_fence();                                               // (the tile before has been read)
+  // values: rows into the LDS, what is not finite as zero
+  uint32_t odd = 0;                                           // rows of the tile that hold such a value
+  constexpr int kPieces = HD / 8;                             // 16-byte pieces of a row
+#pragma unroll
+  for (int i = 0; i < kPieces / 2; i++) {
+    const int at = i * 64 + lane, vr = at / kPieces, piece = at % kPieces;
+    u32x4_t v = *(const u32x4_t *)(vw + (size_t)min(w0 + vr, a.win_rows - 1) * ld + piece * 8);
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const bool lo = (v[j] & 0x7F80u) == 0x7F80u, hi = (v[j] & 0x7F800000u) == 0x7F800000u;
+      v[j] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0xFFFFu : 0xFFFFFFFFu);
+      bad |= lo || hi;
+    }
+    *(u32x4_t *)(v_lds + value_piece<HD>(vr, piece)) = v;
+    uint64_t mask = __builtin_amdgcn_ballot_w64(bad);
+    while (mask) {                                            // (never, as a rule)
+      const int l = __builtin_ctzll(mask);
+      odd |= 1u << ((i * 64 + l) / kPieces);
+      mask &= mask - 1;
+    }
+  }
+  wave_fence();
+  const uint16_t *kr = (const uint16_t *)a.kwin + (size_t)min(w0 + c, a.win_rows - 1) * ld + (size_t)kvh * HD + 8 * g;
+  f32x16_t s;
+#pragma unroll
+  for (int i = 0; i < 16; i++) s[i] = 0.f;
+#pragma unroll
+  for (int t = 0; t < HD / 16; t++) {
+    const u32x4_t k = *(const u32x4_t *)(kr + 16 * t);
+    s = mul_bf16(k, q.hi[t], s);
+    s = mul_bf16(k, q.lo[t], s);
+  }
+  // how often the query sees each key
+  const int first = a.base - a.n_blocks * kKv8Block;
+  float n[16];
+  if (a.anc) {
+    uint32_t *mine = count + c * 8;
+    if (g == 0) *(u32x4_t *)mine = u32x4_t{0, 0, 0, 0};
+    else *(u32x4_t *)(mine + 4) = u32x4_t{0, 0, 0, 0};
+    wave_fence();
+    if (g == 0)
+      for (int d = 0; d <= see.deep; d++) {
+        const uint32_t w = (uint32_t)(path_row(a, row, d) - w0);
+        if (w < 32u) mine[w >> 2] += 1u << (8 * (w & 3));
+      }
+    wave_fence();
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const uint32_t w = mine[2 * i + g];
+#pragma unroll
+      for (int j = 0; j < 4; j++) n[4 * i + j] = (float)((w >> (8 * j)) & 0xFF);
+    }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 16; i++) {
+    const int w = w0 + 8 * (i >> 2) + 4 * g + (i & 3);
+    if (!a.anc) n[i] = w <= see.last ? 1.f : 0.f;
+    else n[i] += w < first && see.deep >= 0 ? 1.f : 0.f;
+    if (w >= a.win_rows) n[i] = 0.f;
+    s[i] = n[i] > 0.f ? s[i] * a.scale : -INFINITY;
+    top = fmaxf(top, s[i]);
+  }
+  r.raise(max_halves(top));
+  const float m = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+  for (int i = 0; i < 16; i++) {
+    s[i] = n[i] > 0.f ? n[i] * exp2_(s[i] - m) : 0.f;
+    r.l += s[i];
+  }
+#pragma unroll
+  for (int h = 0; h < 2; h++) {
+    u32x4_t hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const float x = s[8 * h + 2 * i], y = s[8 * h + 2 * i + 1];
+      hi[i] = pack_bf16x2(x, y);
+      lo[i] = pack_bf16x2(x - __uint_as_float(hi[i] << 16), y - __uint_as_float(hi[i] & 0xFFFF0000u));
+    }
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++) {
+      const u32x4_t v = value_fragment<HD>(v_lds, value_lane<HD>(lane), db, 16 * h);
+      r.o[db] = mul_bf16(v, hi, r.o[db]);
+      r.o[db] = mul_bf16(v, lo, r.o[db]);
+    }
+  }
+  while (odd) {
+    const int w = __builtin_ctz(odd);
+    odd &= odd - 1;
+    float p = 0.f, seen = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i++)
+      if (i == ((w >> 3) << 2 | (w & 3))) { p = s[i]; seen = n[i]; }
+    p = __shfl(p, ((w >> 2) & 1) * 32 + c);
+    seen = __shfl(seen, ((w >> 2) & 1) * 32 + c);
+    const uint16_t *vr = vw + (size_t)min(w0 + w, a.win_rows - 1) * ld;
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) {
+        const uint32_t b = vr[db * 32 + 8 * (i >> 2) + 4 * g + (i & 3)];
+        if (seen > 0.f && (b & 0x7F80u) == 0x7F80u) r.o[db][i] = fmaf(p, bf16_bits_to_f32(b), r.o[db][i]);
+      }
+  }
+}
+
+// A part's result of this lane's query: reference, sum and outputs, or, if the launch has one part, the query's result
+template <int HD> __device__ __forceinline__ size_t part_floats(const Attn8Args &a) { return (size_t)a.rows * a.hq * (HD + 2); }
+template <int HD>
+__device__ __forceinline__ void put_dims(const Attn8Args &a, size_t query, int part, int parts, int db, int g, const f32x16_t &o, float m, float l) {
+  if (parts == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t *out = (uint16_t *)a.out + query * HD + db * 32 + 4 * g;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      *(u32x2_t *)(out + 8 * i) = u32x2_t{pack_bf16x2(o[4 * i] * inv, o[4 * i + 1] * inv), pack_bf16x2(o[4 * i + 2] * inv, o[4 * i + 3] * inv)};
+    return;
+  }
+  float *p = a.part + part * part_floats<HD>(a);
+  float *po = p + (size_t)a.rows * a.hq * 2 + query * HD + db * 32 + 4 * g;
+#pragma unroll
+  for (int i = 0; i < 4; i++) *(f32x4_t *)(po + 8 * i) = f32x4_t{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+  if (db == 0 && g == 0) ((float2 *)p)[query] = make_float2(m, l);
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Which kv head, part and block of queries a workgroup has: ids 8 apart run on one XCD, and there the query blocks of a part follow each other (they read the same keys)
+struct Place8 { int kvh, part, qb; };
+__device__ __forceinline__ bool place_of(const Plan8 &p, int hkv, Place8 &at) {
+  const int parts = p.block_parts + p.win_parts, units = hkv * parts;
+  const int x = (int)blockIdx.x % 8, j = (int)blockIdx.x / 8;
+  const int unit = j / p.query_blocks * 8 + x;
+  at.qb = j % p.query_blocks;
+  if (unit >= units) return false;
+  at.kvh = unit / parts; at.part = unit % parts;
+  return true;
+}
+
+// Many queries: WAVES wavefronts of 32 queries each walk the part's keys together.  A block's codes are widened once, on their way into the LDS (two buffers; the
+// next block's are in registers meanwhile), in the order in which the products read them.
+template <int HD, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void attention8_wide_kernel(Attn8Args a, Plan8 plan) {
+  constexpr int kCodes = 2 * kKv8Block * HD, kUnits = kCodes / 16, kThreads = WAVES * 64, kEach = kUnits / kThreads;   // of 16 codes, per thread
+  static_assert(kEach * kThreads == kUnits, "whole units");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // 2 x 2 kCodes; the window: value rows and counts of each wavefront
+  Place8 at;
+  if (!place_of(plan, a.hkv, at)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, g = lane >> 5;
+  const int G = a.hq / a.hkv, index = (at.qb * WAVES + wave) * 32 + c, parts = plan.block_parts + plan.win_parts;
+  const bool real = index < a.rows * G;
+  const int row = real ? index / G : a.rows - 1;
+  const size_t query = (size_t)row * a.hq + at.kvh * G + (real ? index % G : 0);
+  const float *qp = a.q + query * HD;
+  Running<HD> r;
+  r.clear();
+  if (at.part < plan.block_parts) {
+    const int b0 = range_at(a.n_blocks, plan.block_parts, at.part), b1 = range_at(a.n_blocks, plan.block_parts, at.part + 1);
+    const size_t block_bytes = kv8_block_bytes(a.hkv, HD);
+    const unsigned char *base = a.cache8 + (size_t)at.kvh * kCodes + tid * 16;
+    const unsigned char *exps = a.cache8 + (size_t)a.hkv * kCodes + 2 * at.kvh;
+    const Query8<HD> q = load_query8<HD>(qp, g, a.scale);
+    u32x4_t next[kEach];
+    uint32_t next_exps;
+    auto fetch = [&](int b) {
+      const unsigned char *p = base + (size_t)b * block_bytes;
+#pragma unroll
+      for (int i = 0; i < kEach; i++) next[i] = *(const u32x4_t *)(p + i * kThreads * 16);
+      next_exps = *(const uint16_t *)(exps + (size_t)b * block_bytes);
+    };
+    auto put = [&](unsigned char *buf) {
+#pragma unroll
+      for (int i = 0; i < kEach; i++) {
+        u32x4_t x, y;
+        widen(next[i], x, y);
+        unsigned char *p = buf + ((i * kThreads + tid) >> 6) * 2048 + lane * 16;
+        *(u32x4_t *)p = x;
+        *(u32x4_t *)(p + 1024) = y;
+      }
+    };
+    int top_exp = -127;
+    fetch(b0);
+    put(lds);
+    uint32_t now_exps = __builtin_amdgcn_readfirstlane(next_exps);
+    __syncthreads();
+    for (int b = b0; b < b1; b++) {
+      const unsigned char *buf = lds + ((b - b0) & 1) * 2 * kCodes + lane * 16;
+      if (b + 1 < b1) fetch(b + 1);
+      block_step<HD>(r, q, now_exps, top_exp,
+                     [&](int kt, int s) { return *(const u32x4_t *)(buf + (kt * (HD / 16) + s) * 1024); },
+                     [&](int kt, int db, int h) { return *(const u32x4_t *)(buf + kCodes + (kt * (HD / 16) + 2 * db + h) * 1024); });
+      if (b + 1 < b1) {
+        put(lds + ((b + 1 - b0) & 1) * 2 * kCodes);
+        now_exps = __builtin_amdgcn_readfirstlane(next_exps);
+      }
+      __syncthreads();
+    }
+    const float up = exp2_((float)top_exp);
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
+  } else {
+    const int w_begin = (at.part - plan.block_parts) * plan.win_part, w_stop = min(w_begin + plan.win_part, a.win_rows);
+    const Sight see = sight_of(a, row, real);
+    const int last = __builtin_amdgcn_readfirstlane(wave_reduce(see.last, [](int x, int y) { return max(x, y); }));
+    unsigned char *mine = lds + wave * (64 * HD + 1024);
+    if (w_begin <= last) {
+      const QueryWin<HD> q = load_query_win<HD>(qp, g);
+      for (int w = w_begin; w < w_stop && w <= last; w += 32) window_step<HD>(a, r, q, at.kvh, row, see, w, mine, (uint32_t *)(mine + 64 * HD));
+    }
+  }
+  const float l = sum_halves(r.l);
+  if (!real || (parts == 1 && a.depth[row] < 0)) return;
+#pragma unroll
+  for (int db = 0; db < HD / 32; db++) put_dims<HD>(a, query, at.part, parts, db, g, r.o[db], r.m, l);
+}
+
+// Up to 32 queries: the four wavefronts share the part's keys, a block (or 32 rows of the window) each in turn, straight into registers, and are merged in the LDS.
+constexpr int kFewWaves = 4;
+template <int HD>
+__global__ __launch_bounds__(kFewWaves * 64) void attention8_few_kernel(Attn8Args a, Plan8 plan) {
+  constexpr int kCodes = 2 * kKv8Block * HD, kPieces = kCodes / 1024;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // outputs of each wavefront (or its value rows and counts), then references and sums
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, g = lane >> 5;
+  const int parts = plan.block_parts + plan.win_parts, kvh = blockIdx.x / parts, part = blockIdx.x % parts;
+  const int G = a.hq / a.hkv;
+  const bool real = c < a.rows * G;
+  const int row = real ? c / G : a.rows - 1;
+  const size_t query = (size_t)row * a.hq + kvh * G + (real ? c % G : 0);
+  const float *qp = a.q + query * HD;
+  Running<HD> r;
+  r.clear();
+  if (part < plan.block_parts) {
+    const int b0 = range_at(a.n_blocks, plan.block_parts, part) + wave, b1 = range_at(a.n_blocks, plan.block_parts, part + 1);
+    const size_t block_bytes = kv8_block_bytes(a.hkv, HD);
+    const unsigned char *base = a.cache8 + (size_t)kvh * kCodes + lane * 16;
+    const unsigned char *exps = a.cache8 + (size_t)a.hkv * kCodes + 2 * kvh;
+    u32x4_t next[kPieces], now[kPieces];
+    uint32_t next_exps = 0;
+    auto fetch = [&](int b) {
+      const unsigned char *p = base + (size_t)b * block_bytes;
+#pragma unroll
+      for (int i = 0; i < kPieces; i++) next[i] = *(const u32x4_t *)(p + i * 1024);
+      next_exps = *(const uint16_t *)(exps + (size_t)b * block_bytes);
+    };
+    if (b0 < b1) fetch(b0);
+    const Query8<HD> q = load_query8<HD>(qp, g, a.scale);
+    int top_exp = -127;
+    for (int b = b0; b < b1; b += kFewWaves) {
+#pragma unroll
+      for (int i = 0; i < kPieces; i++) now[i] = next[i];
+      const uint32_t now_exps = __builtin_amdgcn_readfirstlane(next_exps);
+      if (b + kFewWaves < b1) fetch(b + kFewWaves);
+      auto half = [&](const u32x4_t &w, int h) {
+        u32x4_t x, y;
+        widen(w, x, y);
+        return h ? y : x;
+      };
+      block_step<HD>(r, q, now_exps, top_exp, [&](int kt, int s) { return half(now[kt * (HD / 32) + s / 2], s & 1); },
+                     [&](int kt, int db, int h) { return half(now[kPieces / 2 + kt * (HD / 32) + db], h); });
+    }
+    const float up = exp2_((float)top_exp);
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
+  } else {
+    const int w_begin = (part - plan.block_parts) * plan.win_part, w_stop = min(w_begin + plan.win_part, a.win_rows);
+    const Sight see = sight_of(a, row, real);
+    const int last = __builtin_amdgcn_readfirstlane(wave_reduce(see.last, [](int x, int y) { return max(x, y); }));
+    unsigned char *mine = lds + wave * (64 * HD + 1024);
+    if (w_begin + 32 * wave <= last) {
+      const QueryWin<HD> q = load_query_win<HD>(qp, g);
+      for (int w = w_begin + 32 * wave; w < w_stop && w <= last; w += 32 * kFewWaves)
+        window_step<HD>(a, r, q, kvh, row, see, w, mine, (uint32_t *)(mine + 64 * HD));
+    }
+    __syncthreads();                                          // the value rows make place for the outputs
+  }
+  float *outs = (float *)lds;                                 // [wave][db][16][64]
+  float2 *stats = (float2 *)(lds + kFewWaves * HD * 128);     // [wave][32]
+#pragma unroll
+  for (int db = 0; db < HD / 32; db++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) outs[((wave * (HD / 32) + db) * 16 + i) * 64 + lane] = r.o[db][i];
+  const float own_l = sum_halves(r.l);
+  if (g == 0) stats[wave * 32 + c] = make_float2(r.m, own_l);
   __syncthreads();
-  if (tid >= HD) return;
-  for (int t = 1; t < kShares; t++) o += o_sh[t * HD + tid];
-  ((bf16_t *)a.out)[(size_t)i * a.hq * HD + h * HD + tid] = from_f32<bf16_t>(l == 0.f ? 0.f : o / l);
+  if (wave >= HD / 32 || !real || (parts == 1 && a.depth[row] < 0)) return;
+  RowMerge all;                                               // this wavefront joins the dims 32 wave .. + 31
+  f32x16_t o;
+#pragma unroll
+  for (int i = 0; i < 16; i++) o[i] = 0.f;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; w++) {
+    const float2 s = stats[w * 32 + c];
+    if (s.y == 0.f) continue;                                 // saw nothing
+    float weight;
+    const float turn = all.step(s.x, s.y, weight);
+#pragma unroll
+    for (int i = 0; i < 16; i++) o[i] = fmaf(outs[((w * (HD / 32) + wave) * 16 + i) * 64 + lane], weight, o[i] * turn);
+  }
+  put_dims<HD>(a, query, part, parts, wave, g, o, all.m, all.l);
+}
+
+// The parts of a query put together, in ascending order: HD / 4 threads for each query
+template <int HD>
+__global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a, int parts) {
+  constexpr int kThreads = HD / 4;
+  const size_t query = (size_t)blockIdx.x * (256 / kThreads) + threadIdx.x / kThreads;
+  const int d = threadIdx.x % kThreads * 4;
+  if (query >= (size_t)a.rows * a.hq || a.depth[query / a.hq] < 0) return;
+  RowMerge all;
+  f32x4_t o{0.f, 0.f, 0.f, 0.f};
+  const float *p = a.part;
+  for (int i = 0; i < parts; i++, p += part_floats<HD>(a)) {
+    const float2 s = ((const float2 *)p)[query];
+    const f32x4_t x = *(const f32x4_t *)(p + (size_t)a.rows * a.hq * 2 + query * HD + d);
+    if (s.y == 0.f) continue;
+    float weight;
+    const float turn = all.step(s.x, s.y, weight);
+#pragma unroll
+    for (int j = 0; j < 4; j++) o[j] = fmaf(x[j], weight, o[j] * turn);
+  }
+  const float inv = all.l == 0.f ? 0.f : 1.f / all.l;
+  *(u32x2_t *)((uint16_t *)a.out + query * HD + d) = u32x2_t{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+}
+
+Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
+  Plan8 p{};
+  const int64_t queries = (int64_t)rows * (hq / hkv);
+  p.waves = queries <= 32 ? 0 : queries <= 64 ? 2 : queries <= 128 ? 4 : 8;
+  const int of = p.waves ? 32 * p.waves : 32;
+  p.query_blocks = (int)((queries + of - 1) / of);
+  const int64_t units = (int64_t)hkv * p.query_blocks;
+  const int64_t want = 256, most = (n_blocks + (p.waves ? 0 : kFewWaves - 1)) / (p.waves ? 1 : kFewWaves);
+  p.block_parts = n_blocks == 0 ? 0 : (int)(want / units < 1 ? 1 : want / units > most ? most : want / units);
+  p.win_part = 256;
+  while ((win_rows + p.win_part - 1) / p.win_part > 8) p.win_part *= 2;
+  p.win_parts = (win_rows + p.win_part - 1) / p.win_part;
+  return p;
+}
+
+template <int HD, int WAVES> hipError_t launch_wide(const Attn8Args &a, const Plan8 &p, unsigned grid, hipStream_t st) {
+  constexpr int kLds = 512 * HD > WAVES * (64 * HD + 1024) ? 512 * HD : WAVES * (64 * HD + 1024);
+  static bool allowed[64] = {};
+  const hipError_t e = allow_lds((const void *)attention8_wide_kernel<HD, WAVES>, kLds, allowed);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attention8_wide_kernel<HD, WAVES>), dim3(grid), dim3(WAVES * 64), kLds, st, a, p);
+  return hipGetLastError();
+}
+
+template <int HD> hipError_t launch_hd(const Attn8Args &a, hipStream_t st) {
+  const Plan8 p = plan8(a.rows, a.hq, a.hkv, a.n_blocks, a.win_rows);
+  const int parts = p.block_parts + p.win_parts;
+  const int64_t units = (int64_t)a.hkv * parts, grid = (units + 7) / 8 * 8 * p.query_blocks;
+  if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  hipError_t e;
+  if (p.waves == 0) {
+    constexpr int kLds = kFewWaves * (HD * 128 + 256);
+    static_assert(kLds >= kFewWaves * (64 * HD + 1024), "value rows and counts fit");
+    static bool allowed[64] = {};
+    if ((e = allow_lds((const void *)attention8_few_kernel<HD>, kLds, allowed)) != hipSuccess) return e;
+    hipLaunchKernelGGL(attention8_few_kernel<HD>, dim3((unsigned)units), dim3(kFewWaves * 64), kLds, st, a, p);
+    e = hipGetLastError();
+  } else if (p.waves == 2) e = launch_wide<HD, 2>(a, p, (unsigned)grid, st);
+  else if (p.waves == 4) e = launch_wide<HD, 4>(a, p, (unsigned)grid, st);
+  else e = launch_wide<HD, 8>(a, p, (unsigned)grid, st);
+  if (e != hipSuccess || parts == 1) return e;
+  const int64_t groups = ((int64_t)a.rows * a.hq * (HD / 4) + 255) / 256;
+  if (groups > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(attention8_merge_kernel<HD>, dim3((unsigned)groups), dim3(256), 0, st, a, parts);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -158,15 +641,11 @@ hipError_t launch_kv8_load(const void *cache8, int first_block, int n_blocks, in
 }
 
 size_t attention8_scratch_floats(int rows, int hq, int hkv, int hd, int n_blocks, int win_rows) {
-  (void)rows; (void)hq; (void)hkv; (void)hd; (void)n_blocks; (void)win_rows;
-  return 64;
+  const Plan8 p = plan8(rows, hq, hkv, n_blocks, win_rows);
+  const int parts = p.block_parts + p.win_parts;
+  return parts == 1 ? 64 : (size_t)parts * rows * hq * (hd + 2);
 }
 
-hipError_t launch_attention8(const Attn8Args &a, hipStream_t st) {
-  const dim3 grid(a.rows, a.hq);
-  if (a.hd == 128) hipLaunchKernelGGL(attention8_kernel<128>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(attention8_kernel<64>, grid, dim3(256), 0, st, a);
-  return hipGetLastError();
-}
+hipError_t launch_attention8(const Attn8Args &a, hipStream_t st) { return a.hd == 128 ? launch_hd<128>(a, st) : launch_hd<64>(a, st); }
 
 }  // namespace spec
