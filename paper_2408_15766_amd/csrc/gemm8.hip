@@ -146,6 +146,208 @@ __global__ __launch_bounds__(kStreamWaves * 64) void gemm8_stream_kernel(Gemm8Ar
   if (tok < a.m) store4<VEC>((OUT *)a.y + (size_t)tok * a.ldy, rb * 16 + 4 * (lane >> 4), a.rows, s);
 }
 
+// ---- many tokens: tiles ------------------------------------------------------------
+// A workgroup owns WM * TB * 32 tokens x WN * WB * 32 weight rows, a wavefront TB x WB blocks of 32 x 32 of them.  Both operands are copied straight into the LDS, 64 k
+// (half a packed tile) at a time, four stages deep, and read from there in the order of the operands of the 32 x 32 x 64 product (weights as A, so that a lane
+// ends up with four consecutive columns of one token).  One barrier per stage: behind it the next stage is there for everybody and this stage's operands are in registers, so
+// that its buffer takes the copies of four stages on.
+// Every stage buffer is an array of its own, which tells the compiler what a read depends on.  The barrier stands behind the products of a stage's first 32 tokens, which cover the
+// wait for its last operands; operands of tokens are read again, for the next stage, as soon as their products are under way.
+template <int WM, int WN, int TB, int WB>
+struct Tile8 {
+  static constexpr int kWaves = WM * WN, kTok = WM * TB * 32, kRows = WN * WB * 32;
+  static constexpr int kX = kTok * 64, kW = kRows * 64;       // bytes of a stage
+  static constexpr int kXLoads = kX / 1024 / kWaves, kWLoads = kW / 1024 / kWaves;   // 1 KiB copies per wavefront and stage
+  // exponents: 64 bytes per 16-row block, tokens first; a wavefront copies those of kExp blocks into its 256 bytes
+  static constexpr int kBlocks = (kTok + kRows) / 16, kExp = kBlocks / kWaves, kE = kWaves * 256;
+  static constexpr int kLoads = kXLoads + kWLoads + 1;
+  static_assert(kXLoads * kWaves * 1024 == kX && kWLoads * kWaves * 1024 == kW && kExp * kWaves == kBlocks && (kExp == 2 || kExp == 4), "whole copies");
+  static __device__ __forceinline__ constexpr int exp_at(int block32) { return block32 * (256 / (kExp / 2)); }   // where those of 32 rows lie
+};
+constexpr int kStages8 = 4;
+
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((address_space(3))) void lds_void;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *base) {
+  return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7FFFFFFF, 0x00027000);
+}
+// 16 bytes per lane from base + voff (lane) + soff (wave-uniform) straight into the LDS, to dst + 16 * lane; dst is wave-uniform
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t base, int voff, int soff, void *dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (lds_void *)dst, 16, voff, soff, 0, 0);
+}
+// Workgroup barrier that waits for nothing else
+__device__ __forceinline__ void wg_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+struct Half8 { u32x4_t u[2]; };                               // a 32 x 64 operand
+__device__ __forceinline__ i32x8_t operand8(const Half8 &f) {
+  return i32x8_t{(int)f.u[0].x, (int)f.u[0].y, (int)f.u[0].z, (int)f.u[0].w, (int)f.u[1].x, (int)f.u[1].y, (int)f.u[1].z, (int)f.u[1].w};
+}
+struct Wide8 { u32x4_t v[4]; };                               // the same as bf16 operands of 16 k
+__device__ __forceinline__ Wide8 widen8(const Half8 &f, uint32_t e) {
+  const float s = __uint_as_float(e << 23);
+  Wide8 r;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const uint32_t a = f.u[i / 2][(i & 1) * 2], b = f.u[i / 2][(i & 1) * 2 + 1];
+    r.v[i] = u32x4_t{bf16_of_codes<false>(a, s), bf16_of_codes<true>(a, s), bf16_of_codes<false>(b, s), bf16_of_codes<true>(b, s)};
+  }
+  return r;
+}
+
+template <typename OUT, bool VEC, int WM, int WN, int TB, int WB>
+__global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a) {
+  using L = Tile8<WM, WN, TB, WB>;
+  constexpr bool kExact = sizeof(OUT) == 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char x0[L::kX], x1[L::kX], x2[L::kX], x3[L::kX], w0[L::kW], w1[L::kW], w2[L::kW], w3[L::kW];
+  __shared__ __attribute__((aligned(1024))) unsigned char e0[L::kE], e1[L::kE], e2[L::kE], e3[L::kE];
+  const Packed8 pw = packed8(a.rows, a.in), px = packed8(a.m, a.in);
+  const int tok_tiles = (a.m + L::kTok - 1) / L::kTok, row_tiles = (a.rows + L::kRows - 1) / L::kRows;
+  // ids 8 apart run on one XCD: the token tiles of a weight tile follow each other there
+  const int row_tile = (int)blockIdx.x / 8 / tok_tiles * 8 + (int)blockIdx.x % 8, tok_tile = (int)blockIdx.x / 8 % tok_tiles;
+  if (row_tile >= row_tiles) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, g = lane >> 5;
+  const int wm = wave % WM, wn = wave / WM;
+  const int n_stage = 2 * pw.groups;
+
+  // what this wavefront copies: 16-row blocks of tokens and of weights (those past the end: the last one again), and a share of the exponents
+  __amdgpu_buffer_rsrc_t xsrc[L::kXLoads], wsrc[L::kWLoads];
+#pragma unroll
+  for (int i = 0; i < L::kXLoads; i++)
+    xsrc[i] = buffer_of(a.x8 + (size_t)min(tok_tile * (L::kTok / 16) + wave * L::kXLoads + i, px.blocks - 1) * px.groups * kTile8);
+#pragma unroll
+  for (int i = 0; i < L::kWLoads; i++)
+    wsrc[i] = buffer_of(a.w8 + (size_t)min(row_tile * (L::kRows / 16) + wave * L::kWLoads + i, pw.blocks - 1) * pw.groups * kTile8);
+  const int eb = wave * L::kExp + lane / 16 % L::kExp;        // (two blocks: both halves of the wavefront copy the same)
+  const uint32_t *esrc = (const uint32_t *)(eb < L::kTok / 16 ? a.x8 + packed8_exps(px) + (size_t)min(tok_tile * (L::kTok / 16) + eb, px.blocks - 1) * px.quads * 64
+                                                              : a.w8 + packed8_exps(pw) + (size_t)min(row_tile * (L::kRows / 16) + eb - L::kTok / 16, pw.blocks - 1) * pw.quads * 64) + lane % 16;
+  auto copy = [&](unsigned char *x, unsigned char *w, unsigned char *e, int s) __attribute__((always_inline)) {
+    s = min(s, n_stage - 1);                                  // past the end: the last stage again (never read)
+#pragma unroll
+    for (int i = 0; i < L::kWLoads; i++) load_to_lds(wsrc[i], lane * 16, s * 1024, w + (wave * L::kWLoads + i) * 1024);
+#pragma unroll
+    for (int i = 0; i < L::kXLoads; i++) load_to_lds(xsrc[i], lane * 16, s * 1024, x + (wave * L::kXLoads + i) * 1024);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(esrc + (s >> 3) * 16), (lds_void *)(e + wave * 256), 4, 0, 0);
+  };
+
+  f32x16_t acc[WB][TB];
+#pragma unroll
+  for (int b = 0; b < WB; b++)
+#pragma unroll
+    for (int t = 0; t < TB; t++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) acc[b][t][v] = 0.f;
+  // lane (c, g) of a 32-row operand: row c % 16 of block c / 16, its pieces 2 g and 2 g + 1
+  const int at = (c >> 4) * 1024 + (2 * g * 16 + (c & 15)) * 16, e_at = (c >> 4) * 64 + (c & 15) * 4;
+  struct Operand { Half8 h; uint32_t e; };
+  auto read_x = [&](Operand &o, const unsigned char *x, const unsigned char *e, int t, int s) __attribute__((always_inline)) {
+    const unsigned char *p = x + (wm * TB + t) * 2048 + at;
+    o = Operand{{*(const u32x4_t *)p, *(const u32x4_t *)(p + 256)}, e[L::exp_at(wm * TB + t) + e_at + ((s >> 1) & 3)]};
+  };
+  auto read_w = [&](Operand &o, const unsigned char *w, const unsigned char *e, int b, int s) __attribute__((always_inline)) {
+    const unsigned char *p = w + (wn * WB + b) * 2048 + at;
+    o = Operand{{*(const u32x4_t *)p, *(const u32x4_t *)(p + 256)}, e[L::exp_at(L::kTok / 32 + wn * WB + b) + e_at + ((s >> 1) & 3)]};
+  };
+  Operand xo[TB], wo[2][WB];
+  // cw: weight operands of stage s (nw: the next one's); x, w, e: its buffers; xn, wn_, en: those of the next stage
+  auto stage = [&](Operand (&cw)[WB], Operand (&nw)[WB], unsigned char *x, unsigned char *w, unsigned char *e, unsigned char *xn, unsigned char *wn_, unsigned char *en,
+                   int s) __attribute__((always_inline)) {
+    Wide8 ww[kExact ? WB : 1];
+    if constexpr (kExact)
+#pragma unroll
+      for (int b = 0; b < WB; b++) ww[b] = widen8(cw[b].h, cw[b].e);
+#pragma unroll
+    for (int t = 0; t < TB; t++) {
+      if constexpr (!kExact) {
+#pragma unroll
+        for (int b = 0; b < WB; b++)
+          acc[b][t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand8(cw[b].h), operand8(xo[t].h), acc[b][t], 0, 0, 0, (int)cw[b].e, 0, (int)xo[t].e);
+      } else {
+        const Wide8 xw = widen8(xo[t].h, xo[t].e);
+#pragma unroll
+        for (int b = 0; b < WB; b++)
+#pragma unroll
+          for (int i = 0; i < 4; i++)
+            acc[b][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ww[b].v[i]), __builtin_bit_cast(bf16x8_t, xw.v[i]), acc[b][t], 0, 0, 0);
+      }
+      if (t == 0) {
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int kOpen = (kStages8 - 2) * L::kLoads;     // copies that may still be under way
+        __builtin_amdgcn_s_waitcnt(0x0070 | (kOpen & 15) | (kOpen >> 4 << 14));   // vmcnt(kOpen) lgkmcnt(0)
+        wg_barrier();
+        copy(x, w, e, s + kStages8);
+#pragma unroll
+        for (int b = 0; b < WB; b++) read_w(nw[b], wn_, en, b, s + 1);
+      }
+      read_x(xo[t], xn, en, t, s + 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  copy(x0, w0, e0, 0);
+  copy(x1, w1, e1, 1);
+  copy(x2, w2, e2, 2);
+  copy(x3, w3, e3, 3);
+  constexpr int kFirst = (kStages8 - 1) * L::kLoads;
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (kFirst & 15) | (kFirst >> 4 << 14));   // stage 0 here
+  wg_barrier();
+#pragma unroll
+  for (int b = 0; b < WB; b++) read_w(wo[0][b], w0, e0, b, 0);
+#pragma unroll
+  for (int t = 0; t < TB; t++) read_x(xo[t], x0, e0, t, 0);
+  int s = 0;
+  for (; s + 4 <= n_stage; s += 4) {
+    stage(wo[0], wo[1], x0, w0, e0, x1, w1, e1, s);
+    stage(wo[1], wo[0], x1, w1, e1, x2, w2, e2, s + 1);
+    stage(wo[0], wo[1], x2, w2, e2, x3, w3, e3, s + 2);
+    stage(wo[1], wo[0], x3, w3, e3, x0, w0, e0, s + 3);
+  }
+  if (s < n_stage) {                                          // stages come in pairs
+    stage(wo[0], wo[1], x0, w0, e0, x1, w1, e1, s);
+    stage(wo[1], wo[0], x1, w1, e1, x2, w2, e2, s + 1);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);                         // no copy into the LDS outlives the workgroup
+
+#pragma unroll
+  for (int t = 0; t < TB; t++) {
+    const int tok = tok_tile * L::kTok + (wm * TB + t) * 32 + c;
+    if (tok >= a.m) continue;                                 // (both lanes of a token)
+    OUT *y = (OUT *)a.y + (size_t)tok * a.ldy;
+#pragma unroll
+    for (int b = 0; b < WB; b++) {
+      const int col = row_tile * L::kRows + (wn * WB + b) * 32;
+#pragma unroll
+      for (int q = 0; q < 4; q++)
+        store4<VEC>(y, col + 8 * q + 4 * g, a.rows, f32x4_t{acc[b][t][4 * q], acc[b][t][4 * q + 1], acc[b][t][4 * q + 2], acc[b][t][4 * q + 3]});
+    }
+  }
+}
+
+template <typename OUT, bool VEC, int WM, int WN, int TB, int WB>
+hipError_t launch_tile(const Gemm8Args &a, hipStream_t st) {
+  using L = Tile8<WM, WN, TB, WB>;
+  const int64_t tok_tiles = (a.m + L::kTok - 1) / L::kTok, row_tiles = (a.rows + L::kRows - 1) / L::kRows;
+  const int64_t grid = (row_tiles + 7) / 8 * 8 * tok_tiles;
+  if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((gemm8_tile_kernel<OUT, VEC, WM, WN, TB, WB>), dim3((unsigned)grid), dim3(L::kWaves * 64), 0, st, a);
+  return hipGetLastError();
+}
+
+template <typename OUT, bool VEC>
+hipError_t launch_product(const Gemm8Args &a, hipStream_t st) {
+  if (a.m > 64) {
+    auto tiles = [&](int tok, int rows) { return (int64_t)((a.m + tok - 1) / tok) * ((a.rows + rows - 1) / rows); };
+    if (tiles(256, 256) >= 200) return launch_tile<OUT, VEC, 2, 4, 4, 2>(a, st);
+    if (tiles(128, 128) >= 200) return launch_tile<OUT, VEC, 2, 4, 2, 1>(a, st);
+    return launch_tile<OUT, VEC, 2, 2, 1, 1>(a, st);
+  }
+  const dim3 grid((a.rows + 15) / 16, (a.m + 16 * kStreamTiles - 1) / (16 * kStreamTiles));
+  hipLaunchKernelGGL((gemm8_stream_kernel<OUT, VEC>), grid, dim3(kStreamWaves * 64), 0, st, a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_pack_weight8(int dtype, const void *src, int rows, int in, void *dst, hipStream_t st) {
@@ -157,13 +359,8 @@ hipError_t launch_gemm8(int dtype, const void *x, int64_t ldx, int out_dtype, Ge
   const hipError_t e = dtype == 1 ? quant8((const bf16_t *)x, ldx, a.m, a.in, 0, scratch, st) : quant8((const float *)x, ldx, a.m, a.in, 0, scratch, st);
   if (e != hipSuccess) return e;
   const bool vec = ((uintptr_t)a.y & (out_dtype == 1 ? 7 : 15)) == 0 && a.ldy % 4 == 0;
-  const dim3 grid((a.rows + 15) / 16, (a.m + 16 * kStreamTiles - 1) / (16 * kStreamTiles));
-  if (grid.y > 65535) return hipErrorInvalidValue;
-#define SPEC_G8(OUT, VEC) hipLaunchKernelGGL((gemm8_stream_kernel<OUT, VEC>), grid, dim3(kStreamWaves * 64), 0, st, a)
-  if (out_dtype == 1) { if (vec) SPEC_G8(bf16_t, true); else SPEC_G8(bf16_t, false); }
-  else { if (vec) SPEC_G8(float, true); else SPEC_G8(float, false); }
-#undef SPEC_G8
-  return hipGetLastError();
+  if (out_dtype == 1) return vec ? launch_product<bf16_t, true>(a, st) : launch_product<bf16_t, false>(a, st);
+  return vec ? launch_product<float, true>(a, st) : launch_product<float, false>(a, st);
 }
 
 }  // namespace spec
