@@ -38,10 +38,12 @@ extern "C" {
  *   spec_packed8_bytes     : size of the packed form of w (host only; 0 if bad).
  *   spec_pack_weight8      : row-major src [rows, in] in dtype, any alignment of its
  *                            type -> dst, 256-byte aligned; no overlap.
- *   spec_k_gemm8_scratch_bytes : scratch of a call (host only; 0 if bad).
+ *   spec_k_gemm8_scratch_bytes : scratch of a call (host only; 0 if it needs none,
+ *                            as calls of few tokens do, and for bad sizes).
  *   spec_k_gemm8           : x in dtype with row stride ldx >= in; y [m, rows] in
  *                            out_dtype with row stride ldy >= rows (strides in elements;
- *                            what lies between rows is left alone); scratch 256-byte aligned.
+ *                            what lies between rows is left alone); scratch 256-byte aligned,
+ *                            NULL if none is needed.
  * 1 <= m <= 2^20, 1 <= in <= 2^20, 1 <= rows <= 2^24.  y overlaps none of the inputs or the scratch.
  *
  * Sums: with out_dtype fp32 products are exact and added up in fp32.  With bf16 the 8-bit matrix instruction takes 128 k at a time

@@ -10,6 +10,7 @@ import collections
 import ctypes as C
 import dataclasses
 import os
+import struct
 import threading
 import weakref
 from typing import Dict, List, Optional, Sequence
@@ -145,7 +146,7 @@ lib.spec_k_attention8_scratch_bytes.argtypes = [C.c_int32] * 6
 lib.spec_k_attention8.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                   C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]
 lib.spec_rotary_init.argtypes = [C.c_int32, C.c_int32, C.c_double, C.POINTER(spec_rope_scaling), C.POINTER(spec_rotary_plan_t)]
-lib.spec_k_rotary.argtypes = [C.POINTER(spec_rotary_plan_t), C.c_int32, C.POINTER(spec_rotary_part), C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
+lib.spec_k_rotary.argtypes = [C.POINTER(spec_rotary_plan_t), C.c_int32, C.c_char_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
                               C.c_int32, C.c_void_p]
 
 
@@ -570,26 +571,33 @@ def spec_topk_loss(feat_target, feat_draft, lm_head_packed, k: int, scratch=None
 
 
 # ---- a layer in 8 bits (spec_layer8.h) ----------------------------------------------------------
+# The host's share of a small call is longer than its kernels (the checks and allocations of a first version took 11 to 21 us, its kernels 6 to 10), so the functions below ask each
+# thing once, form their messages where they raise them, and hand structures over as packed bytes.
 
-def _here(what: str, *tensors) -> None:
-    """The calls launch on the current device: every tensor has to be on it."""
+def _refuse(what: str, why: str):
+    raise SpecError(SPEC_EINVAL, f"{what}: {why}")
+
+
+def _here(what: str, *tensors) -> int:
+    """The calls launch on the current device's current stream: every tensor has to be there.  Returns the stream."""
     import torch
-    device = torch.cuda.current_device() if torch.cuda.is_available() else None
+    at = tensors[0].get_device()
     for t in tensors:
-        if t is not None and not (t.is_cuda and t.device.index == device):
-            raise SpecError(SPEC_EINVAL, f"{what}: a tensor on {t.device}, and the current device is {'none' if device is None else f'cuda:{device}'}")
+        if t is not None and (t.get_device() != at or at < 0):
+            _refuse(what, f"tensors on {[str(u.device) for u in tensors if u is not None]}")
+    if at != torch.cuda.current_device():
+        _refuse(what, f"tensors on {tensors[0].device}, and the current device is cuda:{torch.cuda.current_device()}")
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (as in _stream_ptr)
+    return raw(at) if raw is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _dtype_code(what: str, dtype) -> int:
     import torch
-    if dtype not in (torch.float32, torch.bfloat16):
-        raise SpecError(SPEC_EINVAL, f"{what}: {dtype} (float32 and bfloat16 are supported)")
-    return 1 if dtype == torch.bfloat16 else 0
-
-
-def _need(what: str, ok: bool, why: str) -> None:
-    if not ok:
-        raise SpecError(SPEC_EINVAL, f"{what}: {why}")
+    if dtype is torch.bfloat16:
+        return 1
+    if dtype is not torch.float32:
+        _refuse(what, f"{dtype} (float32 and bfloat16 are supported)")
+    return 0
 
 
 def spec_packed8_bytes(rows: int, cols: int) -> int:
@@ -600,13 +608,15 @@ def spec_pack_weight8(w):
     """Row-major torch matrix [rows, in] (bf16 or fp32) on the device -> its 8-bit form (uint8 tensor that remembers its shape)."""
     import torch
     what = "spec_pack_weight8"
-    _here(what, w)
+    stream = _here(what, w)
     dtype = _dtype_code(what, w.dtype)
-    _need(what, w.dim() == 2 and w.is_contiguous(), "a contiguous [rows, in] matrix is needed")
+    if w.dim() != 2 or not w.is_contiguous():
+        _refuse(what, "a contiguous [rows, in] matrix is needed")
     n = spec_packed8_bytes(*w.shape)
-    _need(what, n > 0, f"cannot pack a {tuple(w.shape)} matrix")
+    if n == 0:
+        _refuse(what, f"cannot pack a {tuple(w.shape)} matrix")
     dst = torch.empty(n, dtype=torch.uint8, device=w.device)
-    rc = lib.spec_pack_weight8(dtype, w.data_ptr(), w.shape[0], w.shape[1], dst.data_ptr(), _stream_ptr())
+    rc = lib.spec_pack_weight8(dtype, w.data_ptr(), w.shape[0], w.shape[1], dst.data_ptr(), stream)
     if rc:
         raise SpecError(rc, what)
     dst.logical_shape = tuple(w.shape)
@@ -623,22 +633,28 @@ def spec_k_gemm8(x, w8, out_dtype=None, out=None, scratch=None):
     spec_k_gemm8_scratch_bytes(m, in, rows), for callers that keep their workspaces."""
     import torch
     what = "spec_k_gemm8"
-    _here(what, x, w8, out, scratch)
+    stream = _here(what, x, w8, out, scratch)
     rows, cols = w8.logical_shape
-    _need(what, x.dim() == 2 and x.shape[1] == cols and (x.stride(1) == 1 or cols == 1), f"x has to be [m, {cols}] with dense rows")
+    if x.dim() != 2 or x.shape[1] != cols or (x.stride(1) != 1 and cols > 1):
+        _refuse(what, f"x has to be [m, {cols}] with dense rows")
     m = x.shape[0]
     if out is None:
-        out = torch.empty((m, rows), dtype=out_dtype or x.dtype, device=x.device)
-    _need(what, tuple(out.shape) == (m, rows) and (out.stride(1) == 1 or rows == 1) and out_dtype in (None, out.dtype), f"out has to be [{m}, {rows}] with dense rows")
-    n = spec_k_gemm8_scratch_bytes(m, cols, rows)
-    if scratch is None:
-        scratch = torch.empty(n, dtype=torch.uint8, device=x.device)
-    _need(what, scratch.is_contiguous(), "scratch has to be contiguous")
-    ldx, ldy = (x.stride(0), out.stride(0)) if m > 1 else (cols, rows)
-    rc = lib.spec_k_gemm8(_dtype_code(what, x.dtype), x.data_ptr(), ldx, m, cols, w8.data_ptr(), rows, _dtype_code(what, out.dtype), out.data_ptr(), ldy,
-                          scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream_ptr())
+        out = x.new_empty((m, rows), dtype=x.dtype if out_dtype is None else out_dtype)
+    elif tuple(out.shape) != (m, rows) or (out.stride(1) != 1 and rows > 1) or (out_dtype is not None and out_dtype is not out.dtype):
+        _refuse(what, f"out has to be [{m}, {rows}] with dense rows, of out_dtype")
+    n = lib.spec_k_gemm8_scratch_bytes(m, cols, rows)
+    if scratch is not None:
+        if not scratch.is_contiguous():
+            _refuse(what, "scratch has to be contiguous")
+        room = scratch.numel() * scratch.element_size()
+    else:
+        room = n
+        if n:
+            scratch = x.new_empty(n, dtype=torch.uint8)
+    rc = lib.spec_k_gemm8(_dtype_code(what, x.dtype), x.data_ptr(), x.stride(0) if m > 1 else cols, m, cols, w8.data_ptr(), rows, _dtype_code(what, out.dtype),
+                          out.data_ptr(), out.stride(0) if m > 1 else rows, None if scratch is None else scratch.data_ptr(), room, stream)
     if rc:
-        raise SpecError(rc, f"{what}: {m} x {cols} by {rows}")
+        raise SpecError(rc, f"{what}: {m} x {cols} by {rows}, {room} bytes of scratch")
     return out
 
 
@@ -650,30 +666,38 @@ def spec_kv8_alloc(n_blocks: int, hkv: int, hd: int, device=None):
     """An 8-bit cache of n_blocks blocks (uint8 tensor [n_blocks, bytes of a block], not initialised)."""
     import torch
     n = spec_kv8_bytes(1, hkv, hd)
-    _need("spec_kv8_alloc", n > 0 and n_blocks >= 0, f"{n_blocks} blocks of {hkv} heads of {hd}")
+    if n == 0 or n_blocks < 0:
+        _refuse("spec_kv8_alloc", f"{n_blocks} blocks of {hkv} heads of {hd}")
     return torch.empty((n_blocks, n), dtype=torch.uint8, device="cuda" if device is None else device)
 
 
-def _kv8_args(what: str, k, v, cache8, first_block: int, hkv: int, hd: int) -> int:
+def _is_kv8(cache8, hkv: int, hd: int, blocks: int) -> bool:
     import torch
-    _here(what, k, v, cache8)
-    _need(what, k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16, "k and v have to be bfloat16")
-    _need(what, k.dim() == 2 and k.shape == v.shape and k.shape[1] == hkv * hd and k.shape[0] % SPEC_KV8_BLOCK == 0,
-          f"k and v have to be [a multiple of {SPEC_KV8_BLOCK}, {hkv * hd}]")
+    return (cache8 is not None and cache8.dim() == 2 and cache8.dtype is torch.uint8 and cache8.is_contiguous() and cache8.shape[0] >= blocks and
+            cache8.shape[1] == lib.spec_kv8_bytes(1, hkv, hd))
+
+
+def _kv8_args(what: str, k, v, cache8, first_block: int, hkv: int, hd: int):
+    import torch
+    stream = _here(what, k, v, cache8)
+    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+        _refuse(what, "k and v have to be bfloat16")
+    if k.dim() != 2 or k.shape != v.shape or k.shape[1] != hkv * hd or k.shape[0] % SPEC_KV8_BLOCK:
+        _refuse(what, f"k and v have to be [a multiple of {SPEC_KV8_BLOCK}, {hkv * hd}]")
     n = k.shape[0] // SPEC_KV8_BLOCK
-    _need(what, n == 0 or (k.stride() == v.stride() and k.stride(1) == 1), "k and v have to have the same strides and dense rows")
-    _need(what, cache8.dim() == 2 and cache8.dtype == torch.uint8 and cache8.is_contiguous() and cache8.shape[1] == spec_kv8_bytes(1, hkv, hd),
-          f"cache8 is no cache of {hkv} heads of {hd}")
-    _need(what, 0 <= first_block and first_block + n <= cache8.shape[0], f"blocks {first_block} .. {first_block + n} of {cache8.shape[0]}")
-    return n
+    if n and (k.stride() != v.stride() or k.stride(1) != 1):
+        _refuse(what, "k and v have to have the same strides and dense rows")
+    if first_block < 0 or not _is_kv8(cache8, hkv, hd, first_block + n):
+        _refuse(what, f"cache8 has no blocks {first_block} .. {first_block + n - 1} of {hkv} heads of {hd}")
+    return n, stream
 
 
 def spec_k_kv8_store(k, v, cache8, first_block: int, hkv: int, hd: int) -> None:
     """k, v: bf16 torch [64 * n, hkv*hd] (rows may be strided) -> blocks first_block .. of cache8 (spec_kv8_alloc)."""
-    n = _kv8_args("spec_k_kv8_store", k, v, cache8, first_block, hkv, hd)
+    n, stream = _kv8_args("spec_k_kv8_store", k, v, cache8, first_block, hkv, hd)
     if n == 0:
         return
-    rc = lib.spec_k_kv8_store(k.data_ptr(), v.data_ptr(), k.stride(0), n, hkv, hd, cache8.data_ptr(), first_block, _stream_ptr())
+    rc = lib.spec_k_kv8_store(k.data_ptr(), v.data_ptr(), k.stride(0), n, hkv, hd, cache8.data_ptr(), first_block, stream)
     if rc:
         raise SpecError(rc, "spec_k_kv8_store")
 
@@ -681,11 +705,12 @@ def spec_k_kv8_store(k, v, cache8, first_block: int, hkv: int, hd: int) -> None:
 def spec_k_kv8_load(cache8, first_block: int, n_blocks: int, hkv: int, hd: int):
     """Blocks of cache8 as bf16 rows: (k, v), each [64 * n_blocks, hkv*hd]."""
     import torch
-    k, v = (torch.empty((max(n_blocks, 0) * SPEC_KV8_BLOCK, hkv * hd), dtype=torch.bfloat16, device=cache8.device) for _ in range(2))
-    _need("spec_k_kv8_load", n_blocks >= 0, f"{n_blocks} blocks")
-    n = _kv8_args("spec_k_kv8_load", k, v, cache8, first_block, hkv, hd)
+    if n_blocks < 0:
+        _refuse("spec_k_kv8_load", f"{n_blocks} blocks")
+    k, v = (torch.empty((n_blocks * SPEC_KV8_BLOCK, hkv * hd), dtype=torch.bfloat16, device=cache8.device) for _ in range(2))
+    n, stream = _kv8_args("spec_k_kv8_load", k, v, cache8, first_block, hkv, hd)
     if n:
-        rc = lib.spec_k_kv8_load(cache8.data_ptr(), first_block, n, hkv, hd, k.data_ptr(), v.data_ptr(), hkv * hd, _stream_ptr())
+        rc = lib.spec_k_kv8_load(cache8.data_ptr(), first_block, n, hkv, hd, k.data_ptr(), v.data_ptr(), hkv * hd, stream)
         if rc:
             raise SpecError(rc, "spec_k_kv8_load")
     return k, v
@@ -702,44 +727,56 @@ def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, an
     it (else it is read from the device, which waits).  Returns bf16 [rows, hq*hd]."""
     import torch
     what = "spec_k_attention8"
-    _here(what, q, cache8, kwin, vwin, depth, anc, out, scratch)
-    rows = q.shape[0]
-    _need(what, q.dtype == torch.float32 and q.is_contiguous() and tuple(q.shape) == (rows, hq * hd), f"q has to be contiguous float32 [rows, {hq * hd}]")
-    _need(what, kwin.dtype == torch.bfloat16 and vwin.dtype == torch.bfloat16 and kwin.is_contiguous() and vwin.is_contiguous() and kwin.dim() == 2 and
-          kwin.shape == vwin.shape and kwin.shape[1] == hkv * hd, f"kwin and vwin have to be contiguous bfloat16 [rows, {hkv * hd}]")
-    _need(what, depth.dtype == torch.int32 and depth.is_contiguous() and tuple(depth.shape) == (rows,), "depth has to be int32 [rows]")
-    _need(what, anc is None or (anc.dtype == torch.int32 and anc.is_contiguous() and tuple(anc.shape) == (rows, 16)), "anc has to be int32 [rows, 16]")
+    stream = _here(what, q, cache8, kwin, vwin, depth, anc, out, scratch)
+    rows, wide = q.shape[0], hq * hd
+    if q.dtype is not torch.float32 or not q.is_contiguous() or q.dim() != 2 or q.shape[1] != wide:
+        _refuse(what, f"q has to be contiguous float32 [rows, {wide}]")
+    if (kwin.dtype is not torch.bfloat16 or vwin.dtype is not torch.bfloat16 or kwin.dim() != 2 or kwin.shape != vwin.shape or kwin.shape[1] != hkv * hd or
+            not kwin.is_contiguous() or not vwin.is_contiguous()):
+        _refuse(what, f"kwin and vwin have to be contiguous bfloat16 [rows, {hkv * hd}]")
+    if depth.dtype is not torch.int32 or depth.dim() != 1 or depth.shape[0] != rows or not depth.is_contiguous():
+        _refuse(what, "depth has to be int32 [rows]")
+    if anc is not None and (anc.dtype is not torch.int32 or tuple(anc.shape) != (rows, 16) or not anc.is_contiguous()):
+        _refuse(what, "anc has to be int32 [rows, 16]")
     win_rows = kwin.shape[0]
-    n = spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, n_blocks, win_rows)
-    _need(what, n > 0, f"{rows} rows, {hq} heads on {hkv} of {hd}, {n_blocks} blocks, a window of {win_rows} rows")
-    _need(what, n_blocks == 0 or (cache8 is not None and cache8.dim() == 2 and cache8.dtype == torch.uint8 and cache8.is_contiguous() and
-          cache8.shape[1] == spec_kv8_bytes(1, hkv, hd) and cache8.shape[0] >= n_blocks), f"cache8 holds no {n_blocks} blocks of {hkv} heads of {hd}")
+    n = lib.spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, n_blocks, win_rows)
+    if n == 0:
+        _refuse(what, f"{rows} rows, {hq} heads on {hkv} of {hd}, {n_blocks} blocks, a window of {win_rows} rows")
+    if n_blocks and not _is_kv8(cache8, hkv, hd, n_blocks):
+        _refuse(what, f"cache8 holds no {n_blocks} blocks of {hkv} heads of {hd}")
     if max_depth is None:
         max_depth = max(int(depth.max().item()), 0)
     if out is None:
-        out = torch.empty((rows, hq * hd), dtype=torch.bfloat16, device=q.device)
-    _need(what, out.dtype == torch.bfloat16 and out.is_contiguous() and tuple(out.shape) == (rows, hq * hd), f"out has to be contiguous bfloat16 [{rows}, {hq * hd}]")
+        out = q.new_empty((rows, wide), dtype=torch.bfloat16)
+    elif out.dtype is not torch.bfloat16 or not out.is_contiguous() or tuple(out.shape) != (rows, wide):
+        _refuse(what, f"out has to be contiguous bfloat16 [{rows}, {wide}]")
     if scratch is None:
-        scratch = torch.empty(n, dtype=torch.uint8, device=q.device)
-    _need(what, scratch.is_contiguous(), "scratch has to be contiguous")
-    rc = lib.spec_k_attention8(q.data_ptr(), None if n_blocks == 0 else cache8.data_ptr(), n_blocks, kwin.data_ptr(), vwin.data_ptr(), win_rows, rows, hq, hkv,
-                               hd, base, depth.data_ptr(), None if anc is None else anc.data_ptr(), max_depth, scratch.data_ptr(),
-                               scratch.numel() * scratch.element_size(), out.data_ptr(), _stream_ptr())
+        scratch, room = q.new_empty(n, dtype=torch.uint8), n
+    else:
+        room = scratch.numel() * scratch.element_size()
+        if not scratch.is_contiguous():
+            _refuse(what, "scratch has to be contiguous")
+    rc = lib.spec_k_attention8(q.data_ptr(), cache8.data_ptr() if n_blocks else None, n_blocks, kwin.data_ptr(), vwin.data_ptr(), win_rows, rows, hq, hkv, hd, base,
+                               depth.data_ptr(), None if anc is None else anc.data_ptr(), max_depth, scratch.data_ptr(), room, out.data_ptr(), stream)
     if rc:
-        raise SpecError(rc, f"{what}: base {base}, {n_blocks} blocks, max_depth {max_depth}")
+        raise SpecError(rc, f"{what}: base {base}, {n_blocks} blocks, max_depth {max_depth}, {room} bytes of scratch")
     return out
 
 
 def spec_rotary_plan(rot: int, theta: float, layout: str = "half", scaling: str = "none", factor: float = 1.0, trained_len: int = 0,
                      low_freq: float = 1.0, high_freq: float = 4.0, beta_fast: float = 32.0, beta_slow: float = 1.0) -> spec_rotary_plan_t:
     """The frequencies of a rotary embedding over the first `rot` dims of a head (host data; made once)."""
-    _need("spec_rotary_plan", layout in ROPE_LAYOUTS and scaling in ROPE_SCALINGS, f"layout {layout!r}, scaling {scaling!r}")
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        _refuse("spec_rotary_plan", f"layout {layout!r}, scaling {scaling!r}")
     low, high = (beta_slow, beta_fast) if scaling == "yarn" else (low_freq, high_freq)
     plan = spec_rotary_plan_t()
     rc = lib.spec_rotary_init(rot, ROPE_LAYOUTS[layout], theta, C.byref(spec_rope_scaling(ROPE_SCALINGS[scaling], trained_len, factor, low, high)), C.byref(plan))
     if rc:
         raise SpecError(rc, f"spec_rotary_plan: rot {rot}, theta {theta}, {scaling} by {factor}")
     return plan
+
+
+_rotary_parts = [struct.Struct("@" + "QQqqqqiiii" * n).pack for n in range(4)]   # spec_rotary_part, as often as there are tensors
 
 
 def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[Sequence[bool]] = None, out_dtypes: Optional[Sequence] = None, outs=None,
@@ -751,24 +788,30 @@ def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[
     import torch
     what = "spec_k_rotary"
     n = len(xs)
-    _need(what, 1 <= n <= 3, f"{n} tensors")
-    rows, _, hd = xs[0].shape
-    turned = [True] * n if turned is None else turned
+    if not 1 <= n <= 3:
+        _refuse(what, f"{n} tensors")
     if outs is None:
-        kinds = [x.dtype for x in xs] if out_dtypes is None else out_dtypes
-        outs = [torch.empty(x.shape, dtype=d, device=x.device) for x, d in zip(xs, kinds)]
+        outs = [x.new_empty(x.shape) for x in xs] if out_dtypes is None else [x.new_empty(x.shape, dtype=d) for x, d in zip(xs, out_dtypes)]
     at = pos if isinstance(pos, torch.Tensor) else None
-    _here(what, *xs, *outs, at)
-    _need(what, len(outs) == n and len(turned) == n, "as many outputs and flags as tensors")
-    _need(what, at is None or (at.dtype == torch.int32 and at.is_contiguous() and tuple(at.shape) == (rows,)), f"pos has to be int32 [{rows}]")
-    parts = (spec_rotary_part * n)()
-    for p, x, o, turn in zip(parts, xs, outs, turned):
-        _need(what, x.dim() == 3 and x.shape[0] == rows and x.shape[2] == hd and o.shape == x.shape, f"tensors have to be [{rows}, heads, {hd}]")
-        _need(what, hd == 1 or (x.stride(2) == 1 and o.stride(2) == 1), "the dims of a head have to be dense")
-        p.x, p.out, p.ldx, p.hsx, p.ldo, p.hso = x.data_ptr(), o.data_ptr(), x.stride(0), x.stride(1), o.stride(0), o.stride(1)
-        p.heads, p.dtype, p.out_dtype, p.turn = x.shape[1], _dtype_code(what, x.dtype), _dtype_code(what, o.dtype), bool(turn)
-    rc = lib.spec_k_rotary(C.byref(plan), n, parts, hd, rows, None if at is None else at.data_ptr(), 0 if at is not None else int(pos), bool(adjoint),
-                           _stream_ptr())
+    if len(outs) != n or (turned is not None and len(turned) != n):
+        _refuse(what, "as many outputs and flags as tensors are needed")
+    stream = _here(what, *xs, *outs, at)
+    if xs[0].dim() != 3:
+        _refuse(what, "tensors have to be [rows, heads, hd]")
+    rows, _, hd = xs[0].shape
+    if at is not None and (at.dtype is not torch.int32 or at.dim() != 1 or at.shape[0] != rows or not at.is_contiguous()):
+        _refuse(what, f"pos has to be int32 [{rows}]")
+    fields = []
+    for i in range(n):
+        x, o = xs[i], outs[i]
+        if x.shape != o.shape or x.dim() != 3 or x.shape[0] != rows or x.shape[2] != hd:
+            _refuse(what, f"tensors have to be [{rows}, heads, {hd}]")
+        (ldx, hsx, one), (ldo, hso, one_out) = x.stride(), o.stride()
+        if hd > 1 and not one == one_out == 1:
+            _refuse(what, "the dims of a head have to be dense")
+        fields += (x.data_ptr(), o.data_ptr(), ldx, hsx, ldo, hso, x.shape[1], _dtype_code(what, x.dtype), _dtype_code(what, o.dtype), 1 if turned is None else bool(turned[i]))
+    rc = lib.spec_k_rotary(C.byref(plan), n, _rotary_parts[n](*fields), hd, rows, at.data_ptr() if at is not None else None, 0 if at is not None else int(pos),
+                           bool(adjoint), stream)
     if rc:
         raise SpecError(rc, f"{what}: {rows} rows, heads of {hd}, plan over {plan.rot}")
     return list(outs)

@@ -45,17 +45,18 @@ int spec_pack_weight8(int32_t dtype, const void *src, int32_t rows, int32_t in, 
 
 uint64_t spec_k_gemm8_scratch_bytes(int32_t m, int32_t in, int32_t rows) {
   if (m < 1 || m > kMaxM8 || !matrix_ok(rows, in)) return 0;
-  return (packed8_bytes(packed8(m, in)) + 255) / 256 * 256;
+  return (gemm8_scratch_bytes(m, in, rows) + 255) / 256 * 256;
 }
 
 int spec_k_gemm8(int32_t dtype, const void *x, int32_t ldx, int32_t m, int32_t in, const void *w8, int32_t rows, int32_t out_dtype, void *y,
                  int32_t ldy, void *scratch, uint64_t scratch_bytes, void *stream) {
   const uint64_t need = spec_k_gemm8_scratch_bytes(m, in, rows);
-  if (!is_dtype(dtype) || !is_dtype(out_dtype) || !x || !w8 || !y || !scratch || need == 0 || scratch_bytes < need || ldx < in || ldy < rows) return SPEC_EINVAL;
+  if (!is_dtype(dtype) || !is_dtype(out_dtype) || !x || !w8 || !y || m < 1 || m > kMaxM8 || !matrix_ok(rows, in) || ldx < in || ldy < rows) return SPEC_EINVAL;
+  if (need > 0 && (!scratch || scratch_bytes < need)) return SPEC_EINVAL;
   if (!aligned(x, size_of(dtype)) || !aligned(y, size_of(out_dtype)) || !aligned(w8, 256) || !aligned(scratch, 256)) return SPEC_EINVAL;
   Gemm8Args a{};
-  a.w8 = (const unsigned char *)w8; a.m = m; a.in = in; a.rows = rows; a.y = y; a.ldy = ldy;
-  return done(launch_gemm8(dtype, x, ldx, out_dtype, a, scratch, (hipStream_t)stream));
+  a.x = x; a.ldx = ldx; a.w8 = (const unsigned char *)w8; a.m = m; a.in = in; a.rows = rows; a.y = y; a.ldy = ldy;
+  return done(launch_gemm8(dtype, out_dtype, a, scratch, (hipStream_t)stream));
 }
 
 uint64_t spec_kv8_bytes(int32_t n_blocks, int32_t hkv, int32_t hd) {

@@ -288,13 +288,15 @@ hipError_t launch_pending_rows(const AcceptResult *res, const int *n_committed, 
 
 // ---- gemm8.hip (8-bit matrices: layout in fp8.h) ------------------------------------------------
 struct Gemm8Args {
-  const unsigned char *x8, *w8;         // packed: [m, in] (set by launch_gemm8), [rows, in]
+  const void *x;  int64_t ldx;          // [m, in]
+  const unsigned char *x8, *w8;         // packed: x (set by launch_gemm8), [rows, in]
   int m, in, rows;
-  void *y;  int64_t ldy;                // [m, rows] in the output type
+  void *y;  int64_t ldy;                // [m, rows]
 };
 hipError_t launch_pack_weight8(int dtype, const void *src, int rows, int in, void *dst, hipStream_t st);
-// x [m, in] in dtype, row stride ldx, is put into 8 bits in `scratch` (packed8_bytes of [m, in])
-hipError_t launch_gemm8(int dtype, const void *x, int64_t ldx, int out_dtype, Gemm8Args a, void *scratch, hipStream_t st);
+// dtype: x's; scratch: gemm8_scratch_bytes (0: none), for x in 8 bits
+uint64_t gemm8_scratch_bytes(int m, int in, int rows);
+hipError_t launch_gemm8(int dtype, int out_dtype, const Gemm8Args &a, void *scratch, hipStream_t st);
 
 // ---- attention8.hip -------------------------------------------------------------------------------
 constexpr int kKv8Block = 64;           // tokens of a block

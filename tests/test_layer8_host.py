@@ -56,7 +56,7 @@ def refused(rc):
 
 def test_gemm8_refusals(P):
     f = P.lib.spec_k_gemm8
-    good = dict(dtype=1, x=X, ldx=256, m=4, k=256, w8=X, rows=32, out=1, y=X, ldy=32, scratch=X, nbytes=1 << 30)
+    good = dict(dtype=1, x=X, ldx=256, m=40, k=256, w8=X, rows=32, out=1, y=X, ldy=32, scratch=X, nbytes=1 << 30)
     for kw in (dict(dtype=2), dict(x=None), dict(ldx=255), dict(m=0), dict(m=-1), dict(m=(1 << 20) + 1), dict(k=0), dict(k=(1 << 20) + 1, ldx=1 << 21),
                dict(w8=None), dict(w8=X + 128), dict(rows=0), dict(out=3), dict(y=None), dict(y=X + 1), dict(x=X + 1), dict(ldy=31), dict(scratch=None),
                dict(scratch=X + 16), dict(nbytes=10)):
@@ -114,7 +114,7 @@ def test_rotary_refusals(P):
 
     def call(hd=64, rows=4, n=1, pos=X, plan=plan, **kw):
         p = {**dict(x=X, out=X, ldx=256, hsx=64, ldo=256, hso=64, heads=4, dtype=1, out_dtype=1, turn=1), **kw}
-        return P.lib.spec_k_rotary(plan and C.byref(plan), n, (b.spec_rotary_part * 3)(b.spec_rotary_part(**p)), hd, rows, pos, 0, 0, None)
+        return P.lib.spec_k_rotary(plan and C.byref(plan), n, bytes((b.spec_rotary_part * 3)(b.spec_rotary_part(**p))), hd, rows, pos, 0, 0, None)
 
     for kw in (dict(hd=0), dict(hd=62), dict(hd=257), dict(rows=0), dict(rows=(1 << 24) + 1), dict(n=0), dict(n=4), dict(n=2), dict(pos=X + 2), dict(plan=None),
                dict(x=None), dict(out=None), dict(x=X + 1, out=X + 1), dict(ldx=63), dict(ldo=10), dict(hsx=63), dict(hso=0), dict(heads=0), dict(heads=1025),
