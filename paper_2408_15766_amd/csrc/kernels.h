@@ -328,7 +328,9 @@ struct RotaryArgs {
   const int *pos;
   float mscale;
   double turns[kRotaryMaxPlanes];       // of a plane per position
+  int rows_each;                        // set by launch_rotary: rows of a workgroup, ..
+  uint2 row_items[3], head_items[3];    // .. and the divisors of its steps
 };
-hipError_t launch_rotary(const RotaryArgs &a, hipStream_t st);
+hipError_t launch_rotary(RotaryArgs a, hipStream_t st);
 
 }  // namespace spec

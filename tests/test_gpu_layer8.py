@@ -420,7 +420,7 @@ def check_rotary(P, plan, f, m, rot, layout, x, pos, out_dtype, adjoint=False, *
 
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("rows,heads,hd,rot", [(1, 1, 2, 2), (3, 5, 80, 32), (7, 2, 128, 128), (33, 40, 128, 64), (2, 3, 96, 90), (5, 1, 7, 6), (4, 6, 256, 256), (9, 3, 64, 48),
-                                               (130, 1, 33, 2), (1, 1024, 64, 64), (3, 2, 16, 0)])
+                                               (130, 1, 33, 2), (1, 1024, 64, 64), (3, 2, 16, 0), (2, 1024, 255, 254), (700, 2, 64, 64)])
 @pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "fp32")])
 def test_rotary(P, rows, heads, hd, rot, layout, dtype, out):
     kw = dict(scaling="yarn", factor=4.0, trained_len=2048) if rot >= 64 else {}
