@@ -1,4 +1,6 @@
 // Attention over a cache of 64-token blocks in 8 bits with a bf16 window behind it, and the cache's store and load (include/spec_layer8.h).
+#include <type_traits>
+
 #include "common.h"
 #include "fp8.h"
 #include "kernels.h"
@@ -72,6 +74,10 @@ __global__ __launch_bounds__(256) void kv8_load_kernel(const unsigned char *cach
 // weights down to 2^-29 of the largest.  A block's exponents go into the scores' factor and into the weights (relative to the largest of the
 // blocks so far, which the outputs are in units of); nothing is done per value for them.
 constexpr float kRefLift = 7.f;
+// Weights go to fp16 by the conversion that cuts off, two at a time (rounding to nearest takes three instructions): they are made 2^-12 too large first, which
+// centres the error (at most 2^-10 either way, in the mean none), and their sum is corrected for it.
+constexpr float kCutLift = 0.00035223863f;                    // log2(1 + 2^-12)
+constexpr float kCutSum = 1.f / (1.f + 1.f / 4096.f);
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
@@ -82,6 +88,7 @@ __device__ __forceinline__ f32x16_t mul_f16(const u32x4_t &a, const u32x4_t &b, 
 __device__ __forceinline__ f32x16_t mul_bf16(const u32x4_t &a, const u32x4_t &b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
+__device__ __forceinline__ uint32_t cut_f16x2(float lo, float hi) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi)); }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   typedef __attribute__((ext_vector_type(2))) float f2_t;
   typedef __attribute__((ext_vector_type(2))) _Float16 h2_t;
@@ -148,8 +155,38 @@ template <int HD> __device__ __forceinline__ Query8<HD> load_query8(const float 
   return r;
 }
 
-// 64 keys of a block for 32 queries.  keys(kt, s), values(kt, db, a): the fp16 operands (s: 16 dims, a: 16 keys); exps: the block's exponents + 127 of keys and values;
-// top_exp: the largest value exponent so far, r.o is in units of 2^top_exp.
+// The weights of 64 keys of a block for 32 queries, out of their scores; exps: the block's exponents + 127 of keys and values; top_exp: the largest value exponent so
+// far, r.o is in units of 2^top_exp.  p: those of 16 keys each, in fp16.
+template <int HD>
+__device__ __forceinline__ void weigh(Running<HD> &r, float q_scale, uint32_t exps, int &top_exp, f32x16_t (&s)[2], u32x4_t (&p)[4]) {
+  const int ek = (int)(exps & 0xFF) - 127, ev = (int)((exps >> 8) & 0xFF) - 127;
+  if (ev > top_exp) {
+    const float t = exp2_((float)(top_exp - ev));
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++) r.o[db] *= t;
+    top_exp = ev;
+  }
+  const float f = q_scale * pow2(ek);
+  float top = s[0][0];
+#pragma unroll
+  for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) top = __builtin_elementwise_maximum(top, s[kt][i]);   // (with a NaN among them the query's result is NaN, whatever the reference)
+  r.raise(max_halves(top) * f);
+  const float minus = (float)(ev - top_exp) + kCutLift - r.m;   // (the reference of a query whose scores are all NaN stays -inf: its weights are NaN)
+  float sum = 0.f;
+#pragma unroll
+  for (int h = 0; h < 4; h++)
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const float x = exp2_(fmaf(s[h >> 1][8 * (h & 1) + i], f, minus)), y = exp2_(fmaf(s[h >> 1][8 * (h & 1) + i + 1], f, minus));
+      sum += x + y;
+      p[h][i / 2] = cut_f16x2(x, y);
+    }
+  r.l = fmaf(sum, pow2(min(top_exp - ev, 127)), r.l);
+}
+
+// 64 keys of a block for 32 queries.  keys(kt, s), values(kt, db, a): the fp16 operands (s: 16 dims, a: 16 keys)
 template <int HD, typename K, typename V>
 __device__ __forceinline__ void block_step(Running<HD> &r, const Query8<HD> &q, uint32_t exps, int &top_exp, K keys, V values) {
   f32x16_t s[2];
@@ -160,37 +197,15 @@ __device__ __forceinline__ void block_step(Running<HD> &r, const Query8<HD> &q, 
 #pragma unroll
     for (int t = 0; t < HD / 16; t++) s[kt] = mul_f16(keys(kt, t), q.f[t], s[kt]);
   }
-  const int ek = (int)(exps & 0xFF) - 127, ev = (int)((exps >> 8) & 0xFF) - 127;
-  if (ev > top_exp) {
-    const float t = exp2_((float)(top_exp - ev));
+  u32x4_t p[4];
+  weigh<HD>(r, q.scale, exps, top_exp, s, p);
 #pragma unroll
-    for (int db = 0; db < HD / 32; db++) r.o[db] *= t;
-    top_exp = ev;
-  }
-  const float f = q.scale * pow2(ek);
-  float top = fmaxf(s[0][0], s[1][0]);
+  for (int h = 0; h < 4; h++)
 #pragma unroll
-  for (int i = 1; i < 16; i++) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
-  r.raise(max_halves(top) * f);
-  const float minus = (float)(ev - top_exp) - r.m;             // (the reference of a query whose scores are all NaN stays -inf: its weights are NaN)
-  float sum = 0.f;
-#pragma unroll
-  for (int kt = 0; kt < 2; kt++) {
-#pragma unroll
-    for (int i = 0; i < 16; i++) { s[kt][i] = exp2_(fmaf(s[kt][i], f, minus)); sum += s[kt][i]; }
-#pragma unroll
-    for (int a = 0; a < 2; a++) {
-      u32x4_t p;
-#pragma unroll
-      for (int i = 0; i < 4; i++) p[i] = pack_f16x2(s[kt][8 * a + 2 * i], s[kt][8 * a + 2 * i + 1]);
-#pragma unroll
-      for (int db = 0; db < HD / 32; db++) r.o[db] = mul_f16(values(kt, db, a), p, r.o[db]);
-    }
-  }
-  r.l = fmaf(sum, pow2(min(top_exp - ev, 127)), r.l);
+    for (int db = 0; db < HD / 32; db++) r.o[db] = mul_f16(values(h >> 1, db, h & 1), p[h], r.o[db]);
 }
 
-// ---- the window: a wavefront takes 32 of its rows at a time for its 32 queries ----
+// ---- the window: 32 of its rows at a time for a wavefront's 32 queries ----
 // Queries and weights go through the bf16 products as two terms each (value and what its rounding left).  Values that are not finite are taken out of the products, where they
 // would reach every query, and added by hand to those that see them.
 template <int HD> struct QueryWin { u32x4_t hi[HD / 16], lo[HD / 16]; };
@@ -209,107 +224,112 @@ template <int HD> __device__ __forceinline__ QueryWin<HD> load_query_win(const f
   }
   return r;
 }
-// What a query sees of the window: rows below `first`, and its path: rows path[0 .. deep] (anc), or first .. first + deep
-struct Sight { int deep, last; };                             // last: the highest row it sees
-__device__ __forceinline__ int path_row(const Attn8Args &a, int row, int d) {   // -1: outside the window
-  const int64_t r = (int64_t)a.base - a.n_blocks * kKv8Block + a.anc[(size_t)row * kAncStride + d];
-  return r >= 0 && r < a.win_rows ? (int)r : -1;
-}
+// What a query sees of the window: rows below `first`, and its path: rows path[0 .. deep] (anc; -1: outside), or first .. first + deep
+struct Sight { int deep, last, whole, path[kAncStride]; };    // last: the highest row it sees; whole: the rows below this one it sees all, once each
 // Orders this wavefront's LDS accesses for the compiler (the hardware keeps their order)
 __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 __device__ __forceinline__ Sight sight_of(const Attn8Args &a, int row, bool any) {
-  Sight s{any ? min(a.depth[row], a.max_depth) : -1, -1};
-  if (s.deep < 0) return s;
+  Sight s;
   const int first = a.base - a.n_blocks * kKv8Block;
-  if (!a.anc) s.last = first + s.deep;
-  else {
-    s.last = first - 1;
-    for (int d = 0; d <= s.deep; d++) s.last = max(s.last, path_row(a, row, d));
-  }
+  const int deep = a.depth[row];
+  if (a.anc)
+#pragma unroll
+    for (int d = 0; d < kAncStride; d++) s.path[d] = a.anc[(size_t)row * kAncStride + d];   // (all at once: one trip to memory)
+  s.deep = any ? min(deep, a.max_depth) : -1;
+  s.last = s.deep < 0 ? -1 : a.anc ? first - 1 : (int)min((int64_t)first + s.deep, (int64_t)a.win_rows - 1);
+  s.whole = a.anc ? first : s.last + 1;
+  if (a.anc)
+#pragma unroll
+    for (int d = 0; d < kAncStride; d++) {
+      const int64_t r = (int64_t)first + s.path[d];
+      s.path[d] = d <= s.deep && r >= 0 && r < a.win_rows ? (int)r : -1;
+      s.last = max(s.last, s.path[d]);
+      if (s.path[d] >= 0) s.whole = min(s.whole, s.path[d]);
+    }
   s.last = min(s.last, a.win_rows - 1);
+  s.whole = s.deep < 0 ? 0x7FFFFFFF : min(s.whole, a.win_rows);   // (a query that is none takes any weights)
   return s;
 }
+__device__ __forceinline__ int wave_max_i(int x) { return __builtin_amdgcn_readfirstlane(wave_reduce(x, [](int a, int b) { return max(a, b); })); }
 
-template <int HD>
-__device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, const QueryWin<HD> &q, int kvh, int row, const Sight &see, int w0,
-                                            unsigned char *v_lds, uint32_t *count) {
-  const int lane = threadIdx.x & 63, c = lane & 31, g = lane >> 5;
-  const size_t ld = (size_t)a.hkv * HD;
-  const uint16_t *vw = (const uint16_t *)a.vwin + (size_t)kvh * HD;
-  wave_fence();                                               // (the tile before has been read)
-  // values: rows into the LDS, what is not finite as zero
-  uint32_t odd = 0;                                           // rows of the tile that hold such a value
-  constexpr int kPieces = HD / 8;                             // 16-byte pieces of a row
+// A 16-byte piece of a value row without what is not finite in it; whether there was any
+__device__ __forceinline__ bool finite_piece(u32x4_t &v) {
+  uint32_t over = 0;                                          // bit 15 of a half: its magnitude is 0x7F80 or more
 #pragma unroll
-  for (int i = 0; i < kPieces / 2; i++) {
-    const int at = i * 64 + lane, vr = at / kPieces, piece = at % kPieces;
-    u32x4_t v = *(const u32x4_t *)(vw + (size_t)min(w0 + vr, a.win_rows - 1) * ld + piece * 8);
-    bool bad = false;
+  for (int j = 0; j < 4; j++) over |= (v[j] & 0x7FFF7FFFu) + 0x00800080u;
+  if ((over & 0x80008000u) == 0) return false;
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      const bool lo = (v[j] & 0x7F80u) == 0x7F80u, hi = (v[j] & 0x7F800000u) == 0x7F800000u;
-      v[j] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0xFFFFu : 0xFFFFFFFFu);
-      bad |= lo || hi;
-    }
-    *(u32x4_t *)(v_lds + value_piece<HD>(vr, piece)) = v;
-    uint64_t mask = __builtin_amdgcn_ballot_w64(bad);
-    while (mask) {                                            // (never, as a rule)
-      const int l = __builtin_ctzll(mask);
-      odd |= 1u << ((i * 64 + l) / kPieces);
-      mask &= mask - 1;
-    }
+  for (int j = 0; j < 4; j++) {
+    const bool lo = (v[j] & 0x7F80u) == 0x7F80u, hi = (v[j] & 0x7F800000u) == 0x7F800000u;
+    v[j] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0xFFFFu : 0xFFFFFFFFu);
   }
-  wave_fence();
-  const uint16_t *kr = (const uint16_t *)a.kwin + (size_t)min(w0 + c, a.win_rows - 1) * ld + (size_t)kvh * HD + 8 * g;
+  return true;
+}
+
+// Rows w0 .. w0 + 31.  key(t): the operands of 16 dims; v_lds: the value rows (those not finite as zeros; odd: the rows that held such), w0's at row v_row of it; count:
+// 1 KiB of this wavefront.
+template <int HD, typename K>
+__device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, const QueryWin<HD> &q, int kvh, const Sight &see, bool whole, int w0, K key, const unsigned char *v_lds,
+                                            int v_row, uint32_t odd, uint32_t *count) {
+  const int lane = threadIdx.x & 63, c = lane & 31, g = lane >> 5;
   f32x16_t s;
 #pragma unroll
   for (int i = 0; i < 16; i++) s[i] = 0.f;
 #pragma unroll
   for (int t = 0; t < HD / 16; t++) {
-    const u32x4_t k = *(const u32x4_t *)(kr + 16 * t);
+    const u32x4_t k = key(t);
     s = mul_bf16(k, q.hi[t], s);
     s = mul_bf16(k, q.lo[t], s);
   }
-  // how often the query sees each key
   const int first = a.base - a.n_blocks * kKv8Block;
-  float n[16];
-  if (a.anc) {
-    uint32_t *mine = count + c * 8;
-    if (g == 0) *(u32x4_t *)mine = u32x4_t{0, 0, 0, 0};
-    else *(u32x4_t *)(mine + 4) = u32x4_t{0, 0, 0, 0};
-    wave_fence();
-    if (g == 0)
-      for (int d = 0; d <= see.deep; d++) {
-        const uint32_t w = (uint32_t)(path_row(a, row, d) - w0);
-        if (w < 32u) mine[w >> 2] += 1u << (8 * (w & 3));
+  float n[16], top = -INFINITY;                               // how often the query sees each key
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < 16; i++) { n[i] = 1.f; s[i] *= a.scale; top = fmaxf(top, s[i]); }
+  } else {
+    if (a.anc) {
+      wave_fence();                                           // (the counts before have been read)
+      uint32_t *mine = count + c * 8;
+      *(u32x4_t *)(mine + 4 * g) = u32x4_t{0, 0, 0, 0};
+      wave_fence();
+      if (g == 0)
+#pragma unroll
+        for (int d = 0; d < kAncStride; d++) {
+          const uint32_t w = (uint32_t)(see.path[d] - w0);    // (-1 - w0: far beyond)
+          if (w < 32u) __hip_atomic_fetch_add(mine + (w >> 2), 1u << (8 * (w & 3)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+        }
+      wave_fence();
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const uint32_t w = mine[2 * i + g];
+#pragma unroll
+        for (int e = 0; e < 4; e++) n[4 * i + e] = (float)((w >> (8 * e)) & 0xFF);
       }
-    wave_fence();
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const uint32_t w = mine[2 * i + g];
-#pragma unroll
-      for (int j = 0; j < 4; j++) n[4 * i + j] = (float)((w >> (8 * j)) & 0xFF);
     }
-  }
-  float top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < 16; i++) {
-    const int w = w0 + 8 * (i >> 2) + 4 * g + (i & 3);
-    if (!a.anc) n[i] = w <= see.last ? 1.f : 0.f;
-    else n[i] += w < first && see.deep >= 0 ? 1.f : 0.f;
-    if (w >= a.win_rows) n[i] = 0.f;
-    s[i] = n[i] > 0.f ? s[i] * a.scale : -INFINITY;
-    top = fmaxf(top, s[i]);
+    for (int i = 0; i < 16; i++) {
+      const int w = w0 + 8 * (i >> 2) + 4 * g + (i & 3);
+      if (!a.anc) n[i] = w <= see.last ? 1.f : 0.f;
+      else n[i] += w < first && see.deep >= 0 ? 1.f : 0.f;
+      if (w >= a.win_rows) n[i] = 0.f;
+      s[i] = n[i] > 0.f ? s[i] * a.scale : -INFINITY;
+      top = fmaxf(top, s[i]);
+    }
   }
   r.raise(max_halves(top));
   const float m = r.m == -INFINITY ? 0.f : r.m;
+  if (whole) {
 #pragma unroll
-  for (int i = 0; i < 16; i++) {
-    s[i] = n[i] > 0.f ? n[i] * exp2_(s[i] - m) : 0.f;
-    r.l += s[i];
+    for (int i = 0; i < 16; i++) { s[i] = exp2_(s[i] - m); r.l += s[i]; }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      s[i] = n[i] > 0.f ? n[i] * exp2_(s[i] - m) : 0.f;
+      r.l += s[i];
+    }
   }
 #pragma unroll
   for (int h = 0; h < 2; h++) {
@@ -322,21 +342,21 @@ __device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, 
     }
 #pragma unroll
     for (int db = 0; db < HD / 32; db++) {
-      const u32x4_t v = value_fragment<HD>(v_lds, value_lane<HD>(lane), db, 16 * h);
+      const u32x4_t v = value_fragment<HD>(v_lds, value_lane<HD>(lane), db, v_row + 16 * h);
       r.o[db] = mul_bf16(v, hi, r.o[db]);
       r.o[db] = mul_bf16(v, lo, r.o[db]);
     }
   }
-  while (odd) {
+  while (odd) {                                               // (never, as a rule)
     const int w = __builtin_ctz(odd);
     odd &= odd - 1;
+    const uint16_t *vr = (const uint16_t *)a.vwin + (size_t)min(w0 + w, a.win_rows - 1) * ((size_t)a.hkv * HD) + (size_t)kvh * HD;
     float p = 0.f, seen = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i++)
       if (i == ((w >> 3) << 2 | (w & 3))) { p = s[i]; seen = n[i]; }
     p = __shfl(p, ((w >> 2) & 1) * 32 + c);
     seen = __shfl(seen, ((w >> 2) & 1) * 32 + c);
-    const uint16_t *vr = vw + (size_t)min(w0 + w, a.win_rows - 1) * ld;
 #pragma unroll
     for (int db = 0; db < HD / 32; db++)
 #pragma unroll
@@ -344,6 +364,108 @@ __device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, 
         const uint32_t b = vr[db * 32 + 8 * (i >> 2) + 4 * g + (i & 3)];
         if (seen > 0.f && (b & 0x7F80u) == 0x7F80u) r.o[db][i] = fmaf(p, bf16_bits_to_f32(b), r.o[db][i]);
       }
+  }
+}
+
+// Rows from w up to `stop` for WAVES wavefronts of 32 queries each: 64 rows at a time in the LDS (two buffers), keys in the order of the operands.
+template <int HD, int WAVES> struct WindowLds {
+  static constexpr int kKeys = 128 * HD, kBuffer = 2 * kKeys, kCounts = 2 * kBuffer, kOdd = kCounts + WAVES * 1024, kLast = kOdd + 24, total = kLast + WAVES * 4;
+};
+template <int HD, int WAVES>
+__device__ __forceinline__ void window_together(const Attn8Args &a, Running<HD> &r, const float *qp, int row, bool real, int kvh, int w, int stop, unsigned char *lds) {
+  using L = WindowLds<HD, WAVES>;
+  constexpr int kPieces = HD / 8, kEach = 64 * kPieces / (WAVES * 64);   // 16-byte pieces of a row; of the keys (and the values) per thread
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5;
+  const size_t ld = (size_t)a.hkv * HD;
+  const uint16_t *kw = (const uint16_t *)a.kwin + (size_t)kvh * HD, *vw = (const uint16_t *)a.vwin + (size_t)kvh * HD;
+  uint32_t *odd = (uint32_t *)(lds + L::kOdd);                // [3][2]: of a tile's halves, the rows with values that are not finite
+  int *lasts = (int *)(lds + L::kLast);
+  u32x4_t key[kEach], val[kEach];
+  auto fetch = [&](int w0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kEach; i++) {
+      const int at = i * WAVES * 64 + tid;
+      const size_t from = (size_t)min(w0 + at / kPieces, a.win_rows - 1) * ld + at % kPieces * 8;
+      key[i] = *(const u32x4_t *)(kw + from);
+      val[i] = *(const u32x4_t *)(vw + from);
+    }
+  };
+  auto put = [&](int tile) __attribute__((always_inline)) {
+    unsigned char *buf = lds + (tile & 1) * L::kBuffer;
+#pragma unroll
+    for (int i = 0; i < kEach; i++) {
+      const int at = i * WAVES * 64 + tid, wr = at / kPieces, piece = at % kPieces;
+      *(u32x4_t *)(buf + (wr >> 5) * 64 * HD + (piece >> 1) * 1024 + ((piece & 1) * 32 + (wr & 31)) * 16) = key[i];
+      if (finite_piece(val[i])) __hip_atomic_fetch_or(odd + tile % 3 * 2 + (wr >> 5), 1u << (wr & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      *(u32x4_t *)(buf + L::kKeys + value_piece<HD>(wr, piece)) = val[i];
+    }
+    if (tid < 2) odd[(tile + 1) % 3 * 2 + tid] = 0;           // (last read two tiles ago)
+  };
+  fetch(w);
+  const Sight see = sight_of(a, row, real);
+  const QueryWin<HD> q = load_query_win<HD>(qp, g);
+  const int own_last = wave_max_i(see.last), whole = -wave_max_i(-see.whole);
+  if (lane == 0) lasts[wave] = own_last;
+  if (tid < 2) odd[tid] = 0;
+  __syncthreads();
+  int last = lasts[0];
+#pragma unroll
+  for (int i = 1; i < WAVES; i++) last = max(last, lasts[i]);
+  last = min(__builtin_amdgcn_readfirstlane(last), stop - 1);
+  if (w > last) return;
+  put(0);
+  for (int tile = 0; w <= last; tile++, w += 64) {
+    __syncthreads();
+    if (w + 64 <= last) fetch(w + 64);
+    const unsigned char *buf = lds + (tile & 1) * L::kBuffer;
+#pragma unroll 1
+    for (int h = 0; h < 2; h++) {
+      const int w0 = w + 32 * h;
+      if (w0 > own_last || w0 >= stop) break;
+      window_step<HD>(a, r, q, kvh, see, w0 + 32 <= whole, w0, [&](int t) { return *(const u32x4_t *)(buf + h * 64 * HD + t * 1024 + lane * 16); }, buf + L::kKeys, 32 * h,
+                      __builtin_amdgcn_readfirstlane((int)odd[tile % 3 * 2 + h]), (uint32_t *)(lds + L::kCounts) + wave * 256);
+    }
+    if (w + 64 <= last) put(tile + 1);
+  }
+}
+
+// The same for a wavefront alone: rows w .. w + 31, then `by` further on, straight into its registers; v_lds: 64 * HD + 1024 bytes of its own
+template <int HD>
+__device__ __forceinline__ void window_alone(const Attn8Args &a, Running<HD> &r, const float *qp, int row, bool real, int kvh, int w, int by, int stop, unsigned char *v_lds) {
+  const int lane = threadIdx.x & 63, c = lane & 31, g = lane >> 5;
+  const size_t ld = (size_t)a.hkv * HD;
+  constexpr int kPieces = HD / 8;
+  u32x4_t key[HD / 16], val[HD / 16];
+  auto fetch = [&](int w0) __attribute__((always_inline)) {
+    const uint16_t *kr = (const uint16_t *)a.kwin + (size_t)min(w0 + c, a.win_rows - 1) * ld + (size_t)kvh * HD + 8 * g;
+#pragma unroll
+    for (int i = 0; i < HD / 16; i++) key[i] = *(const u32x4_t *)(kr + 16 * i);
+#pragma unroll
+    for (int i = 0; i < HD / 16; i++) {
+      const int at = i * 64 + lane;
+      val[i] = *(const u32x4_t *)((const uint16_t *)a.vwin + (size_t)min(w0 + at / kPieces, a.win_rows - 1) * ld + (size_t)kvh * HD + at % kPieces * 8);
+    }
+  };
+  fetch(w);                                                   // (the queries, paths and rows in one trip to memory)
+  const Sight see = sight_of(a, row, real);
+  const QueryWin<HD> q = load_query_win<HD>(qp, g);
+  const int last = min(wave_max_i(see.last), stop - 1), whole = -wave_max_i(-see.whole);
+  for (; w <= last; w += by) {
+    wave_fence();                                             // (the tile before has been read)
+    uint32_t odd = 0;
+#pragma unroll
+    for (int i = 0; i < HD / 16; i++) {
+      const int at = i * 64 + lane;
+      uint64_t mask = __builtin_amdgcn_ballot_w64(finite_piece(val[i]));
+      *(u32x4_t *)(v_lds + value_piece<HD>(at / kPieces, at % kPieces)) = val[i];
+      while (mask) {
+        odd |= 1u << ((i * 64 + __builtin_ctzll(mask)) / kPieces);
+        mask &= mask - 1;
+      }
+    }
+    wave_fence();
+    window_step<HD>(a, r, q, kvh, see, w + 32 <= whole, w, [&](int t) { return key[t]; }, v_lds, 0, odd, (uint32_t *)(v_lds + 64 * HD));
+    if (w + by <= last) fetch(w + by);
   }
 }
 
@@ -388,7 +510,7 @@ template <int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void attention8_wide_kernel(Attn8Args a, Plan8 plan) {
   constexpr int kCodes = 2 * kKv8Block * HD, kUnits = kCodes / 16, kThreads = WAVES * 64, kEach = kUnits / kThreads;   // of 16 codes, per thread
   static_assert(kEach * kThreads == kUnits, "whole units");
-  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // 2 x 2 kCodes; the window: value rows and counts of each wavefront
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // 2 x 2 kCodes, or WindowLds
   Place8 at;
   if (!place_of(plan, a.hkv, at)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, g = lane >> 5;
@@ -440,18 +562,159 @@ __global__ __launch_bounds__(WAVES * 64) void attention8_wide_kernel(Attn8Args a
       }
       __syncthreads();
     }
+    r.l *= kCutSum;
     const float up = exp2_((float)top_exp);
 #pragma unroll
     for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
   } else {
-    const int w_begin = (at.part - plan.block_parts) * plan.win_part, w_stop = min(w_begin + plan.win_part, a.win_rows);
-    const Sight see = sight_of(a, row, real);
-    const int last = __builtin_amdgcn_readfirstlane(wave_reduce(see.last, [](int x, int y) { return max(x, y); }));
-    unsigned char *mine = lds + wave * (64 * HD + 1024);
-    if (w_begin <= last) {
-      const QueryWin<HD> q = load_query_win<HD>(qp, g);
-      for (int w = w_begin; w < w_stop && w <= last; w += 32) window_step<HD>(a, r, q, at.kvh, row, see, w, mine, (uint32_t *)(mine + 64 * HD));
+    const int w_begin = (at.part - plan.block_parts) * plan.win_part;
+    window_together<HD, WAVES>(a, r, qp, row, real, at.kvh, w_begin, min(w_begin + plan.win_part, a.win_rows), lds);
+  }
+  const float l = sum_halves(r.l);
+  if (!real || (parts == 1 && a.depth[row] < 0)) return;
+#pragma unroll
+  for (int db = 0; db < HD / 32; db++) put_dims<HD>(a, query, at.part, parts, db, g, r.o[db], r.m, l);
+}
+
+// More than 128 queries: eight wavefronts of 32 queries in two teams of four, one of each on a SIMD, that take turns: while one team's products run (outputs of block n - 1, scores of block
+// n), the other makes weights out of its scores (block n or n - 1) and widens its share of the keys and values to come.  A barrier ends each turn, and
+// team 1 is a turn behind.  Keys are needed a block ahead of values; step n of the staging is keys n and values n - 1, two buffers each: team 0 puts its share of step
+// n + 1 there while team 1 is at its products n, team 1 its share of step n + 2 while team 0 is at n + 1; what they write over has been read by both.
+// Without turns the wavefronts of a SIMD ran in step, and products, weights and LDS reads one behind the other: @@.
+template <int HD>
+__global__ __launch_bounds__(512) void attention8_teams_kernel(Attn8Args a, Plan8 plan) {
+  constexpr int kHalf = kKv8Block * HD, kUnits = 2 * kHalf / 16, kEach = kUnits / 512;   // codes of a block's keys (or values); units of 16, per thread
+  static_assert(kEach * 512 == kUnits, "whole units");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // keys, keys, values, values: 2 kHalf each, or WindowLds
+  Place8 at;
+  if (!place_of(plan, a.hkv, at)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, g = lane >> 5;
+  const int G = a.hq / a.hkv, index = (at.qb * 8 + wave) * 32 + c, parts = plan.block_parts + plan.win_parts;
+  const bool real = index < a.rows * G;
+  const int row = real ? index / G : a.rows - 1;
+  const size_t query = (size_t)row * a.hq + at.kvh * G + (real ? index % G : 0);
+  const float *qp = a.q + query * HD;
+  Running<HD> r;
+  r.clear();
+  if (at.part < plan.block_parts) {
+    const int b0 = range_at(a.n_blocks, plan.block_parts, at.part), n = range_at(a.n_blocks, plan.block_parts, at.part + 1) - b0, team = wave >> 2;
+    const size_t block_bytes = kv8_block_bytes(a.hkv, HD);
+    const unsigned char *base = a.cache8 + (size_t)b0 * block_bytes + (size_t)at.kvh * 2 * kHalf + tid * 16;
+    const unsigned char *exps = a.cache8 + (size_t)b0 * block_bytes + (size_t)a.hkv * 2 * kHalf + 2 * at.kvh;
+    u32x4_t next[kEach];
+    auto fetch = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kEach; i++) {
+        const bool values = (i * 512 + wave * 64) * 2 >= kUnits;
+        next[i] = *(const u32x4_t *)(base + (size_t)min(max(step - (values ? 1 : 0), 0), n - 1) * block_bytes + i * 512 * 16);
+      }
+    };
+    auto put = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kEach; i++) {
+        const int piece = i * 8 + wave;                       // 64 units
+        const bool values = piece * 128 >= kUnits;
+        unsigned char *p = lds + (values ? 4 * kHalf + ((step - 1) & 1) * 2 * kHalf + (piece - kUnits / 128) * 2048 : (step & 1) * 2 * kHalf + piece * 2048) + lane * 16;
+        u32x4_t x, y;
+        widen(next[i], x, y);
+        *(u32x4_t *)p = x;
+        *(u32x4_t *)(p + 1024) = y;
+      }
+    };
+    auto end_turn = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0xC07F);                     // this wavefront's LDS accesses done; loads from memory go on
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    fetch(0);
+    const Query8<HD> q = load_query8<HD>(qp, g, a.scale);
+    put(0);                                                   // (its values: any block's, read by nobody)
+    fetch(1);
+    int top_exp = -127;
+    f32x16_t s[2];
+    u32x4_t p[4];                                             // weights of 16 keys each
+    // A turn's products: the outputs of block step - 1, the scores of block step, kAhead operands on their way from the LDS at a time (in the compiler's own order one to three
+    // were, and the products waited for them: @@)
+    constexpr int kOut = 4 * (HD / 32), kScore = 2 * (HD / 16), kAhead = 6;
+    auto products = [&](auto with_outputs, auto with_scores, int step) __attribute__((always_inline)) {
+      constexpr int kFrom = decltype(with_outputs)::value ? 0 : kOut, kTo = decltype(with_scores)::value ? kOut + kScore : kOut;
+      const unsigned char *v = lds + 4 * kHalf + ((step - 1) & 1) * 2 * kHalf + lane * 16, *k = lds + (step & 1) * 2 * kHalf + lane * 16;
+      auto operand = [&](int i) __attribute__((always_inline)) {
+        const int h = i / (HD / 32), db = i % (HD / 32), t = (i - kOut) / 2, kt = (i - kOut) % 2;
+        return i < kOut ? *(const u32x4_t *)(v + ((h >> 1) * (HD / 16) + 2 * db + (h & 1)) * 1024) : *(const u32x4_t *)(k + (kt * (HD / 16) + t) * 1024);
+      };
+      u32x4_t f[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; i++) f[i] = operand(kFrom + i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = kFrom; i < kTo; i++) {
+        const u32x4_t &x = f[(i - kFrom) % kAhead];
+        if (i < kOut) r.o[i % (HD / 32)] = mul_f16(x, p[i / (HD / 32)], r.o[i % (HD / 32)]);
+        else {
+          f32x16_t &to = s[(i - kOut) % 2];
+          if (i - kOut < 2)
+#pragma unroll
+            for (int e = 0; e < 16; e++) to[e] = 0.f;
+          to = mul_f16(x, q.f[(i - kOut) / 2], to);
+        }
+        if (i + kAhead < kTo) f[(i - kFrom) % kAhead] = operand(i + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    using Yes = std::integral_constant<bool, true>;
+    using No = std::integral_constant<bool, false>;
+    uint32_t e = *(const uint16_t *)exps;                     // the next weights' block
+    auto weights = [&](int step) __attribute__((always_inline)) {
+      const uint32_t now = __builtin_amdgcn_readfirstlane((int)e);
+      e = *(const uint16_t *)(exps + (size_t)min(step + 1, n - 1) * block_bytes);
+      weigh<HD>(r, q.scale, now, top_exp, s, p);
+    };
+    end_turn();
+    if (team == 0) {
+      products(No{}, Yes{}, 0);
+      end_turn();
+      for (int i = 0; i < n - 1; i++) {
+        weights(i);
+        put(i + 1);
+        fetch(i + 2);
+        end_turn();
+        products(Yes{}, Yes{}, i + 1);
+        end_turn();
+      }
+      weights(n - 1);
+      put(n);
+      end_turn();
+      products(Yes{}, No{}, n);
+      end_turn();
+    } else {
+      put(1);
+      fetch(2);
+      end_turn();
+      products(No{}, Yes{}, 0);
+      end_turn();
+      for (int i = 0; i < n - 1; i++) {
+        weights(i);
+        put(i + 2);
+        fetch(i + 3);
+        end_turn();
+        products(Yes{}, Yes{}, i + 1);
+        end_turn();
+      }
+      weights(n - 1);
+      end_turn();
+      products(Yes{}, No{}, n);
     }
+    r.l *= kCutSum;
+    const float up = exp2_((float)top_exp);
+#pragma unroll
+    for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
+  } else {
+    const int w_begin = (at.part - plan.block_parts) * plan.win_part;
+    window_together<HD, 8>(a, r, qp, row, real, at.kvh, w_begin, min(w_begin + plan.win_part, a.win_rows), lds);
   }
   const float l = sum_halves(r.l);
   if (!real || (parts == 1 && a.depth[row] < 0)) return;
@@ -503,19 +766,13 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention8_few_kernel(Attn8Arg
       block_step<HD>(r, q, now_exps, top_exp, [&](int kt, int s) { return half(now[kt * (HD / 32) + s / 2], s & 1); },
                      [&](int kt, int db, int h) { return half(now[kPieces / 2 + kt * (HD / 32) + db], h); });
     }
+    r.l *= kCutSum;
     const float up = exp2_((float)top_exp);
 #pragma unroll
     for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
   } else {
     const int w_begin = (part - plan.block_parts) * plan.win_part, w_stop = min(w_begin + plan.win_part, a.win_rows);
-    const Sight see = sight_of(a, row, real);
-    const int last = __builtin_amdgcn_readfirstlane(wave_reduce(see.last, [](int x, int y) { return max(x, y); }));
-    unsigned char *mine = lds + wave * (64 * HD + 1024);
-    if (w_begin + 32 * wave <= last) {
-      const QueryWin<HD> q = load_query_win<HD>(qp, g);
-      for (int w = w_begin + 32 * wave; w < w_stop && w <= last; w += 32 * kFewWaves)
-        window_step<HD>(a, r, q, kvh, row, see, w, mine, (uint32_t *)(mine + 64 * HD));
-    }
+    window_alone<HD>(a, r, qp, row, real, kvh, w_begin + 32 * wave, 32 * kFewWaves, w_stop, lds + wave * (64 * HD + 1024));
     __syncthreads();                                          // the value rows make place for the outputs
   }
   float *outs = (float *)lds;                                 // [wave][db][16][64]
@@ -544,25 +801,56 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention8_few_kernel(Attn8Arg
   put_dims<HD>(a, query, part, parts, wave, g, o, all.m, all.l);
 }
 
-// The parts of a query put together, in ascending order: HD / 4 threads for each query
-template <int HD>
+// The parts of a query put together: HD / 4 threads take a query's dims, GROUPS of them every GROUPS-th part each (up to eight on their way at a time), then the
+// groups' sums in ascending order.
+template <int HD, int GROUPS>
 __global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a, int parts) {
-  constexpr int kThreads = HD / 4;
-  const size_t query = (size_t)blockIdx.x * (256 / kThreads) + threadIdx.x / kThreads;
-  const int d = threadIdx.x % kThreads * 4;
-  if (query >= (size_t)a.rows * a.hq || a.depth[query / a.hq] < 0) return;
+  constexpr int kThreads = HD / 4, kQueries = 256 / (kThreads * GROUPS);
+  static_assert(kQueries >= 1, "threads");
+  __shared__ f32x4_t sums[GROUPS > 1 ? 256 : 1];
+  __shared__ float2 stats[GROUPS > 1 ? kQueries * GROUPS : 1];
+  const int in_query = threadIdx.x % (kThreads * GROUPS), slot = threadIdx.x / (kThreads * GROUPS), group = in_query / kThreads, d = in_query % kThreads * 4;
+  const size_t all_queries = (size_t)a.rows * a.hq, query = (size_t)blockIdx.x * kQueries + slot, at = query < all_queries ? query : all_queries - 1;
   RowMerge all;
   f32x4_t o{0.f, 0.f, 0.f, 0.f};
-  const float *p = a.part;
-  for (int i = 0; i < parts; i++, p += part_floats<HD>(a)) {
-    const float2 s = ((const float2 *)p)[query];
-    const f32x4_t x = *(const f32x4_t *)(p + (size_t)a.rows * a.hq * 2 + query * HD + d);
-    if (s.y == 0.f) continue;
-    float weight;
-    const float turn = all.step(s.x, s.y, weight);
+  const size_t part_size = part_floats<HD>(a);
+  for (int i0 = group; i0 < parts; i0 += 8 * GROUPS) {
+    float2 s[8];
+    f32x4_t x[8];
 #pragma unroll
-    for (int j = 0; j < 4; j++) o[j] = fmaf(x[j], weight, o[j] * turn);
+    for (int j = 0; j < 8; j++) {
+      const float *p = a.part + min(i0 + j * GROUPS, parts - 1) * part_size;
+      s[j] = ((const float2 *)p)[at];
+      x[j] = *(const f32x4_t *)(p + all_queries * 2 + at * HD + d);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      if (i0 + j * GROUPS >= parts || s[j].y == 0.f) continue;   // (it saw nothing: its outputs may be anything)
+      float weight;
+      const float turn = all.step(s[j].x, s[j].y, weight);
+#pragma unroll
+      for (int e = 0; e < 4; e++) o[e] = fmaf(x[j][e], weight, o[e] * turn);
+    }
   }
+  if constexpr (GROUPS > 1) {
+    sums[threadIdx.x] = o;
+    if (d == 0) stats[slot * GROUPS + group] = make_float2(all.m, all.l);
+    __syncthreads();
+    if (group > 0) return;
+    all = RowMerge{};
+    o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < GROUPS; j++) {
+      const float2 s = stats[slot * GROUPS + j];
+      if (s.y == 0.f) continue;
+      float weight;
+      const float turn = all.step(s.x, s.y, weight);
+      const f32x4_t x = sums[threadIdx.x + j * kThreads];
+#pragma unroll
+      for (int e = 0; e < 4; e++) o[e] = fmaf(x[e], weight, o[e] * turn);
+    }
+  }
+  if (query >= all_queries || a.depth[query / a.hq] < 0) return;
   const float inv = all.l == 0.f ? 0.f : 1.f / all.l;
   *(u32x2_t *)((uint16_t *)a.out + query * HD + d) = u32x2_t{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
 }
@@ -573,21 +861,34 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
   p.waves = queries <= 32 ? 0 : queries <= 64 ? 2 : queries <= 128 ? 4 : 8;
   const int of = p.waves ? 32 * p.waves : 32;
   p.query_blocks = (int)((queries + of - 1) / of);
-  const int64_t units = (int64_t)hkv * p.query_blocks;
-  const int64_t want = 256, most = (n_blocks + (p.waves ? 0 : kFewWaves - 1)) / (p.waves ? 1 : kFewWaves);
-  p.block_parts = n_blocks == 0 ? 0 : (int)(want / units < 1 ? 1 : want / units > most ? most : want / units);
   p.win_part = 256;
   while ((win_rows + p.win_part - 1) / p.win_part > 8) p.win_part *= 2;
   p.win_parts = (win_rows + p.win_part - 1) / p.win_part;
+  const int64_t units = (int64_t)hkv * p.query_blocks;
+  // the workgroups that the compute units hold at once (a workgroup of eight wavefronts fills one), the window's among them
+  const int64_t room = p.waves == 8 ? 256 : 512, most = p.waves ? n_blocks : (n_blocks + kFewWaves - 1) / kFewWaves;
+  const int64_t fit = room / units - p.win_parts, parts = fit < 1 ? (room + units - 1) / units : fit;
+  p.block_parts = n_blocks == 0 ? 0 : (int)(parts < 1 ? 1 : parts > most ? most : parts);
   return p;
 }
 
 template <int HD, int WAVES> hipError_t launch_wide(const Attn8Args &a, const Plan8 &p, unsigned grid, hipStream_t st) {
-  constexpr int kLds = 512 * HD > WAVES * (64 * HD + 1024) ? 512 * HD : WAVES * (64 * HD + 1024);
+  constexpr int kLds = WindowLds<HD, WAVES>::total;
+  static_assert(kLds >= 512 * HD, "keys and values fit");
   static bool allowed[64] = {};
   const hipError_t e = allow_lds((const void *)attention8_wide_kernel<HD, WAVES>, kLds, allowed);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((attention8_wide_kernel<HD, WAVES>), dim3(grid), dim3(WAVES * 64), kLds, st, a, p);
+  return hipGetLastError();
+}
+
+template <int HD> hipError_t launch_teams(const Attn8Args &a, const Plan8 &p, unsigned grid, hipStream_t st) {
+  constexpr int kLds = WindowLds<HD, 8>::total;
+  static_assert(kLds >= 512 * HD, "keys and values fit");
+  static bool allowed[64] = {};
+  const hipError_t e = allow_lds((const void *)attention8_teams_kernel<HD>, kLds, allowed);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(attention8_teams_kernel<HD>, dim3(grid), dim3(512), kLds, st, a, p);
   return hipGetLastError();
 }
 
@@ -606,11 +907,20 @@ template <int HD> hipError_t launch_hd(const Attn8Args &a, hipStream_t st) {
     e = hipGetLastError();
   } else if (p.waves == 2) e = launch_wide<HD, 2>(a, p, (unsigned)grid, st);
   else if (p.waves == 4) e = launch_wide<HD, 4>(a, p, (unsigned)grid, st);
-  else e = launch_wide<HD, 8>(a, p, (unsigned)grid, st);
+  else e = launch_teams<HD>(a, p, (unsigned)grid, st);
   if (e != hipSuccess || parts == 1) return e;
-  const int64_t groups = ((int64_t)a.rows * a.hq * (HD / 4) + 255) / 256;
-  if (groups > 0x7FFFFFFFll) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(attention8_merge_kernel<HD>, dim3((unsigned)groups), dim3(256), 0, st, a, parts);
+  const int64_t queries = (int64_t)a.rows * a.hq;
+  if (parts <= 8) {
+    constexpr int kEach = 1024 / HD;
+    const int64_t groups = (queries + kEach - 1) / kEach;
+    if (groups > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((attention8_merge_kernel<HD, 1>), dim3((unsigned)groups), dim3(256), 0, st, a, parts);
+  } else {
+    constexpr int kEach = 128 / HD;
+    const int64_t groups = (queries + kEach - 1) / kEach;
+    if (groups > 0x7FFFFFFFll) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((attention8_merge_kernel<HD, 8>), dim3((unsigned)groups), dim3(256), 0, st, a, parts);
+  }
   return hipGetLastError();
 }
 
