@@ -100,9 +100,16 @@ __device__ __forceinline__ void widen(const u32x4_t &w, u32x4_t &first, u32x4_t 
   second = u32x4_t{f16_of_codes<false>(w.z, 1.f), f16_of_codes<true>(w.z, 1.f), f16_of_codes<false>(w.w, 1.f), f16_of_codes<true>(w.w, 1.f)};
 }
 
-// The work of a launch: parts 0 .. blocks - 1 are ranges of the cache's blocks, the others ranges of the window.
-struct Plan8 { int waves, query_blocks, block_parts, win_parts, win_part; };   // waves: of 32 queries each in a workgroup; 0: few queries
+// The work of a launch.  waves: of 32 queries each in a workgroup; 0: few queries.  Parts 0 .. block_parts - 1 are ranges of the cache's blocks, the others ranges of win_part
+// rows of the window.  Eight wavefronts: the last range of blocks goes on into the whole window instead (win_parts 0), and has as many blocks fewer as the
+// rows that a block of queries sees cost (win_cost: per query block, blocks; win_base: for the first, both in 1/16).
+struct Plan8 { int waves, query_blocks, block_parts, win_parts, win_part, win_base, win_cost; };
 __host__ __device__ inline int range_at(int n, int parts, int i) { return (int)((int64_t)n * i / parts); }
+__device__ __forceinline__ int joined_range_at(const Plan8 &p, int n, int qb, int i) {
+  if (i == p.block_parts) return n;
+  const int64_t all = 16 * (int64_t)n + p.win_base + (int64_t)p.win_cost * qb;
+  return (int)min(all * i / p.block_parts / 16, (int64_t)n);
+}
 
 // Running softmax of 32 queries (this lane's)
 template <int HD> struct Running {
@@ -596,8 +603,10 @@ __global__ __launch_bounds__(512) void attention8_teams_kernel(Attn8Args a, Plan
   const float *qp = a.q + query * HD;
   Running<HD> r;
   r.clear();
-  if (at.part < plan.block_parts) {
-    const int b0 = range_at(a.n_blocks, plan.block_parts, at.part), n = range_at(a.n_blocks, plan.block_parts, at.part + 1) - b0, team = wave >> 2;
+  const int b0 = at.part < plan.block_parts ? joined_range_at(plan, a.n_blocks, at.qb, at.part) : 0;
+  const int n = at.part < plan.block_parts ? joined_range_at(plan, a.n_blocks, at.qb, at.part + 1) - b0 : 0;
+  if (n > 0) {
+    const int team = wave >> 2;
     const size_t block_bytes = kv8_block_bytes(a.hkv, HD);
     const unsigned char *base = a.cache8 + (size_t)b0 * block_bytes + (size_t)at.kvh * 2 * kHalf + tid * 16;
     const unsigned char *exps = a.cache8 + (size_t)b0 * block_bytes + (size_t)a.hkv * 2 * kHalf + 2 * at.kvh;
@@ -712,10 +721,11 @@ __global__ __launch_bounds__(512) void attention8_teams_kernel(Attn8Args a, Plan
     const float up = exp2_((float)top_exp);
 #pragma unroll
     for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
-  } else {
-    const int w_begin = (at.part - plan.block_parts) * plan.win_part;
-    window_together<HD, 8>(a, r, qp, row, real, at.kvh, w_begin, min(w_begin + plan.win_part, a.win_rows), lds);
+    __syncthreads();
   }
+  const int w_begin = plan.win_parts ? (at.part - plan.block_parts) * plan.win_part : 0;
+  if (plan.win_parts ? at.part >= plan.block_parts : at.part == plan.block_parts - 1)
+    window_together<HD, 8>(a, r, qp, row, real, at.kvh, w_begin, plan.win_parts ? min(w_begin + plan.win_part, a.win_rows) : a.win_rows, lds);
   const float l = sum_halves(r.l);
   if (!real || (parts == 1 && a.depth[row] < 0)) return;
 #pragma unroll
@@ -857,17 +867,28 @@ __global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a, int 
 
 Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
   Plan8 p{};
-  const int64_t queries = (int64_t)rows * (hq / hkv);
+  const int G = hq / hkv;
+  const int64_t queries = (int64_t)rows * G;
   p.waves = queries <= 32 ? 0 : queries <= 64 ? 2 : queries <= 128 ? 4 : 8;
   const int of = p.waves ? 32 * p.waves : 32;
   p.query_blocks = (int)((queries + of - 1) / of);
-  p.win_part = 256;
+  const int64_t units = (int64_t)hkv * p.query_blocks;
+  p.win_part = win_rows <= 256 && p.waves < 8 ? 64 : 256;
   while ((win_rows + p.win_part - 1) / p.win_part > 8) p.win_part *= 2;
   p.win_parts = (win_rows + p.win_part - 1) / p.win_part;
-  const int64_t units = (int64_t)hkv * p.query_blocks;
-  // the workgroups that the compute units hold at once (a workgroup of eight wavefronts fills one), the window's among them
-  const int64_t room = p.waves == 8 ? 256 : 512, most = p.waves ? n_blocks : (n_blocks + kFewWaves - 1) / kFewWaves;
-  const int64_t fit = room / units - p.win_parts, parts = fit < 1 ? (room + units - 1) / units : fit;
+  // as many workgroups as the compute units hold at once (one of eight wavefronts fills one)
+  const int64_t most = p.waves ? n_blocks : (n_blocks + kFewWaves - 1) / kFewWaves;
+  if (p.waves == 8 && n_blocks > 0) {
+    p.win_parts = 0;
+    const int64_t parts = (256 + units / 2) / units;
+    p.block_parts = (int)(parts < 1 ? 1 : parts > most ? most : parts);
+    // rows of the window that the first query block sees, if they are a chain, and how many more each further one does; 64 of them cost 1.5 blocks
+    const int each = of / G < 1 ? 1 : of / G, recent = win_rows > rows ? win_rows - rows : 0;
+    p.win_base = (recent + each) * 24 / 64;
+    p.win_cost = each * 24 / 64;
+    return p;
+  }
+  const int64_t parts = 512 / units - p.win_parts;
   p.block_parts = n_blocks == 0 ? 0 : (int)(parts < 1 ? 1 : parts > most ? most : parts);
   return p;
 }
@@ -892,6 +913,14 @@ template <int HD> hipError_t launch_teams(const Attn8Args &a, const Plan8 &p, un
   return hipGetLastError();
 }
 
+template <int HD, int GROUPS> hipError_t launch_merge(const Attn8Args &a, int parts, hipStream_t st) {
+  constexpr int kEach = 1024 / (HD * GROUPS);                 // queries of a workgroup
+  const int64_t grid = ((int64_t)a.rows * a.hq + kEach - 1) / kEach;
+  if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((attention8_merge_kernel<HD, GROUPS>), dim3((unsigned)grid), dim3(256), 0, st, a, parts);
+  return hipGetLastError();
+}
+
 template <int HD> hipError_t launch_hd(const Attn8Args &a, hipStream_t st) {
   const Plan8 p = plan8(a.rows, a.hq, a.hkv, a.n_blocks, a.win_rows);
   const int parts = p.block_parts + p.win_parts;
@@ -909,19 +938,9 @@ template <int HD> hipError_t launch_hd(const Attn8Args &a, hipStream_t st) {
   else if (p.waves == 4) e = launch_wide<HD, 4>(a, p, (unsigned)grid, st);
   else e = launch_teams<HD>(a, p, (unsigned)grid, st);
   if (e != hipSuccess || parts == 1) return e;
-  const int64_t queries = (int64_t)a.rows * a.hq;
-  if (parts <= 8) {
-    constexpr int kEach = 1024 / HD;
-    const int64_t groups = (queries + kEach - 1) / kEach;
-    if (groups > 0x7FFFFFFFll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((attention8_merge_kernel<HD, 1>), dim3((unsigned)groups), dim3(256), 0, st, a, parts);
-  } else {
-    constexpr int kEach = 128 / HD;
-    const int64_t groups = (queries + kEach - 1) / kEach;
-    if (groups > 0x7FFFFFFFll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((attention8_merge_kernel<HD, 8>), dim3((unsigned)groups), dim3(256), 0, st, a, parts);
-  }
-  return hipGetLastError();
+  if (parts <= 8) return launch_merge<HD, 1>(a, parts, st);
+  if (parts <= 16) return launch_merge<HD, 2>(a, parts, st);
+  return parts <= 32 ? launch_merge<HD, 4>(a, parts, st) : launch_merge<HD, 8>(a, parts, st);
 }
 
 }  // namespace
