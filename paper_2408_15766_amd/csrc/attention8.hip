@@ -233,11 +233,6 @@ template <int HD> __device__ __forceinline__ QueryWin<HD> load_query_win(const f
 }
 // What a query sees of the window: rows below `first`, and its path: rows path[0 .. deep] (anc; -1: outside), or first .. first + deep
 struct Sight { int deep, last, whole, path[kAncStride]; };    // last: the highest row it sees; whole: the rows below this one it sees all, once each
-// Orders this wavefront's LDS accesses for the compiler (the hardware keeps their order)
-__device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
 __device__ __forceinline__ Sight sight_of(const Attn8Args &a, int row, bool any) {
   Sight s;
   const int first = a.base - a.n_blocks * kKv8Block;

@@ -32,6 +32,11 @@ template <bool HI> __device__ __forceinline__ uint32_t f16_of_codes(uint32_t w, 
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, HI));
 }
 
+// Orders this wavefront's LDS accesses for the compiler (the hardware keeps their order)
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 // Sixteen consecutive values to fp32; the pointer is aligned to 16 bytes
 __device__ __forceinline__ void load16(const float *p, float (&x)[16]) {
 #pragma unroll

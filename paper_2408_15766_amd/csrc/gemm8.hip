@@ -324,13 +324,11 @@ struct Tile8 {
   static constexpr int kWaves = WM * WN, kTok = WM * TB * 32, kRows = WN * WB * 32;
   static constexpr int kX = kTok * 64, kW = kRows * 64;       // bytes of a stage
   static constexpr int kXLoads = kX / 1024 / kWaves, kWLoads = kW / 1024 / kWaves;   // 1 KiB copies per wavefront and stage
-  // exponents: 64 bytes per 16-row block, tokens first; a wavefront copies those of kExp blocks into its 256 bytes
-  static constexpr int kBlocks = (kTok + kRows) / 16, kExp = kBlocks / kWaves, kE = kWaves * 256;
+  // exponents: 64 bytes per 16-row block, tokens first; a wavefront copies those of four blocks (those past the end: the last again)
+  static constexpr int kBlocks = (kTok + kRows) / 16, kE = kWaves * 256;
   static constexpr int kLoads = kXLoads + kWLoads + 1;
-  static_assert(kXLoads * kWaves * 1024 == kX && kWLoads * kWaves * 1024 == kW && kExp * kWaves == kBlocks && (kExp == 2 || kExp == 4), "whole copies");
-  static __device__ __forceinline__ constexpr int exp_at(int block32) { return block32 * (256 / (kExp / 2)); }   // where those of 32 rows lie
+  static_assert(kXLoads * kWaves * 1024 == kX && kWLoads * kWaves * 1024 == kW && kBlocks <= 4 * kWaves, "whole copies");
 };
-constexpr int kStages8 = 4;
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((address_space(3))) void lds_void;
@@ -364,17 +362,23 @@ __device__ __forceinline__ Wide8 widen8(const Half8 &f, uint32_t e) {
   return r;
 }
 
-template <typename OUT, bool VEC, int WM, int WN, int TB, int WB>
+template <typename OUT, bool VEC, int WM, int WN, int TB, int WB, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a) {
   using L = Tile8<WM, WN, TB, WB>;
   constexpr bool kExact = sizeof(OUT) == 4;
+  static_assert(STAGES == 4 || STAGES == 8, "written out below");
+  constexpr int kMore = STAGES == 8;
   __shared__ __attribute__((aligned(1024))) unsigned char x0[L::kX], x1[L::kX], x2[L::kX], x3[L::kX], w0[L::kW], w1[L::kW], w2[L::kW], w3[L::kW];
   __shared__ __attribute__((aligned(1024))) unsigned char e0[L::kE], e1[L::kE], e2[L::kE], e3[L::kE];
+  __shared__ __attribute__((aligned(1024))) unsigned char x4[kMore ? L::kX : 1], x5[kMore ? L::kX : 1], x6[kMore ? L::kX : 1], x7[kMore ? L::kX : 1];
+  __shared__ __attribute__((aligned(1024))) unsigned char w4[kMore ? L::kW : 1], w5[kMore ? L::kW : 1], w6[kMore ? L::kW : 1], w7[kMore ? L::kW : 1];
+  __shared__ __attribute__((aligned(1024))) unsigned char e4[kMore ? L::kE : 1], e5[kMore ? L::kE : 1], e6[kMore ? L::kE : 1], e7[kMore ? L::kE : 1];
   const Packed8 pw = packed8(a.rows, a.in), px = packed8(a.m, a.in);
-  const int tok_tiles = (a.m + L::kTok - 1) / L::kTok, row_tiles = (a.rows + L::kRows - 1) / L::kRows;
+  const int tok_tiles = (a.m + L::kTok - 1) / L::kTok, row_tiles = (a.row_end - a.row_begin + L::kRows - 1) / L::kRows;
   // ids 8 apart run on one XCD: the token tiles of a weight tile follow each other there
   const int row_tile = (int)blockIdx.x / 8 / tok_tiles * 8 + (int)blockIdx.x % 8, tok_tile = (int)blockIdx.x / 8 % tok_tiles;
   if (row_tile >= row_tiles) return;
+  const int row0 = a.row_begin + row_tile * L::kRows;         // (a multiple of 16)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, g = lane >> 5;
   const int wm = wave % WM, wn = wave / WM;
   const int n_stage = 2 * pw.groups;
@@ -386,10 +390,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a
     xsrc[i] = buffer_of(a.x8 + (size_t)min(tok_tile * (L::kTok / 16) + wave * L::kXLoads + i, px.blocks - 1) * px.groups * kTile8);
 #pragma unroll
   for (int i = 0; i < L::kWLoads; i++)
-    wsrc[i] = buffer_of(a.w8 + (size_t)min(row_tile * (L::kRows / 16) + wave * L::kWLoads + i, pw.blocks - 1) * pw.groups * kTile8);
-  const int eb = wave * L::kExp + lane / 16 % L::kExp;        // (two blocks: both halves of the wavefront copy the same)
+    wsrc[i] = buffer_of(a.w8 + (size_t)min(row0 / 16 + wave * L::kWLoads + i, pw.blocks - 1) * pw.groups * kTile8);
+  const int eb = min(wave * 4 + lane / 16, L::kBlocks - 1);
   const uint32_t *esrc = (const uint32_t *)(eb < L::kTok / 16 ? a.x8 + packed8_exps(px) + (size_t)min(tok_tile * (L::kTok / 16) + eb, px.blocks - 1) * px.quads * 64
-                                                              : a.w8 + packed8_exps(pw) + (size_t)min(row_tile * (L::kRows / 16) + eb - L::kTok / 16, pw.blocks - 1) * pw.quads * 64) + lane % 16;
+                                                              : a.w8 + packed8_exps(pw) + (size_t)min(row0 / 16 + eb - L::kTok / 16, pw.blocks - 1) * pw.quads * 64) + lane % 16;
   auto copy = [&](unsigned char *x, unsigned char *w, unsigned char *e, int s) __attribute__((always_inline)) {
     s = min(s, n_stage - 1);                                  // past the end: the last stage again (never read)
 #pragma unroll
@@ -411,11 +415,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a
   struct Operand { Half8 h; uint32_t e; };
   auto read_x = [&](Operand &o, const unsigned char *x, const unsigned char *e, int t, int s) __attribute__((always_inline)) {
     const unsigned char *p = x + (wm * TB + t) * 2048 + at;
-    o = Operand{{*(const u32x4_t *)p, *(const u32x4_t *)(p + 256)}, e[L::exp_at(wm * TB + t) + e_at + ((s >> 1) & 3)]};
+    o = Operand{{*(const u32x4_t *)p, *(const u32x4_t *)(p + 256)}, e[(wm * TB + t) * 128 + e_at + ((s >> 1) & 3)]};
   };
   auto read_w = [&](Operand &o, const unsigned char *w, const unsigned char *e, int b, int s) __attribute__((always_inline)) {
     const unsigned char *p = w + (wn * WB + b) * 2048 + at;
-    o = Operand{{*(const u32x4_t *)p, *(const u32x4_t *)(p + 256)}, e[L::exp_at(L::kTok / 32 + wn * WB + b) + e_at + ((s >> 1) & 3)]};
+    o = Operand{{*(const u32x4_t *)p, *(const u32x4_t *)(p + 256)}, e[(L::kTok / 32 + wn * WB + b) * 128 + e_at + ((s >> 1) & 3)]};
   };
   Operand xo[TB], wo[2][WB];
   // cw: weight operands of stage s (nw: the next one's); x, w, e: its buffers; xn, wn_, en: those of the next stage
@@ -441,10 +445,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a
       }
       if (t == 0) {
         __builtin_amdgcn_sched_barrier(0);
-        constexpr int kOpen = (kStages8 - 2) * L::kLoads;     // copies that may still be under way
+        constexpr int kOpen = (STAGES - 2) * L::kLoads;       // copies that may still be under way
         __builtin_amdgcn_s_waitcnt(0x0070 | (kOpen & 15) | (kOpen >> 4 << 14));   // vmcnt(kOpen) lgkmcnt(0)
         wg_barrier();
-        copy(x, w, e, s + kStages8);
+        copy(x, w, e, s + STAGES);
 #pragma unroll
         for (int b = 0; b < WB; b++) read_w(nw[b], wn_, en, b, s + 1);
       }
@@ -456,7 +460,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a
   copy(x1, w1, e1, 1);
   copy(x2, w2, e2, 2);
   copy(x3, w3, e3, 3);
-  constexpr int kFirst = (kStages8 - 1) * L::kLoads;
+  if constexpr (kMore) {
+    copy(x4, w4, e4, 4);
+    copy(x5, w5, e5, 5);
+    copy(x6, w6, e6, 6);
+    copy(x7, w7, e7, 7);
+  }
+  constexpr int kFirst = (STAGES - 1) * L::kLoads;
+  static_assert(kFirst < 64, "what the wait can count");
   __builtin_amdgcn_s_waitcnt(0x0F70 | (kFirst & 15) | (kFirst >> 4 << 14));   // stage 0 here
   wg_barrier();
 #pragma unroll
@@ -464,41 +475,109 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a
 #pragma unroll
   for (int t = 0; t < TB; t++) read_x(xo[t], x0, e0, t, 0);
   int s = 0;
-  for (; s + 4 <= n_stage; s += 4) {
+  for (; s + STAGES <= n_stage; s += STAGES) {
     stage(wo[0], wo[1], x0, w0, e0, x1, w1, e1, s);
     stage(wo[1], wo[0], x1, w1, e1, x2, w2, e2, s + 1);
     stage(wo[0], wo[1], x2, w2, e2, x3, w3, e3, s + 2);
-    stage(wo[1], wo[0], x3, w3, e3, x0, w0, e0, s + 3);
+    if constexpr (!kMore) stage(wo[1], wo[0], x3, w3, e3, x0, w0, e0, s + 3);
+    else {
+      stage(wo[1], wo[0], x3, w3, e3, x4, w4, e4, s + 3);
+      stage(wo[0], wo[1], x4, w4, e4, x5, w5, e5, s + 4);
+      stage(wo[1], wo[0], x5, w5, e5, x6, w6, e6, s + 5);
+      stage(wo[0], wo[1], x6, w6, e6, x7, w7, e7, s + 6);
+      stage(wo[1], wo[0], x7, w7, e7, x0, w0, e0, s + 7);
+    }
   }
   if (s < n_stage) {                                          // stages come in pairs
     stage(wo[0], wo[1], x0, w0, e0, x1, w1, e1, s);
     stage(wo[1], wo[0], x1, w1, e1, x2, w2, e2, s + 1);
+    if constexpr (kMore)
+      if (s + 2 < n_stage) {
+        stage(wo[0], wo[1], x2, w2, e2, x3, w3, e3, s + 2);
+        stage(wo[1], wo[0], x3, w3, e3, x4, w4, e4, s + 3);
+        if (s + 4 < n_stage) {
+          stage(wo[0], wo[1], x4, w4, e4, x5, w5, e5, s + 4);
+          stage(wo[1], wo[0], x5, w5, e5, x6, w6, e6, s + 5);
+        }
+      }
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);                         // no copy into the LDS outlives the workgroup
 
+  // Sums go through the LDS (the tokens' buffers, a share for each wavefront) into whole rows: a lane has four columns of one token, and stores of these touch 32 rows at a time.
+  // Pieces of 16 bytes are permuted by the row, so that neither side meets in a bank.
+  constexpr int kCols = WB * 32, kChunks = kCols / 4, kShare = 32 * kCols * 4, kPer = L::kX / kShare;
+  static_assert(L::kWaves * kShare == 4 * L::kX, "a share each");
+  wg_barrier();                                               // everybody's operands are read
+  unsigned char *const mine = (wave / kPer == 0 ? x0 : wave / kPer == 1 ? x1 : wave / kPer == 2 ? x2 : x3) + wave % kPer * kShare;
+  const int col0 = row0 + wn * kCols;
 #pragma unroll
   for (int t = 0; t < TB; t++) {
-    const int tok = tok_tile * L::kTok + (wm * TB + t) * 32 + c;
-    if (tok >= a.m) continue;                                 // (both lanes of a token)
-    OUT *y = (OUT *)a.y + (size_t)tok * a.ldy;
+    const int tok0 = tok_tile * L::kTok + (wm * TB + t) * 32;
+    wave_fence();                                             // (the 32 before have been read)
 #pragma unroll
-    for (int b = 0; b < WB; b++) {
-      const int col = row_tile * L::kRows + (wn * WB + b) * 32;
+    for (int b = 0; b < WB; b++)
 #pragma unroll
       for (int q = 0; q < 4; q++)
-        store4<VEC>(y, col + 8 * q + 4 * g, a.rows, f32x4_t{acc[b][t][4 * q], acc[b][t][4 * q + 1], acc[b][t][4 * q + 2], acc[b][t][4 * q + 3]});
+        *(f32x4_t *)(mine + c * kCols * 4 + ((b * 8 + 2 * q + g) ^ (c & (kChunks - 1))) * 16) = f32x4_t{acc[b][t][4 * q], acc[b][t][4 * q + 1], acc[b][t][4 * q + 2], acc[b][t][4 * q + 3]};
+    wave_fence();
+    if constexpr (VEC) {
+      constexpr int kAtOnce = 64 / kChunks;
+#pragma unroll
+      for (int i = 0; i < 32; i += kAtOnce) {
+        const int r = i + lane / kChunks, chunk = lane % kChunks;
+        const f32x4_t v = *(const f32x4_t *)(mine + r * kCols * 4 + (chunk ^ (r & (kChunks - 1))) * 16);
+        if (tok0 + r < a.m) store4<true>((OUT *)a.y + (size_t)(tok0 + r) * a.ldy, col0 + 4 * chunk, a.row_end, v);
+      }
+    } else {
+      constexpr int kAtOnce = 64 / kCols;
+#pragma unroll 8
+      for (int i = 0; i < 32; i += kAtOnce) {
+        const int r = i + lane / kCols, col = lane % kCols;
+        const float v = *(const float *)(mine + r * kCols * 4 + ((col >> 2) ^ (r & (kChunks - 1))) * 16 + (col & 3) * 4);
+        if (tok0 + r < a.m && col0 + col < a.row_end) ((OUT *)a.y)[(size_t)(tok0 + r) * a.ldy + col0 + col] = from_f32<OUT>(v);
+      }
     }
   }
 }
 
-template <typename OUT, bool VEC, int WM, int WN, int TB, int WB>
+template <typename OUT, bool VEC, int WM, int WN, int TB, int WB, int STAGES>
 hipError_t launch_tile(const Gemm8Args &a, hipStream_t st) {
   using L = Tile8<WM, WN, TB, WB>;
-  const int64_t tok_tiles = (a.m + L::kTok - 1) / L::kTok, row_tiles = (a.rows + L::kRows - 1) / L::kRows;
+  const int64_t tok_tiles = (a.m + L::kTok - 1) / L::kTok, row_tiles = (a.row_end - a.row_begin + L::kRows - 1) / L::kRows;
   const int64_t grid = (row_tiles + 7) / 8 * 8 * tok_tiles;
   if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((gemm8_tile_kernel<OUT, VEC, WM, WN, TB, WB>), dim3((unsigned)grid), dim3(L::kWaves * 64), 0, st, a);
+  hipLaunchKernelGGL((gemm8_tile_kernel<OUT, VEC, WM, WN, TB, WB, STAGES>), dim3((unsigned)grid), dim3(L::kWaves * 64), 0, st, a);
   return hipGetLastError();
+}
+
+// The tile that a launch takes: the one whose workgroups, in rounds over the 256 compute units, are done first.  Measured (us for K = 4096, bf16 results; fp32 results take
+// 1.4 to 1.9 times that for all of them): a round of one workgroup a unit, and a unit's time for each when there are more.
+//   256 x 256: 60, one fits a unit (512 x 512 x 4096 alike for 172 tiles, 52)      256 x 128: 39, one (2048 x 4096: 39 against 51 in 256 x 256 and 46 in 128 x 128)
+//   128 x 128: 26, or two in 44 (1024 x 4096: 26 against 34 in 256 x 128)           64 x 128: 17, then 15.4 each (333 x 4096: 17 against 21 in 128 x 128)
+//   64 x 64, eight stages deep: 11, then 8.6 each (60 x 12288: 15 against 20 in 64 x 128)
+enum { kLargest = 0, kTiles8 = 5 };
+struct TileCost { int tok, rows, fit; float one, fitting; };  // `fit` workgroups on a unit at once take `fitting`
+constexpr TileCost kTileCosts[kTiles8] = {{256, 256, 1, 60.f, 60.f}, {256, 128, 1, 39.f, 39.f}, {128, 128, 2, 26.f, 44.f}, {64, 128, 2, 17.f, 31.f}, {64, 64, 2, 11.f, 17.5f}};
+float tiles_cost(int shape, int m, int rows) {
+  const TileCost &c = kTileCosts[shape];
+  const int64_t tiles = (int64_t)((m + c.tok - 1) / c.tok) * ((rows + c.rows - 1) / c.rows), a_round = 256 * c.fit, left = tiles % a_round;
+  return (float)(tiles / a_round) * c.fitting + (left == 0 ? 0.f : left <= 256 ? c.one : c.fitting);
+}
+struct Tiles8 { int shape; float cost; };
+Tiles8 best_tiles(int m, int rows) {
+  Tiles8 best{kLargest, tiles_cost(kLargest, m, rows)};
+  for (int i = 1; i < kTiles8; i++)
+    if (const float cost = tiles_cost(i, m, rows); cost < best.cost) best = Tiles8{i, cost};
+  return best;
+}
+template <typename OUT, bool VEC> hipError_t launch_tiles(int shape, const Gemm8Args &a, hipStream_t st) {
+  switch (shape) {
+    case kLargest: return launch_tile<OUT, VEC, 2, 4, 4, 2, 4>(a, st);
+    case 1: return launch_tile<OUT, VEC, 4, 2, 2, 2, 4>(a, st);
+    case 2: return launch_tile<OUT, VEC, 2, 4, 2, 1, 4>(a, st);
+    case 3: return launch_tile<OUT, VEC, 1, 4, 2, 1, 4>(a, st);
+    default: return launch_tile<OUT, VEC, 2, 2, 1, 1, 8>(a, st);
+  }
 }
 
 // Up to 16 tokens: they are put into 8 bits by every workgroup for itself where that is little work each, or by a launch ahead (3.8 us), into scratch.  Measured (us, with the launch
@@ -533,12 +612,24 @@ hipError_t launch_typed(Gemm8Args a, void *scratch, hipStream_t st) {
   const hipError_t e = quant8((const X *)a.x, a.ldx, a.m, a.in, 0, scratch, st);
   if (e != hipSuccess) return e;
   a.x8 = (const unsigned char *)scratch;
-  const int blocks = (a.rows + 15) / 16;
-  if (a.m <= 64 && blocks <= 512) return a.m <= 32 ? launch_stream<OUT, VEC, 2, 1>(a, st) : launch_stream<OUT, VEC, 4, 1>(a, st);
-  auto tiles = [&](int tok, int rows) { return (int64_t)((a.m + tok - 1) / tok) * ((a.rows + rows - 1) / rows); };
-  if (tiles(256, 256) >= 200) return launch_tile<OUT, VEC, 2, 4, 4, 2>(a, st);
-  if (tiles(128, 128) >= (a.m <= 64 ? 128 : 200)) return launch_tile<OUT, VEC, 2, 4, 2, 1>(a, st);
-  return launch_tile<OUT, VEC, 2, 2, 1, 1>(a, st);
+  // 17 to 64 tokens through few rows: the weights straight into registers (us, 60 tokens: 4096 rows of 4096 9.1 against 11.1 in tiles of 64 x 64, of 11008 18.9 against 28.1;
+  // 12288 rows of 4096 23.1 against 15.1)
+  if (a.m <= 64 && a.rows <= 4096) return a.m <= 32 ? launch_stream<OUT, VEC, 2, 1>(a, st) : launch_stream<OUT, VEC, 4, 1>(a, st);
+  a.row_begin = 0; a.row_end = a.rows;
+  const Tiles8 all = best_tiles(a.m, a.rows);
+  // whole rounds of the largest tile, and the rows that are left in what suits them: 2048 x 28672 x 4096 (3.5 rounds) @@
+  const int64_t tok = (a.m + 255) / 256, in_rounds = tok * ((a.rows + 255) / 256) / 256 * 256 / tok * 256;
+  if (in_rounds > 0 && in_rounds < a.rows) {
+    const Tiles8 rest = best_tiles(a.m, a.rows - (int)in_rounds);
+    if (tiles_cost(kLargest, a.m, (int)in_rounds) + rest.cost + 3.f < all.cost) {
+      a.row_end = (int)in_rounds;
+      const hipError_t first = launch_tiles<OUT, VEC>(kLargest, a, st);
+      if (first != hipSuccess) return first;
+      a.row_begin = a.row_end; a.row_end = a.rows;
+      return launch_tiles<OUT, VEC>(rest.shape, a, st);
+    }
+  }
+  return launch_tiles<OUT, VEC>(all.shape, a, st);
 }
 
 }  // namespace

@@ -292,6 +292,7 @@ struct Gemm8Args {
   const unsigned char *x8, *w8;         // packed: x (set by launch_gemm8), [rows, in]
   int m, in, rows;
   void *y;  int64_t ldy;                // [m, rows]
+  int row_begin, row_end;               // set by launch_gemm8: the rows of a launch in tiles
 };
 hipError_t launch_pack_weight8(int dtype, const void *src, int rows, int in, void *dst, hipStream_t st);
 // dtype: x's; scratch: gemm8_scratch_bytes (0: none), for x in 8 bits
