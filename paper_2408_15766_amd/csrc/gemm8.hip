@@ -552,12 +552,12 @@ hipError_t launch_tile(const Gemm8Args &a, hipStream_t st) {
 
 // The tile that a launch takes: the one whose workgroups, in rounds over the 256 compute units, are done first.  Measured (us for K = 4096, bf16 results; fp32 results take
 // 1.4 to 1.9 times that for all of them): a round of one workgroup a unit, and a unit's time for each when there are more.
-//   256 x 256: 60, one fits a unit (512 x 512 x 4096 alike for 172 tiles, 52)      256 x 128: 39, one (2048 x 4096: 39 against 51 in 256 x 256 and 46 in 128 x 128)
-//   128 x 128: 26, or two in 44 (1024 x 4096: 26 against 34 in 256 x 128)           64 x 128: 17, then 15.4 each (333 x 4096: 17 against 21 in 128 x 128)
-//   64 x 64, eight stages deep: 11, then 8.6 each (60 x 12288: 15 against 20 in 64 x 128)
+//   256 x 256: 56, one fits a unit (512 x 28672: 60 against 75 in 256 x 128)        256 x 128: 36, one (2048 x 4096: 36 against 50 in 256 x 256 and 42 in 128 x 128)
+//   128 x 128: 24, or two in 41 (1024 x 4096: 24 against 33 in 256 x 128)           64 x 128: 16, or two in 30 (333 x 4096: 16 against 20 in 128 x 128)
+//   64 x 64, eight stages deep: 11, or two in 17.5 (60 x 12288: 15 against 20 in 64 x 128)
 enum { kLargest = 0, kTiles8 = 5 };
 struct TileCost { int tok, rows, fit; float one, fitting; };  // `fit` workgroups on a unit at once take `fitting`
-constexpr TileCost kTileCosts[kTiles8] = {{256, 256, 1, 60.f, 60.f}, {256, 128, 1, 39.f, 39.f}, {128, 128, 2, 26.f, 44.f}, {64, 128, 2, 17.f, 31.f}, {64, 64, 2, 11.f, 17.5f}};
+constexpr TileCost kTileCosts[kTiles8] = {{256, 256, 1, 56.f, 56.f}, {256, 128, 1, 36.f, 36.f}, {128, 128, 2, 24.f, 41.f}, {64, 128, 2, 16.f, 30.f}, {64, 64, 2, 11.f, 17.5f}};
 float tiles_cost(int shape, int m, int rows) {
   const TileCost &c = kTileCosts[shape];
   const int64_t tiles = (int64_t)((m + c.tok - 1) / c.tok) * ((rows + c.rows - 1) / c.rows), a_round = 256 * c.fit, left = tiles % a_round;
@@ -617,7 +617,8 @@ hipError_t launch_typed(Gemm8Args a, void *scratch, hipStream_t st) {
   if (a.m <= 64 && a.rows <= 4096) return a.m <= 32 ? launch_stream<OUT, VEC, 2, 1>(a, st) : launch_stream<OUT, VEC, 4, 1>(a, st);
   a.row_begin = 0; a.row_end = a.rows;
   const Tiles8 all = best_tiles(a.m, a.rows);
-  // whole rounds of the largest tile, and the rows that are left in what suits them: 2048 x 28672 x 4096 (3.5 rounds) @@
+  // whole rounds of the largest tile, and the rows that are left in what suits them: 2048 x 28672 x 4096 (3.5 rounds) 217 -> 205 us, 2048 x
+  // 12288 x 4096 (1.5) 105 -> 94; 2048 x 22016 x 4096 (2.7) would take 177 instead of 164
   const int64_t tok = (a.m + 255) / 256, in_rounds = tok * ((a.rows + 255) / 256) / 256 * 256 / tok * 256;
   if (in_rounds > 0 && in_rounds < a.rows) {
     const Tiles8 rest = best_tiles(a.m, a.rows - (int)in_rounds);
