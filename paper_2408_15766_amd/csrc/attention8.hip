@@ -871,7 +871,6 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
   p.win_part = win_rows <= 256 && p.waves < 8 ? 64 : 256;
   while ((win_rows + p.win_part - 1) / p.win_part > 8) p.win_part *= 2;
   p.win_parts = (win_rows + p.win_part - 1) / p.win_part;
-  // as many workgroups as the compute units hold at once (one of eight wavefronts fills one)
   const int64_t most = p.waves ? n_blocks : (n_blocks + kFewWaves - 1) / kFewWaves;
   if (p.waves == 8 && n_blocks > 0) {
     p.win_parts = 0;
@@ -883,7 +882,9 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
     p.win_cost = each * 24 / 64;
     return p;
   }
-  const int64_t parts = 512 / units - p.win_parts;
+  // One workgroup a unit; two of two wavefronts where each would have eight blocks or more (us: 60 queries on 32 kv heads, 512 keys 15.7 against 18.1 with 512 workgroups, 4096 29 against 25,
+  // 16384 79 against 48; one query on 8, 16384 keys 15 against 22; 104 on 8, 32768 42 against 52)
+  const int64_t parts = (p.waves == 2 && units * n_blocks >= 2048 ? 512 : 256) / units - p.win_parts;
   p.block_parts = n_blocks == 0 ? 0 : (int)(parts < 1 ? 1 : parts > most ? most : parts);
   return p;
 }
