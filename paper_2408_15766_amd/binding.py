@@ -9,6 +9,7 @@ from __future__ import annotations
 import collections
 import ctypes as C
 import dataclasses
+import functools
 import os
 import struct
 import threading
@@ -671,10 +672,15 @@ def spec_kv8_alloc(n_blocks: int, hkv: int, hd: int, device=None):
     return torch.empty((n_blocks, n), dtype=torch.uint8, device="cuda" if device is None else device)
 
 
+@functools.lru_cache(maxsize=None)
+def _kv8_block(hkv: int, hd: int) -> int:
+    return int(lib.spec_kv8_bytes(1, hkv, hd))
+
+
 def _is_kv8(cache8, hkv: int, hd: int, blocks: int) -> bool:
     import torch
     return (cache8 is not None and cache8.dim() == 2 and cache8.dtype is torch.uint8 and cache8.is_contiguous() and cache8.shape[0] >= blocks and
-            cache8.shape[1] == lib.spec_kv8_bytes(1, hkv, hd))
+            cache8.shape[1] == _kv8_block(hkv, hd))
 
 
 def _kv8_args(what: str, k, v, cache8, first_block: int, hkv: int, hd: int):
@@ -740,8 +746,6 @@ def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, an
         _refuse(what, "anc has to be int32 [rows, 16]")
     win_rows = kwin.shape[0]
     n = lib.spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, n_blocks, win_rows)
-    if n == 0:
-        _refuse(what, f"{rows} rows, {hq} heads on {hkv} of {hd}, {n_blocks} blocks, a window of {win_rows} rows")
     if n_blocks and not _is_kv8(cache8, hkv, hd, n_blocks):
         _refuse(what, f"cache8 holds no {n_blocks} blocks of {hkv} heads of {hd}")
     if max_depth is None:
@@ -750,16 +754,18 @@ def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, an
         out = q.new_empty((rows, wide), dtype=torch.bfloat16)
     elif out.dtype is not torch.bfloat16 or not out.is_contiguous() or tuple(out.shape) != (rows, wide):
         _refuse(what, f"out has to be contiguous bfloat16 [{rows}, {wide}]")
-    if scratch is None:
-        scratch, room = q.new_empty(n, dtype=torch.uint8), n
-    else:
+    room = n
+    if scratch is not None:
         room = scratch.numel() * scratch.element_size()
         if not scratch.is_contiguous():
             _refuse(what, "scratch has to be contiguous")
+    elif n:
+        scratch = q.new_empty(n, dtype=torch.uint8)
     rc = lib.spec_k_attention8(q.data_ptr(), cache8.data_ptr() if n_blocks else None, n_blocks, kwin.data_ptr(), vwin.data_ptr(), win_rows, rows, hq, hkv, hd, base,
-                               depth.data_ptr(), None if anc is None else anc.data_ptr(), max_depth, scratch.data_ptr(), room, out.data_ptr(), stream)
+                               depth.data_ptr(), None if anc is None else anc.data_ptr(), max_depth, None if scratch is None else scratch.data_ptr(), room, out.data_ptr(), stream)
     if rc:
-        raise SpecError(rc, f"{what}: base {base}, {n_blocks} blocks, max_depth {max_depth}, {room} bytes of scratch")
+        raise SpecError(rc, f"{what}: {rows} rows, {hq} heads on {hkv} of {hd}, base {base}, {n_blocks} blocks, {win_rows} window rows, max_depth {max_depth}, "
+                            f"{room} bytes of scratch")
     return out
 
 

@@ -89,8 +89,9 @@ uint64_t spec_k_attention8_scratch_bytes(int32_t rows, int32_t hq, int32_t hkv, 
 int spec_k_attention8(const float *q, const void *cache8, int32_t n_blocks, const void *kwin, const void *vwin, int32_t win_rows, int32_t rows,
                       int32_t hq, int32_t hkv, int32_t hd, int32_t base, const int32_t *depth, const int32_t *anc, int32_t max_depth,
                       void *scratch, uint64_t scratch_bytes, void *out, void *stream) {
+  if (!q || (!cache8 && n_blocks > 0) || !kwin || !vwin || !depth || !out || !attention_ok(rows, hq, hkv, hd, n_blocks, win_rows)) return SPEC_EINVAL;
   const uint64_t need = spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, n_blocks, win_rows);
-  if (!q || (!cache8 && n_blocks > 0) || !kwin || !vwin || !depth || !scratch || !out || need == 0 || scratch_bytes < need) return SPEC_EINVAL;
+  if (need > 0 && (!scratch || scratch_bytes < need)) return SPEC_EINVAL;
   if (max_depth < 0 || (anc && max_depth > kMaxDepth) || base < n_blocks * kKv8Block || (int64_t)base + max_depth >= INT32_MAX) return SPEC_EINVAL;
   if (!aligned(q, 16) || !aligned(kwin, 16) || !aligned(vwin, 16) || !aligned(out, 16) || !aligned(cache8, 256) || !aligned(scratch, 256) ||
       !aligned(depth, 4) || !aligned(anc, 4))

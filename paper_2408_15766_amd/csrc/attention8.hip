@@ -101,8 +101,8 @@ __device__ __forceinline__ void widen(const u32x4_t &w, u32x4_t &first, u32x4_t 
 }
 
 // The work of a launch.  waves: of 32 queries each in a workgroup; 0: few queries.  Parts 0 .. block_parts - 1 are ranges of the cache's blocks, the others ranges of win_part
-// rows of the window.  Eight wavefronts: the last range of blocks goes on into the whole window instead (win_parts 0), and has as many blocks fewer as the
-// rows that a block of queries sees cost (win_cost: per query block, blocks; win_base: for the first, both in 1/16).
+// rows of the window, or, with win_parts 0, the last range of blocks goes on into the whole window; of eight wavefronts it has as many blocks fewer as the rows that a
+// block of queries sees cost (win_cost: per query block, win_base: for the first, in 1/16 of a block).
 struct Plan8 { int waves, query_blocks, block_parts, win_parts, win_part, win_base, win_cost; };
 __host__ __device__ inline int range_at(int n, int parts, int i) { return (int)((int64_t)n * i / parts); }
 __device__ __forceinline__ int joined_range_at(const Plan8 &p, int n, int qb, int i) {
@@ -775,8 +775,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention8_few_kernel(Attn8Arg
     const float up = exp2_((float)top_exp);
 #pragma unroll
     for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
-  } else {
-    const int w_begin = (part - plan.block_parts) * plan.win_part, w_stop = min(w_begin + plan.win_part, a.win_rows);
+  }
+  if (part >= plan.block_parts || plan.win_parts == 0) {
+    const int w_begin = plan.win_parts ? (part - plan.block_parts) * plan.win_part : 0, w_stop = plan.win_parts ? min(w_begin + plan.win_part, a.win_rows) : a.win_rows;
     window_alone<HD>(a, r, qp, row, real, kvh, w_begin + 32 * wave, 32 * kFewWaves, w_stop, lds + wave * (64 * HD + 1024));
     __syncthreads();                                          // the value rows make place for the outputs
   }
@@ -872,6 +873,11 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
   while ((win_rows + p.win_part - 1) / p.win_part > 8) p.win_part *= 2;
   p.win_parts = (win_rows + p.win_part - 1) / p.win_part;
   const int64_t most = p.waves ? n_blocks : (n_blocks + kFewWaves - 1) / kFewWaves;
+  if (p.waves == 0 && n_blocks > 0 && n_blocks <= 2 * kFewWaves && win_rows <= 32 * kFewWaves) {   // short: one part, no second launch
+    p.block_parts = 1;
+    p.win_parts = 0;
+    return p;
+  }
   if (p.waves == 8 && n_blocks > 0) {
     p.win_parts = 0;
     const int64_t parts = (256 + units / 2) / units;
@@ -968,7 +974,7 @@ hipError_t launch_kv8_load(const void *cache8, int first_block, int n_blocks, in
 size_t attention8_scratch_floats(int rows, int hq, int hkv, int hd, int n_blocks, int win_rows) {
   const Plan8 p = plan8(rows, hq, hkv, n_blocks, win_rows);
   const int parts = p.block_parts + p.win_parts;
-  return parts == 1 ? 64 : (size_t)parts * rows * hq * (hd + 2);
+  return parts == 1 ? 0 : (size_t)parts * rows * hq * (hd + 2);
 }
 
 hipError_t launch_attention8(const Attn8Args &a, hipStream_t st) { return a.hd == 128 ? launch_hd<128>(a, st) : launch_hd<64>(a, st); }

@@ -393,10 +393,20 @@ def test_attention8_binding_refusals(P):
     ok = dict(q=q, cache8=c, n_blocks=1, kwin=k[64:].contiguous(), vwin=v[64:].contiguous(), base=65, depth=d, anc=None, hq=hq, hkv=hkv, hd=hd)
     for kw in (dict(q=q.bfloat16()), dict(q=q[:, :64]), dict(n_blocks=2), dict(cache8=None), dict(kwin=k[64:].float()), dict(vwin=v[:64]), dict(base=63), dict(depth=d.long()),
                dict(depth=d[:2]), dict(anc=torch.zeros(3, 15, dtype=torch.int32, device="cuda")), dict(hq=3), dict(hd=128), dict(max_depth=-1),
-               dict(scratch=torch.empty(0, dtype=torch.uint8, device="cuda")), dict(out=torch.empty(3, 256, device="cuda")), dict(q=q.cpu()),
+               dict(out=torch.empty(3, 256, device="cuda")), dict(q=q.cpu()),
                dict(kwin=k[64:64], vwin=v[64:64]), dict(anc=torch.zeros(3, 16, dtype=torch.int32, device="cuda"), max_depth=16)):
         with pytest.raises(P.SpecError):
             P.spec_k_attention8(**{**ok, **kw})
+    q, k, v = inputs(60, hq, hkv, hd, 1, 60, 1)                           # a call that needs scratch: too little, and its own kept for two calls
+    many = {**ok, **dict(q=q, kwin=k[64:].contiguous(), vwin=v[64:].contiguous(), base=64, depth=torch.arange(60, dtype=torch.int32, device="cuda"))}
+    n = P.spec_k_attention8_scratch_bytes(60, hq, hkv, hd, 1, 60)
+    P.spec_k_kv8_store(k[:64], v[:64], c, 0, hkv, hd)
+    want = P.spec_k_attention8(**many)
+    kept = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        assert torch.equal(P.spec_k_attention8(**many, scratch=kept), want)
+    with pytest.raises(P.SpecError):
+        P.spec_k_attention8(**many, scratch=kept[:n - 256])
 
 
 # ---- rotary ---------------------------------------------------------------------------------------

@@ -44,7 +44,7 @@ def test_sizes(P):
     assert P.spec_kv8_bytes(100000, 32, 128) > 1 << 35
     for bad in ((0, 8, 8, 64, 1, 1), (1, 12, 4, 64, 1, 1), (1, 8, 8, 64, -1, 1), (1, 8, 8, 64, 1, 0), (1, 7, 2, 64, 1, 1), (1, 8, 8, 80, 1, 1)):
         assert P.spec_k_attention8_scratch_bytes(*bad) == 0
-    assert P.spec_k_attention8_scratch_bytes(60, 32, 8, 128, 64, 100) > 0
+    assert P.spec_k_attention8_scratch_bytes(60, 32, 8, 128, 64, 100) > 0 and P.spec_k_attention8_scratch_bytes(1, 32, 8, 128, 4, 40) == 0
 
 
 X = 4096   # an address that is aligned and never read: every call below is refused first
@@ -77,9 +77,9 @@ def test_kv8_refusals(P):
 
 
 def test_attention8_refusals(P):
-    good = dict(q=X, c=X, nb=2, kw=X, vw=X, win=8, rows=4, hq=8, hkv=2, hd=64, base=128, depth=X, anc=X, md=3, scratch=X, nbytes=1 << 40, out=X)
+    good = dict(q=X, c=X, nb=20, kw=X, vw=X, win=8, rows=4, hq=8, hkv=2, hd=64, base=1280, depth=X, anc=X, md=3, scratch=X, nbytes=1 << 40, out=X)
     for kw in (dict(q=None), dict(q=X + 4), dict(c=None), dict(c=X + 16), dict(nb=-1), dict(kw=None), dict(vw=None), dict(kw=X + 2), dict(win=0), dict(rows=0),
-               dict(hq=9), dict(hq=32), dict(hq=1), dict(hkv=0), dict(hd=80), dict(base=127), dict(base=-1, nb=0), dict(depth=None), dict(md=-1), dict(md=16),
+               dict(hq=9), dict(hq=32), dict(hq=1), dict(hkv=0), dict(hd=80), dict(base=1279), dict(base=-1, nb=0), dict(depth=None), dict(md=-1), dict(md=16),
                dict(anc=None, md=2 ** 31 - 1), dict(scratch=None), dict(scratch=X + 64), dict(nbytes=0), dict(out=None), dict(out=X + 2), dict(anc=X + 1)):
         a = {**good, **kw}
         refused(P.lib.spec_k_attention8(a["q"], a["c"], a["nb"], a["kw"], a["vw"], a["win"], a["rows"], a["hq"], a["hkv"], a["hd"], a["base"], a["depth"],
