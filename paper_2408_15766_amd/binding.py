@@ -794,28 +794,31 @@ def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[
     import torch
     what = "spec_k_rotary"
     n = len(xs)
-    if not 1 <= n <= 3:
-        _refuse(what, f"{n} tensors")
+    if not 1 <= n <= 3 or xs[0].dim() != 3:
+        _refuse(what, "one to three tensors [rows, heads, hd] are needed")
     if outs is None:
-        outs = [x.new_empty(x.shape) for x in xs] if out_dtypes is None else [x.new_empty(x.shape, dtype=d) for x, d in zip(xs, out_dtypes)]
-    at = pos if isinstance(pos, torch.Tensor) else None
+        kinds = [x.dtype for x in xs] if out_dtypes is None else out_dtypes
+        outs = [torch.empty_like(x, dtype=d, memory_format=torch.contiguous_format) for x, d in zip(xs, kinds)]
     if len(outs) != n or (turned is not None and len(turned) != n):
         _refuse(what, "as many outputs and flags as tensors are needed")
+    at = pos if isinstance(pos, torch.Tensor) else None
     stream = _here(what, *xs, *outs, at)
-    if xs[0].dim() != 3:
-        _refuse(what, "tensors have to be [rows, heads, hd]")
     rows, _, hd = xs[0].shape
     if at is not None and (at.dtype is not torch.int32 or at.dim() != 1 or at.shape[0] != rows or not at.is_contiguous()):
         _refuse(what, f"pos has to be int32 [{rows}]")
+    codes = {torch.float32: 0, torch.bfloat16: 1}
     fields = []
-    for i in range(n):
-        x, o = xs[i], outs[i]
-        if x.shape != o.shape or x.dim() != 3 or x.shape[0] != rows or x.shape[2] != hd:
+    for x, o, turn in zip(xs, outs, (True,) * n if turned is None else turned):
+        shape = x.shape
+        if shape != o.shape or len(shape) != 3 or shape[0] != rows or shape[2] != hd:
             _refuse(what, f"tensors have to be [{rows}, heads, {hd}]")
         (ldx, hsx, one), (ldo, hso, one_out) = x.stride(), o.stride()
         if hd > 1 and not one == one_out == 1:
             _refuse(what, "the dims of a head have to be dense")
-        fields += (x.data_ptr(), o.data_ptr(), ldx, hsx, ldo, hso, x.shape[1], _dtype_code(what, x.dtype), _dtype_code(what, o.dtype), 1 if turned is None else bool(turned[i]))
+        dtype, out_dtype = codes.get(x.dtype), codes.get(o.dtype)
+        if dtype is None or out_dtype is None:
+            _refuse(what, f"{x.dtype} to {o.dtype} (float32 and bfloat16 are supported)")
+        fields += (x.data_ptr(), o.data_ptr(), ldx, hsx, ldo, hso, shape[1], dtype, out_dtype, bool(turn))
     rc = lib.spec_k_rotary(C.byref(plan), n, _rotary_parts[n](*fields), hd, rows, at.data_ptr() if at is not None else None, 0 if at is not None else int(pos),
                            bool(adjoint), stream)
     if rc:
