@@ -575,6 +575,9 @@ def spec_topk_loss(feat_target, feat_draft, lm_head_packed, k: int, scratch=None
 # The host's share of a small call is longer than its kernels (the checks and allocations of a first version took 11 to 21 us, its kernels 6 to 10), so the functions below ask each
 # thing once, form their messages where they raise them, and hand structures over as packed bytes.
 
+_INT_MAX = 2 ** 31 - 1
+
+
 def _refuse(what: str, why: str):
     raise SpecError(SPEC_EINVAL, f"{what}: {why}")
 
@@ -606,7 +609,8 @@ def spec_packed8_bytes(rows: int, cols: int) -> int:
 
 
 def spec_pack_weight8(w):
-    """Row-major torch matrix [rows, in] (bf16 or fp32) on the device -> its 8-bit form (uint8 tensor that remembers its shape)."""
+    """Row-major torch matrix [rows, in] (bf16 or fp32) on the device -> its 8-bit form (uint8 tensor that remembers its shape, under a name of its
+    own: calls that take a matrix of spec_pack_weight refuse it)."""
     import torch
     what = "spec_pack_weight8"
     stream = _here(what, w)
@@ -620,7 +624,7 @@ def spec_pack_weight8(w):
     rc = lib.spec_pack_weight8(dtype, w.data_ptr(), w.shape[0], w.shape[1], dst.data_ptr(), stream)
     if rc:
         raise SpecError(rc, what)
-    dst.logical_shape = tuple(w.shape)
+    dst.packed8_shape = tuple(w.shape)
     return dst
 
 
@@ -635,7 +639,9 @@ def spec_k_gemm8(x, w8, out_dtype=None, out=None, scratch=None):
     import torch
     what = "spec_k_gemm8"
     stream = _here(what, x, w8, out, scratch)
-    rows, cols = w8.logical_shape
+    rows, cols = getattr(w8, "packed8_shape", (0, 0))
+    if rows == 0:
+        _refuse(what, "w8 is no result of spec_pack_weight8")
     if x.dim() != 2 or x.shape[1] != cols or (x.stride(1) != 1 and cols > 1):
         _refuse(what, f"x has to be [m, {cols}] with dense rows")
     m = x.shape[0]
@@ -652,8 +658,11 @@ def spec_k_gemm8(x, w8, out_dtype=None, out=None, scratch=None):
         room = n
         if n:
             scratch = x.new_empty(n, dtype=torch.uint8)
-    rc = lib.spec_k_gemm8(_dtype_code(what, x.dtype), x.data_ptr(), x.stride(0) if m > 1 else cols, m, cols, w8.data_ptr(), rows, _dtype_code(what, out.dtype),
-                          out.data_ptr(), out.stride(0) if m > 1 else rows, None if scratch is None else scratch.data_ptr(), room, stream)
+    ldx, ldy = (x.stride(0), out.stride(0)) if m > 1 else (cols, rows)
+    if ldx > _INT_MAX or ldy > _INT_MAX:                        # (ctypes would cut them)
+        _refuse(what, f"rows {ldx} and {ldy} elements apart")
+    rc = lib.spec_k_gemm8(_dtype_code(what, x.dtype), x.data_ptr(), ldx, m, cols, w8.data_ptr(), rows, _dtype_code(what, out.dtype), out.data_ptr(), ldy,
+                          None if scratch is None else scratch.data_ptr(), room, stream)
     if rc:
         raise SpecError(rc, f"{what}: {m} x {cols} by {rows}, {room} bytes of scratch")
     return out
@@ -750,6 +759,8 @@ def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, an
         _refuse(what, f"cache8 holds no {n_blocks} blocks of {hkv} heads of {hd}")
     if max_depth is None:
         max_depth = max(int(depth.max().item()), 0)
+    if not (0 <= base <= _INT_MAX and 0 <= max_depth <= _INT_MAX):
+        _refuse(what, f"base {base}, max_depth {max_depth}")
     if out is None:
         out = q.new_empty((rows, wide), dtype=torch.bfloat16)
     elif out.dtype is not torch.bfloat16 or not out.is_contiguous() or tuple(out.shape) != (rows, wide):
@@ -806,6 +817,8 @@ def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[
     rows, _, hd = xs[0].shape
     if at is not None and (at.dtype is not torch.int32 or at.dim() != 1 or at.shape[0] != rows or not at.is_contiguous()):
         _refuse(what, f"pos has to be int32 [{rows}]")
+    if at is None and not -_INT_MAX - 1 <= int(pos) <= _INT_MAX:
+        _refuse(what, f"position {pos}")
     codes = {torch.float32: 0, torch.bfloat16: 1}
     fields = []
     for x, o, turn in zip(xs, outs, (True,) * n if turned is None else turned):

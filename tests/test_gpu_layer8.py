@@ -142,7 +142,9 @@ def test_gemm8_scratch_is_checked_and_may_be_kept(P):
         assert torch.equal(P.spec_k_gemm8(x, w, scratch=scratch), want)
     for call in (lambda: P.spec_k_gemm8(x, w, scratch=scratch[:n - 256]), lambda: P.spec_k_gemm8(x[:, :100], w), lambda: P.spec_k_gemm8(x.half(), w),
                  lambda: P.spec_k_gemm8(x[:0], w), lambda: P.spec_k_gemm8(x, w, out_dtype=torch.float16), lambda: P.spec_k_gemm8(x.cpu(), w),
-                 lambda: P.spec_k_gemm8(x, w, out=torch.empty(40, 51, device="cuda")), lambda: P.spec_k_gemm8(x.t().contiguous().t(), w)):
+                 lambda: P.spec_k_gemm8(x, w, out=torch.empty(40, 51, device="cuda")), lambda: P.spec_k_gemm8(x.t().contiguous().t(), w),
+                 lambda: P.spec_k_gemm8(x, P.spec_pack_weight(torch.zeros(50, 200, device="cuda"))), lambda: P.spec_k_gemm8(x[:1].expand(40, 200), w),
+                 lambda: P.spec_k_gemm8(x, torch.empty_like(w))):
         with pytest.raises(P.SpecError):
             call()
 
@@ -392,7 +394,7 @@ def test_attention8_binding_refusals(P):
     d = torch.zeros(3, dtype=torch.int32, device="cuda")
     ok = dict(q=q, cache8=c, n_blocks=1, kwin=k[64:].contiguous(), vwin=v[64:].contiguous(), base=65, depth=d, anc=None, hq=hq, hkv=hkv, hd=hd)
     for kw in (dict(q=q.bfloat16()), dict(q=q[:, :64]), dict(n_blocks=2), dict(cache8=None), dict(kwin=k[64:].float()), dict(vwin=v[:64]), dict(base=63), dict(depth=d.long()),
-               dict(depth=d[:2]), dict(anc=torch.zeros(3, 15, dtype=torch.int32, device="cuda")), dict(hq=3), dict(hd=128), dict(max_depth=-1),
+               dict(depth=d[:2]), dict(anc=torch.zeros(3, 15, dtype=torch.int32, device="cuda")), dict(hq=3), dict(hd=128), dict(max_depth=-1), dict(max_depth=2 ** 32), dict(base=2 ** 32 + 65),
                dict(out=torch.empty(3, 256, device="cuda")), dict(q=q.cpu()),
                dict(kwin=k[64:64], vwin=v[64:64]), dict(anc=torch.zeros(3, 16, dtype=torch.int32, device="cuda"), max_depth=16)):
         with pytest.raises(P.SpecError):
@@ -506,6 +508,18 @@ def test_rotary_adjoint_is_the_gradient(P, layout):
         up, down = (P.spec_k_rotary(plan, [x + s * d], 1234)[0].double() for s in (1, -1))
         slope = float(((up - down) * g.double()).sum() / 0.5)
         assert abs(slope - float(gx[at])) <= 2.0 ** -18 * 2 * (float(g.abs().max()) * 4 * float(x.abs().max()) + 1)
+
+
+def test_rotary_binding_refusals(P):
+    plan = P.spec_rotary_plan(64, 1e4)
+    x, pos = torch.zeros(4, 2, 64, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    for call in (lambda: P.spec_k_rotary(plan, [], 0), lambda: P.spec_k_rotary(plan, [x] * 4, 0), lambda: P.spec_k_rotary(plan, [x[0]], 0), lambda: P.spec_k_rotary(plan, [x, x[:3]], 0),
+                 lambda: P.spec_k_rotary(plan, [x, x[..., :32]], 0), lambda: P.spec_k_rotary(plan, [x.half()], 0), lambda: P.spec_k_rotary(plan, [x], pos.long()),
+                 lambda: P.spec_k_rotary(plan, [x], pos[:3]), lambda: P.spec_k_rotary(plan, [x], 2 ** 31), lambda: P.spec_k_rotary(plan, [x], 0, outs=[x, x]),
+                 lambda: P.spec_k_rotary(plan, [x], 0, outs=[x[:, :1]]), lambda: P.spec_k_rotary(plan, [x], 0, turned=[True, False]), lambda: P.spec_k_rotary(plan, [x.cpu()], 0),
+                 lambda: P.spec_k_rotary(plan, [x.transpose(1, 2)], 0), lambda: P.spec_k_rotary(P.spec_rotary_plan(128, 1e4), [x], 0), lambda: P.spec_k_rotary(plan, [x[:0]], 0)):
+        with pytest.raises(P.SpecError):
+            call()
 
 
 def test_rotary_not_finite_values_stay_in_their_plane(P):
