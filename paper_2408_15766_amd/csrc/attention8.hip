@@ -1,6 +1,4 @@
 // Attention over a cache of 64-token blocks in 8 bits with a bf16 window behind it, and the cache's store and load (include/spec_layer8.h).
-#include <type_traits>
-
 #include "common.h"
 #include "fp8.h"
 #include "kernels.h"
@@ -178,7 +176,7 @@ __device__ __forceinline__ void weigh(Running<HD> &r, float q_scale, uint32_t ex
 #pragma unroll
   for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-    for (int i = 0; i < 16; i++) top = __builtin_elementwise_maximum(top, s[kt][i]);   // (with a NaN among them the query's result is NaN, whatever the reference)
+    for (int i = 0; i < 16; i++) top = __builtin_elementwise_maximum(top, s[kt][i]);   // (v_maximum3: no quieting ahead of it; with a NaN among them the query's result is NaN, whatever the reference)
   r.raise(max_halves(top) * f);
   const float minus = (float)(ev - top_exp) + kCutLift - r.m;   // (the reference of a query whose scores are all NaN stays -inf: its weights are NaN)
   float sum = 0.f;
@@ -508,6 +506,9 @@ __device__ __forceinline__ bool place_of(const Plan8 &p, int hkv, Place8 &at) {
 
 // Many queries: WAVES wavefronts of 32 queries each walk the part's keys together.  A block's codes are widened once, on their way into the LDS (two buffers; the
 // next block's are in registers meanwhile), in the order in which the products read them.
+// Eight wavefronts take 1.9 us a block: 256 workgroups together 1.14 PFLOP/s, where products from registers alone reach 1.6 on such data (the clock falls under them).
+// Tried, with the same 1.9: two teams of four wavefronts that take turns at the matrix instructions and at the weights, a barrier between; four wavefronts of 64 queries, scores of the
+// next tile beside the weights of this one (2.4: the sums of 64 queries lie in the accumulation registers, and every read of one is an instruction).
 template <int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void attention8_wide_kernel(Attn8Args a, Plan8 plan) {
   constexpr int kCodes = 2 * kKv8Block * HD, kUnits = kCodes / 16, kThreads = WAVES * 64, kEach = kUnits / kThreads;   // of 16 codes, per thread
@@ -523,8 +524,9 @@ __global__ __launch_bounds__(WAVES * 64) void attention8_wide_kernel(Attn8Args a
   const float *qp = a.q + query * HD;
   Running<HD> r;
   r.clear();
-  if (at.part < plan.block_parts) {
-    const int b0 = range_at(a.n_blocks, plan.block_parts, at.part), b1 = range_at(a.n_blocks, plan.block_parts, at.part + 1);
+  const int b0 = at.part < plan.block_parts ? joined_range_at(plan, a.n_blocks, at.qb, at.part) : 0;
+  const int b1 = at.part < plan.block_parts ? joined_range_at(plan, a.n_blocks, at.qb, at.part + 1) : 0;
+  if (b0 < b1) {
     const size_t block_bytes = kv8_block_bytes(a.hkv, HD);
     const unsigned char *base = a.cache8 + (size_t)at.kvh * kCodes + tid * 16;
     const unsigned char *exps = a.cache8 + (size_t)a.hkv * kCodes + 2 * at.kvh;
@@ -568,159 +570,11 @@ __global__ __launch_bounds__(WAVES * 64) void attention8_wide_kernel(Attn8Args a
     const float up = exp2_((float)top_exp);
 #pragma unroll
     for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
-  } else {
-    const int w_begin = (at.part - plan.block_parts) * plan.win_part;
-    window_together<HD, WAVES>(a, r, qp, row, real, at.kvh, w_begin, min(w_begin + plan.win_part, a.win_rows), lds);
   }
-  const float l = sum_halves(r.l);
-  if (!real || (parts == 1 && a.depth[row] < 0)) return;
-#pragma unroll
-  for (int db = 0; db < HD / 32; db++) put_dims<HD>(a, query, at.part, parts, db, g, r.o[db], r.m, l);
-}
-
-// More than 128 queries: eight wavefronts of 32 queries in two teams of four, one of each on a SIMD, that take turns: while one team's products run (outputs of block n - 1, scores of block
-// n), the other makes weights out of its scores (block n or n - 1) and widens its share of the keys and values to come.  A barrier ends each turn, and
-// team 1 is a turn behind.  Keys are needed a block ahead of values; step n of the staging is keys n and values n - 1, two buffers each: team 0 puts its share of step
-// n + 1 there while team 1 is at its products n, team 1 its share of step n + 2 while team 0 is at n + 1; what they write over has been read by both.
-// Without turns the wavefronts of a SIMD ran in step, and products, weights and LDS reads one behind the other: @@.
-template <int HD>
-__global__ __launch_bounds__(512) void attention8_teams_kernel(Attn8Args a, Plan8 plan) {
-  constexpr int kHalf = kKv8Block * HD, kUnits = 2 * kHalf / 16, kEach = kUnits / 512;   // codes of a block's keys (or values); units of 16, per thread
-  static_assert(kEach * 512 == kUnits, "whole units");
-  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // keys, keys, values, values: 2 kHalf each, or WindowLds
-  Place8 at;
-  if (!place_of(plan, a.hkv, at)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, g = lane >> 5;
-  const int G = a.hq / a.hkv, index = (at.qb * 8 + wave) * 32 + c, parts = plan.block_parts + plan.win_parts;
-  const bool real = index < a.rows * G;
-  const int row = real ? index / G : a.rows - 1;
-  const size_t query = (size_t)row * a.hq + at.kvh * G + (real ? index % G : 0);
-  const float *qp = a.q + query * HD;
-  Running<HD> r;
-  r.clear();
-  const int b0 = at.part < plan.block_parts ? joined_range_at(plan, a.n_blocks, at.qb, at.part) : 0;
-  const int n = at.part < plan.block_parts ? joined_range_at(plan, a.n_blocks, at.qb, at.part + 1) - b0 : 0;
-  if (n > 0) {
-    const int team = wave >> 2;
-    const size_t block_bytes = kv8_block_bytes(a.hkv, HD);
-    const unsigned char *base = a.cache8 + (size_t)b0 * block_bytes + (size_t)at.kvh * 2 * kHalf + tid * 16;
-    const unsigned char *exps = a.cache8 + (size_t)b0 * block_bytes + (size_t)a.hkv * 2 * kHalf + 2 * at.kvh;
-    u32x4_t next[kEach];
-    auto fetch = [&](int step) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < kEach; i++) {
-        const bool values = (i * 512 + wave * 64) * 2 >= kUnits;
-        next[i] = *(const u32x4_t *)(base + (size_t)min(max(step - (values ? 1 : 0), 0), n - 1) * block_bytes + i * 512 * 16);
-      }
-    };
-    auto put = [&](int step) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < kEach; i++) {
-        const int piece = i * 8 + wave;                       // 64 units
-        const bool values = piece * 128 >= kUnits;
-        unsigned char *p = lds + (values ? 4 * kHalf + ((step - 1) & 1) * 2 * kHalf + (piece - kUnits / 128) * 2048 : (step & 1) * 2 * kHalf + piece * 2048) + lane * 16;
-        u32x4_t x, y;
-        widen(next[i], x, y);
-        *(u32x4_t *)p = x;
-        *(u32x4_t *)(p + 1024) = y;
-      }
-    };
-    auto end_turn = [&]() __attribute__((always_inline)) {
-      __builtin_amdgcn_sched_barrier(0);
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt(0xC07F);                     // this wavefront's LDS accesses done; loads from memory go on
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    fetch(0);
-    const Query8<HD> q = load_query8<HD>(qp, g, a.scale);
-    put(0);                                                   // (its values: any block's, read by nobody)
-    fetch(1);
-    int top_exp = -127;
-    f32x16_t s[2];
-    u32x4_t p[4];                                             // weights of 16 keys each
-    // A turn's products: the outputs of block step - 1, the scores of block step, kAhead operands on their way from the LDS at a time (in the compiler's own order one to three
-    // were, and the products waited for them: @@)
-    constexpr int kOut = 4 * (HD / 32), kScore = 2 * (HD / 16), kAhead = 6;
-    auto products = [&](auto with_outputs, auto with_scores, int step) __attribute__((always_inline)) {
-      constexpr int kFrom = decltype(with_outputs)::value ? 0 : kOut, kTo = decltype(with_scores)::value ? kOut + kScore : kOut;
-      const unsigned char *v = lds + 4 * kHalf + ((step - 1) & 1) * 2 * kHalf + lane * 16, *k = lds + (step & 1) * 2 * kHalf + lane * 16;
-      auto operand = [&](int i) __attribute__((always_inline)) {
-        const int h = i / (HD / 32), db = i % (HD / 32), t = (i - kOut) / 2, kt = (i - kOut) % 2;
-        return i < kOut ? *(const u32x4_t *)(v + ((h >> 1) * (HD / 16) + 2 * db + (h & 1)) * 1024) : *(const u32x4_t *)(k + (kt * (HD / 16) + t) * 1024);
-      };
-      u32x4_t f[kAhead];
-#pragma unroll
-      for (int i = 0; i < kAhead; i++) f[i] = operand(kFrom + i);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = kFrom; i < kTo; i++) {
-        const u32x4_t &x = f[(i - kFrom) % kAhead];
-        if (i < kOut) r.o[i % (HD / 32)] = mul_f16(x, p[i / (HD / 32)], r.o[i % (HD / 32)]);
-        else {
-          f32x16_t &to = s[(i - kOut) % 2];
-          if (i - kOut < 2)
-#pragma unroll
-            for (int e = 0; e < 16; e++) to[e] = 0.f;
-          to = mul_f16(x, q.f[(i - kOut) / 2], to);
-        }
-        if (i + kAhead < kTo) f[(i - kFrom) % kAhead] = operand(i + kAhead);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    };
-    using Yes = std::integral_constant<bool, true>;
-    using No = std::integral_constant<bool, false>;
-    uint32_t e = *(const uint16_t *)exps;                     // the next weights' block
-    auto weights = [&](int step) __attribute__((always_inline)) {
-      const uint32_t now = __builtin_amdgcn_readfirstlane((int)e);
-      e = *(const uint16_t *)(exps + (size_t)min(step + 1, n - 1) * block_bytes);
-      weigh<HD>(r, q.scale, now, top_exp, s, p);
-    };
-    end_turn();
-    if (team == 0) {
-      products(No{}, Yes{}, 0);
-      end_turn();
-      for (int i = 0; i < n - 1; i++) {
-        weights(i);
-        put(i + 1);
-        fetch(i + 2);
-        end_turn();
-        products(Yes{}, Yes{}, i + 1);
-        end_turn();
-      }
-      weights(n - 1);
-      put(n);
-      end_turn();
-      products(Yes{}, No{}, n);
-      end_turn();
-    } else {
-      put(1);
-      fetch(2);
-      end_turn();
-      products(No{}, Yes{}, 0);
-      end_turn();
-      for (int i = 0; i < n - 1; i++) {
-        weights(i);
-        put(i + 2);
-        fetch(i + 3);
-        end_turn();
-        products(Yes{}, Yes{}, i + 1);
-        end_turn();
-      }
-      weights(n - 1);
-      end_turn();
-      products(Yes{}, No{}, n);
-    }
-    r.l *= kCutSum;
-    const float up = exp2_((float)top_exp);
-#pragma unroll
-    for (int db = 0; db < HD / 32; db++) r.o[db] *= up;
-    __syncthreads();
+  if (plan.win_parts ? at.part >= plan.block_parts : at.part == plan.block_parts - 1) {   // (behind a loop over blocks: its last barrier frees the LDS)
+    const int w_begin = plan.win_parts ? (at.part - plan.block_parts) * plan.win_part : 0;
+    window_together<HD, WAVES>(a, r, qp, row, real, at.kvh, w_begin, plan.win_parts ? min(w_begin + plan.win_part, a.win_rows) : a.win_rows, lds);
   }
-  const int w_begin = plan.win_parts ? (at.part - plan.block_parts) * plan.win_part : 0;
-  if (plan.win_parts ? at.part >= plan.block_parts : at.part == plan.block_parts - 1)
-    window_together<HD, 8>(a, r, qp, row, real, at.kvh, w_begin, plan.win_parts ? min(w_begin + plan.win_part, a.win_rows) : a.win_rows, lds);
   const float l = sum_halves(r.l);
   if (!real || (parts == 1 && a.depth[row] < 0)) return;
 #pragma unroll
@@ -905,16 +759,6 @@ template <int HD, int WAVES> hipError_t launch_wide(const Attn8Args &a, const Pl
   return hipGetLastError();
 }
 
-template <int HD> hipError_t launch_teams(const Attn8Args &a, const Plan8 &p, unsigned grid, hipStream_t st) {
-  constexpr int kLds = WindowLds<HD, 8>::total;
-  static_assert(kLds >= 512 * HD, "keys and values fit");
-  static bool allowed[64] = {};
-  const hipError_t e = allow_lds((const void *)attention8_teams_kernel<HD>, kLds, allowed);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(attention8_teams_kernel<HD>, dim3(grid), dim3(512), kLds, st, a, p);
-  return hipGetLastError();
-}
-
 template <int HD, int GROUPS> hipError_t launch_merge(const Attn8Args &a, int parts, hipStream_t st) {
   constexpr int kEach = 1024 / (HD * GROUPS);                 // queries of a workgroup
   const int64_t grid = ((int64_t)a.rows * a.hq + kEach - 1) / kEach;
@@ -938,7 +782,7 @@ template <int HD> hipError_t launch_hd(const Attn8Args &a, hipStream_t st) {
     e = hipGetLastError();
   } else if (p.waves == 2) e = launch_wide<HD, 2>(a, p, (unsigned)grid, st);
   else if (p.waves == 4) e = launch_wide<HD, 4>(a, p, (unsigned)grid, st);
-  else e = launch_teams<HD>(a, p, (unsigned)grid, st);
+  else e = launch_wide<HD, 8>(a, p, (unsigned)grid, st);
   if (e != hipSuccess || parts == 1) return e;
   if (parts <= 8) return launch_merge<HD, 1>(a, parts, st);
   if (parts <= 16) return launch_merge<HD, 2>(a, parts, st);
