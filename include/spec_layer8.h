@@ -87,8 +87,9 @@ int spec_k_kv8_load(const void *cache8, int32_t first_block, int32_t n_blocks, i
  * kwin, vwin: [win_rows, hkv*hd] bf16, win_rows >= 1 and 16-byte aligned, as are q, out and cache8 (256).
  * out: [rows, hq*hd] bf16.  depth[i] <= max_depth for every row (a row beyond is taken to be at max_depth); with anc, max_depth <= 15.
  * hd 64 or 128, hq/hkv one of 1, 2, 4, 8; hkv <= 128; rows <= 2^20.  Scratch: spec_k_attention8_scratch_bytes(..), 256-byte aligned
- * (host only; 0 if the call needs none, then scratch may be NULL, and for bad sizes).  Softmax statistics and sums are fp32; the weights of the 8-bit part are rounded to fp16 (2^-12, as queries are there), those of the
- * window to bf16 twice over (2^-17). */
+ * (host only; 0 if the call needs none, then scratch may be NULL, and for bad sizes).  Softmax statistics and sums are fp32.  In the 8-bit part queries are rounded to
+ * fp16 relative to the row's largest value (2^-11) and weights cut to fp16 (at most 2^-10 off, centred); in
+ * the window both go in two bf16 terms (2^-16).  The result of a row may change in its last bits with the rows beside it. */
 uint64_t spec_k_attention8_scratch_bytes(int32_t rows, int32_t hq, int32_t hkv, int32_t hd, int32_t n_blocks, int32_t win_rows);
 int spec_k_attention8(const float *q, const void *cache8, int32_t n_blocks, const void *kwin, const void *vwin, int32_t win_rows, int32_t rows,
                       int32_t hq, int32_t hkv, int32_t hd, int32_t base, const int32_t *depth, const int32_t *anc, int32_t max_depth,

@@ -67,8 +67,8 @@ __global__ __launch_bounds__(256) void kv8_load_kernel(const unsigned char *cach
 // The queries of a kv head are numbered row * G + head in group; a wavefront owns 32 of them as the columns of its products: lane (c = lane % 32, g = lane / 32)
 // holds query c, of a 32-key tile's scores the keys 8 i + 4 g + 0 .. 3 (i < 4), of the outputs the same dims of every 32.
 //
-// In the blocks the products are fp16: codes are exact there, a query row is divided by the power of two of its largest value and rounded once (2^-12), and
-// a weight is rounded once.  Weights are 2^(score - reference + kRefLift): up to 2^15 while the reference lags by kRefSlack, so that fp16 keeps its full precision for
+// In the blocks the products are fp16: codes are exact there, a query row is divided by the power of two of its largest value and rounded once (2^-11), and
+// a weight is cut once.  Weights are 2^(score - reference + kRefLift): up to 2^15 while the reference lags by kRefSlack, so that fp16 keeps its full precision for
 // weights down to 2^-29 of the largest.  A block's exponents go into the scores' factor and into the weights (relative to the largest of the
 // blocks so far, which the outputs are in units of); nothing is done per value for them.
 constexpr float kRefLift = 7.f;
@@ -510,7 +510,7 @@ __device__ __forceinline__ bool place_of(const Plan8 &p, int hkv, Place8 &at) {
 // Tried, with the same 1.9: two teams of four wavefronts that take turns at the matrix instructions and at the weights, a barrier between; four wavefronts of 64 queries, scores of the
 // next tile beside the weights of this one (2.4: the sums of 64 queries lie in the accumulation registers, and every read of one is an instruction).
 template <int HD, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void attention8_wide_kernel(Attn8Args a, Plan8 plan) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 2 ? 1 : 2) void attention8_wide_kernel(Attn8Args a, Plan8 plan) {
   constexpr int kCodes = 2 * kKv8Block * HD, kUnits = kCodes / 16, kThreads = WAVES * 64, kEach = kUnits / kThreads;   // of 16 codes, per thread
   static_assert(kEach * kThreads == kUnits, "whole units");
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];   // 2 x 2 kCodes, or WindowLds

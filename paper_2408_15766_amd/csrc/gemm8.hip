@@ -323,11 +323,14 @@ template <int WM, int WN, int TB, int WB>
 struct Tile8 {
   static constexpr int kWaves = WM * WN, kTok = WM * TB * 32, kRows = WN * WB * 32;
   static constexpr int kX = kTok * 64, kW = kRows * 64;       // bytes of a stage
-  static constexpr int kXLoads = kX / 1024 / kWaves, kWLoads = kW / 1024 / kWaves;   // 1 KiB copies per wavefront and stage
+  static constexpr int kXParts = kX / 1024, kWParts = kW / 1024;   // 1 KiB, 16 rows, each
+  static constexpr int kXLoads = (kXParts + kWaves - 1) / kWaves, kWLoads = (kWParts + kWaves - 1) / kWaves;   // copies per wavefront and stage (some twice where they do not divide)
   // exponents: 64 bytes per 16-row block, tokens first; a wavefront copies those of four blocks (those past the end: the last again)
   static constexpr int kBlocks = (kTok + kRows) / 16, kE = kWaves * 256;
   static constexpr int kLoads = kXLoads + kWLoads + 1;
-  static_assert(kXLoads * kWaves * 1024 == kX && kWLoads * kWaves * 1024 == kW && kBlocks <= 4 * kWaves, "whole copies");
+  static_assert(kBlocks <= 4 * kWaves, "exponents");
+  static __device__ __forceinline__ int x_part(int wave, int i) { return kXParts % kWaves ? min(wave * kXLoads + i, kXParts - 1) : wave * kXLoads + i; }
+  static __device__ __forceinline__ int w_part(int wave, int i) { return kWParts % kWaves ? min(wave * kWLoads + i, kWParts - 1) : wave * kWLoads + i; }
 };
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
@@ -387,19 +390,19 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a
   __amdgpu_buffer_rsrc_t xsrc[L::kXLoads], wsrc[L::kWLoads];
 #pragma unroll
   for (int i = 0; i < L::kXLoads; i++)
-    xsrc[i] = buffer_of(a.x8 + (size_t)min(tok_tile * (L::kTok / 16) + wave * L::kXLoads + i, px.blocks - 1) * px.groups * kTile8);
+    xsrc[i] = buffer_of(a.x8 + (size_t)min(tok_tile * (L::kTok / 16) + L::x_part(wave, i), px.blocks - 1) * px.groups * kTile8);
 #pragma unroll
   for (int i = 0; i < L::kWLoads; i++)
-    wsrc[i] = buffer_of(a.w8 + (size_t)min(row0 / 16 + wave * L::kWLoads + i, pw.blocks - 1) * pw.groups * kTile8);
+    wsrc[i] = buffer_of(a.w8 + (size_t)min(row0 / 16 + L::w_part(wave, i), pw.blocks - 1) * pw.groups * kTile8);
   const int eb = min(wave * 4 + lane / 16, L::kBlocks - 1);
   const uint32_t *esrc = (const uint32_t *)(eb < L::kTok / 16 ? a.x8 + packed8_exps(px) + (size_t)min(tok_tile * (L::kTok / 16) + eb, px.blocks - 1) * px.quads * 64
                                                               : a.w8 + packed8_exps(pw) + (size_t)min(row0 / 16 + eb - L::kTok / 16, pw.blocks - 1) * pw.quads * 64) + lane % 16;
   auto copy = [&](unsigned char *x, unsigned char *w, unsigned char *e, int s) __attribute__((always_inline)) {
     s = min(s, n_stage - 1);                                  // past the end: the last stage again (never read)
 #pragma unroll
-    for (int i = 0; i < L::kWLoads; i++) load_to_lds(wsrc[i], lane * 16, s * 1024, w + (wave * L::kWLoads + i) * 1024);
+    for (int i = 0; i < L::kWLoads; i++) load_to_lds(wsrc[i], lane * 16, s * 1024, w + L::w_part(wave, i) * 1024);
 #pragma unroll
-    for (int i = 0; i < L::kXLoads; i++) load_to_lds(xsrc[i], lane * 16, s * 1024, x + (wave * L::kXLoads + i) * 1024);
+    for (int i = 0; i < L::kXLoads; i++) load_to_lds(xsrc[i], lane * 16, s * 1024, x + L::x_part(wave, i) * 1024);
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(esrc + (s >> 3) * 16), (lds_void *)(e + wave * 256), 4, 0, 0);
   };
 
@@ -505,10 +508,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm8_tile_kernel(Gemm8Args a
 
   // Sums go through the LDS (the tokens' buffers, a share for each wavefront) into whole rows: a lane has four columns of one token, and stores of these touch 32 rows at a time.
   // Pieces of 16 bytes are permuted by the row, so that neither side meets in a bank.
-  constexpr int kCols = WB * 32, kChunks = kCols / 4, kShare = 32 * kCols * 4, kPer = L::kX / kShare;
-  static_assert(L::kWaves * kShare == 4 * L::kX, "a share each");
+  constexpr int kCols = WB * 32, kChunks = kCols / 4, kShare = 32 * kCols * 4, kPer = L::kX / kShare, kPerW = L::kW / kShare;
+  static_assert(kPer >= 1 && (L::kWaves <= 4 * kPer || (kPerW >= 1 && L::kWaves - 4 * kPer <= 2 * kPerW)), "a share each");
   wg_barrier();                                               // everybody's operands are read
-  unsigned char *const mine = (wave / kPer == 0 ? x0 : wave / kPer == 1 ? x1 : wave / kPer == 2 ? x2 : x3) + wave % kPer * kShare;
+  unsigned char *mine = (wave / kPer == 0 ? x0 : wave / kPer == 1 ? x1 : wave / kPer == 2 ? x2 : x3) + wave % kPer * kShare;
+  if constexpr (L::kWaves > 4 * kPer)                         // (the weights' buffers, too)
+    if (const int more = wave - 4 * kPer; more >= 0) mine = (more / kPerW == 0 ? w0 : w1) + more % kPerW * kShare;
   const int col0 = row0 + wn * kCols;
 #pragma unroll
   for (int t = 0; t < TB; t++) {
@@ -555,9 +560,10 @@ hipError_t launch_tile(const Gemm8Args &a, hipStream_t st) {
 //   256 x 256: 56, one fits a unit (512 x 28672: 60 against 75 in 256 x 128)        256 x 128: 36, one (2048 x 4096: 36 against 50 in 256 x 256 and 42 in 128 x 128)
 //   128 x 128: 24, or two in 41 (1024 x 4096: 24 against 33 in 256 x 128)           64 x 128: 16, or two in 30 (333 x 4096: 16 against 20 in 128 x 128)
 //   64 x 64, eight stages deep: 11, or two in 17.5 (60 x 12288: 15 against 20 in 64 x 128)
-enum { kLargest = 0, kTiles8 = 5 };
+//   64 x 96, eight stages deep: 14.3, one (60 x 22016, 230 tiles: 20.6 against 26 in 64 x 64, 64 x 128 and 128 x 128; 60 x 28672, 299 tiles: 33 against 28)
+enum { kLargest = 0, kTiles8 = 6 };
 struct TileCost { int tok, rows, fit; float one, fitting; };  // `fit` workgroups on a unit at once take `fitting`
-constexpr TileCost kTileCosts[kTiles8] = {{256, 256, 1, 56.f, 56.f}, {256, 128, 1, 36.f, 36.f}, {128, 128, 2, 24.f, 41.f}, {64, 128, 2, 16.f, 30.f}, {64, 64, 2, 11.f, 17.5f}};
+constexpr TileCost kTileCosts[kTiles8] = {{256, 256, 1, 56.f, 56.f}, {256, 128, 1, 36.f, 36.f}, {128, 128, 2, 24.f, 41.f}, {64, 128, 2, 16.f, 30.f}, {64, 64, 2, 11.f, 17.5f}, {64, 96, 1, 14.3f, 14.3f}};
 float tiles_cost(int shape, int m, int rows) {
   const TileCost &c = kTileCosts[shape];
   const int64_t tiles = (int64_t)((m + c.tok - 1) / c.tok) * ((rows + c.rows - 1) / c.rows), a_round = 256 * c.fit, left = tiles % a_round;
@@ -576,7 +582,8 @@ template <typename OUT, bool VEC> hipError_t launch_tiles(int shape, const Gemm8
     case 1: return launch_tile<OUT, VEC, 4, 2, 2, 2, 4>(a, st);
     case 2: return launch_tile<OUT, VEC, 2, 4, 2, 1, 4>(a, st);
     case 3: return launch_tile<OUT, VEC, 1, 4, 2, 1, 4>(a, st);
-    default: return launch_tile<OUT, VEC, 2, 2, 1, 1, 8>(a, st);
+    case 4: return launch_tile<OUT, VEC, 2, 2, 1, 1, 8>(a, st);
+    default: return launch_tile<OUT, VEC, 2, 3, 1, 1, 8>(a, st);
   }
 }
 

@@ -5,8 +5,8 @@ Tolerances.  u32 = 2^-24, u16 = 2^-8 (bf16), h = 2^-11 (fp16): the largest relat
 * gemm8, bf16 results: in addition u16 of the result, and what the 8-bit matrix instruction drops: products of 128 k are lined up 2^-13 below
   the largest, so that those from 2^-6 of it on are exact (a product has 8 bits) and smaller ones lose at most that step (one more bit allowed here).
 * attention8: u16 of the result; queries in fp16 move a score by at most d = h sum|q k| / sqrt(hd) + 2^-24 max|q| sum|k| / sqrt(hd) (elements below
-  fp16's normal range beside the row's largest), weights by e^(2 d) - 1 in all, and weights in fp16 by h, taken twice (numerator, and a sum that may hold either
-  form); 2^-17 + 1e-6 for the window's and fp32 arithmetic.
+  fp16's normal range beside the row's largest), weights by e^(2 d) - 1 in all, and weights in fp16 by at most 2 h (cut off and centred; rounded: h);
+  2^-17 + 1e-6 for the window's and fp32 arithmetic.
 * kv8: exact.  rotary: angles below 2^-22 off, so 2^-21 mscale (|a| + |b|), and the output's rounding.
 """
 import math
@@ -73,6 +73,37 @@ def test_gemm8_sizes(P, m, k, rows, dtype, out):
     x = (rand(m * 7 + k, m, k) * gain).to(DT[dtype]).cuda()
     w = rand(rows, rows, k, scale=0.02).to(DT[dtype]).cuda()
     check_gemm(P, x, w, DT[out])
+
+
+def held_gpu(x):
+    """O.held_rows on the device, in float64."""
+    r, k = x.shape
+    y = torch.nn.functional.pad(x.double(), (0, -k % 128)).view(r, -1, 128)
+    m, e = torch.frexp(y.abs().amax(2, keepdim=True) / 448)
+    e = torch.where(m > 0, torch.where(m > 0.5, e, e - 1), -100).clamp(min=-100).double()
+    t = y * torch.exp2(-e)
+    step = torch.exp2((torch.frexp(t)[1] - 1).clamp(min=-6).double() - 3)
+    return torch.round(t / step) * step * torch.exp2(e)
+
+
+@pytest.mark.parametrize("m,k,rows", [(40, 300, 20001), (64, 700, 12290), (300, 130, 12000), (90, 256, 20480), (2047, 130, 28671), (2048, 384, 12288), (2000, 129, 12289),
+                                      (1024, 200, 4100), (600, 512, 4097), (513, 256, 28600), (4096, 256, 4096), (200, 600, 3000)])
+def test_gemm8_launches_of_many_tiles(P, m, k, rows):
+    """Every shape of tile, whole and ragged, and launches in two parts.  (The 8-bit instruction's loss is bounded by 128 times 2^-12 of the largest product of a block.)"""
+    g = torch.Generator(device="cuda").manual_seed(m + rows)
+    x, w = (torch.randn(n, k, generator=g, device="cuda") for n in (m, rows))
+    assert np.array_equal(f64(held_gpu(x[:5])).reshape(5, -1)[:, :k], O.held_rows(f64(x[:5])))
+    xq, wq = held_gpu(x), held_gpu(w)
+    ref, size = xq.flatten(1) @ wq.flatten(1).t(), xq.flatten(1).abs() @ wq.flatten(1).abs().t()
+    lost = 2.0 ** -5 * (xq.abs().amax(2) @ wq.abs().amax(2).t())
+    w8 = P.spec_pack_weight8(w)
+    tol = (k + 8) * U32 * size
+    for out, bound in ((torch.float32, tol), (torch.bfloat16, tol + lost + U16 * (ref.abs() + tol + lost))):
+        wide = torch.full((m, rows + 3), 7.0, dtype=out, device="cuda")
+        for y in (wide[:, 3:], torch.empty(m, rows, dtype=out, device="cuda")):
+            P.spec_k_gemm8(x, w8, out=y)
+            assert bool(((y.double() - ref).abs() <= bound).all())
+        assert bool((wide[:, :3] == 7).all())
 
 
 @pytest.mark.parametrize("m", [1, 5, 40, 300])
