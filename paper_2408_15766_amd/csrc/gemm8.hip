@@ -123,38 +123,27 @@ constexpr int kStreamWaves = 8;
 __device__ __forceinline__ Frag8 stream_frag(const unsigned char *tile, int lane) {
   return Frag8{__builtin_nontemporal_load((const u32x4_t *)(tile + lane * 16)), __builtin_nontemporal_load((const u32x4_t *)(tile + 1024 + lane * 16))};
 }
-// Rows rb0 .. of the weights (those past the end: the last again), with their exponents
-template <int RB> struct Weights8 {
-  const unsigned char *tile[RB];
-  const uint32_t *exp[RB];
-  __device__ __forceinline__ Weights8(const Gemm8Args &a, const Packed8 &pw, int rb0, int lane) {
-#pragma unroll
-    for (int b = 0; b < RB; b++) {
-      const int rb = min(rb0 + b, pw.blocks - 1);
-      tile[b] = a.w8 + (size_t)rb * pw.groups * kTile8;
-      exp[b] = (const uint32_t *)(a.w8 + packed8_exps(pw)) + (size_t)rb * pw.quads * 16 + (lane & 15);
-    }
-  }
+// A 16-row block of the weights, with its exponents
+struct Weights8 {
+  const unsigned char *tile;
+  const uint32_t *exp;
+  __device__ __forceinline__ Weights8(const Gemm8Args &a, const Packed8 &pw, int rb, int lane)
+      : tile(a.w8 + (size_t)rb * pw.groups * kTile8), exp((const uint32_t *)(a.w8 + packed8_exps(pw)) + (size_t)rb * pw.quads * 16 + (lane & 15)) {}
 };
-// The wavefronts' sums of B row blocks x T token tiles, in ascending order, into y
-template <typename OUT, bool VEC, int B, int T>
-__device__ __forceinline__ void join_waves(const Gemm8Args &a, const f32x4_t (&acc)[B][T], f32x4_t (*part)[B * T][64], int rb0, int t0) {
+// The wavefronts' sums of row block rb x T token tiles, in ascending order, into y
+template <typename OUT, bool VEC, int T>
+__device__ __forceinline__ void join_waves(const Gemm8Args &a, const f32x4_t (&acc)[T], f32x4_t (*part)[T][64], int rb) {
+  static_assert(T <= kStreamWaves, "a wavefront each");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-  for (int b = 0; b < B; b++)
-#pragma unroll
-    for (int t = 0; t < T; t++) part[wave][b * T + t][lane] = acc[b][t];
+  for (int t = 0; t < T; t++) part[wave][t][lane] = acc[t];
   __syncthreads();
+  if (wave >= T) return;
+  f32x4_t s = part[0][wave][lane];
 #pragma unroll
-  for (int i0 = 0; i0 < B * T; i0 += kStreamWaves) {
-    const int i = i0 + wave;
-    if (i >= B * T) break;
-    f32x4_t s = part[0][i][lane];
-#pragma unroll
-    for (int w = 1; w < kStreamWaves; w++) s += part[w][i][lane];
-    const int tok = (t0 + i % T) * 16 + (lane & 15);
-    if (tok < a.m) store4<VEC>((OUT *)a.y + (size_t)tok * a.ldy, (rb0 + i / T) * 16 + 4 * (lane >> 4), a.rows, s);
-  }
+  for (int w = 1; w < kStreamWaves; w++) s += part[w][wave][lane];
+  const int tok = wave * 16 + (lane & 15);
+  if (tok < a.m) store4<VEC>((OUT *)a.y + (size_t)tok * a.ldy, rb * 16 + 4 * (lane >> 4), a.rows, s);
 }
 
 // Up to 16 tokens, one 16-row block a workgroup: four tiles on the way in each wavefront.  RAW: the workgroup puts its tokens into 8 bits itself, into the LDS, while its first
@@ -168,7 +157,7 @@ __global__ __launch_bounds__(kStreamWaves * 64, 4) void gemm8_few_kernel(Gemm8Ar
   extern __shared__ __attribute__((aligned(16))) unsigned char tokens[];
   const Packed8 pw = packed8(a.rows, a.in);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
-  const Weights8<1> w(a, pw, blockIdx.x, lane);
+  const Weights8 w(a, pw, blockIdx.x, lane);
   const int g0 = pw.groups * wave / kStreamWaves, n = pw.groups * (wave + 1) / kStreamWaves - g0;
   const unsigned char *exps = RAW ? tokens + ((size_t)pw.groups << (mp_log2 + 7)) : a.x8 + packed8_exps(packed8(a.m, a.in));
   const int tok = RAW ? r16 & ((1 << mp_log2) - 1) : r16;
@@ -176,14 +165,14 @@ __global__ __launch_bounds__(kStreamWaves * 64, 4) void gemm8_few_kernel(Gemm8Ar
   struct Slot { Frag8 w, x; uint32_t ew, ex; };
   auto load = [&](Slot &s, int i) __attribute__((always_inline)) {
     const int g = g0 + i;
-    s.w = stream_frag(w.tile[0] + (size_t)g * kTile8, lane);
-    s.ew = w.exp[0][(g >> 2) * 16];
+    s.w = stream_frag(w.tile + (size_t)g * kTile8, lane);
+    s.ew = w.exp[(g >> 2) * 16];
     if constexpr (!RAW) {
       s.x = load_frag(a.x8 + (size_t)g * kTile8, lane);
       s.ex = ((const uint32_t *)exps)[(g >> 2) * 16 + r16];
     }
   };
-  f32x4_t acc[1][1] = {{f32x4_t{0.f, 0.f, 0.f, 0.f}}};
+  f32x4_t acc[1] = {f32x4_t{0.f, 0.f, 0.f, 0.f}};
   auto compute = [&](Slot &s, int i) __attribute__((always_inline)) {
     const int g = g0 + i, sh = 8 * (g & 3);
     if constexpr (RAW) {
@@ -191,7 +180,7 @@ __global__ __launch_bounds__(kStreamWaves * 64, 4) void gemm8_few_kernel(Gemm8Ar
       s.x = Frag8{*(const u32x4_t *)p, *(const u32x4_t *)(p + (64 << mp_log2))};
       s.ex = exps[(g << mp_log2) + tok];
     } else s.ex >>= sh;
-    acc[0][0] = product<kExact>(s.w, s.ew >> sh, s.x, s.ex, acc[0][0]);
+    acc[0] = product<kExact>(s.w, s.ew >> sh, s.x, s.ex, acc[0]);
   };
   Slot ring[R];
 #pragma unroll
@@ -232,20 +221,18 @@ __global__ __launch_bounds__(kStreamWaves * 64, 4) void gemm8_few_kernel(Gemm8Ar
       compute(ring[u % R], i + u);
       __builtin_amdgcn_sched_barrier(0);
     }
-  join_waves<OUT, VEC, 1, 1>(a, acc, part, blockIdx.x, 0);
+  join_waves<OUT, VEC, 1>(a, acc, part, blockIdx.x);
 }
 
-// 17 to 64 tokens (16 T), RB row blocks a workgroup, so that a token tile read from L2 serves RB weight tiles: a weight tile is read again, for the next 128 k, as soon as its products are under
-// way (RB tiles on the way in each wavefront), the tokens' one 128 k ahead.
-template <typename OUT, bool VEC, int T, int RB>
+// 17 to 64 tokens (16 T), one 16-row block a workgroup: a weight tile is read again, for the next 128 k, as soon as its products are under way, the
+// tokens' (from L2) ahead of them.  (Two to eight row blocks a workgroup, for fewer reads of the tokens, took no less: 60 x 22016 x 4096 28 to 42 us.)
+template <typename OUT, bool VEC, int T>
 __global__ __launch_bounds__(kStreamWaves * 64, 2) void gemm8_stream_kernel(Gemm8Args a) {
   constexpr bool kExact = sizeof(OUT) == 4;
-  constexpr int B = RB % 2 == 0 ? 2 : 1;                      // row blocks joined at a time
-  __shared__ f32x4_t part[kStreamWaves][B * T][64];
+  __shared__ f32x4_t part[kStreamWaves][T][64];
   const Packed8 pw = packed8(a.rows, a.in), px = packed8(a.m, a.in);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15;
-  const int rb0 = blockIdx.x * RB;
-  const Weights8<RB> w(a, pw, rb0, lane);
+  const Weights8 w(a, pw, blockIdx.x, lane);
   const unsigned char *xt[T];
   const uint32_t *xe[T];
 #pragma unroll
@@ -260,31 +247,25 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void gemm8_stream_kernel(Gemm
 #pragma unroll
     for (int t = 0; t < T; t++) { x.f[t] = load_frag(xt[t] + (size_t)g * kTile8, lane); x.e[t] = xe[t][(g >> 2) * 16]; }
   };
-  Frag8 wf[RB];
-  uint32_t we[RB];
-  auto load_w = [&](int b, int g) __attribute__((always_inline)) { wf[b] = stream_frag(w.tile[b] + (size_t)g * kTile8, lane); we[b] = w.exp[b][(g >> 2) * 16]; };
-  f32x4_t acc[RB][T];
+  Frag8 wf;
+  uint32_t we;
+  auto load_w = [&](int g) __attribute__((always_inline)) { wf = stream_frag(w.tile + (size_t)g * kTile8, lane); we = w.exp[(g >> 2) * 16]; };
+  f32x4_t acc[T];
 #pragma unroll
-  for (int b = 0; b < RB; b++)
-#pragma unroll
-    for (int t = 0; t < T; t++) acc[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < T; t++) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   auto step = [&](Tokens &x, Tokens &next, int g) __attribute__((always_inline)) {
     const int ahead = min(g + 1, g1 - 1), sh = 8 * (g & 3);   // (the last one: once more, and not used)
     load_x(next, ahead);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int b = 0; b < RB; b++) {
-#pragma unroll
-      for (int t = 0; t < T; t++) acc[b][t] = product<kExact>(wf[b], we[b] >> sh, x.f[t], x.e[t] >> sh, acc[b][t]);
-      __builtin_amdgcn_sched_barrier(0);
-      load_w(b, ahead);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int t = 0; t < T; t++) acc[t] = product<kExact>(wf, we >> sh, x.f[t], x.e[t] >> sh, acc[t]);
+    __builtin_amdgcn_sched_barrier(0);
+    load_w(ahead);
+    __builtin_amdgcn_sched_barrier(0);
   };
   if (g0 < g1) {
     Tokens x[2];
-#pragma unroll
-    for (int b = 0; b < RB; b++) load_w(b, g0);
+    load_w(g0);
     load_x(x[0], g0);
     int g = g0;
     for (; g + 2 <= g1; g += 2) {
@@ -293,30 +274,20 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void gemm8_stream_kernel(Gemm
     }
     if (g < g1) step(x[0], x[1], g);
   }
-#pragma unroll
-  for (int b = 0; b < RB; b += B) {
-    if (b) __syncthreads();
-    f32x4_t some[B][T];
-#pragma unroll
-    for (int i = 0; i < B; i++)
-#pragma unroll
-      for (int t = 0; t < T; t++) some[i][t] = acc[b + i][t];
-    join_waves<OUT, VEC, B, T>(a, some, part, rb0 + b, 0);
-  }
+  join_waves<OUT, VEC, T>(a, acc, part, blockIdx.x);
 }
 
-template <typename OUT, bool VEC, int T, int RB>
+template <typename OUT, bool VEC, int T>
 hipError_t launch_stream(const Gemm8Args &a, hipStream_t st) {
-  const int blocks = (a.rows + 15) / 16;
-  hipLaunchKernelGGL((gemm8_stream_kernel<OUT, VEC, T, RB>), dim3((blocks + RB - 1) / RB), dim3(kStreamWaves * 64), 0, st, a);
+  hipLaunchKernelGGL((gemm8_stream_kernel<OUT, VEC, T>), dim3((a.rows + 15) / 16), dim3(kStreamWaves * 64), 0, st, a);
   return hipGetLastError();
 }
 
 // ---- many tokens: tiles ------------------------------------------------------------
 // A workgroup owns WM * TB * 32 tokens x WN * WB * 32 weight rows, a wavefront TB x WB blocks of 32 x 32 of them.  Both operands are copied straight into the LDS, 64 k
-// (half a packed tile) at a time, four stages deep, and read from there in the order of the operands of the 32 x 32 x 64 product (weights as A, so that a lane
+// (half a packed tile) at a time, STAGES (four or eight) deep, and read from there in the order of the operands of the 32 x 32 x 64 product (weights as A, so that a lane
 // ends up with four consecutive columns of one token).  One barrier per stage: behind it the next stage is there for everybody and this stage's operands are in registers, so
-// that its buffer takes the copies of four stages on.
+// that its buffer takes the copies of STAGES stages on.
 // Every stage buffer is an array of its own, which tells the compiler what a read depends on.  The barrier stands behind the products of a stage's first 32 tokens, which cover the
 // wait for its last operands; operands of tokens are read again, for the next stage, as soon as their products are under way.
 template <int WM, int WN, int TB, int WB>
@@ -621,7 +592,7 @@ hipError_t launch_typed(Gemm8Args a, void *scratch, hipStream_t st) {
   a.x8 = (const unsigned char *)scratch;
   // 17 to 64 tokens through few rows: the weights straight into registers (us, 60 tokens: 4096 rows of 4096 9.1 against 11.1 in tiles of 64 x 64, of 11008 18.9 against 28.1;
   // 12288 rows of 4096 23.1 against 15.1)
-  if (a.m <= 64 && a.rows <= 4096) return a.m <= 32 ? launch_stream<OUT, VEC, 2, 1>(a, st) : launch_stream<OUT, VEC, 4, 1>(a, st);
+  if (a.m <= 64 && a.rows <= 4096) return a.m <= 32 ? launch_stream<OUT, VEC, 2>(a, st) : launch_stream<OUT, VEC, 4>(a, st);
   a.row_begin = 0; a.row_end = a.rows;
   const Tiles8 all = best_tiles(a.m, a.rows);
   // whole rounds of the largest tile, and the rows that are left in what suits them: 2048 x 28672 x 4096 (3.5 rounds) 217 -> 205 us, 2048 x
