@@ -81,15 +81,18 @@ int spec_k_kv8_load(const void *cache8, int32_t first_block, int32_t n_blocks, i
  * query in q[i] ([hq*hd], fp32), sits at position base + depth[i] (base >= n8) and
  * attends to positions 0 .. base + depth[i]: n8 <= p < base is window row p - n8,
  * p >= base is window row base - n8 + anc[i*16 + p - base] (anc NULL: p - n8, a
- * causal chain).  A position whose window row is negative or not below win_rows is left out; a row that sees nothing, or scores of -infinity only, gets zeros.
+ * causal chain).  A position whose window row is negative or not below win_rows is left out; a row that sees nothing, or only window rows with scores of -infinity, gets zeros.
  * A row of negative depth is padding: its output is left as it was.  What a row
  * does not see does not touch its result, whatever is stored there (NaN included).
- * kwin, vwin: [win_rows, hkv*hd] bf16, win_rows >= 1 and 16-byte aligned, as are q, out and cache8 (256).
- * out: [rows, hq*hd] bf16.  depth[i] <= max_depth for every row (a row beyond is taken to be at max_depth); with anc, max_depth <= 15.
+ * kwin, vwin: [win_rows, hkv*hd] bf16, 1 <= win_rows <= 2^24, 16-byte aligned, as are q, out and cache8 (256).
+ * out: [rows, hq*hd] bf16, overlaps no input.  depth[i] <= max_depth for every row (a row beyond is taken to be at max_depth); with anc, max_depth <= 15.
  * hd 64 or 128, hq/hkv one of 1, 2, 4, 8; hkv <= 128; rows <= 2^20.  Scratch: spec_k_attention8_scratch_bytes(..), 256-byte aligned
  * (host only; 0 if the call needs none, then scratch may be NULL, and for bad sizes).  Softmax statistics and sums are fp32.  In the 8-bit part queries are rounded to
- * fp16 relative to the row's largest value (2^-11) and weights cut to fp16 (at most 2^-10 off, centred); in
- * the window both go in two bf16 terms (2^-16).  The result of a row may change in its last bits with the rows beside it. */
+ * fp16 relative to the row's largest value (2^-11) and weights cut to fp16 (at most 2^-10 off, centred;
+ * where the values' exponents of two blocks are d > 20 apart, 2^(d - 30) of the smaller values); in
+ * the window both go in two bf16 terms (2^-16). 
+ * Sums are weighted by up to 2^45 before the division: values beyond 2^80 may end as infinities.
+ * The result of a row may change in its last bits with the rows beside it. */
 uint64_t spec_k_attention8_scratch_bytes(int32_t rows, int32_t hq, int32_t hkv, int32_t hd, int32_t n_blocks, int32_t win_rows);
 int spec_k_attention8(const float *q, const void *cache8, int32_t n_blocks, const void *kwin, const void *vwin, int32_t win_rows, int32_t rows,
                       int32_t hq, int32_t hkv, int32_t hd, int32_t base, const int32_t *depth, const int32_t *anc, int32_t max_depth,

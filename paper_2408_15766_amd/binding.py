@@ -758,7 +758,7 @@ def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, an
     if n_blocks and not _is_kv8(cache8, hkv, hd, n_blocks):
         _refuse(what, f"cache8 holds no {n_blocks} blocks of {hkv} heads of {hd}")
     if max_depth is None:
-        max_depth = max(int(depth.max().item()), 0)
+        max_depth = max(int(depth.max().item()), 0) if rows else 0
     if not (0 <= base <= _INT_MAX and 0 <= max_depth <= _INT_MAX):
         _refuse(what, f"base {base}, max_depth {max_depth}")
     if out is None:

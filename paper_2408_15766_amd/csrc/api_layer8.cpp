@@ -24,7 +24,7 @@ bool matrix_ok(int32_t rows, int32_t in) { return rows >= 1 && rows <= kMaxRows8
 constexpr int kMaxKvHeads = 128;
 bool heads_ok(int32_t hkv, int32_t hd) { return (hd == 64 || hd == 128) && hkv >= 1 && hkv <= kMaxKvHeads; }
 bool attention_ok(int32_t rows, int32_t hq, int32_t hkv, int32_t hd, int32_t n_blocks, int32_t win_rows) {
-  if (!heads_ok(hkv, hd) || hq < hkv || hq % hkv || rows < 1 || rows > (1 << 20) || n_blocks < 0 || n_blocks > (1 << 24) || win_rows < 1) return false;
+  if (!heads_ok(hkv, hd) || hq < hkv || hq % hkv || rows < 1 || rows > (1 << 20) || n_blocks < 0 || n_blocks > (1 << 24) || win_rows < 1 || win_rows > (1 << 24)) return false;
   const int g = hq / hkv;
   return g == 1 || g == 2 || g == 4 || g == 8;
 }

@@ -178,7 +178,8 @@ __device__ __forceinline__ void weigh(Running<HD> &r, float q_scale, uint32_t ex
 #pragma unroll
     for (int i = 0; i < 16; i++) top = __builtin_elementwise_maximum(top, s[kt][i]);   // (v_maximum3: no quieting ahead of it; with a NaN among them the query's result is NaN, whatever the reference)
   r.raise(max_halves(top) * f);
-  const float minus = (float)(ev - top_exp) + kCutLift - r.m;   // (the reference of a query whose scores are all NaN stays -inf: its weights are NaN)
+  const int under = max(ev - top_exp, -60);                   // (from about -40 on the weights are nothing in fp16, but their sum still has to hold)
+  const float minus = (float)under + kCutLift - r.m;          // (the reference of a query whose scores are all NaN stays -inf: its weights are NaN)
   float sum = 0.f;
 #pragma unroll
   for (int h = 0; h < 4; h++)
@@ -188,7 +189,7 @@ __device__ __forceinline__ void weigh(Running<HD> &r, float q_scale, uint32_t ex
       sum += x + y;
       p[h][i / 2] = cut_f16x2(x, y);
     }
-  r.l = fmaf(sum, pow2(min(top_exp - ev, 127)), r.l);
+  r.l = fmaf(sum, pow2(-under), r.l);
 }
 
 // 64 keys of a block for 32 queries.  keys(kt, s), values(kt, db, a): the fp16 operands (s: 16 dims, a: 16 keys)

@@ -381,6 +381,17 @@ def test_attention8_scales_far_apart(P):
     check_attention(P, q, k, v, blocks, 64 * blocks + 4, np.arange(rows), None, hq, hkv, hd)
 
 
+@pytest.mark.parametrize("rows", [1, 60, 200])
+@pytest.mark.parametrize("large", [1e20, 1e24])
+def test_attention8_blocks_without_values_beside_large_ones(P, rows, large):
+    """Blocks whose values are all zero keep their share of the sum of weights, before and behind a block of values far larger than theirs."""
+    hq, hkv, hd, blocks = 64, 64, 64, 24                                  # (several blocks one after the other in a workgroup)
+    q, k, v = inputs(rows, hq, hkv, hd, blocks, rows, 15)
+    v[:] = 0
+    v[64 * 8:64 * 12] = large * (1 + torch.rand(256, hkv * hd, generator=torch.Generator().manual_seed(1)).cuda())
+    check_attention(P, q, k, v.bfloat16(), blocks, 64 * blocks, np.arange(rows), None, hq, hkv, hd)
+
+
 def test_attention8_one_key_outweighs_all(P):
     hq, hkv, hd, blocks = 2, 1, 128, 20
     q, k, v = inputs(2, hq, hkv, hd, blocks, 2, 5)
@@ -427,7 +438,7 @@ def test_attention8_binding_refusals(P):
     for kw in (dict(q=q.bfloat16()), dict(q=q[:, :64]), dict(n_blocks=2), dict(cache8=None), dict(kwin=k[64:].float()), dict(vwin=v[:64]), dict(base=63), dict(depth=d.long()),
                dict(depth=d[:2]), dict(anc=torch.zeros(3, 15, dtype=torch.int32, device="cuda")), dict(hq=3), dict(hd=128), dict(max_depth=-1), dict(max_depth=2 ** 32), dict(base=2 ** 32 + 65),
                dict(out=torch.empty(3, 256, device="cuda")), dict(q=q.cpu()),
-               dict(kwin=k[64:64], vwin=v[64:64]), dict(anc=torch.zeros(3, 16, dtype=torch.int32, device="cuda"), max_depth=16)):
+               dict(kwin=k[64:64], vwin=v[64:64]), dict(q=q[:0], depth=d[:0]), dict(anc=torch.zeros(3, 16, dtype=torch.int32, device="cuda"), max_depth=16)):
         with pytest.raises(P.SpecError):
             P.spec_k_attention8(**{**ok, **kw})
     q, k, v = inputs(60, hq, hkv, hd, 1, 60, 1)                           # a call that needs scratch: too little, and its own kept for two calls

@@ -78,7 +78,7 @@ def test_kv8_refusals(P):
 
 def test_attention8_refusals(P):
     good = dict(q=X, c=X, nb=20, kw=X, vw=X, win=8, rows=4, hq=8, hkv=2, hd=64, base=1280, depth=X, anc=X, md=3, scratch=X, nbytes=1 << 40, out=X)
-    for kw in (dict(q=None), dict(q=X + 4), dict(c=None), dict(c=X + 16), dict(nb=-1), dict(kw=None), dict(vw=None), dict(kw=X + 2), dict(win=0), dict(rows=0),
+    for kw in (dict(q=None), dict(q=X + 4), dict(c=None), dict(c=X + 16), dict(nb=-1), dict(kw=None), dict(vw=None), dict(kw=X + 2), dict(win=0), dict(win=2 ** 31 - 1), dict(rows=0),
                dict(hq=9), dict(hq=32), dict(hq=1), dict(hkv=0), dict(hd=80), dict(base=1279), dict(base=-1, nb=0), dict(depth=None), dict(md=-1), dict(md=16),
                dict(anc=None, md=2 ** 31 - 1), dict(scratch=None), dict(scratch=X + 64), dict(nbytes=0), dict(out=None), dict(out=X + 2), dict(anc=X + 1)):
         a = {**good, **kw}
