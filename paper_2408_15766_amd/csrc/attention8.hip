@@ -285,53 +285,57 @@ __device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, 
     s = mul_bf16(k, q.hi[t], s);
     s = mul_bf16(k, q.lo[t], s);
   }
-  const int first = a.base - a.n_blocks * kKv8Block;
-  float n[16], top = -INFINITY;                               // how often the query sees each key
+  uint32_t seen = 0xFFFFFFFFu;                                // bit w: the query sees row w0 + w
+  bool counts = false;                                        // one of the queries sees a row more than once
+  float top = -INFINITY;
   if (whole) {
 #pragma unroll
-    for (int i = 0; i < 16; i++) { n[i] = 1.f; s[i] *= a.scale; top = fmaxf(top, s[i]); }
+    for (int i = 0; i < 16; i++) { s[i] *= a.scale; top = fmaxf(top, s[i]); }
   } else {
+    const int below = min(!a.anc ? see.last + 1 : see.deep < 0 ? 0 : a.base - a.n_blocks * kKv8Block, a.win_rows) - w0;   // rows that every position up to the query's brings
+    seen = below >= 32 ? 0xFFFFFFFFu : below <= 0 ? 0u : (1u << below) - 1;
     if (a.anc) {
-      wave_fence();                                           // (the counts before have been read)
-      uint32_t *mine = count + c * 8;
-      *(u32x4_t *)(mine + 4 * g) = u32x4_t{0, 0, 0, 0};
-      wave_fence();
-      if (g == 0)
+      uint32_t again = 0;
 #pragma unroll
-        for (int d = 0; d < kAncStride; d++) {
-          const uint32_t w = (uint32_t)(see.path[d] - w0);    // (-1 - w0: far beyond)
-          if (w < 32u) __hip_atomic_fetch_add(mine + (w >> 2), 1u << (8 * (w & 3)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-        }
-      wave_fence();
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const uint32_t w = mine[2 * i + g];
-#pragma unroll
-        for (int e = 0; e < 4; e++) n[4 * i + e] = (float)((w >> (8 * e)) & 0xFF);
+      for (int d = 0; d < kAncStride; d++) {
+        const uint32_t w = (uint32_t)(see.path[d] - w0), bit = w < 32u ? 1u << w : 0u;   // (-1 - w0: far beyond)
+        again |= seen & bit;
+        seen |= bit;
       }
+      counts = __builtin_amdgcn_ballot_w64(again != 0) != 0;
     }
+    const uint32_t own = seen >> (4 * g);
 #pragma unroll
     for (int i = 0; i < 16; i++) {
-      const int w = w0 + 8 * (i >> 2) + 4 * g + (i & 3);
-      if (!a.anc) n[i] = w <= see.last ? 1.f : 0.f;
-      else n[i] += w < first && see.deep >= 0 ? 1.f : 0.f;
-      if (w >= a.win_rows) n[i] = 0.f;
-      s[i] = n[i] > 0.f ? s[i] * a.scale : -INFINITY;
+      s[i] = (own >> (8 * (i >> 2) + (i & 3))) & 1 ? s[i] * a.scale : -INFINITY;
       top = fmaxf(top, s[i]);
     }
   }
   r.raise(max_halves(top));
   const float m = r.m == -INFINITY ? 0.f : r.m;
-  if (whole) {
 #pragma unroll
-    for (int i = 0; i < 16; i++) { s[i] = exp2_(s[i] - m); r.l += s[i]; }
-  } else {
+  for (int i = 0; i < 16; i++) s[i] = exp2_(s[i] - m);
+  if (counts) {                                               // (paths that hold a row twice: no tree's)
+    wave_fence();                                             // (the counts before have been read)
+    uint32_t *mine = count + c * 8;
+    *(u32x4_t *)(mine + 4 * g) = u32x4_t{0, 0, 0, 0};
+    wave_fence();
+    if (g == 0)
+#pragma unroll
+      for (int d = 0; d < kAncStride; d++) {
+        const uint32_t w = (uint32_t)(see.path[d] - w0);
+        if (w < 32u) __hip_atomic_fetch_add(mine + (w >> 2), 1u << (8 * (w & 3)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+      }
+    wave_fence();
+    const int first = see.deep < 0 ? 0 : a.base - a.n_blocks * kKv8Block;
 #pragma unroll
     for (int i = 0; i < 16; i++) {
-      s[i] = n[i] > 0.f ? n[i] * exp2_(s[i] - m) : 0.f;
-      r.l += s[i];
+      const uint32_t times = ((mine[2 * (i >> 2) + g] >> (8 * (i & 3))) & 0xFF) + (w0 + 8 * (i >> 2) + 4 * g + (i & 3) < first ? 1 : 0);
+      if (times > 1) s[i] *= (float)times;
     }
   }
+#pragma unroll
+  for (int i = 0; i < 16; i++) r.l += s[i];
 #pragma unroll
   for (int h = 0; h < 2; h++) {
     u32x4_t hi, lo;
@@ -352,18 +356,17 @@ __device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, 
     const int w = __builtin_ctz(odd);
     odd &= odd - 1;
     const uint16_t *vr = (const uint16_t *)a.vwin + (size_t)min(w0 + w, a.win_rows - 1) * ((size_t)a.hkv * HD) + (size_t)kvh * HD;
-    float p = 0.f, seen = 0.f;
+    float p = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i++)
-      if (i == ((w >> 3) << 2 | (w & 3))) { p = s[i]; seen = n[i]; }
+      if (i == ((w >> 3) << 2 | (w & 3))) p = s[i];
     p = __shfl(p, ((w >> 2) & 1) * 32 + c);
-    seen = __shfl(seen, ((w >> 2) & 1) * 32 + c);
 #pragma unroll
     for (int db = 0; db < HD / 32; db++)
 #pragma unroll
       for (int i = 0; i < 16; i++) {
         const uint32_t b = vr[db * 32 + 8 * (i >> 2) + 4 * g + (i & 3)];
-        if (seen > 0.f && (b & 0x7F80u) == 0x7F80u) r.o[db][i] = fmaf(p, bf16_bits_to_f32(b), r.o[db][i]);
+        if (((seen >> w) & 1) && (b & 0x7F80u) == 0x7F80u) r.o[db][i] = fmaf(p, bf16_bits_to_f32(b), r.o[db][i]);
       }
   }
 }
@@ -724,7 +727,9 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
   const int of = p.waves ? 32 * p.waves : 32;
   p.query_blocks = (int)((queries + of - 1) / of);
   const int64_t units = (int64_t)hkv * p.query_blocks;
-  p.win_part = win_rows <= 256 && p.waves < 8 ? 64 : 256;
+  // rows of the window per part: the step of a workgroup where the blocks are hardly more than one each, too (us with 32 against 64: 50 queries on 8 kv heads of 64, 512 keys 9.6, 10.7;
+  // 60 on 32, 512 keys 14.4, 14.8, but 16384 keys 48.5, 46.8); long windows come in tiles of 64
+  p.win_part = win_rows > 256 || p.waves == 8 ? 256 : p.waves && units * n_blocks <= 256 ? 32 : 64;
   while ((win_rows + p.win_part - 1) / p.win_part > 8) p.win_part *= 2;
   p.win_parts = (win_rows + p.win_part - 1) / p.win_part;
   const int64_t most = p.waves ? n_blocks : (n_blocks + kFewWaves - 1) / kFewWaves;
