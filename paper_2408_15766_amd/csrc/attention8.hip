@@ -496,13 +496,14 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Which kv head, part and block of queries a workgroup has: ids 8 apart run on one XCD, and there the query blocks of a part follow each other (they read the same keys)
+// Which kv head, part and block of queries a workgroup has: ids 8 apart run on one XCD, and there the query blocks of a part follow each other (they read the same keys), the
+// last, which sees most of the window, first (us the other way round: 4000 rows on 8 kv heads behind 16 blocks 309 -> 385, 3000 behind 64 352 -> 434)
 struct Place8 { int kvh, part, qb; };
 __device__ __forceinline__ bool place_of(const Plan8 &p, int hkv, Place8 &at) {
   const int parts = p.block_parts + p.win_parts, units = hkv * parts;
   const int x = (int)blockIdx.x % 8, j = (int)blockIdx.x / 8;
   const int unit = j / p.query_blocks * 8 + x;
-  at.qb = j % p.query_blocks;
+  at.qb = p.query_blocks - 1 - j % p.query_blocks;
   if (unit >= units) return false;
   at.kvh = unit / parts; at.part = unit % parts;
   return true;
@@ -742,10 +743,11 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
     p.win_parts = 0;
     const int64_t parts = (256 + units / 2) / units;
     p.block_parts = (int)(parts < 1 ? 1 : parts > most ? most : parts);
-    // rows of the window that the first query block sees, if they are a chain, and how many more each further one does; 64 of them cost 1.5 blocks
+    // rows of the window that the first query block sees, if they are a chain, and how many more each further one does; a window costs 2.5 blocks, and 2.25 for 64 rows (us with
+    // this, and with 1.5 for 64 rows alone: 1024 rows on 8 kv heads behind 128 blocks 167, 176, behind 32 blocks and 100 rows 83, 91; a tree of 60 rows behind 512 blocks 79, 83)
     const int each = of / G < 1 ? 1 : of / G, recent = win_rows > rows ? win_rows - rows : 0;
-    p.win_base = (recent + each) * 24 / 64;
-    p.win_cost = each * 24 / 64;
+    p.win_base = 40 + (recent + each) * 36 / 64;
+    p.win_cost = each * 36 / 64;
     return p;
   }
   // One workgroup a unit; two of two wavefronts where each would have eight blocks or more (us: 60 queries on 32 kv heads, 512 keys 15.7 against 18.1 with 512 workgroups, 4096 29 against 25,
