@@ -685,6 +685,60 @@ def test_layer_on_a_stream_and_captured(P):
         torch.cuda.synchronize()
 
 
+def test_two_calls_of_each_at_once(P):
+    """Two streams, each with inputs, outputs and scratch of its own: the bits of one call after the other."""
+    hq, hkv, hd, d, blocks = 8, 2, 128, 640, 6
+    w = P.spec_pack_weight8(rand(1, 900, d).bfloat16().cuda())
+    plan = P.spec_rotary_plan(hd, 1e4)
+    sides = []
+    for i in range(2):
+        rows = (40, 70)[i]
+        q, k, v = inputs(rows, hq, hkv, hd, blocks, rows, 30 + i)
+        sides.append(dict(x=rand(10 + i, rows, d).bfloat16().cuda(), q=q, k=k, v=v, cache=P.spec_kv8_alloc(blocks, hkv, hd), depth=torch.arange(rows, dtype=torch.int32, device="cuda")))
+
+    def run(s):
+        rows, n = s["q"].shape[0], 64 * blocks
+        y = P.spec_k_gemm8(s["x"], w)
+        P.spec_k_kv8_store(s["k"][:n], s["v"][:n], s["cache"], 0, hkv, hd)
+        q, k = P.spec_k_rotary(plan, [s["q"].view(rows, hq, hd), s["k"][n:].view(rows, hkv, hd)], n)
+        return y, P.spec_k_attention8(q.view(rows, -1), s["cache"], blocks, k.view(rows, -1), s["v"][n:], n, s["depth"], None, hq, hkv, hd, max_depth=rows - 1)
+
+    want = [run(s) for s in sides]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sides]
+    for _ in range(5):
+        got = []
+        for s, stream in zip(sides, streams):
+            with torch.cuda.stream(stream):
+                got.append(run(s))
+        torch.cuda.synchronize()
+        for g, t in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(g, t))
+
+
+def test_more_elements_than_31_bits_count(P):
+    """Rows whose first element lies beyond 2^31 elements, against the same rows at the front."""
+    m, k, rows = 270016, 8192, 8192
+    base = rand(1, 64, k).bfloat16().cuda()
+    w = P.spec_pack_weight8(rand(2, rows, k).bfloat16().cuda())
+    y = P.spec_k_gemm8(base.repeat(m // 64, 1), w)
+    assert torch.equal(y[-64:], y[:64]) and y[:64].isfinite().all() and float(y[:64].float().std()) > 1
+    del y, w
+    hq, hkv, hd, m = 128, 16, 128, 140032
+    q, kv, vv = inputs(64, hq, hkv, hd, 1, 1, 7)
+    cache = P.spec_kv8_alloc(1, hkv, hd)
+    P.spec_k_kv8_store(kv[:64], vv[:64], cache, 0, hkv, hd)
+    o = P.spec_k_attention8(q.repeat(m // 64, 1), cache, 1, kv[64:].contiguous(), vv[64:].contiguous(), 64, torch.zeros(m, dtype=torch.int32, device="cuda"), None, hq, hkv, hd, max_depth=0)
+    assert torch.equal(o[-64:], o[:64])
+    want, tol = attention_bound(q, kv, vv, 1, 64, np.zeros(64, np.int32), None, hq, hkv, hd)
+    assert (np.abs(f64(o[:64]) - want) <= tol).all()
+    del o
+    x = rand(3, 64, 64, 128).bfloat16().cuda().repeat(4200, 1, 1)                       # 268800 rows
+    pos = torch.arange(64, dtype=torch.int32, device="cuda").repeat(4200)
+    r = P.spec_k_rotary(P.spec_rotary_plan(128, 1e4), [x], pos, outs=[x])[0]
+    assert torch.equal(r[-64:], r[:64]) and not torch.equal(r[1], r[0])
+
+
 def test_rotary_ahead_of_and_behind_training_attention(P):
     """q and k of a training step turned ahead of spec_hca_attention; relative positions alone matter, so a shift of all positions changes nothing but roundings."""
     b, s, hq, hkv, hd = 2, 96, 4, 2, 64
