@@ -595,6 +595,12 @@ def _here(what: str, *tensors) -> int:
     return raw(at) if raw is not None else torch.cuda.current_stream().cuda_stream
 
 
+def _new(shape, strides, dtype, beside):
+    """An uninitialised dense tensor on the device of another (by empty_strided: 1.4 us, new_empty takes 2.0)."""
+    import torch
+    return torch.empty_strided(shape, strides, dtype=dtype, device=beside.device)
+
+
 def _dtype_code(what: str, dtype) -> int:
     import torch
     if dtype is torch.bfloat16:
@@ -646,7 +652,7 @@ def spec_k_gemm8(x, w8, out_dtype=None, out=None, scratch=None):
         _refuse(what, f"x has to be [m, {cols}] with dense rows")
     m = x.shape[0]
     if out is None:
-        out = x.new_empty((m, rows), dtype=x.dtype if out_dtype is None else out_dtype)
+        out = _new((m, rows), (rows, 1), x.dtype if out_dtype is None else out_dtype, x)
     elif tuple(out.shape) != (m, rows) or (out.stride(1) != 1 and rows > 1) or (out_dtype is not None and out_dtype is not out.dtype):
         _refuse(what, f"out has to be [{m}, {rows}] with dense rows, of out_dtype")
     n = lib.spec_k_gemm8_scratch_bytes(m, cols, rows)
@@ -657,7 +663,7 @@ def spec_k_gemm8(x, w8, out_dtype=None, out=None, scratch=None):
     else:
         room = n
         if n:
-            scratch = x.new_empty(n, dtype=torch.uint8)
+            scratch = _new((n,), (1,), torch.uint8, x)
     ldx, ldy = (x.stride(0), out.stride(0)) if m > 1 else (cols, rows)
     if ldx > _INT_MAX or ldy > _INT_MAX:                        # (ctypes would cut them)
         _refuse(what, f"rows {ldx} and {ldy} elements apart")
@@ -762,7 +768,7 @@ def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, an
     if not (0 <= base <= _INT_MAX and 0 <= max_depth <= _INT_MAX):
         _refuse(what, f"base {base}, max_depth {max_depth}")
     if out is None:
-        out = q.new_empty((rows, wide), dtype=torch.bfloat16)
+        out = _new((rows, wide), (wide, 1), torch.bfloat16, q)
     elif out.dtype is not torch.bfloat16 or not out.is_contiguous() or tuple(out.shape) != (rows, wide):
         _refuse(what, f"out has to be contiguous bfloat16 [{rows}, {wide}]")
     room = n
@@ -771,7 +777,7 @@ def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, an
         if not scratch.is_contiguous():
             _refuse(what, "scratch has to be contiguous")
     elif n:
-        scratch = q.new_empty(n, dtype=torch.uint8)
+        scratch = _new((n,), (1,), torch.uint8, q)
     rc = lib.spec_k_attention8(q.data_ptr(), cache8.data_ptr() if n_blocks else None, n_blocks, kwin.data_ptr(), vwin.data_ptr(), win_rows, rows, hq, hkv, hd, base,
                                depth.data_ptr(), None if anc is None else anc.data_ptr(), max_depth, None if scratch is None else scratch.data_ptr(), room, out.data_ptr(), stream)
     if rc:
@@ -807,31 +813,32 @@ def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[
     n = len(xs)
     if not 1 <= n <= 3 or xs[0].dim() != 3:
         _refuse(what, "one to three tensors [rows, heads, hd] are needed")
-    if outs is None:
+    made = outs is None
+    if made:
         kinds = [x.dtype for x in xs] if out_dtypes is None else out_dtypes
         outs = [torch.empty_like(x, dtype=d, memory_format=torch.contiguous_format) for x, d in zip(xs, kinds)]
     if len(outs) != n or (turned is not None and len(turned) != n):
         _refuse(what, "as many outputs and flags as tensors are needed")
     at = pos if isinstance(pos, torch.Tensor) else None
-    stream = _here(what, *xs, *outs, at)
+    stream = _here(what, *xs, at) if made else _here(what, *xs, *outs, at)
     rows, _, hd = xs[0].shape
     if at is not None and (at.dtype is not torch.int32 or at.dim() != 1 or at.shape[0] != rows or not at.is_contiguous()):
         _refuse(what, f"pos has to be int32 [{rows}]")
     if at is None and not -_INT_MAX - 1 <= int(pos) <= _INT_MAX:
         _refuse(what, f"position {pos}")
-    codes = {torch.float32: 0, torch.bfloat16: 1}
+    bf16, fp32 = torch.bfloat16, torch.float32
     fields = []
     for x, o, turn in zip(xs, outs, (True,) * n if turned is None else turned):
-        shape = x.shape
-        if shape != o.shape or len(shape) != 3 or shape[0] != rows or shape[2] != hd:
+        shape, strides, dtype, out_dtype = x.shape, x.stride(), x.dtype, o.dtype
+        if len(shape) != 3 or shape[0] != rows or shape[2] != hd or not (made or shape == o.shape):
             _refuse(what, f"tensors have to be [{rows}, heads, {hd}]")
-        (ldx, hsx, one), (ldo, hso, one_out) = x.stride(), o.stride()
-        if hd > 1 and not one == one_out == 1:
+        heads = shape[1]
+        ldo, hso, one = (heads * hd, hd, 1) if made else o.stride()
+        if hd > 1 and not strides[2] == one == 1:
             _refuse(what, "the dims of a head have to be dense")
-        dtype, out_dtype = codes.get(x.dtype), codes.get(o.dtype)
-        if dtype is None or out_dtype is None:
-            _refuse(what, f"{x.dtype} to {o.dtype} (float32 and bfloat16 are supported)")
-        fields += (x.data_ptr(), o.data_ptr(), ldx, hsx, ldo, hso, shape[1], dtype, out_dtype, bool(turn))
+        if (dtype is not bf16 and dtype is not fp32) or (out_dtype is not bf16 and out_dtype is not fp32):
+            _refuse(what, f"{dtype} to {out_dtype} (float32 and bfloat16 are supported)")
+        fields += (x.data_ptr(), o.data_ptr(), strides[0], strides[1], ldo, hso, heads, dtype is bf16, out_dtype is bf16, bool(turn))
     rc = lib.spec_k_rotary(C.byref(plan), n, _rotary_parts[n](*fields), hd, rows, at.data_ptr() if at is not None else None, 0 if at is not None else int(pos),
                            bool(adjoint), stream)
     if rc:
