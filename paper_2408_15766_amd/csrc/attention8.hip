@@ -513,7 +513,8 @@ __device__ __forceinline__ bool place_of(const Plan8 &p, int hkv, Place8 &at) {
 // next block's are in registers meanwhile), in the order in which the products read them.
 // Eight wavefronts take 1.84 us a block: 256 workgroups together 1.17 PFLOP/s.  Without reads from the LDS 1.75, without the weights' arithmetic 1.53, without both 1.36 (1.58
 // PFLOP/s: at the clock of 1.5 GHz that the products alone leave the chip), without the products 1.23.
-// Tried, with the same time: two teams of four wavefronts that take turns at the matrix instructions and at the weights, a barrier between; four wavefronts of 64 queries, scores of the
+// Tried, with the same time: two teams of four wavefronts that take turns at the matrix instructions and at the weights, a barrier between; the next block's scores among the
+// instructions of this one's weights; slower: four wavefronts of 64 queries, scores of the
 // next tile beside the weights of this one (2.4: the sums of 64 queries lie in the accumulation registers, and every read of one is an instruction).
 template <int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 2 ? 1 : 2) void attention8_wide_kernel(Attn8Args a, Plan8 plan) {
