@@ -54,6 +54,7 @@ int spec_k_gemm8(int32_t dtype, const void *x, int32_t ldx, int32_t m, int32_t i
   if (!is_dtype(dtype) || !is_dtype(out_dtype) || !x || !w8 || !y || m < 1 || m > kMaxM8 || !matrix_ok(rows, in) || ldx < in || ldy < rows) return SPEC_EINVAL;
   if (need > 0 && (!scratch || scratch_bytes < need)) return SPEC_EINVAL;
   if (!aligned(x, size_of(dtype)) || !aligned(y, size_of(out_dtype)) || !aligned(w8, 256) || !aligned(scratch, 256)) return SPEC_EINVAL;
+  if (y == x || y == w8 || y == scratch) return SPEC_EINVAL;
   Gemm8Args a{};
   a.x = x; a.ldx = ldx; a.w8 = (const unsigned char *)w8; a.m = m; a.in = in; a.rows = rows; a.y = y; a.ldy = ldy;
   return done(launch_gemm8(dtype, out_dtype, a, scratch, (hipStream_t)stream));
@@ -77,7 +78,7 @@ int spec_k_kv8_store(const void *k, const void *v, int64_t ld, int32_t n_blocks,
 }
 
 int spec_k_kv8_load(const void *cache8, int32_t first_block, int32_t n_blocks, int32_t hkv, int32_t hd, void *k, void *v, int64_t ld, void *stream) {
-  if (!kv8_ok(k, v, ld, n_blocks, hkv, hd, cache8, first_block)) return SPEC_EINVAL;
+  if (!kv8_ok(k, v, ld, n_blocks, hkv, hd, cache8, first_block) || k == v) return SPEC_EINVAL;
   return done(launch_kv8_load(cache8, first_block, n_blocks, hkv, hd, k, v, ld, (hipStream_t)stream));
 }
 
@@ -96,6 +97,7 @@ int spec_k_attention8(const float *q, const void *cache8, int32_t n_blocks, cons
   if (!aligned(q, 16) || !aligned(kwin, 16) || !aligned(vwin, 16) || !aligned(out, 16) || !aligned(cache8, 256) || !aligned(scratch, 256) ||
       !aligned(depth, 4) || !aligned(anc, 4))
     return SPEC_EINVAL;
+  if (out == q || out == cache8 || out == kwin || out == vwin || out == scratch) return SPEC_EINVAL;
   Attn8Args a{};
   a.q = q; a.cache8 = (const unsigned char *)cache8; a.n_blocks = n_blocks; a.kwin = kwin; a.vwin = vwin; a.win_rows = win_rows;
   a.rows = rows; a.hq = hq; a.hkv = hkv; a.hd = hd; a.base = base; a.depth = depth; a.anc = anc; a.max_depth = max_depth;
@@ -154,6 +156,8 @@ int spec_k_rotary(const spec_rotary_plan *plan, int32_t n_parts, const spec_rota
     const int64_t most = (int64_t)1 << 40;
     if (p.ldx < 0 || p.hsx < 0 || p.ldo < 0 || p.hso < 0 || p.ldx > most || p.hsx > most || p.ldo > most || p.hso > most) return SPEC_EINVAL;
     if (p.x == p.out && (p.dtype != p.out_dtype || (rows > 1 && p.ldx != p.ldo) || (p.heads > 1 && p.hsx != p.hso))) return SPEC_EINVAL;
+    for (int o = 0; o < n; o++)
+      if (p.out == parts[o].out || p.out == parts[o].x || p.x == parts[o].out) return SPEC_EINVAL;
     a.part[n] = RotaryPart{p.x, p.out, p.ldx, p.hsx, p.ldo, p.hso, p.heads, p.dtype, p.out_dtype, p.turn != 0};
   }
   a.n_parts = n_parts; a.hd = hd; a.rows = rows; a.rot = plan->rot; a.interleaved = plan->layout == SPEC_ROPE_INTERLEAVED;

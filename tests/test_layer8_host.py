@@ -56,10 +56,10 @@ def refused(rc):
 
 def test_gemm8_refusals(P):
     f = P.lib.spec_k_gemm8
-    good = dict(dtype=1, x=X, ldx=256, m=40, k=256, w8=X, rows=32, out=1, y=X, ldy=32, scratch=X, nbytes=1 << 30)
+    good = dict(dtype=1, x=X, ldx=256, m=40, k=256, w8=2 * X, rows=32, out=1, y=3 * X, ldy=32, scratch=4 * X, nbytes=1 << 30)
     for kw in (dict(dtype=2), dict(x=None), dict(ldx=255), dict(m=0), dict(m=-1), dict(m=(1 << 20) + 1), dict(k=0), dict(k=(1 << 20) + 1, ldx=1 << 21),
                dict(w8=None), dict(w8=X + 128), dict(rows=0), dict(out=3), dict(y=None), dict(y=X + 1), dict(x=X + 1), dict(ldy=31), dict(scratch=None),
-               dict(scratch=X + 16), dict(nbytes=10)):
+               dict(scratch=X + 16), dict(nbytes=10), dict(y=X), dict(y=2 * X), dict(y=4 * X)):
         a = {**good, **kw}
         refused(f(a["dtype"], a["x"], a["ldx"], a["m"], a["k"], a["w8"], a["rows"], a["out"], a["y"], a["ldy"], a["scratch"], a["nbytes"], None))
     g = P.lib.spec_pack_weight8
@@ -68,19 +68,21 @@ def test_gemm8_refusals(P):
 
 
 def test_kv8_refusals(P):
-    good = dict(k=X, v=X, ld=512, n=1, hkv=8, hd=64, c=X, first=0)
+    good = dict(k=2 * X, v=3 * X, ld=512, n=1, hkv=8, hd=64, c=X, first=0)
     for kw in (dict(k=None), dict(v=None), dict(ld=511), dict(n=-1), dict(hkv=0), dict(hkv=129, ld=1 << 20), dict(hd=32), dict(c=None), dict(c=X + 16),
                dict(first=-1), dict(first=1 << 24), dict(k=X + 1)):
         a = {**good, **kw}
         refused(P.lib.spec_k_kv8_store(a["k"], a["v"], a["ld"], a["n"], a["hkv"], a["hd"], a["c"], a["first"], None))
         refused(P.lib.spec_k_kv8_load(a["c"], a["first"], a["n"], a["hkv"], a["hd"], a["k"], a["v"], a["ld"], None))
+    refused(P.lib.spec_k_kv8_load(X, 0, 1, 8, 64, 2 * X, 2 * X, 512, None))
 
 
 def test_attention8_refusals(P):
-    good = dict(q=X, c=X, nb=20, kw=X, vw=X, win=8, rows=4, hq=8, hkv=2, hd=64, base=1280, depth=X, anc=X, md=3, scratch=X, nbytes=1 << 40, out=X)
+    good = dict(q=X, c=2 * X, nb=20, kw=3 * X, vw=4 * X, win=8, rows=4, hq=8, hkv=2, hd=64, base=1280, depth=X, anc=X, md=3, scratch=5 * X, nbytes=1 << 40, out=6 * X)
     for kw in (dict(q=None), dict(q=X + 4), dict(c=None), dict(c=X + 16), dict(nb=-1), dict(kw=None), dict(vw=None), dict(kw=X + 2), dict(win=0), dict(win=2 ** 31 - 1), dict(rows=0),
                dict(hq=9), dict(hq=32), dict(hq=1), dict(hkv=0), dict(hd=80), dict(base=1279), dict(base=-1, nb=0), dict(depth=None), dict(md=-1), dict(md=16),
-               dict(anc=None, md=2 ** 31 - 1), dict(scratch=None), dict(scratch=X + 64), dict(nbytes=0), dict(out=None), dict(out=X + 2), dict(anc=X + 1)):
+               dict(anc=None, md=2 ** 31 - 1), dict(scratch=None), dict(scratch=X + 64), dict(nbytes=0), dict(out=None), dict(out=X + 2), dict(anc=X + 1),
+               dict(out=X), dict(out=2 * X), dict(out=3 * X), dict(out=4 * X), dict(out=5 * X)):
         a = {**good, **kw}
         refused(P.lib.spec_k_attention8(a["q"], a["c"], a["nb"], a["kw"], a["vw"], a["win"], a["rows"], a["hq"], a["hkv"], a["hd"], a["base"], a["depth"],
                                         a["anc"], a["md"], a["scratch"], a["nbytes"], a["out"], None))
@@ -120,6 +122,10 @@ def test_rotary_refusals(P):
                dict(x=None), dict(out=None), dict(x=X + 1, out=X + 1), dict(ldx=63), dict(ldo=10), dict(hsx=63), dict(hso=0), dict(heads=0), dict(heads=1025),
                dict(dtype=5), dict(out_dtype=-1), dict(ldx=-256), dict(out_dtype=0), dict(ldo=512)):
         assert call(**kw) == -1, kw
+    part = dict(ldx=256, hsx=64, ldo=256, hso=64, heads=4, dtype=1, out_dtype=1, turn=1)
+    for x, out, x2, out2 in ((X, X, X, X), (X, 2 * X, 3 * X, 2 * X), (X, 2 * X, 2 * X, 3 * X), (X, 2 * X, 3 * X, X)):   # one tensor written twice, or read and written
+        two = bytes((b.spec_rotary_part * 2)(b.spec_rotary_part(x=x, out=out, **part), b.spec_rotary_part(x=x2, out=out2, **part)))
+        assert P.lib.spec_k_rotary(C.byref(plan), 2, two, 64, 4, X, 0, 0, None) == -1
     odd = b.spec_rotary_plan_t(63, 0, 1.0)
     assert call(plan=odd) == -1
     odd = b.spec_rotary_plan_t(64, 7, 1.0)
