@@ -516,6 +516,7 @@ __device__ __forceinline__ bool place_of(const Plan8 &p, int hkv, Place8 &at) {
 // Tried, with the same time: two teams of four wavefronts that take turns at the matrix instructions and at the weights, a barrier between; the next block's scores among the
 // instructions of this one's weights; slower: four wavefronts of 64 queries, scores of the
 // next tile beside the weights of this one (2.4: the sums of 64 queries lie in the accumulation registers, and every read of one is an instruction).
+// Registers: two wavefronts may take 512 each (60 queries on 32 kv heads, 512 keys: 14.4 us against 15.2 with 256), four do better with 256 (104 on 8, 4096 keys: 21.7 against 22.9).
 template <int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 2 ? 1 : 2) void attention8_wide_kernel(Attn8Args a, Plan8 plan) {
   constexpr int kCodes = 2 * kKv8Block * HD, kUnits = kCodes / 16, kThreads = WAVES * 64, kEach = kUnits / kThreads;   // of 16 codes, per thread
@@ -794,6 +795,8 @@ template <int HD> hipError_t launch_hd(const Attn8Args &a, hipStream_t st) {
   else if (p.waves == 4) e = launch_wide<HD, 4>(a, p, (unsigned)grid, st);
   else e = launch_wide<HD, 8>(a, p, (unsigned)grid, st);
   if (e != hipSuccess || parts == 1) return e;
+  // groups that share a query's parts, us for 1, 2, 4, 8 of them (both launches): 8 parts of 1920 queries 14.4, 16.1, 16.2, 17.9; 17 of 32 13.8, 12.7, 11.8, 12.1; 32 of 832 26.7,
+  // 24.9, 24.9, 25.1; 128 of 480 53, 42, 38, 37; 256 of 64 61, 39, 29, 24
   if (parts <= 8) return launch_merge<HD, 1>(a, parts, st);
   if (parts <= 16) return launch_merge<HD, 2>(a, parts, st);
   return parts <= 32 ? launch_merge<HD, 4>(a, parts, st) : launch_merge<HD, 8>(a, parts, st);
