@@ -1,4 +1,6 @@
 // Attention over a cache of 64-token blocks in 8 bits with a bf16 window behind it, and the cache's store and load (include/spec_layer8.h).
+#include <type_traits>
+
 #include "common.h"
 #include "fp8.h"
 #include "kernels.h"
@@ -496,15 +498,20 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Which kv head, part and block of queries a workgroup has: ids 8 apart run on one XCD, and there the query blocks of a part follow each other (they read the same keys), the
-// last, which sees most of the window, first (us the other way round: 4000 rows on 8 kv heads behind 16 blocks 309 -> 385, 3000 behind 64 352 -> 434)
+// Which kv head, part and block of queries a workgroup has.  A unit is a part of a kv head; ids 8 apart run on one XCD, which gets consecutive units (the query blocks of a part read the same
+// keys) as evenly as they go; in launches of several rounds over the compute units whose units do not go into 8, single query blocks in turn.  The last query block, which sees most of the
+// window, comes first (us the other way round: 4000 rows on 8 kv heads behind 16 blocks 309 -> 385, 3000 behind 64 352 -> 434).
 struct Place8 { int kvh, part, qb; };
 __device__ __forceinline__ bool place_of(const Plan8 &p, int hkv, Place8 &at) {
-  const int parts = p.block_parts + p.win_parts, units = hkv * parts;
-  const int x = (int)blockIdx.x % 8, j = (int)blockIdx.x / 8;
-  const int unit = j / p.query_blocks * 8 + x;
-  at.qb = p.query_blocks - 1 - j % p.query_blocks;
-  if (unit >= units) return false;
+  const int parts = p.block_parts + p.win_parts, units = hkv * parts, all = units * p.query_blocks, each = (all + 7) / 8;
+  int id = (int)blockIdx.x;
+  if (units % 8 == 0 || all <= 256) {
+    if (id / 8 >= each) return false;
+    id = id % 8 * each + id / 8;
+  }
+  if (id >= all) return false;
+  const int unit = id / p.query_blocks;
+  at.qb = p.query_blocks - 1 - id % p.query_blocks;
   at.kvh = unit / parts; at.part = unit % parts;
   return true;
 }
@@ -527,6 +534,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 2 ? 1 : 2) void attention8_wid
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, g = lane >> 5;
   const int G = a.hq / a.hkv, index = (at.qb * WAVES + wave) * 32 + c, parts = plan.block_parts + plan.win_parts;
   const bool real = index < a.rows * G;
+  const bool any = index - c < a.rows * G;                    // this wavefront has queries (else it only loads and widens)
   const int row = real ? index / G : a.rows - 1;
   const size_t query = (size_t)row * a.hq + at.kvh * G + (real ? index % G : 0);
   const float *qp = a.q + query * HD;
@@ -562,18 +570,23 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 2 ? 1 : 2) void attention8_wid
     put(lds);
     uint32_t now_exps = __builtin_amdgcn_readfirstlane(next_exps);
     __syncthreads();
-    for (int b = b0; b < b1; b++) {
-      const unsigned char *buf = lds + ((b - b0) & 1) * 2 * kCodes + lane * 16;
-      if (b + 1 < b1) fetch(b + 1);
-      block_step<HD>(r, q, now_exps, top_exp,
-                     [&](int kt, int s) { return *(const u32x4_t *)(buf + (kt * (HD / 16) + s) * 1024); },
-                     [&](int kt, int db, int h) { return *(const u32x4_t *)(buf + kCodes + (kt * (HD / 16) + 2 * db + h) * 1024); });
-      if (b + 1 < b1) {
-        put(lds + ((b + 1 - b0) & 1) * 2 * kCodes);
-        now_exps = __builtin_amdgcn_readfirstlane(next_exps);
+    auto walk = [&](auto with_queries) __attribute__((always_inline)) {
+      for (int b = b0; b < b1; b++) {
+        const unsigned char *buf = lds + ((b - b0) & 1) * 2 * kCodes + lane * 16;
+        if (b + 1 < b1) fetch(b + 1);
+        if constexpr (decltype(with_queries)::value)
+          block_step<HD>(r, q, now_exps, top_exp,
+                         [&](int kt, int s) { return *(const u32x4_t *)(buf + (kt * (HD / 16) + s) * 1024); },
+                         [&](int kt, int db, int h) { return *(const u32x4_t *)(buf + kCodes + (kt * (HD / 16) + 2 * db + h) * 1024); });
+        if (b + 1 < b1) {
+          put(lds + ((b + 1 - b0) & 1) * 2 * kCodes);
+          now_exps = __builtin_amdgcn_readfirstlane(next_exps);
+        }
+        __syncthreads();
       }
-      __syncthreads();
-    }
+    };
+    if (any) walk(std::true_type{});
+    else walk(std::false_type{});                             // (as many barriers, which count wavefronts)
     r.l *= kCutSum;
     const float up = exp2_((float)top_exp);
 #pragma unroll
@@ -727,7 +740,11 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
   Plan8 p{};
   const int G = hq / hkv;
   const int64_t queries = (int64_t)rows * G;
-  p.waves = queries <= 32 ? 0 : queries <= 64 ? 2 : queries <= 128 ? 4 : 8;
+  // Wavefronts by the work, in tiles of 32 queries over 64 keys: eight, which share the widening, where there is much of it; two, for more workgroups with fewer parts, where there is little or
+  // 64 queries are all; else four, of which those without queries only load and widen.  us with 2, 4, 8: 60 queries on 32 kv heads, 8 blocks 16.0, 14.2, 15.5, 128 blocks 32, 35, 35;
+  // 240 on 8, 8 blocks 15.2, 17.0, 19.2, 128 blocks 30, 26, 34, 512 blocks 74, 58, 54; 1200 on 8, 8 blocks 31, 27, 30, 128 blocks 221, 160, 67.
+  const int64_t tiles = (queries + 31) / 32, wide = hkv * tiles, work = wide * (n_blocks + win_rows / 32);
+  p.waves = queries <= 32 ? 0 : tiles <= 2 ? (work <= 4096 ? 4 : 2) : work >= (wide >= 96 ? 6144 : 20480) ? 8 : wide <= 64 && work <= 2304 ? 2 : 4;
   const int of = p.waves ? 32 * p.waves : 32;
   p.query_blocks = (int)((queries + of - 1) / of);
   const int64_t units = (int64_t)hkv * p.query_blocks;
@@ -743,11 +760,20 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
     return p;
   }
   if (p.waves == 8 && n_blocks > 0) {
+    // A window costs 2.5 blocks, and 2.25 for 64 rows.  Joined to the last range of blocks, if that is not more than the range's share of all (us with this, and with 1.5 for 64 rows alone:
+    // 1024 rows on 8 kv heads behind 128 blocks 167, 176, behind 32 blocks and 100 rows 83, 91; a tree of 60 rows behind 512 blocks 79, 83), else as many parts as it has shares.
+    const int parts = (int)(units >= 256 ? 1 : 256 / units);
+    const int64_t win_cost = 40 + (int64_t)win_rows * 36 / 64, all = 16 * (int64_t)n_blocks + win_cost;
+    if (parts > 1 && win_cost * parts > all) {
+      const int shares = (int)((win_cost * parts + all / 2) / all), of_window = shares < 1 ? 1 : shares < parts ? shares : parts - 1;
+      p.win_part = ((win_rows + of_window - 1) / of_window + 63) / 64 * 64;
+      p.win_parts = (win_rows + p.win_part - 1) / p.win_part;
+      p.block_parts = parts - of_window < n_blocks ? parts - of_window : n_blocks;
+      return p;
+    }
     p.win_parts = 0;
-    const int64_t parts = (256 + units / 2) / units;
-    p.block_parts = (int)(parts < 1 ? 1 : parts > most ? most : parts);
-    // rows of the window that the first query block sees, if they are a chain, and how many more each further one does; a window costs 2.5 blocks, and 2.25 for 64 rows (us with
-    // this, and with 1.5 for 64 rows alone: 1024 rows on 8 kv heads behind 128 blocks 167, 176, behind 32 blocks and 100 rows 83, 91; a tree of 60 rows behind 512 blocks 79, 83)
+    p.block_parts = parts < n_blocks ? parts : n_blocks;
+    // rows of the window that the first query block sees, if they are a chain, and how many more each further one does
     const int each = of / G < 1 ? 1 : of / G, recent = win_rows > rows ? win_rows - rows : 0;
     p.win_base = 40 + (recent + each) * 36 / 64;
     p.win_cost = each * 36 / 64;
@@ -781,7 +807,7 @@ template <int HD, int GROUPS> hipError_t launch_merge(const Attn8Args &a, int pa
 template <int HD> hipError_t launch_hd(const Attn8Args &a, hipStream_t st) {
   const Plan8 p = plan8(a.rows, a.hq, a.hkv, a.n_blocks, a.win_rows);
   const int parts = p.block_parts + p.win_parts;
-  const int64_t units = (int64_t)a.hkv * parts, grid = (units + 7) / 8 * 8 * p.query_blocks;
+  const int64_t units = (int64_t)a.hkv * parts, grid = (units * p.query_blocks + 7) / 8 * 8;
   if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
   hipError_t e;
   if (p.waves == 0) {
