@@ -754,7 +754,9 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
   while ((win_rows + p.win_part - 1) / p.win_part > 8) p.win_part *= 2;
   p.win_parts = (win_rows + p.win_part - 1) / p.win_part;
   const int64_t most = p.waves ? n_blocks : (n_blocks + kFewWaves - 1) / kFewWaves;
-  if (p.waves == 0 && n_blocks > 0 && n_blocks <= 2 * kFewWaves && win_rows <= 32 * kFewWaves) {   // short: one part, no second launch
+  // Short: one part, no second launch and no scratch.  us on the card alone, against two launches: a row on 8 kv heads behind 4 blocks 11.3, 10.9 (head_dim 64: 7.9, 8.5), but 8 blocks, two a
+  // wavefront, 12.6, 11.0; a call's host time is 9.3 against 13
+  if (p.waves == 0 && n_blocks > 0 && n_blocks <= kFewWaves && win_rows <= 32 * kFewWaves) {
     p.block_parts = 1;
     p.win_parts = 0;
     return p;
