@@ -98,6 +98,12 @@ int spec_k_attention8(const float *q, const void *cache8, int32_t n_blocks, cons
                       int32_t hq, int32_t hkv, int32_t hd, int32_t base, const int32_t *depth, const int32_t *anc, int32_t max_depth,
                       void *scratch, uint64_t scratch_bytes, void *out, void *stream);
 
+/* How a call of these sizes runs (host only; for tests).  waves: wavefronts of 32 queries in a workgroup, 0: up to 32 queries, whose keys the wavefronts of a workgroup
+ * share; query_blocks: workgroups that the queries of a kv head take; block_parts: ranges of the cache's blocks; win_parts: ranges of the
+ * window, 0: it belongs to the last range of blocks. */
+int spec_k_attention8_plan(int32_t rows, int32_t hq, int32_t hkv, int32_t hd, int32_t n_blocks, int32_t win_rows, int32_t *waves, int32_t *query_blocks,
+                           int32_t *block_parts, int32_t *win_parts);
+
 /* ---- rotary embedding ----------------------------------------------------------
  * The plane j of a head, dims (j, j + rot/2) in the half layout or (2j, 2j + 1) in
  * the interleaved one, j < rot/2, turns by the angle t = pos * freq[j]:

@@ -146,6 +146,7 @@ lib.spec_k_attention8_scratch_bytes.restype = C.c_uint64
 lib.spec_k_attention8_scratch_bytes.argtypes = [C.c_int32] * 6
 lib.spec_k_attention8.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                   C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p]
+lib.spec_k_attention8_plan.argtypes = [C.c_int32] * 6 + [C.POINTER(C.c_int32)] * 4
 lib.spec_rotary_init.argtypes = [C.c_int32, C.c_int32, C.c_double, C.POINTER(spec_rope_scaling), C.POINTER(spec_rotary_plan_t)]
 lib.spec_k_rotary.argtypes = [C.POINTER(spec_rotary_plan_t), C.c_int32, C.c_char_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
                               C.c_int32, C.c_void_p]
@@ -739,6 +740,15 @@ def spec_k_kv8_load(cache8, first_block: int, n_blocks: int, hkv: int, hd: int):
 
 def spec_k_attention8_scratch_bytes(rows: int, hq: int, hkv: int, hd: int, n_blocks: int, win_rows: int) -> int:
     return int(lib.spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, n_blocks, win_rows))
+
+
+def spec_k_attention8_plan(rows: int, hq: int, hkv: int, hd: int, n_blocks: int, win_rows: int):
+    """(wavefronts of a workgroup, workgroups of a kv head's queries, ranges of the blocks, ranges of the window) of a call."""
+    out = [C.c_int32() for _ in range(4)]
+    rc = lib.spec_k_attention8_plan(rows, hq, hkv, hd, n_blocks, win_rows, *(C.byref(o) for o in out))
+    if rc:
+        raise SpecError(rc, "spec_k_attention8_plan")
+    return tuple(o.value for o in out)
 
 
 def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, anc, hq: int, hkv: int, hd: int, max_depth: Optional[int] = None,

@@ -105,6 +105,13 @@ int spec_k_attention8(const float *q, const void *cache8, int32_t n_blocks, cons
   return done(launch_attention8(a, (hipStream_t)stream));
 }
 
+int spec_k_attention8_plan(int32_t rows, int32_t hq, int32_t hkv, int32_t hd, int32_t n_blocks, int32_t win_rows, int32_t *waves, int32_t *query_blocks,
+                           int32_t *block_parts, int32_t *win_parts) {
+  if (!waves || !query_blocks || !block_parts || !win_parts || !attention_ok(rows, hq, hkv, hd, n_blocks, win_rows)) return SPEC_EINVAL;
+  attention8_plan(rows, hq, hkv, n_blocks, win_rows, waves, query_blocks, block_parts, win_parts);
+  return SPEC_OK;
+}
+
 int spec_rotary_init(int32_t rot, int32_t layout, double theta, const spec_rope_scaling *scaling, spec_rotary_plan *plan) {
   static_assert(SPEC_ROPE_MAX_DIM == 2 * kRotaryMaxPlanes, "header and kernel agree on the planes");
   const double kTwoPi = 6.283185307179586476925286766559;

@@ -862,6 +862,11 @@ size_t attention8_scratch_floats(int rows, int hq, int hkv, int hd, int n_blocks
   return parts == 1 ? 0 : (size_t)parts * rows * hq * (hd + 2);
 }
 
+void attention8_plan(int rows, int hq, int hkv, int n_blocks, int win_rows, int *waves, int *query_blocks, int *block_parts, int *win_parts) {
+  const Plan8 p = plan8(rows, hq, hkv, n_blocks, win_rows);
+  *waves = p.waves; *query_blocks = p.query_blocks; *block_parts = p.block_parts; *win_parts = p.win_parts;
+}
+
 hipError_t launch_attention8(const Attn8Args &a, hipStream_t st) { return a.hd == 128 ? launch_hd<128>(a, st) : launch_hd<64>(a, st); }
 
 }  // namespace spec

@@ -318,6 +318,7 @@ struct Attn8Args {
   void *out;                            // bf16 [rows, hq * hd]
 };
 size_t attention8_scratch_floats(int rows, int hq, int hkv, int hd, int n_blocks, int win_rows);
+void attention8_plan(int rows, int hq, int hkv, int n_blocks, int win_rows, int *waves, int *query_blocks, int *block_parts, int *win_parts);
 hipError_t launch_attention8(const Attn8Args &a, hipStream_t st);
 
 // ---- rotary.hip -----------------------------------------------------------------------------------

@@ -453,6 +453,39 @@ def test_attention8_binding_refusals(P):
         P.spec_k_attention8(**many, scratch=kept[:n - 256])
 
 
+# What large calls take: (waves, query blocks, block parts, window parts), so that a case keeps to its path.  Joined ranges that go on into the window, several blocks one after the
+# other in the LDS of 2, 4 and 8 wavefronts and in the registers of few queries, query blocks dealt out in turn (hkv * parts not a multiple of 8, more than 256 workgroups).
+LARGE = [
+    (True, 60, 64, 8, 512, 0, (8, 2, 16, 0)), (True, 60, 64, 8, 510, 40, (8, 2, 16, 0)), (False, 1024, 32, 8, 128, 0, (8, 16, 2, 0)), (False, 300, 16, 2, 130, 40, (8, 10, 11, 1)),
+    (False, 1200, 3, 3, 500, 50, (8, 5, 16, 1)), (False, 700, 16, 4, 40, 0, (8, 11, 3, 2)), (False, 1000, 72, 9, 11, 10, (8, 32, 1, 0)), (False, 1500, 9, 9, 0, 0, (8, 6, 0, 6)),
+    (True, 60, 16, 2, 300, 40, (4, 4, 30, 2)), (False, 104, 8, 8, 101, 6, (4, 1, 30, 2)), (True, 60, 32, 32, 64, 21, (2, 1, 14, 2)), (False, 1, 64, 64, 100, 40, (0, 1, 3, 1)),
+]
+
+
+@pytest.mark.parametrize("is_tree,rows,hq,hkv,blocks,recent,plan", LARGE)
+def test_attention8_large_calls(P, is_tree, rows, hq, hkv, blocks, recent, plan):
+    """Some rows and kv heads of large calls.  Dim d of the values has what the 64 tokens b = d (mod 128) hold, and a hundredth of it elsewhere: a block or window row too many, too
+    few or in the wrong place moves a dim by far more than roundings may."""
+    hd, win = 128, recent + rows
+    assert P.spec_k_attention8_plan(rows, hq, hkv, hd, blocks, win) == plan
+    q, k, _ = inputs(rows, hq, hkv, hd, blocks, win, rows + blocks, 0.5)
+    n = 64 * blocks
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    v = torch.rand(n + win, hkv, hd, generator=g, device="cuda") + 0.5
+    at = torch.arange(n + win, device="cuda") // 64
+    v = (v * torch.where((at % hd)[:, None] == torch.arange(hd, device="cuda"), 1.0, 0.01)[:, None] * torch.exp2((at % 5).float())[:, None, None]).view(n + win, -1).bfloat16()
+    depth, anc = tree(rows, rows) if is_tree else (np.arange(rows, dtype=np.int32), None)
+    got = f64(run8(P, q, k, v, blocks, n + recent, depth, anc, hq, hkv, hd)).reshape(rows, hkv, -1)
+    some = sorted({i for i in (0, 1, rows - 1, rows // 2, 255 * hkv // hq, 256 * hkv // hq) if i < rows})
+    for h in sorted({0, hkv - 1}):
+        group = hq // hkv
+        want, tol = attention_bound(q.view(rows, hkv, -1)[some, h], k[:, h * hd:h * hd + hd], v[:, h * hd:h * hd + hd], blocks, n + recent, depth[some], None if anc is None else anc[some],
+                                    group, 1, hd)
+        bad = ~(np.abs(got[some, h] - want) <= tol)
+        assert not bad.any(), (h, np.argwhere(bad)[:5], got[some, h][bad][:5], want[bad][:5], tol[bad][:5])
+
+
+
 # ---- rotary ---------------------------------------------------------------------------------------
 
 def check_rotary(P, plan, f, m, rot, layout, x, pos, out_dtype, adjoint=False, **kw):

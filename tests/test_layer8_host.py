@@ -141,3 +141,14 @@ def test_binding_refuses_host_tensors(P):
                  lambda: P.spec_k_kv8_load(torch.zeros(1, 16640, dtype=torch.uint8), 0, 1, 1, 128)):
         with pytest.raises(P.SpecError):
             call()
+
+
+def test_attention8_plan(P):
+    """Ranges are at most as many as the blocks; sizes that a call refuses are refused."""
+    for a in ((1, 8, 8, 128, 4, 40), (60, 64, 8, 128, 512, 60), (1024, 32, 8, 64, 128, 1024), (2, 2, 1, 64, 0, 5000)):
+        waves, query_blocks, block_parts, win_parts = P.spec_k_attention8_plan(*a)
+        assert waves in (0, 2, 4, 8) and query_blocks == -(-a[0] * a[1] // a[2] // (32 * max(waves, 1))) and block_parts <= a[4] and block_parts + win_parts >= 1
+    for a in ((0, 8, 8, 64, 1, 1), (1, 12, 4, 64, 1, 1), (1, 8, 8, 64, 1, 0)):
+        with pytest.raises(P.SpecError):
+            P.spec_k_attention8_plan(*a)
+    assert P.lib.spec_k_attention8_plan(1, 8, 8, 64, 1, 1, None, None, None, None) == -1
