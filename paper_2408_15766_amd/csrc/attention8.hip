@@ -289,10 +289,10 @@ __device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, 
   }
   uint32_t seen = 0xFFFFFFFFu;                                // bit w: the query sees row w0 + w
   bool counts = false;                                        // one of the queries sees a row more than once
-  float top = -INFINITY;
+  float top = -INFINITY;                                      // of the scores; NaN if one is
   if (whole) {
 #pragma unroll
-    for (int i = 0; i < 16; i++) { s[i] *= a.scale; top = fmaxf(top, s[i]); }
+    for (int i = 0; i < 16; i++) { s[i] *= a.scale; top = __builtin_elementwise_maximum(top, s[i]); }
   } else {
     const int below = min(!a.anc ? see.last + 1 : see.deep < 0 ? 0 : a.base - a.n_blocks * kKv8Block, a.win_rows) - w0;   // rows that every position up to the query's brings
     seen = below >= 32 ? 0xFFFFFFFFu : below <= 0 ? 0u : (1u << below) - 1;
@@ -310,6 +310,23 @@ __device__ __forceinline__ void window_step(const Attn8Args &a, Running<HD> &r, 
 #pragma unroll
     for (int i = 0; i < 16; i++) {
       s[i] = (own >> (8 * (i >> 2) + (i & 3))) & 1 ? s[i] * a.scale : -INFINITY;
+      top = __builtin_elementwise_maximum(top, s[i]);
+    }
+  }
+  if (__builtin_amdgcn_ballot_w64(top != top)) {              // (never, as a rule)
+    // Where a score is an infinity (by a key's or a query's, or beyond fp32), the products with what the query's rounding left may make NaN of it: such a score is that of the first terms.
+    f32x16_t first;
+#pragma unroll
+    for (int i = 0; i < 16; i++) first[i] = 0.f;
+#pragma unroll
+    for (int t = 0; t < HD / 16; t++) {
+      first = mul_bf16(key(t), q.hi[t], first);
+      __builtin_amdgcn_sched_barrier(0);                      // (one key in registers at a time)
+    }
+    top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      s[i] = s[i] == s[i] ? s[i] : first[i] * a.scale;
       top = fmaxf(top, s[i]);
     }
   }

@@ -369,6 +369,62 @@ def test_attention8_not_finite_where_seen(P):
     assert (got[:, :, 17] == float("inf")).all() and (got[:, :, 18] == float("-inf")).all() and got[:, :, 19:].isfinite().all()
 
 
+@pytest.mark.parametrize("rows,hq,hkv,hd,blocks,is_tree", [(2, 4, 2, 128, 0, False), (2, 4, 2, 128, 2, True), (40, 4, 4, 128, 3, True), (60, 2, 2, 64, 0, True), (300, 8, 2, 128, 130, False)])
+@pytest.mark.parametrize("exact", [True, False])
+def test_attention8_infinite_keys(P, rows, hq, hkv, hd, blocks, is_tree, exact):
+    """A window key whose score is -infinity weighs nothing, whether or not the query is a bf16 value: the call without that row is the reference.  One of +infinity makes NaN."""
+    recent, bad, n = 40, 33, 64 * blocks
+    q, k, v = inputs(rows, hq, hkv, hd, blocks, recent + rows, 21)
+    q = q.abs() + 0.01
+    if exact:
+        q = q.bfloat16().float()
+    depth, anc = tree(rows, 8) if is_tree else (np.arange(rows, dtype=np.int32), None)
+    rest = [torch.cat([t[:n + bad], t[n + bad + 1:]]) for t in (k, v)]
+    for dim, what in ((17, float("-inf")), (hd - 1, float("-inf")), (slice(3, 30, 5), float("-inf"))):
+        k2 = k.clone().view(-1, hkv, hd)
+        k2[n + bad, :, dim] = what
+        got = f64(run8(P, q, k2.view(k.shape), v, blocks, n + recent, depth, anc, hq, hkv, hd))
+        some = [i for i in (0, 1, rows // 2, rows - 1) if i < rows]
+        want, tol = attention_bound(q[some], *rest, blocks, n + recent - 1, depth[some], None if anc is None else anc[some], hq, hkv, hd)
+        assert (np.abs(got[some] - want) <= tol).all()
+        assert np.isfinite(got).all()
+        k2[n + bad, :, dim] = -what
+        assert run8(P, q, k2.view(k.shape), v, blocks, n + recent, depth, anc, hq, hkv, hd).isnan().all()
+        assert torch.isfinite(run8(P, -q, k2.view(k.shape), v, blocks, n + recent, depth, anc, hq, hkv, hd)).all()
+
+
+def test_attention8_infinite_scores(P):
+    """Rows that see nothing but scores of -infinity get zeros; scores beyond fp32 are infinities; a query's own infinity stays in its row."""
+    hq, hkv, hd, rows = 2, 1, 64, 3
+    q, k, v = inputs(rows, hq, hkv, hd, 0, rows, 4)
+    q = q.abs() + 0.01
+    alone = k.clone()
+    alone[0, 9] = float("-inf")
+    got = run8(P, q, alone, v, 0, 0, [0, 1, 2], None, hq, hkv, hd)
+    assert (got[0] == 0).all() and torch.isfinite(got).all()
+    want, tol = attention_bound(q, k[1:], v[1:], 0, 0, [-1, 0, 1], None, hq, hkv, hd)
+    assert (np.abs(f64(got)[1:] - want[1:]) <= tol[1:]).all()
+    for far in (1.2345e30, 1e30 * (1 + 2.0 ** -9 - 2.0 ** -14)):         # (their rests have either sign)
+        big, key = q.clone().view(rows, hq, hd), k.clone()
+        big[:, :, 3], key[:, 3] = far, 0.0
+        key[0, 3] = -1e30
+        got = run8(P, big.view(rows, -1), key, v, 0, 0, [0, 1, 2], None, hq, hkv, hd)
+        big[:, :, 3] = 0.0
+        want, tol = attention_bound(big.view(rows, -1), key[1:], v[1:], 0, 0, [-1, 0, 1], None, hq, hkv, hd)
+        assert (got[0] == 0).all() and (np.abs(f64(got)[1:] - want[1:]) <= tol[1:]).all()
+    clean = run8(P, q, k, v, 0, 0, [0, 1, 2], None, hq, hkv, hd)
+    for sign, check in ((-1, lambda t: (t == 0).all()), (1, lambda t: t.isnan().all())):
+        key, wild = k.clone(), q.clone().view(rows, hq, hd)
+        key[:, 5] = sign * (key[:, 5].abs() + 1)
+        wild[1, 0, 5] = float("inf")
+        same = run8(P, q, key, v, 0, 0, [0, 1, 2], None, hq, hkv, hd).view(rows, hq, hd)
+        got = run8(P, wild.view(rows, -1), key, v, 0, 0, [0, 1, 2], None, hq, hkv, hd).view(rows, hq, hd)
+        assert check(got[1, 0])
+        same[1, 0], got[1, 0] = 0, 0
+        assert torch.equal(same, got)
+    assert torch.isfinite(clean).all()
+
+
 def test_attention8_scales_far_apart(P):
     """Keys, values and queries whose magnitudes differ by block, head and row."""
     hq, hkv, hd, blocks, rows = 4, 2, 128, 12, 6
