@@ -492,8 +492,10 @@ __device__ __forceinline__ void window_alone(const Attn8Args &a, Running<HD> &r,
   }
 }
 
+// A part of the scratch: references and sums of all queries, padded to 16 bytes, then their outputs (every output 16 bytes aligned, whatever the number of queries)
+__host__ __device__ inline size_t part_stats(size_t queries) { return 2 * ((queries + 1) / 2 * 2); }
+__host__ __device__ inline size_t part_floats(size_t queries, int hd) { return part_stats(queries) + queries * hd; }
 // A part's result of this lane's query: reference, sum and outputs, or, if the launch has one part, the query's result
-template <int HD> __device__ __forceinline__ size_t part_floats(const Attn8Args &a) { return (size_t)a.rows * a.hq * (HD + 2); }
 template <int HD>
 __device__ __forceinline__ void put_dims(const Attn8Args &a, size_t query, int part, int parts, int db, int g, const f32x16_t &o, float m, float l) {
   if (parts == 1) {
@@ -504,8 +506,9 @@ __device__ __forceinline__ void put_dims(const Attn8Args &a, size_t query, int p
       *(u32x2_t *)(out + 8 * i) = u32x2_t{pack_bf16x2(o[4 * i] * inv, o[4 * i + 1] * inv), pack_bf16x2(o[4 * i + 2] * inv, o[4 * i + 3] * inv)};
     return;
   }
-  float *p = a.part + part * part_floats<HD>(a);
-  float *po = p + (size_t)a.rows * a.hq * 2 + query * HD + db * 32 + 4 * g;
+  const size_t queries = (size_t)a.rows * a.hq;
+  float *p = a.part + part * part_floats(queries, HD);
+  float *po = p + part_stats(queries) + query * HD + db * 32 + 4 * g;
 #pragma unroll
   for (int i = 0; i < 4; i++) *(f32x4_t *)(po + 8 * i) = f32x4_t{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
   if (db == 0 && g == 0) ((float2 *)p)[query] = make_float2(m, l);
@@ -711,7 +714,7 @@ __global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a, int 
   const size_t all_queries = (size_t)a.rows * a.hq, query = (size_t)blockIdx.x * kQueries + slot, at = query < all_queries ? query : all_queries - 1;
   RowMerge all;
   f32x4_t o{0.f, 0.f, 0.f, 0.f};
-  const size_t part_size = part_floats<HD>(a);
+  const size_t part_size = part_floats(all_queries, HD), stats_size = part_stats(all_queries);
   for (int i0 = group; i0 < parts; i0 += 8 * GROUPS) {
     float2 s[8];
     f32x4_t x[8];
@@ -719,7 +722,7 @@ __global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a, int 
     for (int j = 0; j < 8; j++) {
       const float *p = a.part + min(i0 + j * GROUPS, parts - 1) * part_size;
       s[j] = ((const float2 *)p)[at];
-      x[j] = *(const f32x4_t *)(p + all_queries * 2 + at * HD + d);
+      x[j] = *(const f32x4_t *)(p + stats_size + at * HD + d);
     }
 #pragma unroll
     for (int j = 0; j < 8; j++) {
@@ -876,7 +879,7 @@ hipError_t launch_kv8_load(const void *cache8, int first_block, int n_blocks, in
 size_t attention8_scratch_floats(int rows, int hq, int hkv, int hd, int n_blocks, int win_rows) {
   const Plan8 p = plan8(rows, hq, hkv, n_blocks, win_rows);
   const int parts = p.block_parts + p.win_parts;
-  return parts == 1 ? 0 : (size_t)parts * rows * hq * (hd + 2);
+  return parts == 1 ? 0 : parts * part_floats((size_t)rows * hq, hd);
 }
 
 void attention8_plan(int rows, int hq, int hkv, int n_blocks, int win_rows, int *waves, int *query_blocks, int *block_parts, int *win_parts) {

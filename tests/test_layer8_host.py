@@ -152,3 +152,12 @@ def test_attention8_plan(P):
         with pytest.raises(P.SpecError):
             P.spec_k_attention8_plan(*a)
     assert P.lib.spec_k_attention8_plan(1, 8, 8, 64, 1, 1, None, None, None, None) == -1
+
+
+@pytest.mark.parametrize("rows,hq,hkv,hd,blocks,win", [(3, 1, 1, 128, 1000, 5), (1, 1, 1, 64, 1000, 1), (33, 1, 1, 64, 500, 40), (2, 1, 1, 128, 1000, 5), (5, 3, 3, 128, 700, 9)])
+def test_attention8_scratch_keeps_its_parts_aligned(P, rows, hq, hkv, hd, blocks, win):
+    """Every part is statistics (two floats a query) and outputs, both beginning at multiples of 16 bytes, for odd numbers of queries too."""
+    _, _, block_parts, win_parts = P.spec_k_attention8_plan(rows, hq, hkv, hd, blocks, win)
+    of_part = -(-8 * rows * hq // 16) * 16 + 4 * rows * hq * hd
+    assert block_parts + win_parts > 32
+    assert P.spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, blocks, win) == -(-(block_parts + win_parts) * of_part // 256) * 256
