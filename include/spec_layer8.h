@@ -88,9 +88,9 @@ int spec_k_kv8_load(const void *cache8, int32_t first_block, int32_t n_blocks, i
  * out: [rows, hq*hd] bf16, overlaps no input.  depth[i] <= max_depth for every row (a row beyond is taken to be at max_depth); with anc, max_depth <= 15.
  * hd 64 or 128, hq/hkv one of 1, 2, 4, 8; hkv <= 128; rows <= 2^20.  Scratch: spec_k_attention8_scratch_bytes(..), 256-byte aligned
  * (host only; 0 if the call needs none, then scratch may be NULL, and for bad sizes).  Softmax statistics and sums are fp32.  In the 8-bit part queries are rounded to
- * fp16 relative to the row's largest value (2^-11) and weights cut to fp16 (at most 2^-10 off, centred;
- * where the values' exponents of two blocks are d > 20 apart, 2^(d - 30) of the smaller values); in
- * the window both go in two bf16 terms (2^-16). 
+ * fp16 relative to the row's largest value (2^-11) and weights cut to fp16: with its block's value exponent e a weight w counts as w 2^e, and down to 2^-26 of the largest
+ * weight times the largest 2^e it is at most 2^-10 off, centred; smaller ones are cut to multiples of 2^-36 of that.  In
+ * the window both go in two bf16 terms (2^-16).
  * Sums are weighted by up to 2^45 before the division: values beyond 2^80 may end as infinities.
  * The result of a row may change in its last bits with the rows beside it. */
 uint64_t spec_k_attention8_scratch_bytes(int32_t rows, int32_t hq, int32_t hkv, int32_t hd, int32_t n_blocks, int32_t win_rows);

@@ -70,10 +70,11 @@ __global__ __launch_bounds__(256) void kv8_load_kernel(const unsigned char *cach
 // holds query c, of a 32-key tile's scores the keys 8 i + 4 g + 0 .. 3 (i < 4), of the outputs the same dims of every 32.
 //
 // In the blocks the products are fp16: codes are exact there, a query row is divided by the power of two of its largest value and rounded once (2^-11), and
-// a weight is cut once.  Weights are 2^(score - reference + kRefLift): up to 2^15 while the reference lags by kRefSlack, so that fp16 keeps its full precision for
-// weights down to 2^-29 of the largest.  A block's exponents go into the scores' factor and into the weights (relative to the largest of the
-// blocks so far, which the outputs are in units of); nothing is done per value for them.
-constexpr float kRefLift = 7.f;
+// a weight is cut once.  Weights are 2^(score - reference): the reference is put kRefLift under the largest score and moves when it lags kRefLag more, so that the largest weight is
+// 2^12 to 2^15 and weights keep fp16's full precision (2^-14 on) down to 2^-26 of it; smaller ones are cut to multiples of 2^-36 of it (2^-24).  (A lift of 7 and a lag of 8 moved the reference less
+// often, in the same time, and took up to 2^-6 of weights 2^-25 of the largest, as of keys behind an attention sink.)  A block's exponents go into the scores' factor and into the weights (relative
+// to the largest of the blocks so far, which the outputs are in units of); nothing is done per value for them.
+constexpr float kRefLift = 12.f, kRefLag = 3.f;
 // Weights go to fp16 by the conversion that cuts off, two at a time (rounding to nearest takes three instructions): they are made 2^-12 too large first, which
 // centres the error (at most 2^-10 either way, in the mean none), and their sum is corrected for it.
 constexpr float kCutLift = 0.00035223863f;                    // log2(1 + 2^-12)
@@ -126,9 +127,9 @@ template <int HD> struct Running {
     for (int db = 0; db < HD / 32; db++) o[db] *= t;
     l *= t;
   }
-  // top: the largest score of this query's new keys.  The reference moves where it lags by more than kRefSlack.
+  // top: the largest score of this query's new keys
   __device__ __forceinline__ void raise(float top) {
-    const bool move = top - kRefLift > m + kRefSlack;          // (also the first keys; NaN moves nothing)
+    const bool move = top - kRefLift > m + kRefLag;            // (also the first keys; NaN moves nothing)
     if (__builtin_amdgcn_ballot_w64(move) == 0) return;
     const float m_new = move ? top - kRefLift : m;
     turn_by(move ? exp2_(m - m_new) : 1.f);

@@ -448,6 +448,29 @@ def test_attention8_blocks_without_values_beside_large_ones(P, rows, large):
     check_attention(P, q, k, v.bfloat16(), blocks, 64 * blocks, np.arange(rows), None, hq, hkv, hd)
 
 
+@pytest.mark.parametrize("rows,hq,hkv,hd,blocks", [(1, 2, 2, 64, 9), (1, 64, 64, 128, 100), (60, 32, 32, 64, 40), (104, 8, 8, 128, 101), (60, 64, 8, 128, 300)])
+@pytest.mark.parametrize("bits", [0, 12.2, 20.6, 23.8, 25.7])
+def test_attention8_small_weights_behind_a_sink(P, rows, hq, hkv, hd, blocks, bits):
+    """In every block one key, whose value is zero, outweighs the others by 2^bits: the result is what the others hold, and their weights have the precision that is stated
+    (2^-10 = 2 h).  Queries have one element, exact in fp16, so that scores are off by fp32's roundings only: 100 * 2^-24 in units of log2."""
+    a = round(bits * 64 * math.sqrt(hd) / 192 * math.log(2)) / 64            # (192 is a code)
+    q = torch.zeros(rows, hq, hd)
+    q[:, :, 0] = a
+    k = torch.zeros(64 * blocks + rows, hkv, hd)
+    v = torch.exp(rand(3, 64 * blocks + rows, hkv, hd))
+    for b in range(blocks):
+        at = 64 * b + 17 * b % 64
+        k[at, :, 0], v[at] = 192.0, 0.0
+    q, k, v = q.view(rows, -1).cuda(), k.view(-1, hkv * hd).bfloat16().cuda(), v.view(-1, hkv * hd).bfloat16().cuda()
+    n, depth = 64 * blocks, np.zeros(rows, np.int32)
+    got = f64(run8(P, q, k, v, blocks, n, depth, None, hq, hkv, hd)).reshape(rows, hkv, -1)
+    for h in (0, hkv - 1):
+        kh, vh = (f64(t[:, h * hd:h * hd + hd]) for t in (k, v))
+        want, spread, _, _ = O.attention8(f64(q).reshape(rows, hkv, -1)[:1, h], O.held_kv(kh[:n], 1, hd), O.held_kv(vh[:n], 1, hd), kh[n:], vh[n:], n, depth[:1], None, hq // hkv, 1, hd)
+        tol = U16 * np.abs(want) + (2 * H + 100 * U32 + 2.0 ** -17 + 1e-6) * spread * (1 + U16)
+        assert (np.abs(got[:, h] - want) <= tol).all(), float((np.abs(got[:, h] - want) / tol).max())
+
+
 def test_attention8_one_key_outweighs_all(P):
     hq, hkv, hd, blocks = 2, 1, 128, 20
     q, k, v = inputs(2, hq, hkv, hd, blocks, 2, 5)
