@@ -579,6 +579,11 @@ def spec_topk_loss(feat_target, feat_draft, lm_head_packed, k: int, scratch=None
 _INT_MAX = 2 ** 31 - 1
 
 
+def _fit(*sizes: int) -> bool:
+    """Whether they are 32-bit numbers (ctypes cuts others without a word)."""
+    return all(-_INT_MAX <= n <= _INT_MAX for n in sizes)
+
+
 def _refuse(what: str, why: str):
     raise SpecError(SPEC_EINVAL, f"{what}: {why}")
 
@@ -612,7 +617,7 @@ def _dtype_code(what: str, dtype) -> int:
 
 
 def spec_packed8_bytes(rows: int, cols: int) -> int:
-    return int(lib.spec_packed8_bytes(rows, cols))
+    return int(lib.spec_packed8_bytes(rows, cols)) if _fit(rows, cols) else 0
 
 
 def spec_pack_weight8(w):
@@ -636,7 +641,7 @@ def spec_pack_weight8(w):
 
 
 def spec_k_gemm8_scratch_bytes(m: int, cols: int, rows: int) -> int:
-    return int(lib.spec_k_gemm8_scratch_bytes(m, cols, rows))
+    return int(lib.spec_k_gemm8_scratch_bytes(m, cols, rows)) if _fit(m, cols, rows) else 0
 
 
 def spec_k_gemm8(x, w8, out_dtype=None, out=None, scratch=None):
@@ -652,6 +657,8 @@ def spec_k_gemm8(x, w8, out_dtype=None, out=None, scratch=None):
     if x.dim() != 2 or x.shape[1] != cols or (x.stride(1) != 1 and cols > 1):
         _refuse(what, f"x has to be [m, {cols}] with dense rows")
     m = x.shape[0]
+    if m > _INT_MAX:
+        _refuse(what, f"{m} rows")
     if out is None:
         out = _new((m, rows), (rows, 1), x.dtype if out_dtype is None else out_dtype, x)
     elif tuple(out.shape) != (m, rows) or (out.stride(1) != 1 and rows > 1) or (out_dtype is not None and out_dtype is not out.dtype):
@@ -676,7 +683,7 @@ def spec_k_gemm8(x, w8, out_dtype=None, out=None, scratch=None):
 
 
 def spec_kv8_bytes(n_blocks: int, hkv: int, hd: int) -> int:
-    return int(lib.spec_kv8_bytes(n_blocks, hkv, hd))
+    return int(lib.spec_kv8_bytes(n_blocks, hkv, hd)) if _fit(n_blocks, hkv, hd) else 0
 
 
 def spec_kv8_alloc(n_blocks: int, hkv: int, hd: int, device=None):
@@ -690,7 +697,7 @@ def spec_kv8_alloc(n_blocks: int, hkv: int, hd: int, device=None):
 
 @functools.lru_cache(maxsize=None)
 def _kv8_block(hkv: int, hd: int) -> int:
-    return int(lib.spec_kv8_bytes(1, hkv, hd))
+    return spec_kv8_bytes(1, hkv, hd)
 
 
 def _is_kv8(cache8, hkv: int, hd: int, blocks: int) -> bool:
@@ -739,13 +746,15 @@ def spec_k_kv8_load(cache8, first_block: int, n_blocks: int, hkv: int, hd: int):
 
 
 def spec_k_attention8_scratch_bytes(rows: int, hq: int, hkv: int, hd: int, n_blocks: int, win_rows: int) -> int:
-    return int(lib.spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, n_blocks, win_rows))
+    sizes = (rows, hq, hkv, hd, n_blocks, win_rows)
+    return int(lib.spec_k_attention8_scratch_bytes(*sizes)) if _fit(*sizes) else 0
 
 
 def spec_k_attention8_plan(rows: int, hq: int, hkv: int, hd: int, n_blocks: int, win_rows: int):
     """(wavefronts of a workgroup, workgroups of a kv head's queries, ranges of the blocks, ranges of the window) of a call."""
     out = [C.c_int32() for _ in range(4)]
-    rc = lib.spec_k_attention8_plan(rows, hq, hkv, hd, n_blocks, win_rows, *(C.byref(o) for o in out))
+    sizes = (rows, hq, hkv, hd, n_blocks, win_rows)
+    rc = lib.spec_k_attention8_plan(*sizes, *(C.byref(o) for o in out)) if _fit(*sizes) else SPEC_EINVAL
     if rc:
         raise SpecError(rc, "spec_k_attention8_plan")
     return tuple(o.value for o in out)
@@ -771,7 +780,7 @@ def spec_k_attention8(q, cache8, n_blocks: int, kwin, vwin, base: int, depth, an
         _refuse(what, "anc has to be int32 [rows, 16]")
     win_rows = kwin.shape[0]
     n = lib.spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, n_blocks, win_rows)
-    if n_blocks and not _is_kv8(cache8, hkv, hd, n_blocks):
+    if n_blocks < 0 or n_blocks and not _is_kv8(cache8, hkv, hd, n_blocks):
         _refuse(what, f"cache8 holds no {n_blocks} blocks of {hkv} heads of {hd}")
     if max_depth is None:
         max_depth = max(int(depth.max().item()), 0) if rows else 0
@@ -801,6 +810,8 @@ def spec_rotary_plan(rot: int, theta: float, layout: str = "half", scaling: str 
     """The frequencies of a rotary embedding over the first `rot` dims of a head (host data; made once)."""
     if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
         _refuse("spec_rotary_plan", f"layout {layout!r}, scaling {scaling!r}")
+    if not _fit(rot, trained_len):
+        _refuse("spec_rotary_plan", f"rot {rot}, trained_len {trained_len}")
     low, high = (beta_slow, beta_fast) if scaling == "yarn" else (low_freq, high_freq)
     plan = spec_rotary_plan_t()
     rc = lib.spec_rotary_init(rot, ROPE_LAYOUTS[layout], theta, C.byref(spec_rope_scaling(ROPE_SCALINGS[scaling], trained_len, factor, low, high)), C.byref(plan))
@@ -832,6 +843,8 @@ def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[
     at = pos if isinstance(pos, torch.Tensor) else None
     stream = _here(what, *xs, at) if made else _here(what, *xs, *outs, at)
     rows, _, hd = xs[0].shape
+    if rows > _INT_MAX or hd > _INT_MAX:
+        _refuse(what, f"{rows} rows, heads of {hd}")
     if at is not None and (at.dtype is not torch.int32 or at.dim() != 1 or at.shape[0] != rows or not at.is_contiguous()):
         _refuse(what, f"pos has to be int32 [{rows}]")
     if at is None and not -_INT_MAX - 1 <= int(pos) <= _INT_MAX:
@@ -842,7 +855,7 @@ def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[
         shape, strides, dtype, out_dtype = x.shape, x.stride(), x.dtype, o.dtype
         if len(shape) != 3 or shape[0] != rows or shape[2] != hd or not (made or shape == o.shape):
             _refuse(what, f"tensors have to be [{rows}, heads, {hd}]")
-        heads = shape[1]
+        heads = min(shape[1], _INT_MAX)                           # (more than any call takes)
         ldo, hso, one = (heads * hd, hd, 1) if made else o.stride()
         if hd > 1 and not strides[2] == one == 1:
             _refuse(what, "the dims of a head have to be dense")

@@ -851,6 +851,22 @@ def test_more_elements_than_31_bits_count(P):
     assert torch.equal(r[-64:], r[:64]) and not torch.equal(r[1], r[0])
 
 
+def test_tensors_with_dims_beyond_32_bits_are_refused(P):
+    """2^32 + n rows, dims or blocks are not n of them."""
+    far = 2 ** 32
+    base = torch.empty(far + 64, dtype=torch.bfloat16, device="cuda")
+    one = P.spec_pack_weight8(torch.ones(1, 1, dtype=torch.bfloat16, device="cuda"))
+    plan, none = P.spec_rotary_plan(64, 1e4), P.spec_rotary_plan(0, 1e4)
+    q, k, v = inputs(1, 1, 1, 64, 1, 1, 1)
+    cache, d = P.spec_kv8_alloc(1, 1, 64), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for call in (lambda: P.spec_pack_weight8(base.view(-1, 1)), lambda: P.spec_pack_weight8(base.view(1, -1)), lambda: P.spec_k_gemm8(base.view(-1, 1), one),
+                 lambda: P.spec_k_rotary(none, [base.view(-1, 1, 1)], 0, outs=[base.view(-1, 1, 1)]), lambda: P.spec_k_rotary(none, [base.view(1, -1, 1)], 0, outs=[base.view(1, -1, 1)]),
+                 lambda: P.spec_k_rotary(plan, [base.view(1, 1, -1)], 0, outs=[base.view(1, 1, -1)]),
+                 lambda: P.spec_k_attention8(q, cache, -far, k[:1], v[:1], 0, d, None, 1, 1, 64, max_depth=0), lambda: P.spec_k_attention8(q, cache, -1, k[:1], v[:1], 0, d, None, 1, 1, 64)):
+        with pytest.raises(P.SpecError):
+            call()
+
+
 def test_rotary_ahead_of_and_behind_training_attention(P):
     """q and k of a training step turned ahead of spec_hca_attention; relative positions alone matter, so a shift of all positions changes nothing but roundings."""
     b, s, hq, hkv, hd = 2, 96, 4, 2, 64

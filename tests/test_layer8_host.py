@@ -161,3 +161,23 @@ def test_attention8_scratch_keeps_its_parts_aligned(P, rows, hq, hkv, hd, blocks
     of_part = -(-8 * rows * hq // 16) * 16 + 4 * rows * hq * hd
     assert block_parts + win_parts > 32
     assert P.spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, blocks, win) == -(-(block_parts + win_parts) * of_part // 256) * 256
+
+
+def test_sizes_beyond_32_bits_are_no_sizes(P):
+    """2^32 + n is not n."""
+    far = 2 ** 32
+    assert P.spec_packed8_bytes(far + 16, 1) == P.spec_packed8_bytes(16, far + 128) == P.spec_packed8_bytes(16, -far + 128) == 0
+    assert P.spec_k_gemm8_scratch_bytes(far + 40, 128, 16) == P.spec_k_gemm8_scratch_bytes(40, far + 128, 16) == P.spec_k_gemm8_scratch_bytes(40, 128, far + 16) == 0
+    assert P.spec_kv8_bytes(far + 1, 8, 128) == P.spec_kv8_bytes(1, far + 8, 128) == P.spec_kv8_bytes(1, 8, far + 128) == 0
+    good = (60, 32, 8, 128, 64, 100)
+    for i in range(6):
+        a = tuple(n + far * (j == i) for j, n in enumerate(good))
+        assert P.spec_k_attention8_scratch_bytes(*a) == 0
+        with pytest.raises(P.SpecError):
+            P.spec_k_attention8_plan(*a)
+    for kw in (dict(rot=far + 64), dict(rot=64 - far), dict(rot=64, scaling="yarn", factor=4.0, trained_len=far + 4096)):
+        with pytest.raises(P.SpecError):
+            P.spec_rotary_plan(**{**dict(theta=1e4), **kw})
+    for kw in (dict(hkv=far + 8, hd=128), dict(hkv=8, hd=far + 128)):
+        with pytest.raises(P.SpecError):
+            P.spec_kv8_alloc(1, **kw, device="cpu")
