@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(RotaryArgs a) {
   const int n = blockIdx.y;
   const RotaryPart p = n == 0 ? p0 : n == 1 ? p1 : p2;
   const uint2 head_items = n == 0 ? h0 : n == 1 ? h1 : h2, row_items = n == 0 ? r0 : n == 1 ? r1 : r2;
-  const int64_t row0 = (int64_t)blockIdx.x * a.rows_each;
+  const int64_t row0 = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * a.rows_each;   // (from a.rows on: nothing to do)
   const int rows = (int)min((int64_t)a.rows_each, a.rows - row0), half = a.rot / 2, total = rows * (int)row_items.y;
   const bool pairs = !a.interleaved;                          // a turning step has its planes' partners half further on
   const int turning = !p.turn ? 0 : VEC && a.interleaved ? half / 4 : half / W;   // steps of a head that turn
@@ -189,7 +189,8 @@ hipError_t launch_rotary(RotaryArgs a, hipStream_t st) {
   if (half > 0 && each * half > kRotaryTable) each = kRotaryTable / half;
   while (each > 1 && a.rows / each < 256) each /= 2;          // (rather more workgroups than compute units)
   a.rows_each = each;
-  const dim3 grid((unsigned)(((int64_t)a.rows + each - 1) / each), a.n_parts);
+  const int64_t groups = ((int64_t)a.rows + each - 1) / each, deep = (groups + (1 << 23) - 1) >> 23;   // (a grid's dimension holds less than 2^32 threads)
+  const dim3 grid((unsigned)((groups + deep - 1) / deep), a.n_parts, (unsigned)deep);
   if (vec) hipLaunchKernelGGL(rotary_kernel<true>, grid, dim3(kRotaryThreads), 0, st, a);
   else hipLaunchKernelGGL(rotary_kernel<false>, grid, dim3(kRotaryThreads), 0, st, a);
   return hipGetLastError();

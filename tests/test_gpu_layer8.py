@@ -676,6 +676,19 @@ def test_rotary_binding_refusals(P):
             call()
 
 
+def test_rotary_of_most_rows(P):
+    """2^24 rows, each more than a workgroup's steps, in place: as the same rows by themselves."""
+    rows, heads, hd = 1 << 24, 3, 96
+    plan = P.spec_rotary_plan(2, 1e4, layout="interleaved")
+    some = torch.tensor([0, 1, 77, rows // 2 - 1, rows // 2, rows // 2 + 1, rows - 2, rows - 1], device="cuda")
+    x = torch.empty(rows, heads, hd, dtype=torch.bfloat16, device="cuda")
+    x.view(-1, 64, heads, hd).copy_(rand(1, 64, heads, hd).cuda())
+    want = P.spec_k_rotary(plan, [x[some]], some.to(torch.int32))[0]
+    assert not torch.equal(want, x[some])
+    P.spec_k_rotary(plan, [x], 0, outs=[x])
+    assert torch.equal(x[some], want)
+
+
 def test_rotary_not_finite_values_stay_in_their_plane(P):
     plan = P.spec_rotary_plan(64, 1e4)
     x = rand(1, 4, 2, 64).cuda()
