@@ -843,7 +843,7 @@ def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[
     at = pos if isinstance(pos, torch.Tensor) else None
     stream = _here(what, *xs, at) if made else _here(what, *xs, *outs, at)
     rows, _, hd = xs[0].shape
-    if rows > _INT_MAX or hd > _INT_MAX:
+    if rows > _INT_MAX or hd > SPEC_ROPE_MAX_DIM:
         _refuse(what, f"{rows} rows, heads of {hd}")
     if at is not None and (at.dtype is not torch.int32 or at.dim() != 1 or at.shape[0] != rows or not at.is_contiguous()):
         _refuse(what, f"pos has to be int32 [{rows}]")
@@ -853,9 +853,9 @@ def spec_k_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, turned: Optional[
     fields = []
     for x, o, turn in zip(xs, outs, (True,) * n if turned is None else turned):
         shape, strides, dtype, out_dtype = x.shape, x.stride(), x.dtype, o.dtype
-        if len(shape) != 3 or shape[0] != rows or shape[2] != hd or not (made or shape == o.shape):
-            _refuse(what, f"tensors have to be [{rows}, heads, {hd}]")
-        heads = min(shape[1], _INT_MAX)                           # (more than any call takes)
+        if len(shape) != 3 or shape[0] != rows or shape[2] != hd or shape[1] > 1024 or not (made or shape == o.shape):
+            _refuse(what, f"tensors have to be [{rows}, up to 1024 heads, {hd}]")
+        heads = shape[1]
         ldo, hso, one = (heads * hd, hd, 1) if made else o.stride()
         if hd > 1 and not strides[2] == one == 1:
             _refuse(what, "the dims of a head have to be dense")
