@@ -37,7 +37,7 @@ template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void quant8_kernel(const T *x, int64_t ldx, int rows, int in, int pad, unsigned char *dst) {
   const Packed8 pk = packed8(rows, in);
   const int lane = threadIdx.x & 63, r8 = lane >> 3, piece = lane & 7;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t wave = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int64_t rb8 = wave / pk.groups;                       // eight rows
   const int g = (int)(wave - rb8 * pk.groups);
   const int64_t row = rb8 * 8 + r8;
@@ -69,11 +69,11 @@ template <typename T>
 hipError_t quant8(const T *x, int64_t ldx, int rows, int in, int pad, void *dst, hipStream_t st) {
   const Packed8 pk = packed8(rows, in);
   const int64_t waves = (int64_t)pk.blocks * 2 * pk.groups;
-  const int64_t grid = (waves + 3) / 4;
-  if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  const int64_t groups = (waves + 3) / 4, deep = (groups + (1 << 23) - 1) >> 23;   // (a grid's dimension holds less than 2^32 threads; at most 2^9 deep)
+  const dim3 grid((unsigned)((groups + deep - 1) / deep), (unsigned)deep);
   const bool vec = ((uintptr_t)x & 15) == 0 && ldx % (16 / (int)sizeof(T)) == 0;
-  if (vec) hipLaunchKernelGGL((quant8_kernel<T, true>), dim3((unsigned)grid), dim3(256), 0, st, x, ldx, rows, in, pad, (unsigned char *)dst);
-  else hipLaunchKernelGGL((quant8_kernel<T, false>), dim3((unsigned)grid), dim3(256), 0, st, x, ldx, rows, in, pad, (unsigned char *)dst);
+  if (vec) hipLaunchKernelGGL((quant8_kernel<T, true>), grid, dim3(256), 0, st, x, ldx, rows, in, pad, (unsigned char *)dst);
+  else hipLaunchKernelGGL((quant8_kernel<T, false>), grid, dim3(256), 0, st, x, ldx, rows, in, pad, (unsigned char *)dst);
   return hipGetLastError();
 }
 

@@ -195,6 +195,28 @@ def test_gemm8_weights_beyond_2_gib(P, m):
         assert np.abs(f64(y[:, at:at + 96]) - ref).max() <= 2 * U16 * np.abs(ref).max()
 
 
+def test_gemm8_packs_more_than_2_to_the_36_elements(P):
+    """2^24 rows of 4100 (138 GB): blocks of 16 rows at the ends and in the middle are packed as they are by themselves."""
+    rows, k = 1 << 24, 4100
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 2 * rows * k + P.spec_packed8_bytes(rows, k) + (4 << 30):
+        pytest.skip("not enough free memory")
+    w = torch.empty(rows, k, dtype=torch.bfloat16, device="cuda")
+    firsts = [0, 16, rows // 2 - 16, rows // 2, (1 << 36) // k // 16 * 16, rows - 16]
+    for i, r in enumerate(firsts):
+        w[r:r + 16] = rand(i, 16, k).cuda()
+    w8 = P.spec_pack_weight8(w)
+    tiles, quads = (k + 127) // 128, (k + 511) // 512
+    for r in firsts:
+        one = P.spec_pack_weight8(w[r:r + 16].contiguous())
+        b = r // 16
+        assert torch.equal(w8[b * tiles * 2048:(b + 1) * tiles * 2048], one[:tiles * 2048])
+        exps = rows // 16 * tiles * 2048 + b * quads * 64
+        assert torch.equal(w8[exps:exps + quads * 64], one[tiles * 2048:tiles * 2048 + quads * 64])
+    del w, w8
+    torch.cuda.empty_cache()
+
+
 # ---- cache --------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("hkv,hd", [(1, 64), (3, 128), (8, 128), (128, 64)])
