@@ -712,7 +712,7 @@ __global__ __launch_bounds__(256) void attention8_merge_kernel(Attn8Args a, int 
   __shared__ f32x4_t sums[GROUPS > 1 ? 256 : 1];
   __shared__ float2 stats[GROUPS > 1 ? kQueries * GROUPS : 1];
   const int in_query = threadIdx.x % (kThreads * GROUPS), slot = threadIdx.x / (kThreads * GROUPS), group = in_query / kThreads, d = in_query % kThreads * 4;
-  const size_t all_queries = (size_t)a.rows * a.hq, query = (size_t)blockIdx.x * kQueries + slot, at = query < all_queries ? query : all_queries - 1;
+  const size_t all_queries = (size_t)a.rows * a.hq, query = ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * kQueries + slot, at = query < all_queries ? query : all_queries - 1;
   RowMerge all;
   f32x4_t o{0.f, 0.f, 0.f, 0.f};
   const size_t part_size = part_floats(all_queries, HD), stats_size = part_stats(all_queries);
@@ -821,9 +821,8 @@ template <int HD, int WAVES> hipError_t launch_wide(const Attn8Args &a, const Pl
 
 template <int HD, int GROUPS> hipError_t launch_merge(const Attn8Args &a, int parts, hipStream_t st) {
   constexpr int kEach = 1024 / (HD * GROUPS);                 // queries of a workgroup
-  const int64_t grid = ((int64_t)a.rows * a.hq + kEach - 1) / kEach;
-  if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((attention8_merge_kernel<HD, GROUPS>), dim3((unsigned)grid), dim3(256), 0, st, a, parts);
+  const int64_t groups = ((int64_t)a.rows * a.hq + kEach - 1) / kEach, deep = (groups + (1 << 23) - 1) >> 23;   // (a grid's dimension holds less than 2^32 threads; at most 2^7 deep)
+  hipLaunchKernelGGL((attention8_merge_kernel<HD, GROUPS>), dim3((unsigned)((groups + deep - 1) / deep), (unsigned)deep), dim3(256), 0, st, a, parts);
   return hipGetLastError();
 }
 
@@ -831,7 +830,7 @@ template <int HD> hipError_t launch_hd(const Attn8Args &a, hipStream_t st) {
   const Plan8 p = plan8(a.rows, a.hq, a.hkv, a.n_blocks, a.win_rows);
   const int parts = p.block_parts + p.win_parts;
   const int64_t units = (int64_t)a.hkv * parts, grid = (units * p.query_blocks + 7) / 8 * 8;
-  if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  if (grid * 512 >> 32) return hipErrorInvalidValue;          // (beyond any memory: the limit of a grid's threads)
   hipError_t e;
   if (p.waves == 0) {
     constexpr int kLds = kFewWaves * (HD * 128 + 256);

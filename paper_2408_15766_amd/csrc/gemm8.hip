@@ -521,7 +521,7 @@ hipError_t launch_tile(const Gemm8Args &a, hipStream_t st) {
   using L = Tile8<WM, WN, TB, WB>;
   const int64_t tok_tiles = (a.m + L::kTok - 1) / L::kTok, row_tiles = (a.row_end - a.row_begin + L::kRows - 1) / L::kRows;
   const int64_t grid = (row_tiles + 7) / 8 * 8 * tok_tiles;
-  if (grid > 0x7FFFFFFFll) return hipErrorInvalidValue;
+  if (grid * L::kWaves * 64 >> 32) return hipErrorInvalidValue;   // (beyond any memory: the limit of a grid's threads)
   hipLaunchKernelGGL((gemm8_tile_kernel<OUT, VEC, WM, WN, TB, WB, STAGES>), dim3((unsigned)grid), dim3(L::kWaves * 64), 0, st, a);
   return hipGetLastError();
 }

@@ -530,6 +530,27 @@ def test_attention8_offsets_beyond_2_gib(P):
         assert (np.abs(got[h] - want) <= tol).all()
 
 
+def test_attention8_joins_the_parts_of_2_to_the_28_queries(P):
+    """Rows repeat every 64, and every 64 have the bits of the first: the launch that joins two window parts has more than 2^32 threads (249 GB in all)."""
+    rows, hq, hkv, hd, win = 1 << 20, 264, 33, 64, 300
+    assert P.spec_k_attention8_plan(rows, hq, hkv, hd, 0, win)[2:] == (0, 2)
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 6 * rows * hq * hd + P.spec_k_attention8_scratch_bytes(rows, hq, hkv, hd, 0, win) + (4 << 30):
+        pytest.skip("not enough free memory")
+    base, k, v = inputs(64, hq, hkv, hd, 0, win, 3)
+    q = torch.empty(rows, hq * hd, device="cuda")
+    q.view(-1, 64, hq * hd).copy_(base)
+    out = P.spec_k_attention8(q, None, 0, k, v, win - 1, torch.zeros(rows, dtype=torch.int32, device="cuda"), None, hq, hkv, hd, max_depth=0)
+    for at in range(0, rows, 1 << 17):
+        assert bool((out[at:at + (1 << 17)].view(-1, 64, hq * hd) == out[:64]).all())
+    assert torch.equal(out[-64:], out[:64])
+    h = hkv - 1
+    want, tol = attention_bound(base.view(64, hkv, -1)[:3, h], k[:, h * hd:], v[:, h * hd:], 0, win - 1, np.zeros(3, np.int32), None, hq // hkv, 1, hd)
+    assert (np.abs(f64(out[-64:].view(64, hkv, -1)[:3, h]) - want) <= tol).all()
+    del q, out
+    torch.cuda.empty_cache()
+
+
 def test_attention8_binding_refusals(P):
     hq, hkv, hd = 4, 2, 64
     q, k, v = inputs(3, hq, hkv, hd, 1, 4, 1)
