@@ -109,8 +109,8 @@ int spec_k_attention8_plan(int32_t rows, int32_t hq, int32_t hkv, int32_t hd, in
  * the interleaved one, j < rot/2, turns by the angle t = pos * freq[j]:
  *     (a, b) -> mscale * (a cos t - b sin t,  b cos t + a sin t);
  * dims rot .. hd-1 pass unchanged.  adjoint != 0 turns by -t: the transpose, which
- * takes the gradient of the output to that of the input.  Angles are formed in 64
- * bits, so that far positions keep their phase; the turning is fp32.
+ * takes the gradient of the output to that of the input.  Angles, cosines and sines, mscale
+ * in them, are formed in 64 bits, so that far positions keep their phase, and rounded once; the turning is fp32.
  *
  * The frequencies are theta^(-2j/rot), changed for contexts beyond the trained
  * length as the plan says (host only, once; a plan is plain data and may be copied):

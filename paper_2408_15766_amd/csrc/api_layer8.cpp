@@ -168,7 +168,7 @@ int spec_k_rotary(const spec_rotary_plan *plan, int32_t n_parts, const spec_rota
     a.part[n] = RotaryPart{p.x, p.out, p.ldx, p.hsx, p.ldo, p.hso, p.heads, p.dtype, p.out_dtype, p.turn != 0};
   }
   a.n_parts = n_parts; a.hd = hd; a.rows = rows; a.rot = plan->rot; a.interleaved = plan->layout == SPEC_ROPE_INTERLEAVED;
-  a.adjoint = adjoint != 0; a.pos = pos; a.pos0 = pos0; a.mscale = (float)plan->mscale;
+  a.adjoint = adjoint != 0; a.pos = pos; a.pos0 = pos0; a.mscale = plan->mscale;
   for (int j = 0; j < plan->rot / 2; j++) a.turns[j] = plan->freq[j] / 6.283185307179586476925286766559;
   return done(launch_rotary(a, (hipStream_t)stream));
 }

@@ -328,7 +328,7 @@ struct RotaryArgs {
   RotaryPart part[3];
   int n_parts, hd, rows, rot, interleaved, adjoint, pos0;
   const int *pos;
-  float mscale;
+  double mscale;
   double turns[kRotaryMaxPlanes];       // of a plane per position
   int rows_each;                        // set by launch_rotary: rows of a workgroup, ..
   uint2 row_items[3], head_items[3];    // .. and the divisors of its steps

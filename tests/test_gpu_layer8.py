@@ -719,6 +719,25 @@ def test_rotary_binding_refusals(P):
             call()
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("hd,rot", [(128, 128), (90, 66)])
+@pytest.mark.parametrize("kw", [dict(), dict(scaling="yarn", factor=16.0, trained_len=4096), dict(scaling="yarn", factor=5.3, trained_len=300)])
+def test_rotary_sines_and_cosines_are_rounded_once(P, layout, hd, rot, kw):
+    """Planes (1, 0) and (0, 1) become mscale (cos t, sin t) and mscale (-sin t, cos t) as they are held: half a step of fp32 off (and 4 roundings of 64 bits of angles up to 5000, and
+    the series' 4e-13 mscale)."""
+    plan = P.spec_rotary_plan(rot, 1e4, layout=layout, **kw)
+    pos = np.concatenate([np.arange(0, 200), np.random.default_rng(1).integers(-5000, 5000, 300)])
+    t = pos[:, None].astype(np.float64) * np.array(plan.freq[:rot // 2])
+    first, second = (slice(0, rot // 2), slice(rot // 2, rot)) if layout == "half" else (slice(0, rot, 2), slice(1, rot, 2))
+    x = torch.zeros(len(pos), 2, hd)
+    x[:, 0, first], x[:, 1, second] = 1.0, 1.0
+    for adjoint in (False, True):
+        y = f64(P.spec_k_rotary(plan, [x.cuda()], torch.from_numpy(pos.astype(np.int32)).cuda(), adjoint=adjoint)[0])
+        c, s = plan.mscale * np.cos(t), plan.mscale * np.sin(t) * (-1 if adjoint else 1)
+        for got, want in ((y[:, 0, first], c), (y[:, 0, second], s), (y[:, 1, first], -s), (y[:, 1, second], c)):
+            assert (np.abs(got - want) <= U32 * np.abs(want) + plan.mscale * (4 * 5000 * 2.0 ** -53 + 5e-13)).all()
+
+
 def test_rotary_of_most_rows(P):
     """2^24 rows, each more than a workgroup's steps, in place: as the same rows by themselves."""
     rows, heads, hd = 1 << 24, 3, 96
