@@ -18,7 +18,7 @@
  * is held as code(x / 2^e), rounded to nearest, ties to even, and stands for
  * code * 2^e.  The division is exact, so that a value is rounded once: by at most
  * 2^-4 of itself, or 2^(e - 10) if that is more.  Infinities and NaN are held as
- * NaN.  (A power of two as the scale: the matrix instructions and the conversions
+ * NaN; magnitudes from 1.9375 * 2^127 on stand for 2^128, which is read as an infinity.  (A power of two as the scale: the matrix instructions and the conversions
  * apply it for nothing.)
  */
 #ifndef SPEC_LAYER8_H_
@@ -50,7 +50,8 @@ extern "C" {
  * and lets go of what is under 2^-14 of its largest product (measured: 1.4e-5 of
  * a sum of normally distributed values, a hundredth of the result's rounding);
  * its results are added up in fp32.  A non-finite x makes its row of y NaN, a non-finite weight its
- * column.  The order of a sum may change with m. */
+ * column.  The order of a sum may change with m, so that a row's last bits may
+ * change with the rows beside it. */
 uint64_t spec_packed8_bytes(int32_t rows, int32_t in);
 int spec_pack_weight8(int32_t dtype, const void *src, int32_t rows, int32_t in, void *dst, void *stream);
 uint64_t spec_k_gemm8_scratch_bytes(int32_t m, int32_t in, int32_t rows);
@@ -67,7 +68,7 @@ int spec_k_gemm8(int32_t dtype, const void *x, int32_t ldx, int32_t m, int32_t i
  *                      other: a cache may be copied, cut or joined at multiples of spec_kv8_bytes(1, ..).
  *   spec_k_kv8_store : rows k, v [n_blocks * SPEC_KV8_BLOCK, hkv*hd] bf16, row stride ld
  *                      -> blocks first_block .. of cache8 (256-byte aligned).
- *   spec_k_kv8_load  : the same back: what the codes stand for, which bf16 holds exactly.
+ *   spec_k_kv8_load  : the same back: what the codes stand for, which bf16 holds exactly (but 2^128).
  * hd 64 or 128, 1 <= hkv <= 128, ld >= hkv*hd.  The caller sees to it that cache8 holds
  * first_block + n_blocks blocks.  n_blocks = 0 does nothing. */
 #define SPEC_KV8_BLOCK 64
@@ -92,7 +93,8 @@ int spec_k_kv8_load(const void *cache8, int32_t first_block, int32_t n_blocks, i
  * weight times the largest 2^e it is at most 2^-10 off, centred; smaller ones are cut to multiples of 2^-36 of that.  In
  * the window both go in two bf16 terms (2^-16).
  * Sums are weighted by up to 2^45 before the division: values beyond 2^80 may end as infinities.
- * The result of a row may change in its last bits with the rows beside it. */
+ * The result of a row may change in its last bits with the rows beside it (another kernel, other ranges): unlike spec_k_attention's, a row verified in a tree need not
+ * have the bits of the row decoded alone, and a greedy choice between logits that close may differ. */
 uint64_t spec_k_attention8_scratch_bytes(int32_t rows, int32_t hq, int32_t hkv, int32_t hd, int32_t n_blocks, int32_t win_rows);
 int spec_k_attention8(const float *q, const void *cache8, int32_t n_blocks, const void *kwin, const void *vwin, int32_t win_rows, int32_t rows,
                       int32_t hq, int32_t hkv, int32_t hd, int32_t base, const int32_t *depth, const int32_t *anc, int32_t max_depth,

@@ -544,7 +544,9 @@ __device__ __forceinline__ bool place_of(const Plan8 &p, int hkv, Place8 &at) {
 // Tried, with the same time: two teams of four wavefronts that take turns at the matrix instructions and at the weights, a barrier between; the next block's scores among the
 // instructions of this one's weights; slower: four wavefronts of 64 queries, scores of the
 // next tile beside the weights of this one (2.4: the sums of 64 queries lie in the accumulation registers, and every read of one is an instruction).
-// Registers: two wavefronts may take 512 each (60 queries on 32 kv heads, 512 keys: 14.4 us against 15.2 with 256), four do better with 256 (104 on 8, 4096 keys: 21.7 against 22.9).
+// Registers: two wavefronts may take 512 each (us, and with 256, of which 85 would lie in memory: 300 queries on 4 kv heads behind 20 blocks 25.4, 32.1, 64 on 32 of 64 behind 256 blocks 30.2, 32.2,
+// 60 on 32 behind 64 blocks 24.5, 23.6, but 104 on 8 behind 64 blocks 20.6, 18.3). Four do better with 256, of which 11 of heads of 128 lie in memory (480 queries on 2 behind 300 blocks 29.9, with 512 34.0; 240 on 8
+// behind 128 blocks 29.1, 33.9; 60 on 32 behind 8 blocks 14.3, 15.7).
 template <int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 2 ? 1 : 2) void attention8_wide_kernel(Attn8Args a, Plan8 plan) {
   constexpr int kCodes = 2 * kKv8Block * HD, kUnits = kCodes / 16, kThreads = WAVES * 64, kEach = kUnits / kThreads;   // of 16 codes, per thread
@@ -761,8 +763,8 @@ Plan8 plan8(int rows, int hq, int hkv, int n_blocks, int win_rows) {
   Plan8 p{};
   const int G = hq / hkv;
   const int64_t queries = (int64_t)rows * G;
-  // Wavefronts by the work, in tiles of 32 queries over 64 keys: eight, which share the widening, where there is much of it; two, for more workgroups with fewer parts, where there is little or
-  // 64 queries are all; else four, of which those without queries only load and widen.  us with 2, 4, 8: 60 queries on 32 kv heads, 8 blocks 16.0, 14.2, 15.5, 128 blocks 32, 35, 35;
+  // Wavefronts by the work, in tiles of 32 queries over 64 keys.  Up to 64 queries: four, of which those without queries only load and widen, where there is little work, two, for more workgroups, where
+  // there is much.  More queries: eight, which share the widening, where there is much work, two where there is little in few tiles, else four.  us with 2, 4, 8: 60 queries on 32 kv heads, 8 blocks 16.0, 14.2, 15.5, 128 blocks 32, 35, 35;
   // 240 on 8, 8 blocks 15.2, 17.0, 19.2, 128 blocks 30, 26, 34, 512 blocks 74, 58, 54; 1200 on 8, 8 blocks 31, 27, 30, 128 blocks 221, 160, 67.
   const int64_t tiles = (queries + 31) / 32, wide = hkv * tiles, work = wide * (n_blocks + win_rows / 32);
   p.waves = queries <= 32 ? 0 : tiles <= 2 ? (work <= 4096 ? 4 : 2) : work >= (wide >= 96 ? 6144 : 20480) ? 8 : wide <= 64 && work <= 2304 ? 2 : 4;

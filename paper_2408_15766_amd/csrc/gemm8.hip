@@ -527,7 +527,8 @@ hipError_t launch_tile(const Gemm8Args &a, hipStream_t st) {
 }
 
 // The tile that a launch takes: the one whose workgroups, in rounds over the 256 compute units, are done first.  Measured (us for K = 4096, bf16 results; fp32 results take
-// 1.4 to 1.9 times that for all of them): a round of one workgroup a unit, and a unit's time for each when there are more.
+// 1.4 to 1.9 times that for all of them): a round of one workgroup a unit, and a unit's time for each when there are more.  The table serves every K and both types: it compares shapes whose
+// times grow alike with K; at other K it is not measured.
 //   256 x 256: 56, one fits a unit (512 x 28672: 60 against 75 in 256 x 128)        256 x 128: 36, one (2048 x 4096: 36 against 50 in 256 x 256 and 42 in 128 x 128)
 //   128 x 128: 24, or two in 41 (1024 x 4096: 24 against 33 in 256 x 128)           64 x 128: 16, or two in 30 (333 x 4096: 16 against 20 in 128 x 128)
 //   64 x 64, eight stages deep: 11, or two in 17.5 (60 x 12288: 15 against 20 in 64 x 128)
@@ -596,7 +597,7 @@ hipError_t launch_typed(Gemm8Args a, void *scratch, hipStream_t st) {
   a.row_begin = 0; a.row_end = a.rows;
   const Tiles8 all = best_tiles(a.m, a.rows);
   // whole rounds of the largest tile, and the rows that are left in what suits them: 2048 x 28672 x 4096 (3.5 rounds) 217 -> 205 us, 2048 x
-  // 12288 x 4096 (1.5) 105 -> 94; 2048 x 22016 x 4096 (2.7) would take 177 instead of 164
+  // 12288 x 4096 (1.5) 105 -> 94; 2048 x 22016 x 4096 (2.7) would take 177 instead of 164.  (The 3 us of another launch are against the costs of K = 4096.)
   const int64_t tok = (a.m + 255) / 256, in_rounds = tok * ((a.rows + 255) / 256) / 256 * 256 / tok * 256;
   if (in_rounds > 0 && in_rounds < a.rows) {
     const Tiles8 rest = best_tiles(a.m, a.rows - (int)in_rounds);
