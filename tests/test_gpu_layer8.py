@@ -829,6 +829,32 @@ def test_layer_prompt_then_trees(P):
         committed += len(path)
 
 
+def test_layer_example_of_the_readme_runs(P):
+    """Its code as it stands, twice: the rows of the path are in the window, and then in a block."""
+    import pathlib
+    import re
+    readme = (pathlib.Path(__file__).resolve().parent.parent / "README.md").read_text()
+    code, = [c for c in re.findall(r"```python\n(.*?)```", readme, re.S) if "spec_k_attention8" in c]
+    hq, hkv, hd, d, rows, recent = 8, 2, 128, 256, 10, 62
+    depth, anc = tree(rows, 2)
+    path = torch.from_numpy(anc[int(np.argmax(depth))][:depth.max() + 1].astype(np.int64)).cuda()
+    w = {"qkv": P.spec_pack_weight8(rand(1, (hq + 2 * hkv) * hd, d, scale=0.05).bfloat16().cuda()), "o": P.spec_pack_weight8(rand(2, d, hq * hd, scale=0.05).bfloat16().cuda())}
+    kwin, vwin = (rand(i, 128, hkv * hd).bfloat16().cuda() for i in (3, 4))
+    env = dict(torch=torch, P=P, hq=hq, hkv=hkv, hd=hd, max_tokens=640, rows=rows, w=w, x=rand(5, rows, d).bfloat16().cuda(), kwin=kwin, vwin=vwin, blocks=0, recent=recent, path=path,
+               depth=torch.from_numpy(depth).cuda(), anc=torch.from_numpy(anc).cuda(), deepest=int(depth.max()), pos=torch.from_numpy((recent + depth).astype(np.int32)).cuda())
+    exec(code, env)
+    n = recent + len(path)
+    assert env["y"].shape == (rows, d) and env["y"].isfinite().all()
+    kept, at = (n - 64, 64) if n >= 64 else (n, 0)
+    assert (env["blocks"], env["recent"]) == (int(n >= 64), kept)
+    turned = P.spec_k_rotary(env["plan"], [env["k"]], env["pos"], out_dtypes=[torch.bfloat16])[0].view(rows, -1)
+    assert n >= 64 and torch.equal(kwin[:kept], turned[path][at - recent:]) and torch.equal(vwin[:kept], env["v"].reshape(rows, -1).bfloat16()[path][at - recent:])
+    block = P.spec_k_kv8_load(env["cache"], 0, 1, hkv, hd)[1]
+    first = torch.cat([rand(4, 128, hkv * hd).bfloat16()[:recent].cuda(), env["v"].reshape(rows, -1).bfloat16()[path]])[:64]
+    assert np.array_equal(f64(block), O.held_kv(f64(first), hkv, hd))
+    exec(code.split("# once per layer")[1].split("\n", 1)[1], {**env, "pos": env["pos"] + len(path)})
+
+
 def test_layer_on_a_stream_and_captured(P):
     """The same calls on a stream of their own, and captured and replayed with other work between: the bits of the eager calls."""
     hq, hkv, hd, d, rows, blocks, recent = 8, 2, 128, 512, 26, 5, 9
