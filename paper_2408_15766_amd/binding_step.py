@@ -1,0 +1,269 @@
+"""ctypes binding of the operators of a training step (spec_step.h): same names as the C ABI, argument marshalling only.
+
+As in binding.py: torch is used for device memory and for the current HIP stream, every tensor has to be on the current device, what
+a call does not support is refused with SpecError before anything is launched.  The functions compute gradients when they are asked to and register nothing
+with autograd.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import struct
+from typing import Optional, Sequence
+
+from .binding import SPEC_EINVAL, SPEC_ROPE_MAX_DIM, SpecError, _INT_MAX, _dtype_code, _fit, _here, _new, _refuse, lib, spec_rotary_plan_t
+
+SPEC_GRAD_SUMS = 1024
+
+lib.spec_k_embed.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+lib.spec_k_embed_grad_scratch_bytes.restype = C.c_uint64
+lib.spec_k_embed_grad_scratch_bytes.argtypes = [C.c_int32] * 3
+lib.spec_k_embed_grad.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_int32, C.c_int32, C.c_void_p,
+                                  C.c_int64, C.c_void_p, C.c_uint64, C.c_void_p]
+lib.spec_k_headnorm_rotary.argtypes = [C.POINTER(spec_rotary_plan_t), C.c_int32, C.c_char_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_void_p]
+lib.spec_k_headnorm_rotary_grad_scratch_bytes.restype = C.c_uint64
+lib.spec_k_headnorm_rotary_grad_scratch_bytes.argtypes = [C.c_int32] * 2
+lib.spec_k_headnorm_rotary_grad.argtypes = [C.POINTER(spec_rotary_plan_t), C.c_int32, C.c_char_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_float,
+                                            C.c_void_p, C.c_uint64, C.c_void_p]
+lib.spec_k_grad_sums.argtypes = [C.c_int32, C.c_char_p, C.c_void_p, C.c_void_p]
+lib.spec_k_grad_clip.argtypes = [C.c_int32, C.c_char_p, C.c_void_p, C.c_double, C.c_void_p, C.c_void_p]
+
+
+def _room(what: str, scratch, n: int, beside):
+    """(the scratch tensor, its bytes): the caller's, or a new one of n bytes."""
+    import torch
+    if scratch is None:
+        return (_new((n,), (1,), torch.uint8, beside) if n else None), n
+    if not scratch.is_contiguous():
+        _refuse(what, "scratch has to be contiguous")
+    return scratch, scratch.numel() * scratch.element_size()
+
+
+def _matrix(what: str, name: str, t, rows: Optional[int] = None, cols: Optional[int] = None) -> int:
+    """The row stride of a matrix with dense rows."""
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols) or (t.shape[1] > 1 and t.stride(1) != 1):
+        _refuse(what, f"{name} has to be [{'rows' if rows is None else rows}, {'columns' if cols is None else cols}] with dense rows")
+    if t.shape[0] > _INT_MAX or t.shape[1] > _INT_MAX:
+        _refuse(what, f"{name} is {tuple(t.shape)}")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _tokens(what: str, tok):
+    import torch
+    if tok.dtype is not torch.int32 or tok.dim() != 1 or not tok.is_contiguous() or tok.shape[0] > _INT_MAX:
+        _refuse(what, "tok has to be int32 [rows]")
+    return tok.shape[0]
+
+
+# ---- embedding ----------------------------------------------------------------------------------
+
+def spec_k_embed(table, tok, scale: float = 1.0, out_dtype=None, out=None):
+    """table: [vocab, d] (bf16 or fp32, rows may be strided), tok: int32 [rows] -> scale * table[tok] in out_dtype (default: the table's), zeros for
+    tokens outside the table (padding).  out: optional [rows, d] tensor (rows may be strided)."""
+    what = "spec_k_embed"
+    stream = _here(what, table, tok, out)
+    ldt, rows = _matrix(what, "table", table), _tokens(what, tok)
+    vocab, d = table.shape
+    if out is None:
+        out = _new((rows, d), (d, 1), table.dtype if out_dtype is None else out_dtype, table)
+    elif out_dtype is not None and out_dtype is not out.dtype:
+        _refuse(what, "out has to be of out_dtype")
+    ldo = _matrix(what, "out", out, rows, d)
+    rc = lib.spec_k_embed(_dtype_code(what, table.dtype), table.data_ptr(), ldt, vocab, d, tok.data_ptr(), rows, scale, _dtype_code(what, out.dtype), out.data_ptr(),
+                          ldo, stream)
+    if rc:
+        raise SpecError(rc, f"{what}: {rows} rows of a {vocab} x {d} table")
+    return out
+
+
+def spec_k_embed_grad_scratch_bytes(rows: int, vocab: int, d: int) -> int:
+    return int(lib.spec_k_embed_grad_scratch_bytes(rows, vocab, d)) if _fit(rows, vocab, d) else 0
+
+
+def spec_k_embed_grad(dy, tok, vocab: int, scale: float = 1.0, out_dtype=None, out=None, accumulate: bool = False, scratch=None):
+    """The gradient of spec_k_embed's table: dy [rows, d] (bf16 or fp32, rows may be strided), tok int32 [rows] -> [vocab, d] in out_dtype (default:
+    dy's).  out: optional tensor for it (rows may be strided); accumulate: the gradient is added to out's values, and rows without a token stay untouched.
+    scratch: optional uint8 tensor of spec_k_embed_grad_scratch_bytes(rows, vocab, d)."""
+    import torch
+    what = "spec_k_embed_grad"
+    stream = _here(what, dy, tok, out, scratch)
+    rows = _tokens(what, tok)
+    ldy = _matrix(what, "dy", dy, rows)
+    d = dy.shape[1]
+    if out is None:
+        if accumulate:
+            _refuse(what, "accumulate needs an out")
+        if not 1 <= vocab <= _INT_MAX:
+            _refuse(what, f"a vocabulary of {vocab}")
+        out = _new((vocab, d), (d, 1), dy.dtype if out_dtype is None else out_dtype, dy)
+    elif out_dtype is not None and out_dtype is not out.dtype:
+        _refuse(what, "out has to be of out_dtype")
+    ldt = _matrix(what, "out", out, vocab, d)
+    scratch, room = _room(what, scratch, lib.spec_k_embed_grad_scratch_bytes(rows, vocab, d), dy)
+    rc = lib.spec_k_embed_grad(_dtype_code(what, dy.dtype), dy.data_ptr(), ldy, tok.data_ptr(), rows, d, vocab, scale, bool(accumulate), _dtype_code(what, out.dtype),
+                               out.data_ptr(), ldt, None if scratch is None else scratch.data_ptr(), room, stream)
+    if rc:
+        raise SpecError(rc, f"{what}: {rows} rows, a {vocab} x {d} table, {room} bytes of scratch")
+    return out
+
+
+# ---- norms of heads, with the rotary embedding -----------------------------------------------------
+
+_part = "QQqqqqiiii"
+_norm_parts = [struct.Struct("@" + (_part + "Qif") * n).pack for n in range(4)]          # spec_headnorm_part, as often as there are tensors
+_norm_grad_parts = [struct.Struct("@" + (_part + "QifQqqQii") * n).pack for n in range(4)]
+
+
+def _heads(what: str, name: str, t, shape):
+    """Row and head strides of a tensor of heads."""
+    if tuple(t.shape) != tuple(shape) or (shape[2] > 1 and t.stride(2) != 1):
+        _refuse(what, f"{name} has to be {tuple(shape)} with dense heads")
+    return t.stride(0), t.stride(1)
+
+
+def _positions(what: str, pos, rows: int):
+    """(pointer, first position) of the rows' positions."""
+    import torch
+    if isinstance(pos, torch.Tensor):
+        if pos.dtype is not torch.int32 or pos.dim() != 1 or pos.shape[0] != rows or not pos.is_contiguous():
+            _refuse(what, f"pos has to be int32 [{rows}]")
+        return pos.data_ptr(), 0
+    if not -_INT_MAX - 1 <= int(pos) <= _INT_MAX:
+        _refuse(what, f"position {pos}")
+    return None, int(pos)
+
+
+def _part_shape(what: str, t, rows: int, hd: int):
+    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != hd or not 1 <= t.shape[1] <= 1024 or rows > _INT_MAX or hd > SPEC_ROPE_MAX_DIM:
+        _refuse(what, f"tensors have to be [{rows}, up to 1024 heads, {hd}]")
+    return t.shape
+
+
+def _weight(what: str, w, hd: int):
+    if w is None:
+        return 0, 0
+    if w.dim() != 1 or w.shape[0] != hd or not w.is_contiguous():
+        _refuse(what, f"weights have to be [{hd}]")
+    return w.data_ptr(), _dtype_code(what, w.dtype)
+
+
+def spec_k_headnorm_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, weights: Sequence, eps: float = 1e-6, offset: float = 0.0, turned: Optional[Sequence[bool]] = None,
+                           out_dtypes: Optional[Sequence] = None, outs=None):
+    """spec_k_rotary (xs, pos, turned, out_dtypes, outs as there) with a norm of every head before it: x / sqrt(mean x^2 + eps) * (offset + weights[i]), weights[i]
+    a [hd] tensor, or None: that tensor is not normed."""
+    import torch
+    what = "spec_k_headnorm_rotary"
+    n = len(xs)
+    if not 1 <= n <= 3 or xs[0].dim() != 3:
+        _refuse(what, "one to three tensors [rows, heads, hd] are needed")
+    if outs is None:
+        kinds = [x.dtype for x in xs] if out_dtypes is None else out_dtypes
+        outs = [torch.empty_like(x, dtype=d, memory_format=torch.contiguous_format) for x, d in zip(xs, kinds)]
+    if len(outs) != n or len(weights) != n or (turned is not None and len(turned) != n):
+        _refuse(what, "as many outputs, weights and flags as tensors are needed")
+    stream = _here(what, *xs, *outs, *weights, pos if isinstance(pos, torch.Tensor) else None)
+    rows, _, hd = xs[0].shape
+    at, first = _positions(what, pos, rows)
+    fields = []
+    for x, o, w, turn in zip(xs, outs, weights, (True,) * n if turned is None else turned):
+        shape = _part_shape(what, x, rows, hd)
+        wp, wd = _weight(what, w, hd)
+        fields += (x.data_ptr(), o.data_ptr(), *_heads(what, "x", x, shape), *_heads(what, "an output", o, shape), shape[1], _dtype_code(what, x.dtype),
+                   _dtype_code(what, o.dtype), bool(turn), wp, wd, offset)
+    rc = lib.spec_k_headnorm_rotary(C.byref(plan), n, _norm_parts[n](*fields), hd, rows, at, first, eps, stream)
+    if rc:
+        raise SpecError(rc, f"{what}: {rows} rows, heads of {hd}, plan over {plan.rot}, eps {eps}")
+    return list(outs)
+
+
+def spec_k_headnorm_rotary_grad_scratch_bytes(n_parts: int, hd: int) -> int:
+    return int(lib.spec_k_headnorm_rotary_grad_scratch_bytes(n_parts, hd)) if _fit(n_parts, hd) else 0
+
+
+def spec_k_headnorm_rotary_grad(plan: spec_rotary_plan_t, dys: Sequence, xs: Sequence, pos, weights: Sequence, eps: float = 1e-6, offset: float = 0.0,
+                                turned: Optional[Sequence[bool]] = None, out_dtypes: Optional[Sequence] = None, outs=None, scratch=None):
+    """The gradients of spec_k_headnorm_rotary: dys, those of its outputs, and its inputs xs (None where weights[i] is None) -> (gradients of xs, in
+    out_dtypes (default: each dy's) or `outs` (an entry may be the dy itself), gradients of weights: fp32 [hd] each, None where weights[i] is None).
+    scratch: optional uint8 tensor of spec_k_headnorm_rotary_grad_scratch_bytes(len(dys), hd)."""
+    import torch
+    what = "spec_k_headnorm_rotary_grad"
+    n = len(dys)
+    if not 1 <= n <= 3 or dys[0].dim() != 3:
+        _refuse(what, "one to three tensors [rows, heads, hd] are needed")
+    if outs is None:
+        kinds = [t.dtype for t in dys] if out_dtypes is None else out_dtypes
+        outs = [torch.empty_like(t, dtype=d, memory_format=torch.contiguous_format) for t, d in zip(dys, kinds)]
+    if len(outs) != n or len(xs) != n or len(weights) != n or (turned is not None and len(turned) != n):
+        _refuse(what, "as many inputs, outputs, weights and flags as gradients are needed")
+    stream = _here(what, *dys, *outs, *xs, *weights, scratch, pos if isinstance(pos, torch.Tensor) else None)
+    rows, _, hd = dys[0].shape
+    if hd > SPEC_ROPE_MAX_DIM:
+        _refuse(what, f"heads of {hd}")
+    at, first = _positions(what, pos, rows)
+    dws, fields = [], []
+    for dy, x, o, w, turn in zip(dys, xs, outs, weights, (True,) * n if turned is None else turned):
+        shape = _part_shape(what, dy, rows, hd)
+        wp, wd = _weight(what, w, hd)
+        dw = None if w is None else _new((hd,), (1,), torch.float32, dy)
+        dws.append(dw)
+        if w is not None and x is None:
+            _refuse(what, "the input of a normed tensor is needed")
+        given = (0, 0, 0) if w is None else (x.data_ptr(), *_heads(what, "x", x, shape))
+        fields += (dy.data_ptr(), o.data_ptr(), *_heads(what, "dy", dy, shape), *_heads(what, "an output", o, shape), shape[1], _dtype_code(what, dy.dtype),
+                   _dtype_code(what, o.dtype), bool(turn), wp, wd, offset, *given, 0 if dw is None else dw.data_ptr(), 0 if w is None else _dtype_code(what, x.dtype), 0)
+    need = lib.spec_k_headnorm_rotary_grad_scratch_bytes(n, hd) if any(w is not None for w in weights) else 0
+    scratch, room = _room(what, scratch, need, dys[0])
+    rc = lib.spec_k_headnorm_rotary_grad(C.byref(plan), n, _norm_grad_parts[n](*fields), hd, rows, at, first, eps, None if scratch is None else scratch.data_ptr(), room,
+                                         stream)
+    if rc:
+        raise SpecError(rc, f"{what}: {rows} rows, heads of {hd}, plan over {plan.rot}, eps {eps}, {room} bytes of scratch")
+    return list(outs), dws
+
+
+# ---- gradient clipping ------------------------------------------------------------------------------
+
+_grad_part = struct.Struct("@QQqii")
+
+
+def _grad_fields(what: str, grads, outs):
+    packed = bytearray(_grad_part.size * len(grads))
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        if not g.is_contiguous() or not o.is_contiguous() or g.shape != o.shape:
+            _refuse(what, "gradients and outputs have to be contiguous, of the same shapes")
+        _grad_part.pack_into(packed, i * _grad_part.size, g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(what, g.dtype), _dtype_code(what, o.dtype))
+    return bytes(packed)
+
+
+def spec_k_grad_sums(grads: Sequence, sums=None):
+    """The squares of all elements of the tensors (bf16 or fp32, contiguous), summed up: a float64 tensor [SPEC_GRAD_SUMS] whose sum is the square of their norm (processes
+    that each hold a part of the gradients all-reduce it).  sums: optional tensor for it."""
+    import torch
+    what = "spec_k_grad_sums"
+    if not grads and sums is None:
+        _refuse(what, "tensors or sums are needed")
+    beside = grads[0] if grads else sums
+    if sums is None:
+        sums = _new((SPEC_GRAD_SUMS,), (1,), torch.float64, beside)
+    elif sums.dtype is not torch.float64 or tuple(sums.shape) != (SPEC_GRAD_SUMS,) or not sums.is_contiguous():
+        _refuse(what, f"sums has to be float64 [{SPEC_GRAD_SUMS}]")
+    stream = _here(what, *grads, sums)
+    rc = lib.spec_k_grad_sums(len(grads), _grad_fields(what, grads, grads), sums.data_ptr(), stream)
+    if rc:
+        raise SpecError(rc, f"{what}: {len(grads)} tensors")
+    return sums
+
+
+def spec_k_grad_clip(grads: Sequence, sums, max_norm: float, outs: Optional[Sequence] = None):
+    """The tensors times min(1, max_norm / (norm + 1e-6)), norm^2 the sum of `sums` (spec_k_grad_sums): in place, or into `outs` (same shapes, bf16 or fp32).  Returns the
+    norm before that, a float32 tensor [] on the device; nothing waits for it."""
+    import torch
+    what = "spec_k_grad_clip"
+    if sums.dtype is not torch.float64 or tuple(sums.shape) != (SPEC_GRAD_SUMS,) or not sums.is_contiguous():
+        _refuse(what, f"sums has to be float64 [{SPEC_GRAD_SUMS}]")
+    if outs is not None and len(outs) != len(grads):
+        _refuse(what, "as many outputs as gradients are needed")
+    stream = _here(what, sums, *grads, *(() if outs is None else outs))
+    norm = _new((), (), torch.float32, sums)
+    rc = lib.spec_k_grad_clip(len(grads), _grad_fields(what, grads, grads if outs is None else outs), sums.data_ptr(), max_norm, norm.data_ptr(), stream)
+    if rc:
+        raise SpecError(rc, f"{what}: {len(grads)} tensors, max_norm {max_norm} (outputs may overlap nothing but their own gradient, in place)")
+    return norm

@@ -1,0 +1,268 @@
+// Rows of an embedding table, and the gradient of the table (include/spec_step.h).
+//
+// The gradient sums rows of dy by token.  The positions are sorted by (token, position), so that a table row's sum is a walk over neighbours and its order is
+// fixed: in tiles of kTile positions a position's place is the number of smaller ones (counted, kTile comparisons for each), and over several tiles
+// its place in its own plus those that binary searches find in the others.  Padding sorts behind the vocabulary and is never read.
+// Tokens that occur often (padding apart, the most frequent word is a tenth of a text) would keep one workgroup busy long after the others: aligned runs of 32
+// and of 1024 sorted positions that hold one token are summed first, by workgroups of their own, and the walk takes a run's sum where it meets one.
+// Bound: memory (dy once in, the table once out).
+#include "common.h"
+#include "elements.h"
+#include "kernels.h"
+
+namespace spec {
+
+namespace {
+
+constexpr int kTile = 4096, kRun = 32, kRuns = 1024;          // positions of a tile and of the two lengths of runs
+constexpr int kEmbedThreads = 256;
+
+// Eight columns of a row at a time (VEC), or one.  A thread's columns do not change from row to row.
+template <bool VEC>
+__global__ __launch_bounds__(kEmbedThreads) void embed_kernel(const void *table, int64_t ldt, int vocab, int d, const int *tok, int rows, float scale, int dtype,
+                                                              int out_dtype, void *out, int64_t ldo) {
+  constexpr int W = VEC ? 8 : 1;
+  const int cols = (d + W - 1) / W, per = cols < kEmbedThreads ? kEmbedThreads / cols : 1;   // rows that the workgroup's threads share out
+  const int mine = cols < kEmbedThreads ? threadIdx.x / cols : 0, c0 = cols < kEmbedThreads ? threadIdx.x % cols : threadIdx.x;
+  if (mine >= per) return;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * per + mine;
+  if (row >= rows) return;
+  const int t = tok[row];
+  const bool real = t >= 0 && t < vocab;
+  for (int c = c0; c < cols; c += kEmbedThreads) {
+    if constexpr (VEC) {
+      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (real) {
+        widen8(load8(table, t * ldt + c * 8, dtype), dtype, x);
+#pragma unroll
+        for (int j = 0; j < 8; j++) x[j] *= scale;
+      }
+      store8(out, row * ldo + c * 8, out_dtype, x);
+    } else {
+      store1(out, row * ldo + c, out_dtype, real ? scale * load1(table, t * ldt + c, dtype) : 0.f);
+    }
+  }
+}
+
+// ---- sorting ------------------------------------------------------------------------------------
+
+constexpr int kRankThreads = 1024, kRankMine = 64;            // a workgroup places 64 positions; each of its 16 wavefronts counts in a sixteenth of the tile
+// The key of a position: its token, padding behind all tokens
+__device__ __forceinline__ int key_of(int t, int vocab) { return t >= 0 && t < vocab ? t : vocab; }
+
+__global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(const int *tok, int rows, int vocab, int *keys, int *order) {
+  __shared__ __attribute__((aligned(16))) int sh[kTile];
+  __shared__ int count[kRankThreads];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = blockIdx.x * kRankMine, tile = first / kTile * kTile, n = min(rows - tile, kTile);
+  for (int i = threadIdx.x; i < kTile; i += kRankThreads) sh[i] = i < n ? key_of(tok[tile + i], vocab) : 0x7FFFFFFF;
+  __syncthreads();
+  const int me = first - tile + lane, key = sh[me];
+  constexpr int kEach = kTile / 16;
+  const int j0 = wave * kEach;
+  int smaller = 0;
+  const bool own = j0 <= first - tile && first - tile < j0 + kEach;   // this share holds the workgroup's positions
+  const int below = key + (j0 < first - tile ? 1 : 0);        // equal keys of earlier positions count
+  for (int j = j0; j < j0 + kEach && j < n; j += 4) {         // (what lies behind n is larger than any key)
+    const int4 k = *(const int4 *)(sh + j);
+    if (own) smaller += (k.x < key + (j < me)) + (k.y < key + (j + 1 < me)) + (k.z < key + (j + 2 < me)) + (k.w < key + (j + 3 < me));
+    else smaller += (k.x < below) + (k.y < below) + (k.z < below) + (k.w < below);
+  }
+  count[threadIdx.x] = smaller;
+  __syncthreads();
+  if (wave != 0 || me >= n) return;
+  int place = 0;
+#pragma unroll
+  for (int w = 0; w < 16; w++) place += count[w * 64 + lane];
+  keys[tile + place] = key;
+  order[tile + place] = tile + me;
+}
+
+// Several tiles: the place of each among all
+__global__ __launch_bounds__(kRankThreads) void embed_merge_kernel(const int *tile_keys, const int *tile_order, int rows, int *keys, int *order) {
+  __shared__ int sh[kTile];
+  const int i = blockIdx.x * kRankThreads + threadIdx.x, mine = blockIdx.x * kRankThreads / kTile;
+  const int key = i < rows ? tile_keys[i] : 0;
+  int place = i - mine * kTile;
+  const int tiles = (rows + kTile - 1) / kTile;
+  for (int t = 0; t < tiles; t++) {
+    if (t == mine) continue;
+    const int n = min(rows - t * kTile, kTile);
+    __syncthreads();
+    for (int j = threadIdx.x; j < n; j += kRankThreads) sh[j] = tile_keys[t * kTile + j];
+    __syncthreads();
+    const int below = key + (t < mine ? 1 : 0);               // how many of this tile come before: keys under `below`
+    int lo = 0, hi = n;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (sh[mid] < below) lo = mid + 1; else hi = mid;
+    }
+    place += lo;
+  }
+  if (i < rows) { keys[place] = key; order[place] = tile_order[i]; }
+}
+
+// ---- sums ---------------------------------------------------------------------------------------
+
+template <int W> struct Columns { float x[W]; };
+template <int W> __device__ __forceinline__ void add_columns(Columns<W> &s, const Columns<W> &v) {
+#pragma unroll
+  for (int j = 0; j < W; j++) s.x[j] += v.x[j];
+}
+template <int W> __device__ __forceinline__ Columns<W> row_columns(const void *p, int64_t i, int bf16) {
+  Columns<W> r;
+  if constexpr (W == 8) widen8(load8(p, i, bf16), bf16, r.x);
+  else r.x[0] = load1(p, i, bf16);
+  return r;
+}
+
+// The first sorted position of every token (starts[vocab]: where padding begins), and the runs of 32.
+template <int W>
+__global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(EmbedGradArgs a, const int *keys, const int *order, int *starts, int start_groups, float *runs) {
+  if ((int)blockIdx.x < start_groups) {
+    if (blockIdx.y != 0) return;
+    const int v = blockIdx.x * kEmbedThreads + threadIdx.x;
+    if (v > a.vocab) return;
+    int lo = 0, hi = a.rows;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (keys[mid] < v) lo = mid + 1; else hi = mid;
+    }
+    starts[v] = lo;
+    return;
+  }
+  const int run = blockIdx.x - start_groups;
+  const int key = keys[run * kRun];
+  if (key >= a.vocab || key != keys[run * kRun + kRun - 1]) return;
+  for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * W; c < a.d; c += gridDim.y * kEmbedThreads * W) {
+    Columns<W> s = row_columns<W>(a.dy, order[run * kRun] * a.ldy + c, a.dtype);
+#pragma unroll 8
+    for (int i = 1; i < kRun; i++) add_columns<W>(s, row_columns<W>(a.dy, order[run * kRun + i] * a.ldy + c, a.dtype));
+    if constexpr (W == 8) store8(runs, (int64_t)run * a.d + c, 0, s.x);
+    else runs[(int64_t)run * a.d + c] = s.x[0];
+  }
+}
+
+// The runs of 1024, out of those of 32
+__global__ __launch_bounds__(kEmbedThreads) void embed_long_runs_kernel(const int *keys, int vocab, int d, const float *runs, float *long_runs) {
+  const int run = blockIdx.x, key = keys[run * kRuns];
+  if (key >= vocab || key != keys[run * kRuns + kRuns - 1]) return;
+  for (int c = blockIdx.y * kEmbedThreads + threadIdx.x; c < d; c += gridDim.y * kEmbedThreads) {
+    const float *p = runs + (int64_t)run * (kRuns / kRun) * d + c;
+    float s = p[0];
+#pragma unroll 8
+    for (int i = 1; i < kRuns / kRun; i++) s += p[(int64_t)i * d];
+    long_runs[(int64_t)run * d + c] = s;
+  }
+}
+
+// A few table rows to a workgroup (blockIdx.y: its share of the columns).
+constexpr int kTableRows = 8;
+template <int W>
+__global__ __launch_bounds__(kEmbedThreads) void embed_table_kernel(EmbedGradArgs a, const int *order, const int *starts, const float *runs, const float *long_runs) {
+  const int v0 = blockIdx.x * kTableRows, vn = min(a.vocab - v0, kTableRows);
+  for (int r = 0; r < vn; r++) {
+    const int v = v0 + r, s0 = starts[v], s1 = starts[v + 1];
+    if (a.accumulate && s0 == s1) continue;
+    for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * W; c < a.d; c += gridDim.y * kEmbedThreads * W) {
+      Columns<W> s;
+#pragma unroll
+      for (int j = 0; j < W; j++) s.x[j] = 0.f;
+      int i = s0;
+      auto single = [&](int to) {
+#pragma unroll 4
+        for (; i < to; i++) add_columns<W>(s, row_columns<W>(a.dy, order[i] * a.ldy + c, a.dtype));
+      };
+      auto whole = [&](const float *p, int length, int to) {  // runs, from a multiple of their length on
+#pragma unroll 4
+        for (; i + length <= to; i += length) add_columns<W>(s, row_columns<W>(p, (int64_t)(i / length) * a.d + c, 0));
+      };
+      single(min(s1, (i + kRun - 1) / kRun * kRun));
+      if (i + kRun <= s1) {
+        whole(runs, kRun, min(s1, (i + kRuns - 1) / kRuns * kRuns));
+        whole(long_runs, kRuns, s1);
+        whole(runs, kRun, s1);
+      }
+      single(s1);
+      const int64_t at = v * a.ldt + c;
+#pragma unroll
+      for (int j = 0; j < W; j++) s.x[j] *= a.scale;
+      if (a.accumulate) {
+        const Columns<W> was = row_columns<W>(a.dtable, at, a.out_dtype);
+        add_columns<W>(s, was);
+      }
+      if constexpr (W == 8) store8(a.dtable, at, a.out_dtype, s.x);
+      else store1(a.dtable, at, a.out_dtype, s.x[0]);
+    }
+  }
+}
+
+// What the scratch holds, in order
+struct EmbedScratch { uint64_t keys, order, tile_keys, tile_order, starts, runs, long_runs, bytes; };
+EmbedScratch embed_scratch(int rows, int vocab, int d) {
+  EmbedScratch s{};
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) { const uint64_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+  s.keys = take(4ull * rows);
+  s.order = take(4ull * rows);
+  s.tile_keys = take(rows > kTile ? 4ull * rows : 0);
+  s.tile_order = take(rows > kTile ? 4ull * rows : 0);
+  s.starts = take(4ull * (vocab + 1));
+  s.runs = take(4ull * (rows / kRun) * d);
+  s.long_runs = take(4ull * (rows / kRuns) * d);
+  s.bytes = at;
+  return s;
+}
+
+bool eights(const void *p, int64_t ld, int bf16, int64_t rows) { return ((uintptr_t)p & 15) == 0 && (rows <= 1 || ld % (bf16 ? 8 : 4) == 0); }
+
+template <int W> hipError_t embed_sums(const EmbedGradArgs &a, const EmbedScratch &s, char *base, hipStream_t st) {
+  int *keys = (int *)(base + s.keys), *order = (int *)(base + s.order), *starts = (int *)(base + s.starts);
+  float *runs = (float *)(base + s.runs), *long_runs = (float *)(base + s.long_runs);
+  const int slices = (a.d + kEmbedThreads * W - 1) / (kEmbedThreads * W), start_groups = (a.vocab + kEmbedThreads) / kEmbedThreads;
+  const int ys = slices > 64 ? 64 : slices;
+  hipLaunchKernelGGL(embed_runs_kernel<W>, dim3(start_groups + a.rows / kRun, ys), dim3(kEmbedThreads), 0, st, a, keys, order, starts, start_groups, runs);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.rows >= kRuns) {
+    const int wide = (a.d + kEmbedThreads - 1) / kEmbedThreads;
+    hipLaunchKernelGGL(embed_long_runs_kernel, dim3(a.rows / kRuns, wide > 64 ? 64 : wide), dim3(kEmbedThreads), 0, st, keys, a.vocab, a.d, runs, long_runs);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(embed_table_kernel<W>, dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_embed(int dtype, const void *table, int64_t ldt, int vocab, int d, const int *tok, int rows, float scale, int out_dtype, void *out, int64_t ldo,
+                        hipStream_t st) {
+  const bool vec = d % 8 == 0 && eights(table, ldt, dtype, vocab) && eights(out, ldo, out_dtype, rows);
+  const int cols = vec ? d / 8 : d, per = cols < kEmbedThreads ? kEmbedThreads / cols : 1;
+  const int64_t groups = ((int64_t)rows + per - 1) / per, deep = (groups + (1 << 23) - 1) >> 23;   // (a grid's dimension holds less than 2^32 threads)
+  const dim3 grid((unsigned)((groups + deep - 1) / deep), (unsigned)deep);
+  if (vec) hipLaunchKernelGGL(embed_kernel<true>, grid, dim3(kEmbedThreads), 0, st, table, ldt, vocab, d, tok, rows, scale, dtype, out_dtype, out, ldo);
+  else hipLaunchKernelGGL(embed_kernel<false>, grid, dim3(kEmbedThreads), 0, st, table, ldt, vocab, d, tok, rows, scale, dtype, out_dtype, out, ldo);
+  return hipGetLastError();
+}
+
+uint64_t embed_grad_scratch_bytes(int rows, int vocab, int d) { return embed_scratch(rows, vocab, d).bytes; }
+
+hipError_t launch_embed_grad(EmbedGradArgs a, void *scratch, hipStream_t st) {
+  const EmbedScratch s = embed_scratch(a.rows, a.vocab, a.d);
+  char *base = (char *)scratch;
+  const bool tiled = a.rows > kTile;
+  int *keys = (int *)(base + (tiled ? s.tile_keys : s.keys)), *order = (int *)(base + (tiled ? s.tile_order : s.order));
+  hipLaunchKernelGGL(embed_rank_kernel, dim3((a.rows + kRankMine - 1) / kRankMine), dim3(kRankThreads), 0, st, a.tok, a.rows, a.vocab, keys, order);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (tiled) {
+    hipLaunchKernelGGL(embed_merge_kernel, dim3((a.rows + kRankThreads - 1) / kRankThreads), dim3(kRankThreads), 0, st, keys, order, a.rows,
+                       (int *)(base + s.keys), (int *)(base + s.order));
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  const bool vec = a.d % 8 == 0 && eights(a.dy, a.ldy, a.dtype, a.rows) && eights(a.dtable, a.ldt, a.out_dtype, a.vocab);
+  return vec ? embed_sums<8>(a, s, base, st) : embed_sums<1>(a, s, base, st);
+}
+
+}  // namespace spec

@@ -335,4 +335,52 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(RotaryArgs a, hipStream_t st);
 
+// ---- gradclip.hip ---------------------------------------------------------------------------------
+constexpr int kGradTensors = 112;       // of a launch: its arguments stay under 4 KB
+constexpr int kGradSums = 1024;
+constexpr int64_t kGradCount = ((int64_t)1 << 48) - 1, kGradBf16 = (int64_t)1 << 60, kGradToBf16 = (int64_t)1 << 61;
+struct GradTensor { const void *g; void *out; int64_t count; };   // count: elements, and the two flags
+struct GradArgs {
+  GradTensor t[kGradTensors];
+  int begin[kGradTensors];              // first chunk of a tensor
+  int n, chunks, first;                 // first: the sums begin here (else they are added to)
+  double *sums;
+  double max_norm;
+  float *norm;
+};
+static_assert(sizeof(GradArgs) <= 4096, "kernel arguments");
+int64_t grad_chunks(const void *g, int64_t n, int bf16);
+hipError_t launch_grad_sums(const GradArgs &a, hipStream_t st);
+hipError_t launch_grad_clip(const GradArgs &a, hipStream_t st);
+
+// ---- embed.hip ------------------------------------------------------------------------------------
+hipError_t launch_embed(int dtype, const void *table, int64_t ldt, int vocab, int d, const int *tok, int rows, float scale, int out_dtype, void *out, int64_t ldo,
+                        hipStream_t st);
+struct EmbedGradArgs {
+  const void *dy;  int64_t ldy;  int dtype;
+  const int *tok;
+  int rows, d, vocab, accumulate;
+  float scale;
+  void *dtable;  int64_t ldt;  int out_dtype;
+  int vec;                              // set by launch_embed_grad: eight columns at a time
+};
+uint64_t embed_grad_scratch_bytes(int rows, int vocab, int d);
+hipError_t launch_embed_grad(EmbedGradArgs a, void *scratch, hipStream_t st);
+
+// ---- headnorm.hip ---------------------------------------------------------------------------------
+struct HeadnormPart { RotaryPart p; const void *w; const void *x; int64_t ld, hs; float *dw; float offset; int w_dtype, x_dtype; };   // x .. dw, x_dtype: gradients only
+struct HeadnormArgs {
+  HeadnormPart part[3];
+  int n_parts, hd, rows, rot, interleaved, pos0;
+  const int *pos;
+  double mscale;
+  double turns[kRotaryMaxPlanes];
+  float eps;
+  float *scratch;                       // gradients: [part][workgroup][hd]
+  int rows_each, items, group;          // set by the launch
+};
+int headnorm_grad_groups();             // workgroups of a part that leave a share of dw
+hipError_t launch_headnorm(HeadnormArgs a, hipStream_t st);
+hipError_t launch_headnorm_grad(HeadnormArgs a, hipStream_t st);
+
 }  // namespace spec

@@ -1,0 +1,404 @@
+"""Operators of a training step on the GPU, against their definitions in 64 bits (oracle/step.py).
+
+Tolerances.  u32 = 2^-24, u16 = 2^-8 (bf16): the largest relative error of a rounding.
+* embed: one product in fp32 and the output's rounding.
+* embed_grad: a sum of n terms in fp32 is off by at most n u32 sum|dy|; the product with the scale (and the sum with what was there), and the output's rounding.
+* headnorm: a sum of hd squares in fp32 is off by at most hd u32 of itself, its root by half of that; with the division, the products, the weight and the turning, (hd/2 + 16) u32 of
+  what a turned plane can be (the table's entries are off by u32), and the output's rounding.
+* its gradients: dz as above, a mean of hd products; with R = r (|w dz| + |x| r^2 mean|w dz x|) of the plane, (2 hd + 48) u32 R.  Gradients of weights: sums of n terms, (n + hd + 32) u32 sum|dz x r|.
+* grad_clip: 64-bit sums; the norm is rounded to fp32 (u32), the factor too, the product once more, then to the output's type.
+"""
+import numpy as np
+import pytest
+
+from oracle import layer8 as L
+from oracle import step as O
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+U32, U16 = 2.0 ** -24, 2.0 ** -8
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2408_15766_amd as pkg
+    assert torch.cuda.is_available()
+    return pkg
+
+
+def rand(seed, *shape, scale=1.0):
+    return torch.from_numpy((np.random.default_rng(seed).standard_normal(shape) * scale).astype(np.float32))
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def unit(dtype):
+    return U16 if dtype is torch.bfloat16 else U32
+
+
+def close(got, want, tol):
+    bad = ~(np.abs(f64(got) - want) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:5], f64(got)[bad][:5], want[bad][:5], np.broadcast_to(tol, want.shape)[bad][:5])
+
+
+# ---- embedding ------------------------------------------------------------------------------------
+
+def tokens(seed, rows, vocab, padding=0.1):
+    r = np.random.default_rng(seed)
+    t = np.minimum((np.exp(r.random(rows) * np.log(vocab + 1)) - 1).astype(np.int64), vocab - 1)   # small ids often
+    t[r.random(rows) < padding] = -1
+    return torch.from_numpy(t.astype(np.int32)).cuda()
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("rows,vocab,d", [(1, 1, 1), (1, 100, 4096), (5, 7, 3), (60, 1000, 256), (33, 50, 33), (300, 20, 8), (129, 300, 2056), (7, 9, 6000), (1000, 64, 40)])
+def test_embed(P, rows, vocab, d, dtype, out):
+    table, tok = rand(1, vocab, d).to(DT[dtype]).cuda(), tokens(2, rows, vocab)
+    tok[rows // 2] = vocab                                               # outside the table too
+    wide = torch.full((rows, d + 5), 7.0, dtype=DT[out], device="cuda")
+    for o in (None, wide[:, 5:], wide[:, :d]):
+        got = P.spec_k_embed(table, tok, scale=0.3, out_dtype=DT[out], out=o)
+        want = O.embed(f64(table), tok.cpu().numpy(), np.float32(0.3))
+        close(got, want, np.abs(want) * (U32 + 1.01 * unit(DT[out])) + 1e-40)
+    part = rand(3, vocab, d + 11).to(DT[dtype]).cuda()[:, 3:3 + d]       # rows of a wider table
+    want = O.embed(f64(part), tok.cpu().numpy())
+    close(P.spec_k_embed(part, tok, out_dtype=DT[out]), want, np.abs(want) * 1.01 * unit(DT[out]))
+
+
+def test_embed_leaves_what_lies_between_rows(P):
+    table, tok = rand(1, 50, 64).cuda(), tokens(1, 20, 50)
+    wide = torch.full((20, 80), 7.0, device="cuda")
+    P.spec_k_embed(table, tok, out=wide[:, 8:72])
+    assert (wide[:, :8] == 7).all() and (wide[:, 72:] == 7).all()
+    dt = torch.full((50, 80), 7.0, device="cuda")
+    P.spec_k_embed_grad(wide[:, 8:72], tok, 50, out=dt[:, 8:72])
+    assert (dt[:, :8] == 7).all() and (dt[:, 72:] == 7).all()
+
+
+def check_embed_grad(P, dy, tok, vocab, scale=1.0, out_dtype=None, **kw):
+    got = P.spec_k_embed_grad(dy, tok, vocab, scale=scale, out_dtype=out_dtype, **kw)
+    src, t = f64(torch.where((tok >= 0)[:, None], dy, torch.zeros_like(dy))), tok.cpu().numpy()
+    s = float(np.float32(scale))
+    want, size = O.embed_grad(src, t, vocab, s), O.embed_grad(np.abs(src), t, vocab, abs(s))
+    count = np.bincount(t[(t >= 0) & (t < vocab)], minlength=vocab)[:, None]
+    tol = (count + 2) * U32 * size
+    close(got, want, tol + unit(got.dtype) * (np.abs(want) + tol) + 1e-40)
+    return got
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("rows,vocab,d", [(1, 1, 1), (1, 300, 64), (3, 2, 5), (31, 9, 8), (32, 1, 16), (33, 1, 16), (64, 3, 33), (1000, 40, 24), (1024, 1, 8), (4096, 17, 9), (4097, 600, 16),
+                                          (9000, 50, 40), (12288, 2, 8), (700, 5000, 2056)])
+def test_embed_grad(P, rows, vocab, d, dtype, out):
+    dy, tok = rand(rows, rows, d).to(DT[dtype]).cuda(), tokens(rows + 1, rows, vocab)
+    if rows > 2:
+        tok[1] = vocab + 5
+        dy[tok < 0] = float("nan")                                       # rows without a token have no part in it
+        dy[1] = float("inf")
+    tok_ = torch.where(tok < vocab, tok, -1)
+    got = check_embed_grad(P, dy, tok_, vocab, 0.7, DT[out])
+    assert torch.equal(P.spec_k_embed_grad(dy, tok, vocab, scale=0.7, out_dtype=DT[out]), got)      # the same bits again
+
+
+@pytest.mark.parametrize("rows,length", [(4096, 1), (5000, 5000), (6000, 1024), (3000, 32), (3100, 31), (5000, 33), (40000, 7000)])
+def test_embed_grad_runs(P, rows, length):
+    """Tokens that occur `length` times each, at neighbouring or scattered positions; sums of whole numbers are exact."""
+    vocab, d = -(-rows // length), 24
+    tok = torch.arange(rows, device="cuda", dtype=torch.int32) // length
+    dy = torch.randint(-8, 9, (rows, d), device="cuda").float()
+    for order in (torch.arange(rows, device="cuda"), torch.from_numpy(np.random.default_rng(rows).permutation(rows)).cuda()):
+        want = torch.zeros(vocab, d, dtype=torch.float64, device="cuda").index_add_(0, tok[order].long(), dy[order].double())
+        assert torch.equal(P.spec_k_embed_grad(dy[order].contiguous(), tok[order].contiguous(), vocab).double(), want)
+
+
+def test_embed_grad_order_does_not_depend_on_the_other_tokens_place(P):
+    """Rows of a token are summed in the order of their positions: one long row of fp32 values against the same walk in fp32."""
+    rows = 31
+    dy = rand(3, rows, 8).cuda()
+    got = P.spec_k_embed_grad(dy, torch.full((rows,), 4, dtype=torch.int32, device="cuda"), 9)
+    s = torch.zeros(8, device="cuda")
+    for r in dy:
+        s = s + r
+    assert torch.equal(got[4], s) and (got[[0, 1, 2, 3, 5, 6, 7, 8]] == 0).all()
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+def test_embed_grad_accumulates(P, out):
+    rows, vocab, d = 500, 800, 72
+    dy, tok = rand(1, rows, d).cuda(), tokens(2, rows, vocab)
+    was = rand(3, vocab, d).to(DT[out]).cuda()
+    empty = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    empty[tok[tok >= 0].long()] = False
+    was[empty] = float("nan")                                            # rows without a token: not touched
+    acc = was.clone()
+    assert P.spec_k_embed_grad(dy, tok, vocab, scale=2.0, out=acc, accumulate=True) is acc
+    t = tok.cpu().numpy()
+    want, size = O.embed_grad(f64(dy), t, vocab, 2.0), O.embed_grad(np.abs(f64(dy)), t, vocab, 2.0)
+    some = ~empty.cpu().numpy()
+    want, size = (want + f64(was))[some], size[some]
+    tol = 60 * U32 * (size + np.abs(want)) + (rows + 2) * U32 * size
+    close(acc[~empty], want, tol + unit(DT[out]) * (np.abs(want) + tol))
+    assert torch.isnan(acc[empty]).all()
+
+
+def test_embed_grad_is_the_gradient(P):
+    """<embed(table + h) - embed(table), g> = <h, embed_grad(g)>."""
+    table, h, tok = rand(1, 40, 16).cuda(), rand(2, 40, 16).cuda(), tokens(3, 200, 40)
+    g = rand(4, 200, 16).cuda()
+    dt = P.spec_k_embed_grad(g, tok, 40, scale=0.5)
+    moved = (P.spec_k_embed(table + h, tok, scale=0.5).double() - P.spec_k_embed(table, tok, scale=0.5).double())
+    a, b = float((moved * g.double()).sum()), float((h.double() * dt.double()).sum())
+    assert abs(a - b) < 1e-5 * float((moved * g.double()).abs().sum())
+
+
+# ---- norms of heads ---------------------------------------------------------------------------------
+
+def planes(size, rot, layout):
+    """Per dim what its plane holds in all."""
+    a, b = (slice(0, rot // 2), slice(rot // 2, rot)) if layout == "half" else (slice(0, rot, 2), slice(1, rot, 2))
+    out = size.copy()
+    out[..., a] = out[..., b] = size[..., a] + size[..., b]
+    return out
+
+
+def norm_bound(x, w, eps, offset, pos, f, m, rot, layout, out_dtype):
+    hd = x.shape[-1]
+    want = O.headnorm_rotary(x, w, eps, offset, pos, f, m, rot, layout)
+    size = planes(np.abs(O.headnorm(x, w, eps, 0.0)) + abs(offset) * np.abs(O.headnorm(x, np.ones(hd), eps)), rot, layout) * max(m, 1.0)
+    tol = (hd / 2 + 16) * U32 * size
+    return want, tol + unit(out_dtype) * (np.abs(want) + tol) + 1e-37
+
+
+def grad_bound(dy, x, w, eps, offset, pos, f, m, rot, layout, out_dtype):
+    hd = x.shape[-1]
+    dx, dw = O.headnorm_rotary_grad(dy, x, w, eps, offset, pos, f, m, rot, layout)
+    dz = planes(np.abs(dy), rot, layout) * max(m, 1.0)
+    wa = np.abs(np.asarray(w, np.float64)) + abs(offset)
+    r = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    size = r * (wa * dz + np.abs(x) * r * r * (wa * dz * np.abs(x)).mean(-1, keepdims=True))
+    tol = (2 * hd + 48) * U32 * size
+    n = dy.shape[0] * dy.shape[1]
+    return dx, tol + unit(out_dtype) * (np.abs(dx) + tol) + 1e-37, dw, (n + hd + 32) * U32 * (dz * np.abs(x) * r).sum((0, 1)) + 1e-37
+
+
+SHAPES = [(1, 1, 2, 2), (3, 5, 80, 32), (7, 2, 128, 128), (33, 40, 128, 64), (2, 3, 96, 90), (5, 1, 7, 6), (4, 6, 256, 256), (9, 3, 64, 48), (130, 1, 33, 2), (1, 1024, 64, 64), (3, 2, 16, 0),
+          (2, 200, 255, 254), (700, 2, 64, 64), (6, 3, 72, 72), (5, 2, 8, 0), (1, 1, 1, 0), (40, 8, 256, 32)]
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("rows,heads,hd,rot", SHAPES)
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "fp32")])
+def test_headnorm_rotary_and_gradients(P, rows, heads, hd, rot, layout, dtype, out):
+    kw = dict(scaling="yarn", factor=4.0, trained_len=2048) if rot >= 64 else {}
+    plan = P.spec_rotary_plan(rot, 1e4, layout=layout, **kw)
+    f, m = L.rope_frequencies(rot, 1e4, **kw) if rot else (np.zeros(0), 1.0)
+    x = (rand(rows + hd, rows, heads, hd) * torch.exp(rand(5, hd))).to(DT[dtype]).cuda()
+    dy = rand(rows + 3, rows, heads, hd).to(DT[dtype]).cuda()
+    pos = torch.from_numpy(np.random.default_rng(1).integers(0, 200000, rows).astype(np.int32)).cuda()
+    at = f64(pos)
+    for w, offset, eps in ((rand(8, hd).to(DT[out]).cuda(), 0.0, 1e-5), (rand(9, hd, scale=0.2).to(DT[dtype]).cuda(), 1.0, 0.0)):
+        got = P.spec_k_headnorm_rotary(plan, [x], pos, [w], eps=eps, offset=offset, out_dtypes=[DT[out]])[0]
+        close(got, *norm_bound(f64(x), f64(w), eps, offset, at, f, m, rot, layout, DT[out]))
+        (dx,), (dw,) = P.spec_k_headnorm_rotary_grad(plan, [dy], [x], pos, [w], eps=eps, offset=offset, out_dtypes=[DT[out]])
+        want, tol, want_w, tol_w = grad_bound(f64(dy), f64(x), f64(w), eps, offset, at, f, m, rot, layout, DT[out])
+        close(dx, want, tol)
+        close(dw, want_w, tol_w)
+        assert dw.dtype == torch.float32
+        again = P.spec_k_headnorm_rotary_grad(plan, [dy], [x], pos, [w], eps=eps, offset=offset, out_dtypes=[DT[out]])
+        assert torch.equal(again[0][0], dx) and torch.equal(again[1][0], dw)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_headnorm_without_weights_is_the_rotary_embedding(P, layout):
+    x = rand(1, 50, 6, 96).bfloat16().cuda()
+    plan = P.spec_rotary_plan(64, 1e4, layout=layout)
+    want = P.spec_k_rotary(plan, [x, x], 77, turned=[True, False])
+    got = P.spec_k_headnorm_rotary(plan, [x, x], 77, [None, None], turned=[True, False])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    back, none = P.spec_k_headnorm_rotary_grad(plan, [x, x], [None, None], 77, [None, None], turned=[True, False])
+    want = P.spec_k_rotary(plan, [x, x], 77, turned=[True, False], adjoint=True)
+    assert none == [None, None] and all(torch.equal(a, b) for a, b in zip(back, want))
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("hd,rot,off", [(128, 128, 0), (128, 64, 8), (64, 64, 1), (80, 48, 3)])
+def test_headnorm_strides_orders_and_in_place(P, layout, hd, rot, off):
+    rows, heads = 11, 3
+    plan = P.spec_rotary_plan(rot, 1e4, layout=layout)
+    f, m = L.rope_frequencies(rot, 1e4)
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda") * 37
+    w = rand(4, hd + 1).cuda()[1:]                                       # (aligned to its type only)
+    for dtype in (torch.bfloat16, torch.float32):
+        flat = rand(5, rows, heads * hd + 40).to(dtype).cuda()
+        a = flat[:, off:off + heads * hd].unflatten(1, (heads, hd))
+        b = rand(6, heads, rows, hd).to(dtype).cuda().transpose(0, 1)
+        wide = flat.clone()
+        o = wide[:, off:off + heads * hd].unflatten(1, (heads, hd))
+        for x, dy in ((a, b), (b, a)):
+            P.spec_k_headnorm_rotary(plan, [x], pos, [w], outs=[o])
+            close(o, *norm_bound(f64(x), f64(w), 1e-6, 0.0, f64(pos), f, m, rot, layout, dtype))
+            (dx,), (dw,) = P.spec_k_headnorm_rotary_grad(plan, [dy], [x], pos, [w], outs=[o])
+            want, tol, want_w, tol_w = grad_bound(f64(dy), f64(x), f64(w), 1e-6, 0.0, f64(pos), f, m, rot, layout, dtype)
+            close(o, want, tol)
+            close(dw, want_w, tol_w)
+        assert torch.equal(wide[:, :off], flat[:, :off]) and torch.equal(wide[:, off + heads * hd:], flat[:, off + heads * hd:])
+        keep = P.spec_k_headnorm_rotary(plan, [b], pos, [w])[0]
+        keep_dx = P.spec_k_headnorm_rotary_grad(plan, [b], [a], pos, [w])[0][0]
+        c = b.clone()
+        P.spec_k_headnorm_rotary(plan, [b], pos, [w], outs=[b])
+        assert torch.equal(b, keep)
+        P.spec_k_headnorm_rotary_grad(plan, [c], [a], pos, [w], outs=[c])
+        assert torch.equal(c, keep_dx)
+
+
+def test_headnorm_three_parts(P):
+    rows, hq, hkv, hd = 60, 32, 8, 128
+    plan = P.spec_rotary_plan(hd, 5e5, scaling="llama3", factor=8.0, trained_len=8192)
+    f, m = L.rope_frequencies(hd, 5e5, scaling="llama3", factor=8.0, trained_len=8192)
+    qkv = rand(1, rows, (hq + 2 * hkv) * hd).cuda()
+    xs = [t.unflatten(1, (-1, hd)) for t in qkv.split([hq * hd, hkv * hd, hkv * hd], 1)]
+    ws = [rand(2, hd).bfloat16().cuda(), rand(3, hd).cuda(), None]
+    window = torch.zeros(rows + 5, hkv * hd, dtype=torch.bfloat16, device="cuda")
+    outs = [torch.empty(rows, hq, hd, device="cuda"), window[5:].unflatten(1, (hkv, hd)), torch.empty(rows, hkv, hd, dtype=torch.bfloat16, device="cuda")]
+    P.spec_k_headnorm_rotary(plan, xs, 100000, ws, outs=outs, turned=[True, True, False])
+    at = 100000 + np.arange(rows)
+    for n in range(2):
+        close(outs[n], *norm_bound(f64(xs[n]), f64(ws[n]), 1e-6, 0.0, at, f, m, hd, "half", outs[n].dtype))
+    assert torch.equal(outs[2], xs[2].bfloat16()) and (window[:5] == 0).all()
+    dys = [rand(7 + n, *x.shape).cuda() for n, x in enumerate(xs)]
+    dxs, dws = P.spec_k_headnorm_rotary_grad(plan, dys, xs, 100000, ws, turned=[True, True, False], out_dtypes=[torch.float32, torch.bfloat16, torch.float32])
+    for n in range(2):
+        want, tol, want_w, tol_w = grad_bound(f64(dys[n]), f64(xs[n]), f64(ws[n]), 1e-6, 0.0, at, f, m, hd, "half", dxs[n].dtype)
+        close(dxs[n], want, tol)
+        close(dws[n], want_w, tol_w)
+    assert torch.equal(dxs[2], dys[2]) and dws[2] is None
+
+
+def test_headnorm_many_rows(P):
+    """More runs of rows than workgroups: sampled rows, and the weights' gradient in all, against 64 bits on the device."""
+    rows, heads, hd = 9001, 16, 64
+    plan = P.spec_rotary_plan(hd, 1e4)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (torch.randn(rows, heads, hd, generator=g, device="cuda") for _ in range(2))
+    w = torch.rand(hd, generator=g, device="cuda") + 0.5
+    (dx,), (dw,) = P.spec_k_headnorm_rotary_grad(plan, [dy], [x], 0, [w])
+    f, m = L.rope_frequencies(hd, 1e4)
+    some = [0, 1, 4095, 4096, 8191, 8999, 9000]
+    for r in some:
+        want, tol, _, _ = grad_bound(f64(dy[r:r + 1]), f64(x[r:r + 1]), f64(w), 1e-6, 0.0, np.array([r]), f, m, hd, "half", torch.float32)
+        close(dx[r:r + 1], want, tol)
+    back = P.spec_k_rotary(plan, [dy], 0, adjoint=True)[0].double()
+    terms = back * x.double() / torch.sqrt((x.double() ** 2).mean(-1, keepdim=True) + 1e-6)
+    # a lane adds up at most 9001 * 16 / 512 / 64 + 18 heads, 64 slots and 512 / 8 + 8 workgroups follow: under 200 additions in a row; dz and r as above
+    assert bool(((dw.double() - terms.sum((0, 1))).abs() <= (200 + hd + 32) * U32 * terms.abs().sum((0, 1))).all())
+
+
+def test_headnorm_zeros_and_nonfinite(P):
+    plan = P.spec_rotary_plan(64, 1e4)
+    w = torch.ones(64, device="cuda")
+    x = rand(1, 6, 2, 64).cuda()
+    clean = P.spec_k_headnorm_rotary(plan, [x], 0, [w])[0]
+    x[2, 1] = 0
+    x[3, 0, 5] = float("nan")
+    x[4, 1, 7] = float("inf")
+    y = P.spec_k_headnorm_rotary(plan, [x], 0, [w])[0]
+    assert (y[2, 1] == 0).all() and torch.isnan(y[3, 0]).all() and torch.isnan(y[4, 1]).any()
+    same = torch.ones(6, 2, dtype=torch.bool, device="cuda")
+    same[2, 1] = same[3, 0] = same[4, 1] = False
+    assert torch.equal(y[same], clean[same])                             # other heads of the same rows
+    assert torch.isnan(P.spec_k_headnorm_rotary(plan, [x], 0, [w], eps=0.0)[0][2, 1]).all()
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_headnorm_gradients_against_differences(P, layout):
+    rows, heads, hd = 3, 2, 32
+    plan = P.spec_rotary_plan(24, 1e4, layout=layout)
+    x, w, g = rand(1, rows, heads, hd).cuda(), rand(2, hd).cuda(), rand(3, rows, heads, hd).cuda()
+    (dx,), (dw,) = P.spec_k_headnorm_rotary_grad(plan, [g], [x], 50, [w], offset=1.0)
+
+    def value(x, w):
+        return float((P.spec_k_headnorm_rotary(plan, [x], 50, [w], offset=1.0)[0].double() * g.double()).sum())
+
+    step = 2.0 ** -6
+    for seed in range(4):
+        hx, hw = rand(10 + seed, rows, heads, hd).cuda(), rand(20 + seed, hd).cuda()
+        for got, a, b in ((dx, (x + step * hx, w), (x - step * hx, w)), (dw, (x, w + step * hw), (x, w - step * hw))):
+            slope = (value(*a) - value(*b)) / (2 * step)
+            along = float((got.double() * (hx if got is dx else hw).double()).sum())
+            # the third derivative along hx is of the size of |g| |hx|^3 / |x|^2, times step^2 / 6; fp32 results: 2^-20 |g| |y| / step
+            assert abs(slope - along) <= (step ** 2 * 2 + 2.0 ** -13) * float(g.abs().sum())
+
+
+# ---- clipping ---------------------------------------------------------------------------------------
+
+def check_clip(P, grads, limit, outs=None):
+    want, scaled = O.grad_clip([f64(g) for g in grads], limit)
+    norm = P.spec_k_grad_clip(grads, P.spec_k_grad_sums(grads), limit, outs=outs)
+    assert norm.shape == ()
+    if want >= 2.0 ** 128:                                               # beyond fp32, in which the norm is returned (the factor is formed in 64 bits)
+        assert float(norm) == float("inf")
+    else:
+        assert abs(float(norm) - want) <= 1.01 * U32 * want + 2.0 ** -150   # (below 2^-126 fp32's numbers are 2^-149 apart, a rounding is off by half of that)
+    for o, s in zip(grads if outs is None else outs, scaled):
+        close(o.reshape(-1), s.reshape(-1), np.abs(s.reshape(-1)) * (2.1 * U32 + 1.01 * unit(o.dtype)) + 1e-40)
+    return norm
+
+
+@pytest.mark.parametrize("limit", [0.5, 1e9, 0.0])
+@pytest.mark.parametrize("kinds", ["bf16", "fp32", "mixed"])
+@pytest.mark.parametrize("sizes", [[1], [0, 3, 0], [8192], [8191, 8193], [7, 5, 100000, 1, 33], [50000] * 3, [3] * 250, list(range(1, 120))])
+def test_clip(P, sizes, kinds, limit):
+    def kind(n):
+        return DT[kinds] if kinds in DT else (torch.bfloat16, torch.float32)[n % 2]
+    grads = [rand(n, size).to(kind(n)).cuda() for n, size in enumerate(sizes)]
+    for out in (None, "bf16", "fp32"):
+        outs = [torch.full_like(g, 3.0, dtype=g.dtype if out is None else DT[out]) for g in grads]
+        check_clip(P, grads, limit, outs)
+    before = [g.clone() for g in grads]
+    check_clip(P, grads, limit)                                          # in place
+    if limit > 1e6:
+        assert all(torch.equal(a, b) for a, b in zip(grads, before))
+
+
+def test_clip_unaligned_views(P):
+    """Views of flat buffers at every offset, neighbours of each other: what lies beside them stays."""
+    for dtype in (torch.bfloat16, torch.float32):
+        flat = rand(1, 70000).to(dtype).cuda()
+        out = torch.full((70003,), 7.0, dtype=torch.float32, device="cuda")
+        cuts = [1, 2, 5, 9, 17, 8200, 8201, 24600, 24607, 69999]
+        grads = [flat[a:b] for a, b in zip(cuts[:-1], cuts[1:])]
+        check_clip(P, grads, 0.25, [out[a + 2:b + 2] for a, b in zip(cuts[:-1], cuts[1:])])
+        assert (out[:3] == 7).all() and (out[70001:] == 7).all()
+        keep = flat.clone()
+        check_clip(P, grads, 0.25)
+        assert torch.equal(flat[:1], keep[:1]) and torch.equal(flat[69999:], keep[69999:])
+
+
+def test_clip_large_values_do_not_overflow(P):
+    g = [torch.full((1000,), 3e38, device="cuda"), torch.full((1000,), 1e-38, device="cuda")]
+    check_clip(P, g, 1.0)
+    check_clip(P, [torch.full((5,), 1e-42, device="cuda")], 1e-3)
+
+
+def test_clip_nonfinite_norms(P):
+    for bad, first, rest in ((float("inf"), torch.isnan, lambda t: t == 0), (float("nan"), torch.isnan, torch.isnan)):
+        g = rand(1, 100).cuda()
+        g[0] = bad
+        norm = P.spec_k_grad_clip([g], P.spec_k_grad_sums([g]), 0.5)
+        assert not torch.isfinite(norm) and first(g[:1]).all() and rest(g[1:]).all()
+
+
+def test_clip_sums_of_two_parts_add_up(P):
+    """Two processes' shares: each sums its own, the sums are added, both scale by the same factor."""
+    a, b = [rand(1, 5000).cuda()], [rand(2, 777).bfloat16().cuda(), rand(3, 9).cuda()]
+    sums = P.spec_k_grad_sums(a) + P.spec_k_grad_sums(b)
+    want, scaled = O.grad_clip([f64(t) for t in a + b], 0.5)
+    for part, s in ((a, scaled[:1]), (b, scaled[1:])):
+        assert abs(float(P.spec_k_grad_clip(part, sums, 0.5)) - want) <= 1.01 * U32 * want
+        for g, v in zip(part, s):
+            close(g, v, np.abs(v) * (2.1 * U32 + 1.01 * unit(g.dtype)))
+    kept = torch.empty(P.SPEC_GRAD_SUMS, dtype=torch.float64, device="cuda")
+    assert float(P.spec_k_grad_clip([], P.spec_k_grad_sums([], sums=kept), 0.5)) == 0.0
