@@ -85,6 +85,34 @@ uint64_t spec_k_headnorm_rotary_grad_scratch_bytes(int32_t n_parts, int32_t hd);
 int spec_k_headnorm_rotary_grad(const spec_rotary_plan *plan /* host */, int32_t n_parts, const spec_headnorm_grad_part *parts /* host */, int32_t hd, int32_t rows,
                                 const int32_t *pos, int32_t pos0, float eps, void *scratch, uint64_t scratch_bytes, void *stream);
 
+/* ---- gated feed-forward block ------------------------------------------------------
+ * h = act(x w_gate^T) * (x w_up^T): x [rows, d], w_gate and w_up [f, d], h [rows, f], all bf16 and row-major, as a
+ * program trains them (spec_k_gemm_swiglu and spec_k_gemm8 take weights that are packed once).
+ *   SPEC_ACT_SILU       g / (1 + e^-g)
+ *   SPEC_ACT_GELU       g (1 + erf(g / sqrt 2)) / 2
+ *   SPEC_ACT_GELU_TANH  g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2
+ * Sums and activations in fp32.  Row strides ldx, ldw, .. in elements; d, f and the strides are multiples of 8,
+ * pointers of 16 bytes.  1 <= rows <= 2^20, d, f <= 2^20, rows * d, rows * f and d * f <= 2^36, strides <=
+ * 2^21.  What lies between rows is left alone.  h overlaps no input.  Up to 64 rows the call reads the weights once
+ * and is bound by that (decoding with weights as they are trained); the order of a sum depends on the number of rows, so that a row's last bits may change
+ * with it. */
+#define SPEC_ACT_SILU 0
+#define SPEC_ACT_GELU 1
+#define SPEC_ACT_GELU_TANH 2
+int spec_k_ffn_gated(const void *x, int64_t ldx, int32_t rows, int32_t d, const void *w_gate, const void *w_up, int64_t ldw, int32_t f, int32_t act,
+                     void *h, int64_t ldh, void *stream);
+
+/* Its gradients for dh [rows, f] (row stride lddh), from x and the weights: with g = x w_gate^T and u = x w_up^T formed again
+ *     dg = dh u act'(g),  du = dh act(g),
+ *     dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x.
+ * dx [rows, d] and dw_gate, dw_up [f, d] in bf16; dx may be NULL, and dw_gate and dw_up together.
+ * dg and du are rounded to bf16 before the products that follow (one rounding more than the results', of the same size); sums in fp32.  No output
+ * overlaps an input or another output.  scratch: spec_k_ffn_gated_grad_scratch_bytes (host only; 0 for bad sizes), 256-byte aligned. */
+uint64_t spec_k_ffn_gated_grad_scratch_bytes(int32_t rows, int32_t d, int32_t f);
+int spec_k_ffn_gated_grad(const void *x, int64_t ldx, int32_t rows, int32_t d, const void *w_gate, const void *w_up, int64_t ldw, int32_t f, int32_t act,
+                          const void *dh, int64_t lddh, void *dx, int64_t lddx, void *dw_gate, void *dw_up, int64_t lddw, void *scratch,
+                          uint64_t scratch_bytes, void *stream);
+
 /* ---- gradient clipping ------------------------------------------------------------
  * The norm of n tensors' elements together, n = sqrt(sum g^2), and the tensors scaled by
  * min(1, max_norm / (norm + 1e-6)), without a wait in between:

@@ -13,6 +13,7 @@ from typing import Optional, Sequence
 from .binding import SPEC_EINVAL, SPEC_ROPE_MAX_DIM, SpecError, _INT_MAX, _dtype_code, _fit, _here, _new, _refuse, lib, spec_rotary_plan_t
 
 SPEC_GRAD_SUMS = 1024
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 lib.spec_k_embed.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
 lib.spec_k_embed_grad_scratch_bytes.restype = C.c_uint64
@@ -24,6 +25,11 @@ lib.spec_k_headnorm_rotary_grad_scratch_bytes.restype = C.c_uint64
 lib.spec_k_headnorm_rotary_grad_scratch_bytes.argtypes = [C.c_int32] * 2
 lib.spec_k_headnorm_rotary_grad.argtypes = [C.POINTER(spec_rotary_plan_t), C.c_int32, C.c_char_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_float,
                                             C.c_void_p, C.c_uint64, C.c_void_p]
+lib.spec_k_ffn_gated.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+lib.spec_k_ffn_gated_grad_scratch_bytes.restype = C.c_uint64
+lib.spec_k_ffn_gated_grad_scratch_bytes.argtypes = [C.c_int32] * 3
+lib.spec_k_ffn_gated_grad.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
+                                      C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_uint64, C.c_void_p]
 lib.spec_k_grad_sums.argtypes = [C.c_int32, C.c_char_p, C.c_void_p, C.c_void_p]
 lib.spec_k_grad_clip.argtypes = [C.c_int32, C.c_char_p, C.c_void_p, C.c_double, C.c_void_p, C.c_void_p]
 
@@ -217,6 +223,79 @@ def spec_k_headnorm_rotary_grad(plan: spec_rotary_plan_t, dys: Sequence, xs: Seq
     if rc:
         raise SpecError(rc, f"{what}: {rows} rows, heads of {hd}, plan over {plan.rot}, eps {eps}, {room} bytes of scratch")
     return list(outs), dws
+
+
+# ---- gated feed-forward block -----------------------------------------------------------------------
+
+def _ffn_args(what: str, x, w_gate, w_up, act: str):
+    """(rows, d, f, ldx, ldw) of a call."""
+    import torch
+    if act not in ACTIVATIONS:
+        _refuse(what, f"activation {act!r} ({', '.join(ACTIVATIONS)} are supported)")
+    for t in (x, w_gate, w_up):
+        if t.dtype is not torch.bfloat16:
+            _refuse(what, f"{t.dtype} (bfloat16 is supported)")
+    ldx, ldw = _matrix(what, "x", x), _matrix(what, "w_gate", w_gate, None, x.shape[1])
+    if _matrix(what, "w_up", w_up, *w_gate.shape) != ldw:
+        _refuse(what, "w_gate and w_up have to have the same strides")
+    return x.shape[0], x.shape[1], w_gate.shape[0], ldx, ldw
+
+
+def _bf16_out(what: str, name: str, t, rows: int, cols: int, beside):
+    """(an output, its row stride): the caller's, or a new one."""
+    import torch
+    if t is None:
+        return _new((rows, cols), (cols, 1), torch.bfloat16, beside), cols
+    if t.dtype is not torch.bfloat16:
+        _refuse(what, f"{name} has to be bfloat16")
+    return t, _matrix(what, name, t, rows, cols)
+
+
+def spec_k_ffn_gated(x, w_gate, w_up, act: str = "silu", out=None):
+    """act(x w_gate^T) * (x w_up^T): x [rows, d], w_gate and w_up [f, d] as they are trained, bf16 (rows may be strided, by multiples of 8; d and f are multiples
+    of 8) -> bf16 [rows, f].  act: silu, gelu or gelu_tanh.  out: optional tensor for it (rows may be strided)."""
+    what = "spec_k_ffn_gated"
+    stream = _here(what, x, w_gate, w_up, out)
+    rows, d, f, ldx, ldw = _ffn_args(what, x, w_gate, w_up, act)
+    out, ldh = _bf16_out(what, "out", out, rows, f, x)
+    rc = lib.spec_k_ffn_gated(x.data_ptr(), ldx, rows, d, w_gate.data_ptr(), w_up.data_ptr(), ldw, f, ACTIVATIONS[act], out.data_ptr(), ldh, stream)
+    if rc:
+        raise SpecError(rc, f"{what}: {rows} rows, {d} by {f} (multiples of 8, 16-byte aligned), strides {ldx}, {ldw}, {ldh}")
+    return out
+
+
+def spec_k_ffn_gated_grad_scratch_bytes(rows: int, d: int, f: int) -> int:
+    return int(lib.spec_k_ffn_gated_grad_scratch_bytes(rows, d, f)) if _fit(rows, d, f) else 0
+
+
+def spec_k_ffn_gated_grad(x, w_gate, w_up, dh, act: str = "silu", outs: Optional[Sequence] = None, want: Sequence[bool] = (True, True), scratch=None):
+    """The gradients of spec_k_ffn_gated for dh [rows, f] (bf16): (dx [rows, d], dw_gate [f, d], dw_up [f, d]), bf16.  want: whether those of x and of the weights are
+    formed (None in the place of what is not).  outs: optional three tensors for them (or None each; rows may be strided, both weights' alike).  scratch: optional uint8 tensor of
+    spec_k_ffn_gated_grad_scratch_bytes(rows, d, f)."""
+    import torch
+    what = "spec_k_ffn_gated_grad"
+    dx, dwg, dwu = (None, None, None) if outs is None else outs
+    stream = _here(what, x, w_gate, w_up, dh, dx, dwg, dwu, scratch)
+    rows, d, f, ldx, ldw = _ffn_args(what, x, w_gate, w_up, act)
+    if dh.dtype is not torch.bfloat16:
+        _refuse(what, f"{dh.dtype} (bfloat16 is supported)")
+    lddh = _matrix(what, "dh", dh, rows, f)
+    if (dx is not None and not want[0]) or ((dwg is not None or dwu is not None) and not want[1]) or not any(want):
+        _refuse(what, "an output that is not wanted")
+    lddx = lddw = 0
+    if want[0]:
+        dx, lddx = _bf16_out(what, "dx", dx, rows, d, x)
+    if want[1]:
+        (dwg, lddw), (dwu, other) = _bf16_out(what, "dw_gate", dwg, f, d, x), _bf16_out(what, "dw_up", dwu, f, d, x)
+        if lddw != other:
+            _refuse(what, "dw_gate and dw_up have to have the same strides")
+    scratch, room = _room(what, scratch, lib.spec_k_ffn_gated_grad_scratch_bytes(rows, d, f), x)
+    rc = lib.spec_k_ffn_gated_grad(x.data_ptr(), ldx, rows, d, w_gate.data_ptr(), w_up.data_ptr(), ldw, f, ACTIVATIONS[act], dh.data_ptr(), lddh,
+                                   None if dx is None else dx.data_ptr(), lddx, None if dwg is None else dwg.data_ptr(), None if dwu is None else dwu.data_ptr(), lddw,
+                                   None if scratch is None else scratch.data_ptr(), room, stream)
+    if rc:
+        raise SpecError(rc, f"{what}: {rows} rows, {d} by {f} (multiples of 8, 16-byte aligned), strides {ldx}, {ldw}, {lddh}, {lddx}, {lddw}, {room} bytes of scratch")
+    return dx, dwg, dwu
 
 
 # ---- gradient clipping ------------------------------------------------------------------------------

@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspec.so")
 SOURCES = ["gemm.hip", "rowops.hip", "attention.hip", "hca.hip", "distill.hip", "select.hip", "noalloc.hip", "gemm8.hip",
-           "attention8.hip", "rotary.hip", "embed.hip", "headnorm.hip", "gradclip.hip", "api.cpp", "api_layer8.cpp", "api_step.cpp"]
+           "attention8.hip", "rotary.hip", "ffn.hip", "embed.hip",
+           "headnorm.hip", "gradclip.hip", "api.cpp", "api_layer8.cpp", "api_step.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed fp32 instructions stay off (device code only; the host pass ignores the feature)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -50,6 +50,17 @@ HeadnormArgs headnorm_args(const spec_rotary_plan *plan, int32_t n_parts, int32_
 }
 RotaryPart rotary_part(const spec_rotary_part &p) { return RotaryPart{p.x, p.out, p.ldx, p.hsx, p.ldo, p.hso, p.heads, p.dtype, p.out_dtype, p.turn != 0}; }
 
+// ---- feed-forward block
+bool ffn_sizes_ok(int32_t rows, int32_t d, int32_t f) {
+  const int most = 1 << 20;
+  if (rows < 1 || rows > most || d < 8 || d > most || d % 8 || f < 8 || f > most || f % 8) return false;
+  const int64_t area = (int64_t)1 << 36;
+  return (int64_t)rows * d <= area && (int64_t)rows * f <= area && (int64_t)d * f <= area;
+}
+bool ffn_matrix_ok(const void *p, int64_t ld, int64_t rows, int64_t cols) {   // rows so far apart that 256 of them fit 31 bits
+  return p && aligned(p, 16) && ld >= 0 && ld <= (1 << 21) && (rows == 1 || (ld >= cols && ld % 8 == 0));
+}
+
 // ---- clipping
 bool grad_ok(const spec_grad_part &p, bool clip) {
   if (p.n < 0 || p.n > kMostStride || !is_dtype(p.dtype)) return false;
@@ -174,6 +185,40 @@ int spec_k_headnorm_rotary_grad(const spec_rotary_plan *plan, int32_t n_parts, c
   if (sums && (!scratch || !aligned(scratch, 256) || scratch_bytes < spec_k_headnorm_rotary_grad_scratch_bytes(n_parts, hd))) return SPEC_EINVAL;
   a.scratch = (float *)scratch;
   return done(launch_headnorm_grad(a, (hipStream_t)stream));
+}
+
+int spec_k_ffn_gated(const void *x, int64_t ldx, int32_t rows, int32_t d, const void *w_gate, const void *w_up, int64_t ldw, int32_t f, int32_t act,
+                     void *h, int64_t ldh, void *stream) {
+  static_assert(SPEC_ACT_SILU == kActSilu && SPEC_ACT_GELU == kActGelu && SPEC_ACT_GELU_TANH == kActGeluTanh, "header and kernel agree on the activations");
+  if (!ffn_sizes_ok(rows, d, f) || act < SPEC_ACT_SILU || act > SPEC_ACT_GELU_TANH) return SPEC_EINVAL;
+  if (!ffn_matrix_ok(x, ldx, rows, d) || !ffn_matrix_ok(w_gate, ldw, f, d) || !ffn_matrix_ok(w_up, ldw, f, d) || !ffn_matrix_ok(h, ldh, rows, f)) return SPEC_EINVAL;
+  if (h == x || h == w_gate || h == w_up) return SPEC_EINVAL;
+  FfnCall c{};
+  c.x = x; c.ldx = ldx; c.wg = w_gate; c.wu = w_up; c.ldw = ldw; c.rows = rows; c.d = d; c.f = f; c.act = act; c.h = h; c.ldh = ldh;
+  return done(launch_ffn(c, (hipStream_t)stream));
+}
+
+uint64_t spec_k_ffn_gated_grad_scratch_bytes(int32_t rows, int32_t d, int32_t f) {
+  return ffn_sizes_ok(rows, d, f) ? ffn_grad_scratch_bytes(rows, d, f) : 0;
+}
+
+int spec_k_ffn_gated_grad(const void *x, int64_t ldx, int32_t rows, int32_t d, const void *w_gate, const void *w_up, int64_t ldw, int32_t f, int32_t act,
+                          const void *dh, int64_t lddh, void *dx, int64_t lddx, void *dw_gate, void *dw_up, int64_t lddw, void *scratch,
+                          uint64_t scratch_bytes, void *stream) {
+  if (!ffn_sizes_ok(rows, d, f) || act < SPEC_ACT_SILU || act > SPEC_ACT_GELU_TANH) return SPEC_EINVAL;
+  if (!ffn_matrix_ok(x, ldx, rows, d) || !ffn_matrix_ok(w_gate, ldw, f, d) || !ffn_matrix_ok(w_up, ldw, f, d) || !ffn_matrix_ok(dh, lddh, rows, f)) return SPEC_EINVAL;
+  if ((dx && !ffn_matrix_ok(dx, lddx, rows, d)) || !dw_gate != !dw_up) return SPEC_EINVAL;
+  if (dw_gate && (!ffn_matrix_ok(dw_gate, lddw, f, d) || !ffn_matrix_ok(dw_up, lddw, f, d))) return SPEC_EINVAL;
+  if (!scratch || !aligned(scratch, 256) || scratch_bytes < ffn_grad_scratch_bytes(rows, d, f)) return SPEC_EINVAL;
+  const void *in[4] = {x, w_gate, w_up, dh}, *out[4] = {dx, dw_gate, dw_up, scratch};
+  for (int o = 0; o < 4; o++) {
+    for (int i = 0; i < 4; i++)
+      if (out[o] == in[i] || (out[o] && i < o && out[o] == out[i])) return SPEC_EINVAL;
+  }
+  FfnCall c{};
+  c.x = x; c.ldx = ldx; c.wg = w_gate; c.wu = w_up; c.ldw = ldw; c.rows = rows; c.d = d; c.f = f; c.act = act; c.h = const_cast<void *>(dh); c.ldh = lddh;
+  c.dx = dx; c.lddx = lddx; c.dwg = dw_gate; c.dwu = dw_up; c.lddw = lddw;
+  return done(launch_ffn_grad(c, scratch, (hipStream_t)stream));
 }
 
 int spec_k_grad_sums(int32_t n_parts, const spec_grad_part *parts, double *sums, void *stream) {

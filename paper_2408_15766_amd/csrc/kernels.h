@@ -353,6 +353,29 @@ int64_t grad_chunks(const void *g, int64_t n, int bf16);
 hipError_t launch_grad_sums(const GradArgs &a, hipStream_t st);
 hipError_t launch_grad_clip(const GradArgs &a, hipStream_t st);
 
+// ---- ffn.hip --------------------------------------------------------------------------------------
+enum { kActSilu = 0, kActGelu = 1, kActGeluTanh = 2 };
+struct FfnCall {                        // bf16, strides in elements
+  const void *x;  int64_t ldx;          // [rows, d]
+  const void *wg, *wu;  int64_t ldw;    // [f, d]
+  int rows, d, f, act;
+  void *h;  int64_t ldh;                // [rows, f]: the result, or (gradients, not written) its gradient
+  void *dx;  int64_t lddx;              // may be null
+  void *dwg, *dwu;  int64_t lddw;       // both null, or none
+};
+struct FfnArgs {                        // out[m][n] = sum over k of the two sides
+  const void *m_src[2], *n_src[2];  int64_t ldm, ldn;
+  int m, n, k, segs, halves;            // k: of a segment; halves: products side by side, with an m side and a result each
+  int act;
+  const void *dh;  int64_t lddh;
+  void *out[2];  int64_t ldo;
+  float *part;                          // [range][half][m][n]
+  int m_tiles, n_tiles, splits;
+};
+uint64_t ffn_grad_scratch_bytes(int rows, int d, int f);
+hipError_t launch_ffn(const FfnCall &c, hipStream_t st);
+hipError_t launch_ffn_grad(const FfnCall &c, void *scratch, hipStream_t st);
+
 // ---- embed.hip ------------------------------------------------------------------------------------
 hipError_t launch_embed(int dtype, const void *table, int64_t ldt, int vocab, int d, const int *tok, int rows, float scale, int out_dtype, void *out, int64_t ldo,
                         hipStream_t st);

@@ -6,6 +6,9 @@ Tolerances.  u32 = 2^-24, u16 = 2^-8 (bf16): the largest relative error of a rou
 * headnorm: a sum of hd squares in fp32 is off by at most hd u32 of itself, its root by half of that; with the division, the products, the weight and the turning, (hd/2 + 16) u32 of
   what a turned plane can be (the table's entries are off by u32), and the output's rounding.
 * its gradients: dz as above, a mean of hd products; with R = r (|w dz| + |x| r^2 mean|w dz x|) of the plane, (2 hd + 48) u32 R.  Gradients of weights: sums of n terms, (n + hd + 32) u32 sum|dz x r|.
+* ffn_gated: sums of d products in fp32, t = (d + 8) u32 sum|x w|; an activation's slope is at most 1.2, its second derivative too; activations are relatively (|z| + 32) 2 u32 off (z the
+  exponential's argument, whose rounding moves the exponential by |z| u32); the output's rounding.
+* its gradients: dg and du from these, each rounded to bf16 (u16), then sums of 2 f (of rows) products in fp32 and the output's rounding.
 * grad_clip: 64-bit sums; the norm is rounded to fp32 (u32), the factor too, the product once more, then to the output's type.
 """
 import numpy as np
@@ -330,6 +333,159 @@ def test_headnorm_gradients_against_differences(P, layout):
             along = float((got.double() * (hx if got is dx else hw).double()).sum())
             # the third derivative along hx is of the size of |g| |hx|^3 / |x|^2, times step^2 / 6; fp32 results: 2^-20 |g| |y| / step
             assert abs(slope - along) <= (step ** 2 * 2 + 2.0 ** -13) * float(g.abs().sum())
+
+
+# ---- gated feed-forward block -----------------------------------------------------------------------
+
+def act64(act, g):
+    """act(g), its slope and how far the kernels' may be off (relative to |g| p, and absolute), on the device in 64 bits."""
+    if act == "silu":
+        z, dz = g, torch.ones_like(g)
+        p = torch.sigmoid(g)
+    elif act == "gelu_tanh":
+        c = 2 * (2 / np.pi) ** 0.5
+        z, dz = c * (g + 0.044715 * g ** 3), c * (1 + 3 * 0.044715 * g * g)
+        p = torch.sigmoid(z)
+    else:
+        p = 0.5 * torch.erfc(-g * 0.5 ** 0.5)
+        slope = p + g * torch.exp(-g * g / 2) / (2 * np.pi) ** 0.5
+        off = (g * g + 32) * 2 * U32
+        return g * p, slope, off, (1 + g.abs()) * off
+    off = (z.abs() + 32) * 2 * U32
+    return g * p, p + g * dz * p * (1 - p), off, (1 + g.abs() * dz * p) * 2 * off
+
+
+def ffn_want(x, wg, wu, act, dh=None):
+    """[(exact, largest error allowed)] of h, or of dx, dw_gate and dw_up."""
+    x, wg, wu = x.double(), wg.double(), wu.double()
+    d, f = x.shape[1], wg.shape[0]
+    g, u = x @ wg.t(), x @ wu.t()
+    tg, tu = ((d + 8) * U32 * (x.abs() @ w.abs().t()) for w in (wg, wu))
+    a, slope, off, slope_off = act64(act, g)
+    ta = 1.2 * tg + a.abs() * off
+    if dh is None:
+        h = a * u
+        t = ta * (u.abs() + tu) + a.abs() * tu + 4 * U32 * h.abs()
+        return [(h, t + U16 * (h.abs() + t) + 1e-38)]
+    dh = dh.double()
+    dg, du = dh * u * slope, dh * a
+    tdg = dh.abs() * ((1.2 * tg + slope_off) * (u.abs() + tu) + slope.abs() * tu) + 4 * U32 * dg.abs()
+    tdu = dh.abs() * ta + 4 * U32 * du.abs()
+    tdg, tdu = tdg + U16 * (dg.abs() + tdg) + 1e-38, tdu + U16 * (du.abs() + tdu) + 1e-38
+    res = [(dg @ wg + du @ wu, tdg @ wg.abs() + tdu @ wu.abs() + (2 * f + 40) * U32 * (dg.abs() @ wg.abs() + du.abs() @ wu.abs()))]
+    for v, t in ((dg, tdg), (du, tdu)):
+        res.append((v.t() @ x, t.t() @ x.abs() + (x.shape[0] + 40) * U32 * (v.abs().t() @ x.abs())))
+    return [(y, t + U16 * (y.abs() + t) + 1e-38) for y, t in res]
+
+
+def ffn_case(seed, rows, d, f):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+    return randn(rows, d).bfloat16(), (randn(f, d) * 2 / d ** 0.5).bfloat16(), (randn(f, d) / d ** 0.5).bfloat16(), (randn(rows, f) * 1e-2).bfloat16()
+
+
+def within(got, want, tol):
+    bad = ~((got.double() - want).abs() <= tol)
+    assert got.shape == want.shape and not bool(bad.any()), (int(bad.sum()), torch.nonzero(bad)[:5], got[bad][:5], want[bad][:5], tol[bad][:5])
+
+
+FFN_SIZES = [(1, 8, 8), (1, 4096, 136), (2, 72, 24), (5, 200, 1000), (15, 64, 16), (16, 136, 40), (17, 256, 128), (31, 1000, 72), (33, 520, 264), (47, 64, 4096), (49, 8, 8), (60, 4096, 72), (64, 328, 200),
+             (65, 64, 64), (65, 8, 8), (100, 1000, 136), (127, 72, 264), (128, 128, 128), (129, 136, 520), (255, 64, 256), (257, 320, 128), (300, 200, 1000), (777, 1000, 344), (520, 264, 2056)]
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("rows,d,f", FFN_SIZES)
+def test_ffn_gated_and_gradients(P, rows, d, f, act):
+    x, wg, wu, dh = ffn_case(rows + d, rows, d, f)
+    within(P.spec_k_ffn_gated(x, wg, wu, act=act), *ffn_want(x, wg, wu, act)[0])
+    got = P.spec_k_ffn_gated_grad(x, wg, wu, dh, act=act)
+    for o, (want, tol) in zip(got, ffn_want(x, wg, wu, act, dh)):
+        within(o, want, tol)
+    again = P.spec_k_ffn_gated_grad(x, wg, wu, dh, act=act)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+    dx, none, _ = P.spec_k_ffn_gated_grad(x, wg, wu, dh, act=act, want=(True, False))
+    nix, dwg, dwu = P.spec_k_ffn_gated_grad(x, wg, wu, dh, act=act, want=(False, True))
+    assert none is None and nix is None and torch.equal(dx, got[0]) and torch.equal(dwg, got[1]) and torch.equal(dwu, got[2])
+
+
+@pytest.mark.parametrize("rows,d,f", [(2100, 72, 4200), (4096, 200, 2056), (1000, 136, 4000), (4200, 4104, 72), (2048, 2056, 328), (72, 4200, 4104), (200, 1032, 2056), (8200, 40, 264), (130, 3000, 3000)])
+def test_ffn_gated_of_many_tiles(P, rows, d, f):
+    """Whole and ragged tiles of every shape, several to a die, and products whose k is cut into ranges or not."""
+    x, wg, wu, dh = ffn_case(rows, rows, d, f)
+    within(P.spec_k_ffn_gated(x, wg, wu), *ffn_want(x, wg, wu, "silu")[0])
+    for o, (want, tol) in zip(P.spec_k_ffn_gated_grad(x, wg, wu, dh), ffn_want(x, wg, wu, "silu", dh)):
+        within(o, want, tol)
+
+
+@pytest.mark.parametrize("rows", [3, 60, 200])
+def test_ffn_gated_strides(P, rows):
+    """Parts of wider matrices, in and out; both weights in one matrix; what lies between rows stays."""
+    d, f = 136, 264
+    x, wg, wu, dh = ffn_case(7, rows, d, f)
+    want, back = P.spec_k_ffn_gated(x, wg, wu), P.spec_k_ffn_gated_grad(x, wg, wu, dh)
+
+    def wider(t, left, right):
+        w = torch.full((t.shape[0], left + t.shape[1] + right), 7.0, dtype=t.dtype, device="cuda")
+        w[:, left:left + t.shape[1]] = t
+        return w[:, left:left + t.shape[1]]
+    both = torch.cat([wg, wu])
+    xs, dhs = wider(x, 8, 16), wider(dh, 16, 0)
+    for w in ((wider(wg, 0, 24), wider(wu, 8, 16)), (both[:f], both[f:])):
+        out = wider(torch.zeros_like(want), 8, 8)
+        assert P.spec_k_ffn_gated(xs, *w, out=out) is out and torch.equal(out, want)
+        outs = [wider(torch.zeros_like(t), 8, 8) for t in back]
+        P.spec_k_ffn_gated_grad(xs, *w, dhs, outs=outs)
+        assert all(torch.equal(o, t) for o, t in zip(outs, back))
+        for o in [out] + outs:
+            assert (o._base[:, :8] == 7).all() and (o._base[:, -8:] == 7).all()
+
+
+@pytest.mark.parametrize("rows,bad", [(5, 2), (64, 63), (200, 0), (200, 130)])
+def test_ffn_gated_keeps_nonfinite_rows_to_themselves(P, rows, bad):
+    """A row with NaN and infinities, at sizes whose last stage of k is part of a stage: the others have the results that they have without it."""
+    d, f = 72, 40
+    x, wg, wu, dh = ffn_case(9, rows, d, f)
+    h, (dx, _, _) = P.spec_k_ffn_gated(x, wg, wu), P.spec_k_ffn_gated_grad(x, wg, wu, dh)
+    x[bad, 0] = float("nan")
+    x[bad, 64] = float("inf")
+    h2, (dx2, dwg, _) = P.spec_k_ffn_gated(x, wg, wu), P.spec_k_ffn_gated_grad(x, wg, wu, dh)
+    keep = torch.arange(rows, device="cuda") != bad
+    assert torch.equal(h2[keep], h[keep]) and torch.equal(dx2[keep], dx[keep]) and torch.isnan(h2[bad]).all() and torch.isnan(dwg).all()
+
+
+def test_ffn_gated_large_and_small_gates(P):
+    """Gates far out on both sides: act(g) is g or next to nothing, its slope one or nothing."""
+    d = f = 64
+    x = torch.zeros(70, d, device="cuda", dtype=torch.bfloat16)
+    x[:, 0] = torch.linspace(-200, 200, 70, device="cuda").bfloat16()
+    x[:, 1] = 1
+    wg, wu = torch.zeros(f, d, device="cuda").bfloat16(), torch.zeros(f, d, device="cuda").bfloat16()
+    wg[:, 0], wu[:, 1] = torch.linspace(0.01, 1, f, device="cuda").bfloat16(), 1
+    dh = torch.ones(70, f, device="cuda").bfloat16()
+    for act in ("silu", "gelu", "gelu_tanh"):
+        for rows in (5, 70):
+            within(P.spec_k_ffn_gated(x[:rows], wg, wu, act=act), *ffn_want(x[:rows], wg, wu, act)[0])
+        for o, (want, tol) in zip(P.spec_k_ffn_gated_grad(x, wg, wu, dh, act=act), ffn_want(x, wg, wu, act, dh)):
+            within(o, want, tol)
+
+
+def test_ffn_gated_gradients_against_differences(P):
+    rows, d, f = 70, 64, 72
+    x, wg, wu, dh = ffn_case(3, rows, d, f)
+    dx, dwg, dwu = P.spec_k_ffn_gated_grad(x, wg, wu, dh)
+
+    def value(x, wg, wu):
+        g, u = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+        return float((g * torch.sigmoid(g) * u * dh.double()).sum())
+    for n, got in ((0, dx), (1, dwg), (2, dwu)):
+        args = [t.double() for t in (x, wg, wu)]
+        h = torch.randn(args[n].shape, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda", dtype=torch.float64)
+        step = 1e-5
+        hi, lo = ([a + (s * h if i == n else 0) for i, a in enumerate(args)] for s in (step, -step))
+        slope, along = (value(*hi) - value(*lo)) / (2 * step), got.double() * h
+        assert abs(slope - float(along.sum())) <= 4 * U16 * float(along.norm()) + 1e-6 * float(along.abs().sum())   # (independent roundings of dg, du and the result, four times their size)
 
 
 # ---- clipping ---------------------------------------------------------------------------------------
