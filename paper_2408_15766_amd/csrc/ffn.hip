@@ -14,7 +14,6 @@ namespace spec {
 
 namespace {
 
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -40,11 +39,13 @@ template <bool SLOPE> __device__ __forceinline__ Act activation(int act, float g
 // ---- tiles -----------------------------------------------------------------------------------------
 // Stages of 64 k in the LDS, copied there straight from memory, 16 bytes a lane and 1 KB a wavefront's instruction.
 // K along the rows (MAJOR = false): a row's 128 bytes, their eight pieces permuted by row / 2 so that sixteen rows' reads of one piece touch all banks.  K across
-// (MAJOR = true): per k the tile's columns, their chunks of 32 permuted by k so that the four k of a transposing read touch all banks.
+// (MAJOR = true): per k the tile's columns, their chunks of 16 permuted by k so that the eight k of half a transposing read touch all banks.
+// Products of 16 x 16 x 32: from registers alone they run at 2.00 PFLOP/s on normally distributed data where those of 32 x 32 x 16, which move their sums twice as often,
+// run at 1.78 (what limits both is the power).
 constexpr int kStageK = 64;
-template <int TW_, int TB_, int WQ_, int WB_> struct Tile {
-  static constexpr int TW = TW_, TB = TB_, WQ = WQ_, WB = WB_;
-  static constexpr int kWaves = TW * WQ, kThreads = kWaves * 64, kM = TW * TB * 32, kN = WQ * WB * 32;
+template <int TW_, int MB_, int WQ_, int NB_> struct Tile {   // wavefronts and 16-blocks of each along m and n
+  static constexpr int TW = TW_, MB = MB_, WQ = WQ_, NB = NB_;
+  static constexpr int kWaves = TW * WQ, kThreads = kWaves * 64, kM = TW * MB * 16, kN = WQ * NB * 16;
   static constexpr int kMBytes = kM * 128, kNBytes = kN * 128;       // of a stage
   static constexpr int kMLoads = kM / 8 / kWaves, kNLoads = kN / 8 / kWaves;   // copies of a wavefront
 };
@@ -54,185 +55,275 @@ __device__ __forceinline__ void wg_barrier() {                 // (without a wai
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+// Which 16 columns of a row of k (MAJOR) stand where: chunk ^ chunk_turn(k)
+__device__ __forceinline__ int chunk_turn(int k) { return (k & 3) | ((k >> 1) & 4); }
 
-// One side of a tile: LOADS copies of this wavefront per stage
+// One side of a tile: LOADS copies of this wavefront per stage.  The buffer ends with the matrix: what lies behind it (rows past the last, k past the end in the last row) is not
+// accessed; rows and columns past the tile's are never used, and k past the end is cleared.
 template <int LOADS, bool MAJOR, int COLS> struct Side {
-  const char *base;                                           // of the segment, at the tile's first row (column, if MAJOR)
-  uint32_t off[LOADS];                                        // of a lane, in the first stage
-  int k[LOADS];                                               // of a lane within a stage
+  const char *base[2], *end[2];                               // of the segment: the tile's first row (column, if MAJOR), and the matrix's end; [1]: of the copies from the fourth on, if they have their own
+  uint32_t off[LOADS];                                        // of a lane
   int64_t step;                                               // bytes from one stage to the next
-  // rows: how many there are from the tile's first on; ld in elements
-  __device__ __forceinline__ void place(int q0, int lane, int rows, int64_t ld) {
-#pragma unroll
-    for (int i = 0; i < LOADS; i++) {
-      const int q = q0 + i;
-      if constexpr (!MAJOR) {
-        const int r = q * 8 + (lane >> 3), piece = (lane & 7) ^ ((r >> 1) & 7);
-        off[i] = (uint32_t)min(r, rows - 1) * (uint32_t)(2 * ld) + piece * 16;
-        k[i] = piece * 8;
-      } else {
-        constexpr int kSlots = COLS / 8;
-        const int kr = q * (64 / kSlots) + lane / kSlots, slot = lane % kSlots, col = ((slot >> 2) ^ (kr & 3)) * 32 + (slot & 3) * 8;
-        off[i] = (uint32_t)kr * (uint32_t)(2 * ld) + (uint32_t)(col < rows ? col : 0) * 2;
-        k[i] = kr;
-      }
+  // k within a stage of copy q's lane
+  static __device__ __forceinline__ int k_of(int q, int lane) {
+    if constexpr (MAJOR) return q * (512 / COLS) + lane / (COLS / 8);
+    return ((lane & 7) ^ ((q * 4 + (lane >> 4)) & 7)) * 8;
+  }
+  // copy i is copy q of the tile's rows (columns); ld in elements
+  __device__ __forceinline__ void place(int i, int q, int lane, int64_t ld) {
+    const int k = k_of(q, lane);
+    if constexpr (!MAJOR) {
+      off[i] = (uint32_t)(q * 8 + (lane >> 3)) * (uint32_t)(2 * ld) + k * 2;
+    } else {
+      const int slot = lane % (COLS / 8);
+      off[i] = (uint32_t)k * (uint32_t)(2 * ld) + (uint32_t)(((slot >> 1) ^ chunk_turn(k)) * 32 + (slot & 1) * 16);
     }
     step = MAJOR ? (int64_t)kStageK * ld * 2 : kStageK * 2;
   }
-  // stage s of the segment, of which `left` k are there from its first on
-  __device__ __forceinline__ void copy(int s, int left, int64_t ld, unsigned char *to, int i0, int i1) const {
-    const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc((void *)(base + s * step), 0, 0x7FFFFFFF, 0x00027000);
+  // copies i0 .. of stage s of the segment
+  __device__ __forceinline__ void copy(int s, unsigned char *to, int i0, int i1, bool two = false) const {
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
       if (i < i0 || i >= i1) continue;
-      uint32_t o = off[i];
-      if (left < kStageK && k[i] >= left) o -= MAJOR ? (uint32_t)k[i] * (uint32_t)(2 * ld) : (uint32_t)k[i] * 2;   // past the end: the stage's first k, cleared when it is here
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void *)(to + i * 1024), 16, (int)o, 0, 0, 0);
+      const int h = two && i >= 4;
+      const char *at = (h ? base[1] : base[0]) + s * step;
+      const int64_t left = (h ? end[1] : end[0]) - at;
+      const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, left < 0x7FFFFFFF ? (int)left : 0x7FFFFFFF, 0x00027000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void *)(to + i * 1024), 16, (int)off[i], 0, 0, 0);
     }
   }
-  __device__ __forceinline__ void clear(int left, unsigned char *mine, int lane) const {   // mine: this wavefront's share of the stage
+  __device__ __forceinline__ void clear(int left, int q0, unsigned char *mine) const {   // mine: this wavefront's share of the stage, from its copy q0 on
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                            // (nothing of this is worth registers outside)
 #pragma unroll
     for (int i = 0; i < LOADS; i++)
-      if (k[i] >= left) *(u32x4_t *)(mine + i * 1024 + lane * 16) = u32x4_t{0u, 0u, 0u, 0u};
+      if (k_of(q0 + i, lane) >= left) *(u32x4_t *)(mine + i * 1024 + lane * 16) = u32x4_t{0u, 0u, 0u, 0u};
   }
 };
-// Fragments of a block of 32 rows (columns): lane (c, g) has row c at k = 16 j + 8 g + 0 .. 7
+// Fragments of a block of 16 rows (columns): lane 16 q + r has row r at k = 32 j + 8 q + 0 .. 7
 template <bool MAJOR, int COLS> __device__ __forceinline__ int frag_lane(int lane, int block) {
-  const int c = lane & 31, g = lane >> 5;
-  if constexpr (!MAJOR) return (block * 32 + c) * 128 + ((g ^ ((c >> 1) & 7)) * 16);
-  const int kr = 8 * g + ((lane & 15) >> 2);
-  return kr * COLS * 2 + ((block ^ (kr & 3)) * 64) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  const int r = lane & 15, q = lane >> 4;
+  if constexpr (!MAJOR) return (block * 16 + r) * 128 + ((q ^ (r >> 1)) * 16);
+  const int kr = 8 * q + (r >> 2);
+  return kr * COLS * 2 + ((block ^ chunk_turn(kr)) * 32) + (r & 3) * 8;
 }
 template <bool MAJOR, int COLS> __device__ __forceinline__ u32x4_t frag(const unsigned char *p, int at, int t, int j) {   // block t of those that `at` begins with
-  if constexpr (!MAJOR) return *(const u32x4_t *)(p + (at ^ (j * 32)) + t * 4096);
-  const unsigned char *q = p + (at ^ (t * 64)) + j * 16 * COLS * 2;
+  if constexpr (!MAJOR) return *(const u32x4_t *)(p + (at ^ (j * 64)) + t * 2048);
+  const unsigned char *q = p + (at ^ (t * 32)) + j * 32 * COLS * 2;
   const u32x2_t a = read_columns(q), b = read_columns(q + 4 * COLS * 2);
   return u32x4_t{a.x, a.y, b.x, b.y};
 }
 
-// Two bf16 pairs of the lanes (c, 0) and (c, 1), four values each of the columns 8 b + 4 g and 8 (b + 1) + 4 g, to eight consecutive columns a lane: 8 (b + g) ..
+// Four bf16 of block a (columns 4 q ..) and of block b in each of the lanes 16 q + r, to eight consecutive columns a lane: those from 8 (q / 2) on of block a (q even) or b
 __device__ __forceinline__ u32x4_t gather8(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
-  const auto x = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), y = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+  const auto x = __builtin_amdgcn_permlane16_swap(a0, b0, false, false), y = __builtin_amdgcn_permlane16_swap(a1, b1, false, false);
   return u32x4_t{x[0], y[0], x[1], y[1]};
 }
+__device__ __forceinline__ u32x4_t gather8(f32x4_t a, f32x4_t b) { return gather8(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y), pack_bf16x2(b.z, b.w)); }
 
 enum { kToH = 0, kToDgu = 1, kToOut = 2, kToParts = 3 };
 
-// One tile and range of stages.  SEGS: segments of k (two: dx).
+// A wavefront's sums to where they go: rows from m0 on, columns from n0 on (gated: of h)
+template <int MB, int NB, int TO>
+__device__ __forceinline__ void finish(const FfnArgs &a, const f32x4_t (&acc)[NB][MB], int m0, int n0, int half, float *part) {
+  constexpr bool kGated = TO == kToH || TO == kToDgu;
+  const int r = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
+  // lane 16 q + r holds row r of a block of m at the columns 4 q + 0 .. 3 of a block of n
+  u32x2_t dhs[TO == kToDgu ? MB : 1][TO == kToDgu ? NB / 2 : 1];   // (all asked for at once: block by block every block waited for its own)
+  if constexpr (TO == kToDgu) {
+#pragma unroll
+    for (int t = 0; t < MB; t++)
+#pragma unroll
+      for (int e = 0; e < NB / 2; e++) {
+        const int m = m0 + t * 16 + r, n = n0 + 16 * e + 4 * q;
+        dhs[t][e] = u32x2_t{0u, 0u};
+        if (m < a.m && n < a.n) dhs[t][e] = *(const u32x2_t *)((const bf16_t *)a.dh + (int64_t)m * a.lddh + n);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int t = 0; t < MB; t++) {
+    const int m = m0 + t * 16 + r;
+    const bool there = m < a.m;
+    if constexpr (kGated) {
+#pragma unroll
+      for (int p = 0; p < NB / 4; p++) {                      // 32 columns: gate sums in the blocks 4 p and 4 p + 1, up sums in the two behind
+        const int n1 = n0 + p * 32;
+        f32x4_t first[2], second[2];                          // h, or dg; du
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          float dh[4] = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (TO == kToDgu) {
+            const u32x2_t d = dhs[t][2 * p + e];
+            dh[0] = __uint_as_float(d.x << 16); dh[1] = __uint_as_float(d.x & 0xFFFF0000u);
+            dh[2] = __uint_as_float(d.y << 16); dh[3] = __uint_as_float(d.y & 0xFFFF0000u);
+          }
+#pragma unroll
+          for (int v = 0; v < 4; v++) {
+            const float gate = acc[4 * p + e][t][v], up = acc[4 * p + 2 + e][t][v];
+            const Act c = activation<TO == kToDgu>(a.act, gate);
+            if constexpr (TO == kToH) first[e][v] = gate * c.p * up;
+            else { first[e][v] = dh[v] * up * c.slope; second[e][v] = dh[v] * (gate * c.p); }
+          }
+        }
+        const int n = n1 + 16 * (q & 1) + 8 * (q >> 1);
+        const bool store = there && n < a.n;
+        const u32x4_t h = gather8(first[0], first[1]);
+        if (store) *(u32x4_t *)((bf16_t *)a.out[0] + (int64_t)m * a.ldo + n) = h;
+        if constexpr (TO == kToDgu) {
+          const u32x4_t d = gather8(second[0], second[1]);
+          if (store) *(u32x4_t *)((bf16_t *)a.out[1] + (int64_t)m * a.ldo + n) = d;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < NB; b += 2) {
+        const int n1 = n0 + b * 16;
+        if constexpr (TO == kToParts) {
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            const int n = n1 + 16 * e + 4 * q;
+            if (there && n < a.n) *(f32x4_t *)(part + (int64_t)m * a.n + n) = acc[b + e][t];
+          }
+        } else {
+          const u32x4_t o = gather8(acc[b][t], acc[b + 1][t]);
+          const int n = n1 + 16 * (q & 1) + 8 * (q >> 1);
+          if (there && n < a.n) *(u32x4_t *)((bf16_t *)(half ? a.out[1] : a.out[0]) + (int64_t)m * a.ldo + n) = o;
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);                        // one block at a time: registers
+  }
+}
+
+// One tile and range of stages.
 template <class L, bool MM, bool NM, int TO>
 __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, int n0, int s0, int s1, float *part, unsigned char *ms0, unsigned char *ms1, unsigned char *ns0,
                                           unsigned char *ns1, unsigned char *ns2) {
-  constexpr int ML = L::kMLoads, NL = L::kNLoads, TB = L::TB, WB = L::WB;
+  constexpr int ML = L::kMLoads, NL = L::kNLoads, MB = L::MB, NB = L::NB;
   constexpr bool kGated = TO == kToH || TO == kToDgu;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 31, g = lane >> 5, th = wave % L::TW, wq = wave / L::TW;
+  const int r = lane & 15, q = lane >> 4, th = wave % L::TW, wq = wave / L::TW;
   const int seg_stages = (a.k + kStageK - 1) / kStageK;       // of a segment
   Side<ML, MM, L::kM> ms;
   Side<NL, NM, L::kN> ns;
   const int64_t ldm = a.ldm, ldn = a.ldn;
-  ms.place(wave * ML, lane, a.m - m0, ldm);
-  if constexpr (kGated) {                                     // blocks of 32: gate, up, gate, .. of the same columns; a wavefront's copies are of one of them
-    static_assert(NL == 4 || NL == 2, "a wavefront copies a block, or half of one");
-    const int q0 = wave * NL, block = q0 / 4;
-    ns.place(q0 - block * 4, lane, a.n - n0 - block / 2 * 32 > 0 ? a.n - n0 - block / 2 * 32 : 1, ldn);
-    const int first = min(n0 + block / 2 * 32, a.n - 1);
-    ns.base = (const char *)(block & 1 ? a.n_src[1] : a.n_src[0]) + (int64_t)first * ldn * 2;
+#pragma unroll
+  for (int i = 0; i < ML; i++) ms.place(i, wave * ML + i, lane, ldm);
+  // where a matrix of a segment begins for this tile, and where it ends
+  auto m_base = [&](int seg) {
+    const char *p = (const char *)((MM ? half : seg) ? a.m_src[1] : a.m_src[0]);
+    ms.base[0] = p + (MM ? (int64_t)m0 * 2 : (int64_t)m0 * ldm * 2);
+    ms.end[0] = p + ((int64_t)((MM ? a.k : a.m) - 1) * ldm + (MM ? a.m : a.k)) * 2;
+  };
+  auto n_base = [&](int seg) {
+    const char *p = (const char *)(seg ? a.n_src[1] : a.n_src[0]);
+    ns.base[0] = p + (NM ? (int64_t)n0 * 2 : (int64_t)n0 * ldn * 2);
+    ns.end[0] = p + ((int64_t)((NM ? a.k : a.n) - 1) * ldn + (NM ? a.n : a.k)) * 2;
+  };
+  m_base(0);
+  if constexpr (kGated) {                                     // blocks of 32: gate, up, gate, .. of the same columns; a wavefront copies one, two, or half of one
+    static_assert(NL == 2 || NL == 4 || NL == 8, "whole shares of blocks");
+#pragma unroll
+    for (int h = 0; h < (NL + 3) / 4; h++) {
+      const int q0 = wave * NL + 4 * h, block = q0 / 4, first = min(n0 + block / 2 * 32, a.n - 1);
+      const char *p = (const char *)(block & 1 ? a.n_src[1] : a.n_src[0]);
+      ns.base[h] = p + (int64_t)first * ldn * 2;
+      ns.end[h] = p + ((int64_t)(a.n - 1) * ldn + a.k) * 2;
+#pragma unroll
+      for (int i = 4 * h; i < 4 * h + 4 && i < NL; i++) ns.place(i, q0 - block * 4 + i - 4 * h, lane, ldn);
+    }
   } else {
-    ns.place(wave * NL, lane, a.n - n0, ldn);
+#pragma unroll
+    for (int i = 0; i < NL; i++) ns.place(i, wave * NL + i, lane, ldn);
+    n_base(0);
   }
-  auto m_base = [&](int seg) { return (const char *)(MM ? (half ? a.m_src[1] : a.m_src[0]) : (seg ? a.m_src[1] : a.m_src[0])) + (MM ? (int64_t)m0 * 2 : (int64_t)m0 * ldm * 2); };
-  auto n_base = [&](int seg) { return (const char *)(seg ? a.n_src[1] : a.n_src[0]) + (NM ? (int64_t)n0 * 2 : (int64_t)n0 * ldn * 2); };
-  ms.base = m_base(0);
-  if constexpr (!kGated) ns.base = n_base(0);
 
   struct At { int s, left; bool second; };                    // a stage within its segment
   auto at_of = [&](int s) {
     s = min(s, s1 - 1);                                       // past the end: the last stage again (never read)
-    At r;
-    r.second = s >= seg_stages;
-    r.s = r.second ? s - seg_stages : s;
-    r.left = a.k - r.s * kStageK;
-    return r;
+    At p;
+    p.second = s >= seg_stages;
+    p.s = p.second ? s - seg_stages : s;
+    p.left = a.k - p.s * kStageK;
+    return p;
   };
   auto load_n = [&](unsigned char *buf, int s, int i0, int i1) __attribute__((always_inline)) {
     const At at = at_of(s);
-    if constexpr (!kGated) { if (a.segs == 2) ns.base = n_base(at.second); }
-    ns.copy(at.s, at.left, ldn, buf + wave * NL * 1024, i0, i1);
+    if constexpr (!kGated) { if (a.segs == 2) n_base(at.second); }
+    ns.copy(at.s, buf + wave * NL * 1024, i0, i1, kGated && NL == 8);
   };
-  auto load_m = [&](unsigned char *buf, int s) __attribute__((always_inline)) {
+  auto load_m = [&](unsigned char *buf, int s, int i0, int i1) __attribute__((always_inline)) {
     const At at = at_of(s);
-    if (a.segs == 2) ms.base = m_base(at.second);
-    ms.copy(at.s, at.left, ldm, buf + wave * ML * 1024, 0, ML);
+    if constexpr (!kGated && !MM) { if (a.segs == 2) m_base(at.second); }
+    ms.copy(at.s, buf + wave * ML * 1024, i0, i1);
   };
   auto clear_end = [&](unsigned char *mb, unsigned char *nb, int s) __attribute__((always_inline)) {   // what was copied for k past the end
     const At at = at_of(s);
     if (at.left >= kStageK) return;
-    ms.clear(at.left, mb + wave * ML * 1024, lane);
-    ns.clear(at.left, nb + wave * NL * 1024, lane);
+    ms.clear(at.left, wave * ML, mb + wave * ML * 1024);
+    ns.clear(at.left, wave * NL, nb + wave * NL * 1024);
     __builtin_amdgcn_s_waitcnt(0xC07F);                       // lgkmcnt(0)
   };
 
-  f32x16_t acc[WB][TB];
+  f32x4_t acc[NB][MB];
 #pragma unroll
-  for (int b = 0; b < WB; b++)
+  for (int b = 0; b < NB; b++)
 #pragma unroll
-    for (int t = 0; t < TB; t++)
+    for (int t = 0; t < MB; t++) acc[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const int mat_ = frag_lane<MM, L::kM>(lane, th * MB), nat_ = frag_lane<NM, L::kN>(lane, wq * NB);
+  // A step is the products of 32 k, block by block of m.  Behind block t's products block t + 3 (of this step or the next) is read, three blocks
+  // ahead of its turn; the next step's blocks of n are read behind the last products of this one.  `last`: the step ends its stage, and what follows is read from the next one, after the barrier
+  // that is behind the stage's last read.
+  u32x4_t fm[4], fn[2][NB];
+  constexpr int kBarrier = MB - 4, kEach = (NB + 1) / 2;
+  static_assert(MB % 4 == 0, "a ring of four blocks");
+  auto step = [&](int now, bool last, unsigned char *mc, unsigned char *nc, unsigned char *mn, unsigned char *nn, auto copies, auto turn) __attribute__((always_inline)) {
+    int mat = mat_, nat = nat_;
+    asm volatile("" : "+v"(mat), "+v"(nat));                  // (else the addresses of all steps are kept in registers at once)
 #pragma unroll
-      for (int v = 0; v < 16; v++) acc[b][t][v] = 0.f;
-  const int mat = frag_lane<MM, L::kM>(lane, th * TB), nat = frag_lane<NM, L::kN>(lane, wq * WB);
-  struct Frag { u32x4_t m[TB], n[WB]; };
-  auto read = [&](Frag &f, const unsigned char *mb, const unsigned char *nb, int j) __attribute__((always_inline)) {
+    for (int t = 0; t < MB; t++) {
 #pragma unroll
-    for (int b = 0; b < WB; b++) f.n[b] = frag<NM, L::kN>(nb, nat, b, j);
+      for (int b = 0; b < NB; b++)
+        acc[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, fn[now][b]), __builtin_bit_cast(bf16x8_t, fm[t & 3]), acc[b][t], 0, 0, 0);
+      if (t + 3 < MB) fm[(t + 3) & 3] = frag<MM, L::kM>(mc, mat, t + 3, last ? 1 : 0);
+      if (t == kBarrier) turn();
+      if (t > kBarrier) {                                     // the next step's
+        const int u = t - kBarrier - 1;
+        fm[u & 3] = frag<MM, L::kM>(last ? mn : mc, mat, u, last ? 0 : 1);
 #pragma unroll
-    for (int t = 0; t < TB; t++) f.m[t] = frag<MM, L::kM>(mb, mat, t, j);
-  };
-  auto mul = [&](const Frag &f) __attribute__((always_inline)) {
-#pragma unroll
-    for (int b = 0; b < WB; b++)
-#pragma unroll
-      for (int t = 0; t < TB; t++)
-        acc[b][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f.n[b]), __builtin_bit_cast(bf16x8_t, f.m[t]), acc[b][t], 0, 0, 0);
-  };
-  Frag f[2];
-  constexpr int kReads = TB * (MM ? 2 : 1) + WB * (NM ? 2 : 1);
-  auto spread = [&]() __attribute__((always_inline)) {        // the next step's reads behind the first products, the copies behind the others
-#pragma unroll
-    for (int i = 0; i < TB * WB; i++) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // a matrix instruction
-      __builtin_amdgcn_sched_group_barrier(0x100, (kReads + TB * WB - 1) / (TB * WB), 0);
-      if (i >= 2) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        for (int b = u * kEach; b < (u + 1) * kEach && b < NB; b++) fn[now ^ 1][b] = frag<NM, L::kN>(last ? nn : nc, nat, b, last ? 0 : 1);
+      }
+      copies(t);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);
   };
   auto stage = [&](unsigned char *mc, unsigned char *nc, unsigned char *mn, unsigned char *nn, unsigned char *np, int s) __attribute__((always_inline)) {
-    // on entry f[0] = the fragments of step 0
-#pragma unroll
-    for (int j = 0; j < 3; j++) {
-      read(f[(j + 1) & 1], mc, nc, j + 1);
-      if (j == 0) load_n(np, s + 2, 0, NL / 2);
-      if (j == 1) load_n(np, s + 2, NL / 2, NL);
-      mul(f[j & 1]);
-      spread();
-    }
-    // every fragment of this stage is in registers, and this wavefront's share of the next one has arrived (only the copies of the n side
-    // of the stage after it may still be under way)
-    __builtin_amdgcn_s_waitcnt(0x0070 | NL);                  // vmcnt(NL) lgkmcnt(0)
-    clear_end(mn, nn, s + 1);
-    wg_barrier();
-    read(f[0], mn, nn, 0);
-    load_m(mc, s + 2);
-    mul(f[1]);
-    spread();
+    step(0, false, mc, nc, mn, nn, [&](int t) __attribute__((always_inline)) { load_n(np, s + 2, min(t, NL), min(t + 1, NL)); if (t == MB - 1) load_n(np, s + 2, min(MB, NL), NL); },
+         []() {});
+    step(1, true, mc, nc, mn, nn, [&](int t) __attribute__((always_inline)) {
+      constexpr int kHalf = (ML + 1) / 2;
+      if (t > kBarrier) load_m(mc, s + 2, min((t - kBarrier - 1) * kHalf, ML), min((t - kBarrier) * kHalf, ML));
+    }, [&]() __attribute__((always_inline)) {
+      // every fragment of this stage is in registers, and this wavefront's share of the next one has arrived (only the copies of the n side
+      // of the stage after it may still be under way)
+      __builtin_amdgcn_s_waitcnt(0x0070 | NL);                // vmcnt(NL) lgkmcnt(0)
+      clear_end(mn, nn, s + 1);
+      wg_barrier();
+    });
   };
   load_n(ns0, s0, 0, NL);
-  load_m(ms0, s0);
+  load_m(ms0, s0, 0, ML);
   load_n(ns1, s0 + 1, 0, NL);
-  load_m(ms1, s0 + 1);
-  __builtin_amdgcn_s_waitcnt(0x0F70 | (ML + NL));             // the first stage is here
+  load_m(ms1, s0 + 1, 0, ML);
+  static_assert(ML + NL < 64 && NL < 16, "the counts of the waits");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | ((ML + NL) & 15) | (((ML + NL) >> 4) << 14));   // the first stage is here
   clear_end(ms0, ns0, s0);
   wg_barrier();
-  read(f[0], ms0, ns0, 0);
+#pragma unroll
+  for (int b = 0; b < NB; b++) fn[0][b] = frag<NM, L::kN>(ns0, nat_, b, 0);
+#pragma unroll
+  for (int t = 0; t < 3; t++) fm[t] = frag<MM, L::kM>(ms0, mat_, t, 0);
   int s = s0;
   for (; s + 6 <= s1; s += 6) {
     stage(ms0, ns0, ms1, ns1, ns2, s);
@@ -249,91 +340,54 @@ __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, in
   if (s + 4 < s1) stage(ms0, ns1, ms1, ns2, ns0, s + 4);
   __builtin_amdgcn_s_waitcnt(0x0F70);                         // no copy into the LDS outlives the workgroup
 
-  // lane (c, g) holds row c of a block of m at the columns 8 (v / 4) + 4 g + v % 4 of a block of n
-#pragma unroll
-  for (int t = 0; t < TB; t++) {
-    const int m = m0 + (th * TB + t) * 32 + c;
-    const bool there = m < a.m;
-    if constexpr (kGated) {
-      static_assert(!kGated || WB == 2, "gate and up");
-      const int n1 = n0 + wq * 32;
-#pragma unroll
-      for (int q = 0; q < 2; q++) {                           // columns 16 q ..
-        uint32_t first[4], second[4];                         // h, or dg; du
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const int b = 2 * q + e, n = n1 + 8 * b + 4 * g;
-          float dh[4] = {0.f, 0.f, 0.f, 0.f};
-          if constexpr (TO == kToDgu) {
-            if (there && n < a.n) {
-              const u32x2_t d = *(const u32x2_t *)((const bf16_t *)a.dh + (int64_t)m * a.lddh + n);
-              dh[0] = __uint_as_float(d.x << 16); dh[1] = __uint_as_float(d.x & 0xFFFF0000u);
-              dh[2] = __uint_as_float(d.y << 16); dh[3] = __uint_as_float(d.y & 0xFFFF0000u);
-            }
-          }
-          float x[4], y[4];
-#pragma unroll
-          for (int v = 0; v < 4; v++) {
-            const float gate = acc[0][t][4 * b + v], up = acc[WB - 1][t][4 * b + v];
-            const Act r = activation<TO == kToDgu>(a.act, gate);
-            if constexpr (TO == kToH) { x[v] = gate * r.p * up; y[v] = 0.f; }
-            else { x[v] = dh[v] * up * r.slope; y[v] = dh[v] * (gate * r.p); }
-          }
-          first[2 * e] = pack_bf16x2(x[0], x[1]); first[2 * e + 1] = pack_bf16x2(x[2], x[3]);
-          second[2 * e] = pack_bf16x2(y[0], y[1]); second[2 * e + 1] = pack_bf16x2(y[2], y[3]);
-        }
-        const u32x4_t h = gather8(first[0], first[1], first[2], first[3]);
-        const int n = n1 + 16 * q + 8 * g;
-        const bool store = there && n < a.n;
-        if (store) *(u32x4_t *)((bf16_t *)a.out[0] + (int64_t)m * a.ldo + n) = h;
-        if constexpr (TO == kToDgu) {
-          const u32x4_t d = gather8(second[0], second[1], second[2], second[3]);
-          if (store) *(u32x4_t *)((bf16_t *)a.out[1] + (int64_t)m * a.ldo + n) = d;
-        }
-      }
-    } else {
-#pragma unroll
-      for (int w = 0; w < WB; w++) {
-        const int n1 = n0 + (wq * WB + w) * 32;
-        if constexpr (TO == kToParts) {
-#pragma unroll
-          for (int b = 0; b < 4; b++) {
-            const int n = n1 + 8 * b + 4 * g;
-            if (there && n < a.n)
-              *(f32x4_t *)(part + (int64_t)m * a.n + n) = f32x4_t{acc[w][t][4 * b], acc[w][t][4 * b + 1], acc[w][t][4 * b + 2], acc[w][t][4 * b + 3]};
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < 2; q++) {
-            const f32x16_t &s_ = acc[w][t];
-            const u32x4_t o = gather8(pack_bf16x2(s_[8 * q], s_[8 * q + 1]), pack_bf16x2(s_[8 * q + 2], s_[8 * q + 3]), pack_bf16x2(s_[8 * q + 4], s_[8 * q + 5]),
-                                      pack_bf16x2(s_[8 * q + 6], s_[8 * q + 7]));
-            const int n = n1 + 16 * q + 8 * g;
-            if (there && n < a.n) *(u32x4_t *)((bf16_t *)(half ? a.out[1] : a.out[0]) + (int64_t)m * a.ldo + n) = o;
-          }
-        }
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);                        // one block at a time: registers
-  }
+  finish<MB, NB, TO>(a, acc, m0 + th * MB * 16, n0 + wq * NB * (kGated ? 8 : 16), half, part);
 }
 
-// The tile of a workgroup.  Ids 8 apart run on one XCD: it has the n tiles x, x + 8, .. and walks them four at a time, for each m tile those four.
+// The tile of a workgroup.  Ids 8 apart run on one XCD.  The XCDs share the tiles out in m_parts x 8 / m_parts: XCD x has the m tiles x % m_parts, + m_parts, .. and the n
+// tiles x / m_parts, + 8 / m_parts, .., and walks them four n tiles at a time, for each m tile those four (32 compute units then read 8 + 4 panels).
+constexpr int kGroup = 4, kXcdUnits = 32;
+struct TilePlace { int m, n, count; };                        // count: tiles of this XCD
+__device__ __forceinline__ TilePlace tile_place(const FfnArgs &a, int j) {
+  const int x = (int)blockIdx.x % 8, xm = x % a.m_parts, xn = x / a.m_parts, n_parts = 8 / a.m_parts;
+  const int ms = (a.m_tiles * a.halves - xm + a.m_parts - 1) / a.m_parts, ns = (a.n_tiles - xn + n_parts - 1) / n_parts;
+  TilePlace p{-1, -1, ms * ns};
+  if (j >= p.count) return p;
+  const int group = j / (kGroup * ms), in = j - group * kGroup * ms, wide = min(ns - group * kGroup, kGroup);
+  p.n = (group * kGroup + in % wide) * n_parts + xn;
+  p.m = (in / wide) * a.m_parts + xm;
+  return p;
+}
 template <class L, bool MM, bool NM, int TO>
-__global__ __launch_bounds__(L::kThreads, L::kThreads == 512 ? 2 : 2) void ffn_tile_kernel(FfnArgs a) {
-  __shared__ __attribute__((aligned(1024))) unsigned char ms0[L::kMBytes], ms1[L::kMBytes], ns0[L::kNBytes], ns1[L::kNBytes], ns2[L::kNBytes];
-  constexpr int kGroup = 4;
-  const int mt = a.m_tiles * a.halves, x = (int)blockIdx.x % 8, j = (int)blockIdx.x / 8;
-  const int mine = (a.n_tiles - x + 7) / 8;                   // n tiles of this XCD
-  if (j >= mine * mt) return;
-  const int group = j / (kGroup * mt), in = j - group * kGroup * mt, wide = min(mine - group * kGroup, kGroup);
-  const int nt = (group * kGroup + in % wide) * 8 + x, m = in / wide, half = m / a.m_tiles;
-  const int total = a.segs * ((a.k + kStageK - 1) / kStageK), split = blockIdx.y;
+__device__ __forceinline__ void tile_at(const FfnArgs &a, int mt, int nt, int rows, unsigned char *ms0, unsigned char *ms1, unsigned char *ns0, unsigned char *ns1, unsigned char *ns2) {
+  // rows: of the m tile, how far in the body begins
+  const int total = a.segs * ((a.k + kStageK - 1) / kStageK), split = blockIdx.y, half = mt / a.m_tiles;
   const int s0 = (int)((int64_t)total * split / a.splits), s1 = (int)((int64_t)total * (split + 1) / a.splits);
   float *part = TO == kToParts ? a.part + ((int64_t)split * a.halves + half) * (int64_t)a.m * a.n : nullptr;
-  tile_body<L, MM, NM, TO>(a, __builtin_amdgcn_readfirstlane(half), __builtin_amdgcn_readfirstlane((m - half * a.m_tiles) * L::kM),
+  tile_body<L, MM, NM, TO>(a, __builtin_amdgcn_readfirstlane(half), __builtin_amdgcn_readfirstlane((mt - half * a.m_tiles) * a.tile_m + rows),
                            __builtin_amdgcn_readfirstlane(nt * (TO == kToH || TO == kToDgu ? L::kN / 2 : L::kN)), __builtin_amdgcn_readfirstlane(s0),
                            __builtin_amdgcn_readfirstlane(s1), part, ms0, ms1, ns0, ns1, ns2);
+}
+template <class L, bool MM, bool NM, int TO>
+__global__ __launch_bounds__(L::kThreads, 2) void ffn_tile_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char ms0[L::kMBytes], ms1[L::kMBytes], ns0[L::kNBytes], ns1[L::kNBytes], ns2[L::kNBytes];
+  const TilePlace p = tile_place(a, (int)blockIdx.x / 8);
+  if (p.m >= 0) tile_at<L, MM, NM, TO>(a, p.m, p.n, 0, ms0, ms1, ns0, ns1, ns2);
+}
+using Big = Tile<2, 8, 4, 4>;                                 // 256 x 256
+using Mid = Tile<2, 4, 4, 4>;                                 // 128 x 256
+using Small = Tile<2, 4, 2, 4>;                               // 128 x 128
+// Tiles of 256 x 256, and halves of 128 x 256 for what an XCD's compute units would be half empty with (up to 16 tiles behind the last whole round) and for ends of m of up to 128 rows.
+__host__ __device__ inline int halved_tiles(int count) { return count % kXcdUnits <= kXcdUnits / 2 ? count % kXcdUnits : 0; }
+template <bool MM, bool NM, int TO>
+__global__ __launch_bounds__(Big::kThreads, 2) void ffn_mixed_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char ms0[Big::kMBytes], ms1[Big::kMBytes], ns0[Big::kNBytes], ns1[Big::kNBytes], ns2[Big::kNBytes];
+  const int j = (int)blockIdx.x / 8, count = tile_place(a, 0x7FFFFFFF).count, whole = count - halved_tiles(count);
+  const TilePlace p = tile_place(a, j < whole ? j : whole + (j - whole) / 2);
+  if (p.m < 0) return;
+  const int left = a.m - (p.m % a.m_tiles) * Big::kM, rows = j < whole ? 0 : ((j - whole) & 1) * Mid::kM;   // of the tile; of those, where this workgroup begins
+  if (rows >= left) return;
+  if (j < whole && left > Mid::kM) tile_at<Big, MM, NM, TO>(a, p.m, p.n, 0, ms0, ms1, ns0, ns1, ns2);
+  else tile_at<Mid, MM, NM, TO>(a, p.m, p.n, rows, ms0, ms1, ns0, ns1, ns2);
 }
 
 // The ranges' sums, in ascending order: eight columns a thread
@@ -353,10 +407,10 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(const float *part, int sp
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------
-// Up to 64 rows: the weights are read once and little is done with them.  A workgroup has 16 columns of h, its four wavefronts a quarter of k each, with a ring
+// Up to 16 rows: the weights are read once and little is done with them.  A workgroup has 16 columns of h, its four wavefronts a quarter of k each, with a ring
 // of stages of their own in the LDS (16 gate and 16 up rows x 64 k, 4 KB): nobody waits for anybody until the quarters meet.  x comes out of the L2, straight
 // into registers, as many stages ahead.
-constexpr int kFewStage = 4096, kFewRows = 64;
+constexpr int kFewStage = 4096, kFewRows = 16;
 template <int TB>                                             // blocks of 16 rows of x
 __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char r0[4 * kFewStage], r1[4 * kFewStage], r2[4 * kFewStage];   // (arrays of their own: the compiler waits for the copies into what it reads)
@@ -468,39 +522,112 @@ __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
   if (m < a.m && n < a.n) *(u32x2_t *)((bf16_t *)a.out[0] + (int64_t)m * a.ldo + n) = u32x2_t{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
 }
 
-// ---- launches -----------------------------------------------------------------------------------------
+// ---- some rows ---------------------------------------------------------------------------------------
+// 17 to 128 rows: still bound by the weights' way from memory, but x has to come through the LDS too (read by every wavefront for itself it took twice the weights' way: 98 us
+// for 60 rows, 4096 x 14336).  A workgroup has all rows and 32 columns of h, so that there are workgroups enough to keep the memory busy (tiles of 64 columns: 66 us); four
+// wavefronts with a quarter of the rows each; a ring of four (three) stages of 64 k, two workgroups to a compute unit.
+template <int MB, int TO>                                     // MB: blocks of 16 rows of a wavefront
+__global__ __launch_bounds__(256, 2) void ffn_some_kernel(FfnArgs a) {
+  constexpr int kRows = MB * 64, NB = 4, ML = MB * 2, NL = 2, kRing = MB == 1 ? 4 : 3, kBytes = (kRows + 64) * 128;
+  __shared__ __attribute__((aligned(1024))) unsigned char b0[kBytes], b1[kBytes], b2[kBytes], b3[kRing > 3 ? kBytes : 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n0 = blockIdx.x * 32;
+  const int stages = (a.k + kStageK - 1) / kStageK;
+  Side<ML, false, kRows> ms;
+  Side<NL, false, 64> ns;
+#pragma unroll
+  for (int i = 0; i < ML; i++) ms.place(i, wave * ML + i, lane, a.ldm);
+  ms.base[0] = (const char *)a.m_src[0];
+  ms.end[0] = ms.base[0] + ((int64_t)(a.m - 1) * a.ldm + a.k) * 2;
+#pragma unroll
+  for (int i = 0; i < NL; i++) ns.place(i, (wave & 1) * NL + i, lane, a.ldn);   // wavefronts 0 and 1 copy the gate rows, 2 and 3 the up rows
+  const char *w = (const char *)(wave >> 1 ? a.n_src[1] : a.n_src[0]);
+  ns.base[0] = w + (int64_t)n0 * a.ldn * 2;
+  ns.end[0] = w + ((int64_t)(a.n - 1) * a.ldn + a.k) * 2;
+  unsigned char *const ring[4] = {b0, b1, b2, b3};
+  auto copy = [&](unsigned char *to, int s) __attribute__((always_inline)) {
+    s = min(s, stages - 1);                                   // past the end: the last stage again (never read)
+    ns.copy(s, to + kRows * 128 + wave * NL * 1024, 0, NL);
+    ms.copy(s, to + wave * ML * 1024, 0, ML);
+  };
+  f32x4_t acc[NB][MB];
+#pragma unroll
+  for (int b = 0; b < NB; b++)
+#pragma unroll
+    for (int t = 0; t < MB; t++) acc[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const int mat = frag_lane<false, kRows>(lane, wave * MB), nat = kRows * 128 + frag_lane<false, 64>(lane, 0);
+  auto stage = [&](unsigned char *now, unsigned char *free, int s) __attribute__((always_inline)) {
+    // this wavefront's share of the stage has arrived, its reads of the stage before are in registers
+    __builtin_amdgcn_s_waitcnt(0x0070 | ((kRing - 2) * (ML + NL)));
+    const int left = a.k - s * kStageK;
+    if (left < kStageK) {
+      ms.clear(left, wave * ML, now + wave * ML * 1024);
+      ns.clear(left, (wave & 1) * NL, now + kRows * 128 + wave * NL * 1024);
+      __builtin_amdgcn_s_waitcnt(0xC07F);                     // lgkmcnt(0)
+    }
+    wg_barrier();
+    copy(free, s + kRing - 1);
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+      u32x4_t fm[MB], fn[NB];
+#pragma unroll
+      for (int b = 0; b < NB; b++) fn[b] = frag<false, 64>(now, nat, b, j);
+#pragma unroll
+      for (int t = 0; t < MB; t++) fm[t] = frag<false, kRows>(now, mat, t, j);
+#pragma unroll
+      for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int t = 0; t < MB; t++)
+          acc[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, fn[b]), __builtin_bit_cast(bf16x8_t, fm[t]), acc[b][t], 0, 0, 0);
+    }
+  };
+  static_assert((kRing - 2) * (ML + NL) < 16, "the count of the wait");
+#pragma unroll
+  for (int i = 0; i < kRing - 1; i++) copy(ring[i], i);
+  for (int s = 0; s < stages; s += kRing) {
+    stage(b0, ring[kRing - 1], s);
+    if (s + 1 < stages) stage(b1, b0, s + 1);
+    if (s + 2 < stages) stage(b2, b1, s + 2);
+    if constexpr (kRing > 3) { if (s + 3 < stages) stage(b3, b2, s + 3); }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);                         // no copy into the LDS outlives the workgroup
+  finish<MB, NB, TO>(a, acc, wave * MB * 16, n0, 0, nullptr);
+}
 
-using Big = Tile<2, 4, 4, 2>;                                 // 256 x 256
-using Mid = Tile<2, 2, 4, 2>;                                 // 128 x 256
-using Small = Tile<2, 2, 2, 2>;                               // 128 x 128
+// ---- launches -----------------------------------------------------------------------------------------
 
 template <class L, bool MM, bool NM, int TO> hipError_t launch_tiles(FfnArgs a, hipStream_t st) {
   constexpr int kCols = TO == kToH || TO == kToDgu ? L::kN / 2 : L::kN;
+  a.tile_m = L::kM;
   a.m_tiles = (a.m + L::kM - 1) / L::kM;
   a.n_tiles = (a.n + kCols - 1) / kCols;
-  const int64_t grid = (int64_t)a.m_tiles * a.halves * ((a.n_tiles + 7) / 8) * 8;
+  const int mt = a.m_tiles * a.halves;
+  a.m_parts = mt > 1 ? 2 : 1;
+  // the fullest XCD's workgroups, the first one's
+  const int n_parts = 8 / a.m_parts;
+  const int64_t count = (int64_t)((mt + a.m_parts - 1) / a.m_parts) * ((a.n_tiles + n_parts - 1) / n_parts);
+  constexpr bool kMixed = L::kM == 256;
+  const int64_t grid = 8 * (kMixed ? count + kXcdUnits / 2 : count);   // (an XCD may have fewer tiles and more halves)
   if (grid > 0x7FFFFFFF / L::kThreads) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((ffn_tile_kernel<L, MM, NM, TO>), dim3((unsigned)grid, a.splits), dim3(L::kThreads), 0, st, a);
+  if constexpr (kMixed) hipLaunchKernelGGL((ffn_mixed_kernel<MM, NM, TO>), dim3((unsigned)grid, a.splits), dim3(L::kThreads), 0, st, a);
+  else hipLaunchKernelGGL((ffn_tile_kernel<L, MM, NM, TO>), dim3((unsigned)grid, a.splits), dim3(L::kThreads), 0, st, a);
   return hipGetLastError();
 }
 
 // Which tile, and into how many ranges k is cut (1: not at all)
-struct FfnPlan { int tile, splits; };                         // tile: 0 .. 2, as above
-constexpr int kTileM[3] = {256, 128, 128}, kTileN[3] = {256, 256, 128};
+struct FfnPlan { int tile, splits; };                         // tile 0: 256 x 256 and halves, 1: 128 x 128
+constexpr int kTileM[2] = {256, 128}, kTileN[2] = {256, 128};
 FfnPlan ffn_plan(int64_t m, int64_t n, int64_t k, int halves, int segs, bool gated) {
   const int stages = segs * (int)((k + kStageK - 1) / kStageK);
-  FfnPlan p{0, 1};
   auto tiles = [&](int t) { const int64_t cols = gated ? kTileN[t] / 2 : kTileN[t]; return ((m + kTileM[t] - 1) / kTileM[t]) * ((n + cols - 1) / cols) * halves; };
-  while (p.tile < 2 && tiles(p.tile) < 256) p.tile++;
-  if (!gated && tiles(p.tile) < 256) {
-    int64_t s = 256 / tiles(p.tile);
-    s = s < stages / 4 ? s : stages / 4;
-    p.splits = s < 1 ? 1 : s > 32 ? 32 : (int)s;
-  }
+  FfnPlan p{tiles(0) >= 64 ? 0 : 1, 1};
+  if (gated) return p;
+  const int64_t ranges = p.tile == 0 ? 128 / tiles(0) : 512 / tiles(1), most = stages / 4 < 16 ? stages / 4 : 16;
+  p.splits = (int)(ranges < most ? ranges : most);
+  if (p.splits < 1) p.splits = 1;
   return p;
 }
 template <bool MM, bool NM, int TO> hipError_t launch_planned(const FfnArgs &a, int tile, hipStream_t st) {
-  return tile == 0 ? launch_tiles<Big, MM, NM, TO>(a, st) : tile == 1 ? launch_tiles<Mid, MM, NM, TO>(a, st) : launch_tiles<Small, MM, NM, TO>(a, st);
+  return tile == 0 ? launch_tiles<Big, MM, NM, TO>(a, st) : launch_tiles<Small, MM, NM, TO>(a, st);
 }
 // A product into out, through ranges' sums if k is cut
 template <bool MM, bool NM> hipError_t launch_product(FfnArgs a, hipStream_t st) {
@@ -527,13 +654,21 @@ uint64_t ffn_grad_scratch_bytes(int rows, int d, int f) {
   return 2 * up256((uint64_t)rows * f * 2) + up256(x > w ? x : w);
 }
 
+// Which of the three takes a forward call (us; few / some / tiles of 128 x 128): 16 rows of 4096 x 11008 37.8 / 45.6 / 58.2, 24 46.5 / 45.8 / 58.6, 60 74 / 48.9 / 61.4, 128 - / 62.2 / 65.8;
+// of 4096 x 14336 16 48.7 / 52.2 / 60.9, 60 98 / 55.0 / 64.0, 128 - / 66.2 / 68.1; of 1024 x 2752 16 6.1 / 9.7 / 14.1, 60 11.3 / 10.1 / 14.5.  Where the tiles fill the
+// chip by themselves they have less of x to read: 8192 x 28672 16 165 / 174 / 177, 32 208 / 177 / 177, 60 304 / 189 / 176, 128 - / 240 / 178.
+static bool some_pays(int rows, int f) { return rows <= 32 || (rows <= 128 && (f + 63) / 64 < 256); }
+
 hipError_t launch_ffn(const FfnCall &c, hipStream_t st) {
   FfnArgs a{};
   a.m = c.rows; a.n = c.f; a.k = c.d; a.segs = a.halves = a.splits = 1; a.act = c.act;
   a.m_src[0] = c.x; a.ldm = c.ldx; a.n_src[0] = c.wg; a.n_src[1] = c.wu; a.ldn = c.ldw; a.out[0] = c.h; a.ldo = c.ldh;
+  if (c.rows > kFewRows && some_pays(c.rows, c.f)) {
+    hipLaunchKernelGGL((c.rows <= 64 ? ffn_some_kernel<1, kToH> : ffn_some_kernel<2, kToH>), dim3((c.f + 31) / 32), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
   if (c.rows > kFewRows) return launch_planned<false, false, kToH>(a, ffn_plan(a.m, a.n, a.k, 1, 1, true).tile, st);
-  const auto kernel = c.rows <= 16 ? ffn_few_kernel<1> : c.rows <= 32 ? ffn_few_kernel<2> : c.rows <= 48 ? ffn_few_kernel<3> : ffn_few_kernel<4>;
-  hipLaunchKernelGGL(kernel, dim3((c.f + 15) / 16), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(ffn_few_kernel<1>, dim3((c.f + 15) / 16), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -371,6 +371,7 @@ struct FfnArgs {                        // out[m][n] = sum over k of the two sid
   void *out[2];  int64_t ldo;
   float *part;                          // [range][half][m][n]
   int m_tiles, n_tiles, splits;
+  int tile_m, m_parts;                  // rows of an m tile; parts of the m tiles that XCDs share out
 };
 uint64_t ffn_grad_scratch_bytes(int rows, int d, int f);
 hipError_t launch_ffn(const FfnCall &c, hipStream_t st);
