@@ -15,6 +15,7 @@ namespace spec {
 namespace {
 
 constexpr int kTile = 4096, kRun = 32, kRuns = 1024;          // positions of a tile and of the two lengths of runs
+constexpr int kLongLeast = 8192;                              // positions from which on the longer runs are summed (below, a walk meets 256 sums at most)
 constexpr int kEmbedThreads = 256;
 
 // Eight columns of a row at a time (VEC), or one.  A thread's columns do not change from row to row.
@@ -61,12 +62,21 @@ __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(const int *tok
   constexpr int kEach = kTile / 16;
   const int j0 = wave * kEach;
   int smaller = 0;
-  const bool own = j0 <= first - tile && first - tile < j0 + kEach;   // this share holds the workgroup's positions
-  const int below = key + (j0 < first - tile ? 1 : 0);        // equal keys of earlier positions count
-  for (int j = j0; j < j0 + kEach && j < n; j += 4) {         // (what lies behind n is larger than any key)
-    const int4 k = *(const int4 *)(sh + j);
-    if (own) smaller += (k.x < key + (j < me)) + (k.y < key + (j + 1 < me)) + (k.z < key + (j + 2 < me)) + (k.w < key + (j + 3 < me));
-    else smaller += (k.x < below) + (k.y < below) + (k.z < below) + (k.w < below);
+  auto under = [&](int from, int to, int limit) {             // keys under the limit in part of the share (what lies behind n is larger than any key)
+#pragma unroll 8
+    for (int j = from; j < to; j += 4) {
+      const int4 k = *(const int4 *)(sh + j);
+      smaller += (k.x < limit) + (k.y < limit) + (k.z < limit) + (k.w < limit);
+    }
+  };
+  if (j0 < n) {                                               // equal keys of earlier positions count
+    const int begin = min(max(first - tile, j0), j0 + kEach), end = min(max(first - tile + kRankMine, j0), j0 + kEach);   // the workgroup's own positions
+    under(j0, begin, key + 1);
+    for (int j = begin; j < end; j += 4) {
+      const int4 k = *(const int4 *)(sh + j);
+      smaller += (k.x < key + (j < me)) + (k.y < key + (j + 1 < me)) + (k.z < key + (j + 2 < me)) + (k.w < key + (j + 3 < me));
+    }
+    under(end, j0 + kEach, key);
   }
   count[threadIdx.x] = smaller;
   __syncthreads();
@@ -85,12 +95,24 @@ __global__ __launch_bounds__(kRankThreads) void embed_merge_kernel(const int *ti
   const int key = i < rows ? tile_keys[i] : 0;
   int place = i - mine * kTile;
   const int tiles = (rows + kTile - 1) / kTile;
+  constexpr int kEach = kTile / kRankThreads;
+  int ahead[kEach];                                           // the next tile's keys, asked for before this one's are searched
+  auto ask = [&](int t) {
+#pragma unroll
+    for (int e = 0; e < kEach; e++) {
+      const int j = t * kTile + e * kRankThreads + threadIdx.x;
+      ahead[e] = t < tiles && j < rows ? tile_keys[j] : 0;
+    }
+  };
+  ask(mine == 0 ? 1 : 0);
   for (int t = 0; t < tiles; t++) {
     if (t == mine) continue;
     const int n = min(rows - t * kTile, kTile);
     __syncthreads();
-    for (int j = threadIdx.x; j < n; j += kRankThreads) sh[j] = tile_keys[t * kTile + j];
+#pragma unroll
+    for (int e = 0; e < kEach; e++) sh[e * kRankThreads + threadIdx.x] = ahead[e];
     __syncthreads();
+    ask(t + 1 == mine ? t + 2 : t + 1);
     const int below = key + (t < mine ? 1 : 0);               // how many of this tile come before: keys under `below`
     int lo = 0, hi = n;
     while (lo < hi) {
@@ -109,21 +131,43 @@ template <int W> __device__ __forceinline__ void add_columns(Columns<W> &s, cons
 #pragma unroll
   for (int j = 0; j < W; j++) s.x[j] += v.x[j];
 }
-template <int W> __device__ __forceinline__ Columns<W> row_columns(const void *p, int64_t i, int bf16) {
+template <int W> __device__ __forceinline__ Columns<W> row_columns(const void *p, int64_t i, bool bf16) {
   Columns<W> r;
   if constexpr (W == 8) widen8(load8(p, i, bf16), bf16, r.x);
   else r.x[0] = load1(p, i, bf16);
   return r;
 }
 
-// The first sorted position of every token (starts[vocab]: where padding begins), and the runs of 32.
-template <int W>
+// The number of keys below v, by one wavefront: 64 places are looked at at a time.  Every lane gets it.
+__device__ __forceinline__ int keys_below(const int *keys, int rows, int v) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = rows;                                      // keys[i] < v for i < lo, not for i >= hi
+  while (lo < hi) {
+    const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const uint64_t less = __ballot(at < hi && keys[min(at, rows - 1)] < v);   // (a run of the first lanes: the keys are sorted)
+    const int n = __popcll(less);
+    if (n == 0) return lo;
+    hi = min(hi, lo + n * step);
+    lo += (n - 1) * step + 1;
+  }
+  return lo;
+}
+
+// The first sorted position of every token (starts[vocab]: where padding begins; a workgroup has 256 tokens, whose share of the keys two of its wavefronts look up first), and the runs of 32.
+// BF16: dy's type (asked at each load, every load waited for the one before).
+template <int W, bool BF16>
 __global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(EmbedGradArgs a, const int *keys, const int *order, int *starts, int start_groups, float *runs) {
+  __shared__ int range[2];
   if ((int)blockIdx.x < start_groups) {
     if (blockIdx.y != 0) return;
-    const int v = blockIdx.x * kEmbedThreads + threadIdx.x;
+    const int v0 = blockIdx.x * kEmbedThreads, v = v0 + threadIdx.x, wave = threadIdx.x >> 6;
+    if (wave < 2) {
+      const int n = keys_below(keys, a.rows, v0 + wave * kEmbedThreads);
+      if ((threadIdx.x & 63) == 0) range[wave] = n;
+    }
+    __syncthreads();
     if (v > a.vocab) return;
-    int lo = 0, hi = a.rows;
+    int lo = range[0], hi = range[1];
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       if (keys[mid] < v) lo = mid + 1; else hi = mid;
@@ -135,9 +179,9 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(EmbedGradArgs
   const int key = keys[run * kRun];
   if (key >= a.vocab || key != keys[run * kRun + kRun - 1]) return;
   for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * W; c < a.d; c += gridDim.y * kEmbedThreads * W) {
-    Columns<W> s = row_columns<W>(a.dy, order[run * kRun] * a.ldy + c, a.dtype);
-#pragma unroll 8
-    for (int i = 1; i < kRun; i++) add_columns<W>(s, row_columns<W>(a.dy, order[run * kRun + i] * a.ldy + c, a.dtype));
+    Columns<W> s = row_columns<W>(a.dy, order[run * kRun] * a.ldy + c, BF16);
+#pragma unroll 16
+    for (int i = 1; i < kRun; i++) add_columns<W>(s, row_columns<W>(a.dy, order[run * kRun + i] * a.ldy + c, BF16));
     if constexpr (W == 8) store8(runs, (int64_t)run * a.d + c, 0, s.x);
     else runs[(int64_t)run * a.d + c] = s.x[0];
   }
@@ -158,12 +202,26 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_long_runs_kernel(const in
 
 // A few table rows to a workgroup (blockIdx.y: its share of the columns).
 constexpr int kTableRows = 8;
-template <int W>
+template <int W, bool BF16>
 __global__ __launch_bounds__(kEmbedThreads) void embed_table_kernel(EmbedGradArgs a, const int *order, const int *starts, const float *runs, const float *long_runs) {
   const int v0 = blockIdx.x * kTableRows, vn = min(a.vocab - v0, kTableRows);
-  for (int r = 0; r < vn; r++) {
-    const int v = v0 + r, s0 = starts[v], s1 = starts[v + 1];
-    if (a.accumulate && s0 == s1) continue;
+  int start[kTableRows + 1];                                  // (all asked for at once; most rows of a large vocabulary have no token, and their zeros go out first)
+#pragma unroll
+  for (int r = 0; r <= kTableRows; r++) start[r] = starts[min(v0 + r, a.vocab)];
+  uint32_t full = 0;
+#pragma unroll
+  for (int r = 0; r < kTableRows; r++) {
+    if (start[r] != start[r + 1]) full |= 1u << r;
+    else if (!a.accumulate && r < vn)
+      for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * W; c < a.d; c += gridDim.y * kEmbedThreads * W) {
+        const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const int64_t at = (v0 + r) * a.ldt + c;
+        if constexpr (W == 8) store8(a.dtable, at, a.out_dtype, zero);
+        else store1(a.dtable, at, a.out_dtype, 0.f);
+      }
+  }
+  for (; full != 0; full &= full - 1) {
+    const int v = v0 + __builtin_ctz(full), s0 = starts[v], s1 = starts[v + 1];
     for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * W; c < a.d; c += gridDim.y * kEmbedThreads * W) {
       Columns<W> s;
 #pragma unroll
@@ -171,16 +229,18 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_table_kernel(EmbedGradArg
       int i = s0;
       auto single = [&](int to) {
 #pragma unroll 4
-        for (; i < to; i++) add_columns<W>(s, row_columns<W>(a.dy, order[i] * a.ldy + c, a.dtype));
+        for (; i < to; i++) add_columns<W>(s, row_columns<W>(a.dy, order[i] * a.ldy + c, BF16));
       };
       auto whole = [&](const float *p, int length, int to) {  // runs, from a multiple of their length on
-#pragma unroll 4
-        for (; i + length <= to; i += length) add_columns<W>(s, row_columns<W>(p, (int64_t)(i / length) * a.d + c, 0));
+#pragma unroll 8
+        for (; i + length <= to; i += length) add_columns<W>(s, row_columns<W>(p, (int64_t)(i / length) * a.d + c, false));
       };
       single(min(s1, (i + kRun - 1) / kRun * kRun));
       if (i + kRun <= s1) {
-        whole(runs, kRun, min(s1, (i + kRuns - 1) / kRuns * kRuns));
-        whole(long_runs, kRuns, s1);
+        if (a.rows >= kLongLeast) {
+          whole(runs, kRun, min(s1, (i + kRuns - 1) / kRuns * kRuns));
+          whole(long_runs, kRuns, s1);
+        }
         whole(runs, kRun, s1);
       }
       single(s1);
@@ -209,27 +269,27 @@ EmbedScratch embed_scratch(int rows, int vocab, int d) {
   s.tile_order = take(rows > kTile ? 4ull * rows : 0);
   s.starts = take(4ull * (vocab + 1));
   s.runs = take(4ull * (rows / kRun) * d);
-  s.long_runs = take(4ull * (rows / kRuns) * d);
+  s.long_runs = take(rows >= kLongLeast ? 4ull * (rows / kRuns) * d : 0);
   s.bytes = at;
   return s;
 }
 
 bool eights(const void *p, int64_t ld, int bf16, int64_t rows) { return ((uintptr_t)p & 15) == 0 && (rows <= 1 || ld % (bf16 ? 8 : 4) == 0); }
 
-template <int W> hipError_t embed_sums(const EmbedGradArgs &a, const EmbedScratch &s, char *base, hipStream_t st) {
+template <int W, bool BF16> hipError_t embed_sums(const EmbedGradArgs &a, const EmbedScratch &s, char *base, hipStream_t st) {
   int *keys = (int *)(base + s.keys), *order = (int *)(base + s.order), *starts = (int *)(base + s.starts);
   float *runs = (float *)(base + s.runs), *long_runs = (float *)(base + s.long_runs);
   const int slices = (a.d + kEmbedThreads * W - 1) / (kEmbedThreads * W), start_groups = (a.vocab + kEmbedThreads) / kEmbedThreads;
   const int ys = slices > 64 ? 64 : slices;
-  hipLaunchKernelGGL(embed_runs_kernel<W>, dim3(start_groups + a.rows / kRun, ys), dim3(kEmbedThreads), 0, st, a, keys, order, starts, start_groups, runs);
+  hipLaunchKernelGGL((embed_runs_kernel<W, BF16>), dim3(start_groups + a.rows / kRun, ys), dim3(kEmbedThreads), 0, st, a, keys, order, starts, start_groups, runs);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.rows >= kRuns) {
+  if (a.rows >= kLongLeast) {
     const int wide = (a.d + kEmbedThreads - 1) / kEmbedThreads;
     hipLaunchKernelGGL(embed_long_runs_kernel, dim3(a.rows / kRuns, wide > 64 ? 64 : wide), dim3(kEmbedThreads), 0, st, keys, a.vocab, a.d, runs, long_runs);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(embed_table_kernel<W>, dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
+  hipLaunchKernelGGL((embed_table_kernel<W, BF16>), dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
   return hipGetLastError();
 }
 
@@ -262,7 +322,8 @@ hipError_t launch_embed_grad(EmbedGradArgs a, void *scratch, hipStream_t st) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   const bool vec = a.d % 8 == 0 && eights(a.dy, a.ldy, a.dtype, a.rows) && eights(a.dtable, a.ldt, a.out_dtype, a.vocab);
-  return vec ? embed_sums<8>(a, s, base, st) : embed_sums<1>(a, s, base, st);
+  if (vec) return a.dtype ? embed_sums<8, true>(a, s, base, st) : embed_sums<8, false>(a, s, base, st);
+  return a.dtype ? embed_sums<1, true>(a, s, base, st) : embed_sums<1, false>(a, s, base, st);
 }
 
 }  // namespace spec

@@ -13,7 +13,7 @@ namespace spec {
 
 namespace {
 
-constexpr int kGradThreads = 256, kGradUnroll = 4, kGradChunk = kGradThreads * kGradUnroll * 8;
+constexpr int kGradThreads = 256, kGradUnroll = 8, kGradChunk = kGradThreads * kGradUnroll * 8;
 
 struct Chunk { int tensor; int64_t first; };                  // first: the chunk's first element, from -7 on
 __device__ __forceinline__ Chunk chunk_of(const GradArgs &a, int c) {
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_clip_kernel(GradArgs a) {
   const float factor = ratio < 1.0 ? (float)frexp(ratio, &down) : ratio == ratio ? 1.f : (float)ratio;
   const bool none = factor == 1.f && down == 0;
   for (int b = blockIdx.x; b < a.chunks; b += gridDim.x) {
-    const Chunk at = chunk_of(a, b);
+    const Chunk at = chunk_of(a, a.chunks - 1 - b);           // (last first: what the sums have read last is still in the last-level cache)
     const GradTensor t = a.t[at.tensor];
     if (t.out == t.g && none) continue;
     const int64_t n = t.count & kGradCount;

@@ -14,7 +14,9 @@ namespace spec {
 namespace {
 
 constexpr int kNormWg = 256, kNormTable = 1024;               // threads, and table entries of a workgroup
-constexpr int kGradGroups = 512;                              // workgroups of a part that leave shares of dw
+// Workgroups of a launch, shared out among the parts by their heads: as many as run at once (gradients three to a compute unit, else four), so that every one has about the
+// same number of rows and their table is made once.
+constexpr int kGradGroups = 768, kForwardGroups = 1024;
 
 // Sum over the aligned group of 2^n lanes that a lane is in; all 64 lanes take part
 __device__ __forceinline__ float group_sum(float x, int group) {
@@ -123,36 +125,40 @@ template <bool VEC, bool INTER> __device__ __forceinline__ void turn_dims(float 
   }
 }
 
-// Part blockIdx.y; runs of rows_each rows, every gridDim.x-th of them.
-template <bool VEC, bool GRAD, bool INTER>
+// Runs of rows_each rows of a part, every groups-th of them.  TYPE: of x (and dy) in all parts, or kAny: asked at each access (then one waits for the other).
+enum { kFp32 = 0, kBf16 = 1, kAny = 2 };
+template <bool VEC, bool GRAD, bool INTER, int TYPE>
 __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
   constexpr int E = Dims<VEC>::kElems;
   __shared__ float2 table[kNormTable];
   __shared__ float shares[GRAD ? kNormWg * E : 1];            // of dw: [element of a lane][thread]
-  const HeadnormPart p = a.part[blockIdx.y];
+  const int n = (int)blockIdx.x >= a.first[2] ? 2 : (int)blockIdx.x >= a.first[1] ? 1 : 0, wg = blockIdx.x - a.first[n];
+  const HeadnormPart p = a.part[n];
   const int group = a.group, slots = kNormWg / group, lane = threadIdx.x & (group - 1), slot = threadIdx.x / group;
   const int half = a.rot / 2, heads = p.p.heads, hd = a.hd;
   const Dims<VEC> m = dims_of<VEC>(lane, a.items, group, a.rot, a.interleaved != 0);
   const bool normed = p.w != nullptr;
+  const int y_type = TYPE == kAny ? p.p.dtype : TYPE, x_type = TYPE == kAny ? p.x_dtype : TYPE;
   float w[E], dw[E];
 #pragma unroll
   for (int j = 0; j < E; j++) w[j] = dw[j] = 0.f;
   if (normed) {
-    if constexpr (VEC) {                                      // (one at a time: w need not be aligned to more than its type)
+    if (VEC && ((uintptr_t)p.w & 15) != 0) {                  // (aligned to its type only)
 #pragma unroll
       for (int j = 0; j < 8; j++) {
-        if (m.kind[0] != kIdle) w[j] = p.offset + load1(p.w, m.first[0] + j, p.w_dtype);
-        if (m.kind[0] == kPairs) w[8 + j] = p.offset + load1(p.w, m.first[0] + half + j, p.w_dtype);
+        if (m.kind[0] != kIdle) w[j] = load1(p.w, m.first[0] + j, p.w_dtype);
+        if (VEC && m.kind[0] == kPairs) w[E - 8 + j] = load1(p.w, m.first[0] + half + j, p.w_dtype);
       }
     } else {
       widen_dims<VEC>(load_dims<VEC>(p.w, 0, p.w_dtype, m, half), p.w_dtype, m, w);
-#pragma unroll
-      for (int j = 0; j < E; j++) w[j] += p.offset;           // (of absent dims: meets zeros)
     }
+#pragma unroll
+    for (int j = 0; j < E; j++) w[j] += p.offset;             // (of absent dims: meets zeros)
   }
   const float each = 1.0f / (float)hd;
-  for (int64_t row0 = (int64_t)blockIdx.x * a.rows_each; row0 < a.rows; row0 += (int64_t)gridDim.x * a.rows_each) {
-    const int rows = (int)min((int64_t)a.rows_each, a.rows - row0), total = rows * heads;
+  const int rows_each = a.rows_each[n], groups = a.first[n + 1] - a.first[n];
+  for (int64_t row0 = (int64_t)wg * rows_each; row0 < a.rows; row0 += (int64_t)groups * rows_each) {
+    const int rows = (int)min((int64_t)rows_each, a.rows - row0), total = rows * heads;
     struct Place { int row; int64_t y, x, o; };
     auto place_of = [&](int i) {
       Place q;
@@ -170,8 +176,8 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
     auto ask = [&](int i) {
       if (i >= total) return;                                 // (the last values again, never used)
       next = place_of(i);
-      ny = load_dims<VEC>(p.p.x, next.y, p.p.dtype, m, half);
-      if (GRAD && normed) nx = load_dims<VEC>(p.x, next.x, p.x_dtype, m, half);
+      ny = load_dims<VEC>(p.p.x, next.y, y_type, m, half);
+      if (GRAD && normed) nx = load_dims<VEC>(p.x, next.x, x_type, m, half);
     };
     ask(slot);
     __syncthreads();                                          // nobody reads the last rows' table any more
@@ -187,8 +193,8 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
       const bool mine = i < total;
       const Place now = next;
       float y[E], x[E];
-      widen_dims<VEC>(ny, p.p.dtype, m, y);
-      if (GRAD && normed) widen_dims<VEC>(nx, p.x_dtype, m, x);
+      widen_dims<VEC>(ny, y_type, m, y);
+      if (GRAD && normed) widen_dims<VEC>(nx, x_type, m, x);
       ask(i + slots);
       const float2 *cs = table + (mine ? now.row : 0) * half;
       if constexpr (!GRAD) {
@@ -225,9 +231,9 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
 #pragma unroll
     for (int j = 0; j < E; j++) shares[j * kNormWg + threadIdx.x] = dw[j];
     __syncthreads();
-    float *out = a.scratch + ((int64_t)blockIdx.y * kGradGroups + blockIdx.x) * hd;
-    for (int n = threadIdx.x; n < group * E; n += kNormWg) {
-      const int l = n / E, j = n - l * E;
+    float *out = a.scratch + ((int64_t)n * kGradGroups + wg) * hd;
+    for (int i = threadIdx.x; i < group * E; i += kNormWg) {
+      const int l = i / E, j = i - l * E;
       const Dims<VEC> d = dims_of<VEC>(l, a.items, group, a.rot, a.interleaved != 0);
       int dim = -1;
       if constexpr (VEC) {
@@ -249,12 +255,13 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
 }
 
 // The workgroups' shares of dw, in their order: a thread adds up every eighth, then eight threads meet.
-__global__ __launch_bounds__(256) void headnorm_dw_kernel(HeadnormArgs a, int groups) {
+__global__ __launch_bounds__(256) void headnorm_dw_kernel(HeadnormArgs a) {
   __shared__ float sh[256];
   const HeadnormPart p = a.part[blockIdx.y];
   if (p.dw == nullptr) return;
   const int dim = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
   const float *share = a.scratch + (int64_t)blockIdx.y * kGradGroups * a.hd;
+  const int groups = a.first[blockIdx.y + 1] - a.first[blockIdx.y];
   float s = 0.f;
   if (dim < a.hd) {
 #pragma unroll 8
@@ -270,40 +277,51 @@ __global__ __launch_bounds__(256) void headnorm_dw_kernel(HeadnormArgs a, int gr
 
 bool eights(const void *p, int64_t ld, int64_t hs, int bf16) { const int64_t e = bf16 ? 8 : 4; return ((uintptr_t)p & 15) == 0 && ld % e == 0 && hs % e == 0; }
 
+template <bool GRAD, bool INTER> auto of_type(int type) {
+  return type == kFp32 ? headnorm_kernel<true, GRAD, INTER, kFp32> : type == kBf16 ? headnorm_kernel<true, GRAD, INTER, kBf16> : headnorm_kernel<true, GRAD, INTER, kAny>;
+}
+
 hipError_t launch(HeadnormArgs a, bool grad, hipStream_t st) {
   // eight dims at a time where every access is a multiple of 16 bytes from a multiple of 16 bytes
   bool vec = a.hd % 8 == 0 && a.rot % (a.interleaved ? 8 : 16) == 0;
-  int most = 0;
+  int heads = 0;
   for (int n = 0; n < a.n_parts; n++) {
     const HeadnormPart &p = a.part[n];
     vec = vec && eights(p.p.x, p.p.ldx, p.p.hsx, p.p.dtype) && eights(p.p.out, p.p.ldo, p.p.hso, p.p.out_dtype);
     if (grad && p.w) vec = vec && eights(p.x, p.ld, p.hs, p.x_dtype);
-    most = p.p.heads > most ? p.p.heads : most;
+    heads += p.p.heads;
   }
   const int half = a.rot / 2;
   a.items = vec ? (a.interleaved ? a.hd / 8 : half / 8 + (a.hd - a.rot) / 8) : half + a.hd - a.rot;
   a.group = 1;
   while (a.group < (vec ? a.items : 64)) a.group *= 2;
-  const int slots = kNormWg / a.group;
-  int each = (grad ? 4 : 2) * slots / most;                   // heads that a lane meets in a run of rows
-  each = each < 1 ? 1 : each > 32 ? 32 : each;
-  if (half > 0 && each * half > kNormTable) each = kNormTable / half;
-  while (each > 1 && a.rows / each < 256) each /= 2;          // (rather more workgroups than compute units)
-  a.rows_each = each;
-  int64_t groups = ((int64_t)a.rows + each - 1) / each;
-  const int64_t limit = grad ? kGradGroups : 1 << 20;         // (further runs are taken in turn)
-  groups = groups < limit ? groups : limit;
-  const dim3 grid((unsigned)groups, a.n_parts);
-  const auto kernel = !vec ? (grad ? headnorm_kernel<false, true, false> : headnorm_kernel<false, false, false>)
-                      : a.interleaved ? (grad ? headnorm_kernel<true, true, true> : headnorm_kernel<true, false, true>)
-                                      : (grad ? headnorm_kernel<true, true, false> : headnorm_kernel<true, false, false>);
+  const int slots = kNormWg / a.group, all = grad ? kGradGroups : kForwardGroups, most_rows = half > 0 ? kNormTable / half : 1024;
+  a.first[0] = 0;
+  for (int n = 0; n < 3; n++) {
+    if (n >= a.n_parts) { a.first[n + 1] = 0x7FFFFFFF; a.rows_each[n] = 1; continue; }
+    int64_t groups = (int64_t)all * a.part[n].p.heads / heads;
+    groups = groups < 1 ? 1 : groups;
+    int64_t each = (a.rows + groups - 1) / groups;
+    const int64_t fill = slots / a.part[n].p.heads < a.rows / 512 ? slots / a.part[n].p.heads : a.rows / 512;   // (a lane group each, where there are rows for it)
+    each = each < fill ? fill : each;
+    each = each < 1 ? 1 : each > most_rows ? most_rows : each;
+    const int64_t runs = (a.rows + each - 1) / each;
+    a.rows_each[n] = (int)each;
+    a.first[n + 1] = a.first[n] + (int)(runs < groups ? runs : groups);
+  }
+  const dim3 grid((unsigned)a.first[a.n_parts]);
+  int type = a.part[0].p.dtype;
+  for (int n = 0; n < a.n_parts; n++)
+    if (a.part[n].p.dtype != type || (grad && a.part[n].w && a.part[n].x_dtype != type)) type = kAny;
+  const auto kernel = !vec ? (grad ? headnorm_kernel<false, true, false, kAny> : headnorm_kernel<false, false, false, kAny>)
+                      : a.interleaved ? (grad ? of_type<true, true>(type) : of_type<false, true>(type)) : (grad ? of_type<true, false>(type) : of_type<false, false>(type));
   hipLaunchKernelGGL(kernel, grid, dim3(kNormWg), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !grad) return e;
   bool any = false;
   for (int n = 0; n < a.n_parts; n++) any = any || a.part[n].dw != nullptr;
   if (!any) return hipSuccess;
-  hipLaunchKernelGGL(headnorm_dw_kernel, dim3((a.hd + 31) / 32, a.n_parts), dim3(256), 0, st, a, (int)groups);
+  hipLaunchKernelGGL(headnorm_dw_kernel, dim3((a.hd + 31) / 32, a.n_parts), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

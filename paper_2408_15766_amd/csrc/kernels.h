@@ -401,7 +401,8 @@ struct HeadnormArgs {
   double turns[kRotaryMaxPlanes];
   float eps;
   float *scratch;                       // gradients: [part][workgroup][hd]
-  int rows_each, items, group;          // set by the launch
+  int items, group;                     // set by the launch: steps of a head, lanes of one,
+  int rows_each[3], first[4];           // rows of a workgroup's run in a part, and the part's first workgroup
 };
 int headnorm_grad_groups();             // workgroups of a part that leave a share of dw
 hipError_t launch_headnorm(HeadnormArgs a, hipStream_t st);
