@@ -7,6 +7,7 @@ with autograd.
 from __future__ import annotations
 
 import ctypes as C
+import itertools
 import struct
 from typing import Optional, Sequence
 
@@ -119,13 +120,6 @@ _norm_parts = [struct.Struct("@" + (_part + "Qif") * n).pack for n in range(4)] 
 _norm_grad_parts = [struct.Struct("@" + (_part + "QifQqqQii") * n).pack for n in range(4)]
 
 
-def _heads(what: str, name: str, t, shape):
-    """Row and head strides of a tensor of heads."""
-    if tuple(t.shape) != tuple(shape) or (shape[2] > 1 and t.stride(2) != 1):
-        _refuse(what, f"{name} has to be {tuple(shape)} with dense heads")
-    return t.stride(0), t.stride(1)
-
-
 def _positions(what: str, pos, rows: int):
     """(pointer, first position) of the rows' positions."""
     import torch
@@ -138,10 +132,29 @@ def _positions(what: str, pos, rows: int):
     return None, int(pos)
 
 
-def _part_shape(what: str, t, rows: int, hd: int):
-    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != hd or not 1 <= t.shape[1] <= 1024 or rows > _INT_MAX or hd > SPEC_ROPE_MAX_DIM:
-        _refuse(what, f"tensors have to be [{rows}, up to 1024 heads, {hd}]")
-    return t.shape
+# (Most of a small call is the host's share, 10 us beside a kernel of 5: each thing is asked once, in the loop.)
+
+def _outs(like, dtypes):
+    """New dense tensors [rows, heads, hd] beside those of `like`."""
+    made = []
+    for t, d in zip(like, dtypes):
+        rows, heads, hd = t.shape
+        made.append(_new((rows, heads, hd), (heads * hd, hd, 1), d, t))
+    return made
+
+
+def _rotary_fields(what: str, x, o, turn, rows: int, hd: int, name: str):
+    """spec_rotary_part of a tensor and its output."""
+    import torch
+    shape, dtype, out_dtype, bf16, fp32 = x.shape, x.dtype, o.dtype, torch.bfloat16, torch.float32
+    if len(shape) != 3 or shape[0] != rows or shape[2] != hd or shape != o.shape or shape[1] > 1024:
+        _refuse(what, f"{name} and outputs have to be [{rows}, up to 1024 heads, {hd}]")
+    (ldx, hsx, one), (ldo, hso, two) = x.stride(), o.stride()
+    if hd > 1 and not one == two == 1:
+        _refuse(what, "the dims of a head have to be dense")
+    if (dtype is not bf16 and dtype is not fp32) or (out_dtype is not bf16 and out_dtype is not fp32):
+        _refuse(what, f"{dtype} to {out_dtype} (float32 and bfloat16 are supported)")
+    return (x.data_ptr(), o.data_ptr(), ldx, hsx, ldo, hso, shape[1], dtype is bf16, out_dtype is bf16, bool(turn))
 
 
 def _weight(what: str, w, hd: int):
@@ -159,22 +172,23 @@ def spec_k_headnorm_rotary(plan: spec_rotary_plan_t, xs: Sequence, pos, weights:
     import torch
     what = "spec_k_headnorm_rotary"
     n = len(xs)
-    if not 1 <= n <= 3 or xs[0].dim() != 3:
+    if not 1 <= n <= 3 or any(x.dim() != 3 for x in xs):
         _refuse(what, "one to three tensors [rows, heads, hd] are needed")
-    if outs is None:
-        kinds = [x.dtype for x in xs] if out_dtypes is None else out_dtypes
-        outs = [torch.empty_like(x, dtype=d, memory_format=torch.contiguous_format) for x, d in zip(xs, kinds)]
+    made = outs is None
+    if made:
+        outs = _outs(xs, [x.dtype for x in xs] if out_dtypes is None else out_dtypes)
     if len(outs) != n or len(weights) != n or (turned is not None and len(turned) != n):
         _refuse(what, "as many outputs, weights and flags as tensors are needed")
-    stream = _here(what, *xs, *outs, *weights, pos if isinstance(pos, torch.Tensor) else None)
+    stream = _here(what, *xs, *(() if made else outs), *weights, pos if isinstance(pos, torch.Tensor) else None)
     rows, _, hd = xs[0].shape
+    if rows > _INT_MAX or hd > SPEC_ROPE_MAX_DIM:
+        _refuse(what, f"{rows} rows, heads of {hd}")
     at, first = _positions(what, pos, rows)
     fields = []
     for x, o, w, turn in zip(xs, outs, weights, (True,) * n if turned is None else turned):
-        shape = _part_shape(what, x, rows, hd)
-        wp, wd = _weight(what, w, hd)
-        fields += (x.data_ptr(), o.data_ptr(), *_heads(what, "x", x, shape), *_heads(what, "an output", o, shape), shape[1], _dtype_code(what, x.dtype),
-                   _dtype_code(what, o.dtype), bool(turn), wp, wd, offset)
+        fields += _rotary_fields(what, x, o, turn, rows, hd, "tensors")
+        fields += _weight(what, w, hd)
+        fields.append(offset)
     rc = lib.spec_k_headnorm_rotary(C.byref(plan), n, _norm_parts[n](*fields), hd, rows, at, first, eps, stream)
     if rc:
         raise SpecError(rc, f"{what}: {rows} rows, heads of {hd}, plan over {plan.rot}, eps {eps}")
@@ -193,29 +207,32 @@ def spec_k_headnorm_rotary_grad(plan: spec_rotary_plan_t, dys: Sequence, xs: Seq
     import torch
     what = "spec_k_headnorm_rotary_grad"
     n = len(dys)
-    if not 1 <= n <= 3 or dys[0].dim() != 3:
+    if not 1 <= n <= 3 or any(t.dim() != 3 for t in dys):
         _refuse(what, "one to three tensors [rows, heads, hd] are needed")
-    if outs is None:
-        kinds = [t.dtype for t in dys] if out_dtypes is None else out_dtypes
-        outs = [torch.empty_like(t, dtype=d, memory_format=torch.contiguous_format) for t, d in zip(dys, kinds)]
+    made = outs is None
+    if made:
+        outs = _outs(dys, [t.dtype for t in dys] if out_dtypes is None else out_dtypes)
     if len(outs) != n or len(xs) != n or len(weights) != n or (turned is not None and len(turned) != n):
         _refuse(what, "as many inputs, outputs, weights and flags as gradients are needed")
-    stream = _here(what, *dys, *outs, *xs, *weights, scratch, pos if isinstance(pos, torch.Tensor) else None)
+    stream = _here(what, *dys, *(() if made else outs), *xs, *weights, scratch, pos if isinstance(pos, torch.Tensor) else None)
     rows, _, hd = dys[0].shape
-    if hd > SPEC_ROPE_MAX_DIM:
-        _refuse(what, f"heads of {hd}")
+    if rows > _INT_MAX or hd > SPEC_ROPE_MAX_DIM:
+        _refuse(what, f"{rows} rows, heads of {hd}")
     at, first = _positions(what, pos, rows)
     dws, fields = [], []
     for dy, x, o, w, turn in zip(dys, xs, outs, weights, (True,) * n if turned is None else turned):
-        shape = _part_shape(what, dy, rows, hd)
-        wp, wd = _weight(what, w, hd)
-        dw = None if w is None else _new((hd,), (1,), torch.float32, dy)
+        fields += _rotary_fields(what, dy, o, turn, rows, hd, "gradients")
+        fields += _weight(what, w, hd)
+        fields.append(offset)
+        if w is None:
+            dws.append(None)
+            fields += (0, 0, 0, 0, 0, 0)
+            continue
+        if x is None or x.shape != dy.shape or (hd > 1 and x.stride(2) != 1):
+            _refuse(what, f"the input of a normed tensor has to be {tuple(dy.shape)} with dense heads")
+        dw = _new((hd,), (1,), torch.float32, dy)
         dws.append(dw)
-        if w is not None and x is None:
-            _refuse(what, "the input of a normed tensor is needed")
-        given = (0, 0, 0) if w is None else (x.data_ptr(), *_heads(what, "x", x, shape))
-        fields += (dy.data_ptr(), o.data_ptr(), *_heads(what, "dy", dy, shape), *_heads(what, "an output", o, shape), shape[1], _dtype_code(what, dy.dtype),
-                   _dtype_code(what, o.dtype), bool(turn), wp, wd, offset, *given, 0 if dw is None else dw.data_ptr(), 0 if w is None else _dtype_code(what, x.dtype), 0)
+        fields += (x.data_ptr(), x.stride(0), x.stride(1), dw.data_ptr(), _dtype_code(what, x.dtype), 0)
     need = lib.spec_k_headnorm_rotary_grad_scratch_bytes(n, hd) if any(w is not None for w in weights) else 0
     scratch, room = _room(what, scratch, need, dys[0])
     rc = lib.spec_k_headnorm_rotary_grad(C.byref(plan), n, _norm_grad_parts[n](*fields), hd, rows, at, first, eps, None if scratch is None else scratch.data_ptr(), room,
@@ -300,16 +317,27 @@ def spec_k_ffn_gated_grad(x, w_gate, w_up, dh, act: str = "silu", outs: Optional
 
 # ---- gradient clipping ------------------------------------------------------------------------------
 
-_grad_part = struct.Struct("@QQqii")
+_grad_dtypes = {}                                               # torch's two types -> the C ABI's (torch is imported by the first call)
 
 
 def _grad_fields(what: str, grads, outs):
-    packed = bytearray(_grad_part.size * len(grads))
-    for i, (g, o) in enumerate(zip(grads, outs)):
-        if not g.is_contiguous() or not o.is_contiguous() or g.shape != o.shape:
-            _refuse(what, "gradients and outputs have to be contiguous, of the same shapes")
-        _grad_part.pack_into(packed, i * _grad_part.size, g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(what, g.dtype), _dtype_code(what, o.dtype))
-    return bytes(packed)
+    """spec_grad_part, as often as there are tensors.  By maps over the tensors' methods: a loop took 2 us a tensor."""
+    import torch
+    tensor, device = torch.Tensor, torch.cuda.current_device()
+    if not _grad_dtypes:
+        _grad_dtypes.update({torch.float32: 0, torch.bfloat16: 1})
+    every = grads if outs is grads else [*grads, *outs]
+    if not all(map(tensor.is_contiguous, every)):
+        _refuse(what, "gradients and outputs have to be contiguous")
+    if any(at != device for at in map(tensor.get_device, every)):
+        _refuse(what, f"tensors on {sorted({str(t.device) for t in every})}, and the current device is cuda:{device}")
+    types = [_grad_dtypes.get(t.dtype) for t in every]
+    if None in types:
+        _refuse(what, f"{[t.dtype for t in every][types.index(None)]} (float32 and bfloat16 are supported)")
+    where, sizes, n = list(map(tensor.data_ptr, every)), list(map(tensor.numel, every)), len(grads)
+    if sizes[:n] != sizes[-n:] and n:
+        _refuse(what, "outputs have to have as many elements as their gradients")
+    return struct.pack("@" + "QQqii" * n, *itertools.chain.from_iterable(zip(where[:n], where[-n:], sizes, types[:n], types[-n:]))) if n else b""
 
 
 def spec_k_grad_sums(grads: Sequence, sums=None):
@@ -324,7 +352,7 @@ def spec_k_grad_sums(grads: Sequence, sums=None):
         sums = _new((SPEC_GRAD_SUMS,), (1,), torch.float64, beside)
     elif sums.dtype is not torch.float64 or tuple(sums.shape) != (SPEC_GRAD_SUMS,) or not sums.is_contiguous():
         _refuse(what, f"sums has to be float64 [{SPEC_GRAD_SUMS}]")
-    stream = _here(what, *grads, sums)
+    stream = _here(what, sums)
     rc = lib.spec_k_grad_sums(len(grads), _grad_fields(what, grads, grads), sums.data_ptr(), stream)
     if rc:
         raise SpecError(rc, f"{what}: {len(grads)} tensors")
@@ -332,7 +360,7 @@ def spec_k_grad_sums(grads: Sequence, sums=None):
 
 
 def spec_k_grad_clip(grads: Sequence, sums, max_norm: float, outs: Optional[Sequence] = None):
-    """The tensors times min(1, max_norm / (norm + 1e-6)), norm^2 the sum of `sums` (spec_k_grad_sums): in place, or into `outs` (same shapes, bf16 or fp32).  Returns the
+    """The tensors times min(1, max_norm / (norm + 1e-6)), norm^2 the sum of `sums` (spec_k_grad_sums): in place, or into `outs` (of as many elements, bf16 or fp32).  Returns the
     norm before that, a float32 tensor [] on the device; nothing waits for it."""
     import torch
     what = "spec_k_grad_clip"
@@ -340,7 +368,7 @@ def spec_k_grad_clip(grads: Sequence, sums, max_norm: float, outs: Optional[Sequ
         _refuse(what, f"sums has to be float64 [{SPEC_GRAD_SUMS}]")
     if outs is not None and len(outs) != len(grads):
         _refuse(what, "as many outputs as gradients are needed")
-    stream = _here(what, sums, *grads, *(() if outs is None else outs))
+    stream = _here(what, sums)
     norm = _new((), (), torch.float32, sums)
     rc = lib.spec_k_grad_clip(len(grads), _grad_fields(what, grads, grads if outs is None else outs), sums.data_ptr(), max_norm, norm.data_ptr(), stream)
     if rc:

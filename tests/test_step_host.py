@@ -1,0 +1,153 @@
+"""Operators of a training step, what needs no GPU: sizes of scratch, refusals of the C ABI, and the oracle against itself."""
+import ctypes as C
+import itertools
+import struct
+
+import numpy as np
+import pytest
+
+from oracle import step as O
+
+X = 1 << 20   # an address that is aligned and never read: every call below is refused first
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2408_15766_amd as pkg
+    return pkg
+
+
+def refused(rc):
+    assert rc == -1
+
+
+def test_scratch_sizes(P):
+    for bad in ((0, 8, 8), (-1, 8, 8), ((1 << 20) + 1, 8, 8), (8, 0, 8), (8, (1 << 24) + 1, 8), (8, 8, 0), (8, 8, (1 << 20) + 1), (2 ** 32 + 1, 8, 8)):
+        assert P.spec_k_embed_grad_scratch_bytes(*bad) == 0
+    assert P.spec_k_embed_grad_scratch_bytes(1, 1, 1) % 256 == 0 and P.spec_k_embed_grad_scratch_bytes(1 << 20, 1 << 24, 1 << 20) > 1 << 36
+    assert P.spec_k_headnorm_rotary_grad_scratch_bytes(0, 64) == 0 and P.spec_k_headnorm_rotary_grad_scratch_bytes(4, 64) == 0
+    assert P.spec_k_headnorm_rotary_grad_scratch_bytes(1, 257) == 0 and P.spec_k_headnorm_rotary_grad_scratch_bytes(3, 256) > 0
+    for bad in ((0, 64, 64), (64, 60, 64), (64, 64, 4), (64, 0, 64), ((1 << 20) + 1, 64, 64), (64, (1 << 20) + 8, 64), (1 << 20, 1 << 17, 8), (8, 1 << 19, 1 << 18), (2 ** 32 + 8, 8, 8)):
+        assert P.spec_k_ffn_gated_grad_scratch_bytes(*bad) == 0
+    assert P.spec_k_ffn_gated_grad_scratch_bytes(64, 64, 64) >= 2 * 64 * 64 * 2
+    assert P.spec_k_ffn_gated_grad_scratch_bytes(1 << 20, 8, 1 << 16) >= 1 << 38
+
+
+def test_embed_refusals(P):
+    good = dict(dtype=1, table=X, ldt=64, vocab=100, d=64, tok=2 * X, rows=8, out_dtype=0, out=3 * X, ldo=64)
+    for kw in (dict(dtype=2), dict(out_dtype=-1), dict(table=None), dict(tok=None), dict(out=None), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(d=0), dict(d=(1 << 20) + 1), dict(rows=0),
+               dict(rows=-5), dict(rows=(1 << 24) + 1), dict(ldt=63), dict(ldo=63), dict(ldt=-64), dict(ldo=1 << 41), dict(table=X + 1), dict(out=3 * X + 2), dict(tok=2 * X + 2), dict(out=X),
+               dict(out=2 * X)):
+        a = {**good, **kw}
+        refused(P.lib.spec_k_embed(a["dtype"], a["table"], a["ldt"], a["vocab"], a["d"], a["tok"], a["rows"], 1.0, a["out_dtype"], a["out"], a["ldo"], None))
+    good = dict(dtype=1, dy=X, ldy=64, tok=2 * X, rows=8, d=64, vocab=100, out_dtype=0, dt=3 * X, ldt=64, scratch=4 * X, n=1 << 40)
+    for kw in (dict(dtype=2), dict(out_dtype=2), dict(dy=None), dict(tok=None), dict(dt=None), dict(scratch=None), dict(rows=0), dict(rows=(1 << 20) + 1), dict(d=0), dict(vocab=0), dict(ldy=60),
+               dict(ldt=60), dict(scratch=4 * X + 16), dict(n=100), dict(dy=X + 1), dict(dt=X), dict(dt=2 * X), dict(dt=4 * X), dict(scratch=X), dict(scratch=2 * X)):
+        a = {**good, **kw}
+        refused(P.lib.spec_k_embed_grad(a["dtype"], a["dy"], a["ldy"], a["tok"], a["rows"], a["d"], a["vocab"], 1.0, 0, a["out_dtype"], a["dt"], a["ldt"], a["scratch"], a["n"], None))
+
+
+ROTARY = dict(x=X, out=2 * X, ldx=256, hsx=64, ldo=256, hso=64, heads=4, dtype=1, out_dtype=1, turn=1)
+ROTARY_BAD = (dict(x=0), dict(out=0), dict(ldx=63), dict(hsx=63), dict(ldo=-1), dict(hso=10), dict(heads=0), dict(heads=1025), dict(dtype=2), dict(out_dtype=5), dict(x=X + 1), dict(out=2 * X + 1),
+              dict(out=X, out_dtype=0), dict(out=X, ldo=320), dict(ldx=1 << 41))
+
+
+def fields(d, more):
+    return struct.pack("@QQqqqqiiii" + more[0], *d.values(), *more[1:])
+
+
+def test_headnorm_refusals(P):
+    plan = P.spec_rotary_plan(32, 1e4)
+
+    def call(parts, n=1, hd=64, rows=8, pos=None, eps=1e-6, plan=plan):
+        return P.lib.spec_k_headnorm_rotary(C.byref(plan) if plan else None, n, parts, hd, rows, pos, 0, eps, None)
+    ok = fields(ROTARY, ("Qif", 3 * X, 1, 0.0))
+    for kw in (dict(n=0), dict(n=4), dict(hd=0), dict(hd=257), dict(hd=30), dict(rows=0), dict(rows=(1 << 24) + 1), dict(pos=X + 2), dict(eps=-1.0), dict(eps=float("nan")),
+               dict(eps=float("inf")), dict(plan=None)):
+        refused(call(ok * 4, **kw))
+    refused(call(None))
+    for kw in ROTARY_BAD:
+        refused(call(fields({**ROTARY, **kw}, ("Qif", 3 * X, 1, 0.0))))
+    for w in (("Qif", 3 * X + 1, 1, 0.0), ("Qif", 3 * X, 2, 0.0), ("Qif", 3 * X, 1, float("inf")), ("Qif", 2 * X, 1, 0.0)):
+        refused(call(fields(ROTARY, w)))
+    other = {**ROTARY, "x": 4 * X, "out": 5 * X}
+    for a, b in ((ROTARY, {**other, "out": 2 * X}), (ROTARY, {**other, "out": X}), (ROTARY, {**other, "x": 2 * X}), (ROTARY, {**other, "out": 3 * X})):
+        refused(call(fields(a, ("Qif", 3 * X, 1, 0.0)) + fields(b, ("Qif", 6 * X, 1, 0.0)), n=2))
+
+
+def test_headnorm_grad_refusals(P):
+    plan = P.spec_rotary_plan(32, 1e4)
+
+    def more(w=3 * X, wd=1, off=0.0, x=4 * X, ld=256, hs=64, dw=5 * X, xd=1):
+        return ("QifQqqQii", w, wd, off, x, ld, hs, dw, xd, 0)
+
+    def call(parts, n=1, hd=64, rows=8, pos=None, eps=1e-6, scratch=6 * X, room=1 << 40):
+        return P.lib.spec_k_headnorm_rotary_grad(C.byref(plan), n, parts, hd, rows, pos, 0, eps, scratch, room, None)
+    ok = fields(ROTARY, more())
+    for kw in (dict(n=0), dict(n=4), dict(hd=257), dict(rows=0), dict(pos=X + 1), dict(eps=-1.0), dict(scratch=None), dict(scratch=6 * X + 64), dict(room=0), dict(scratch=X), dict(scratch=4 * X)):
+        refused(call(ok * 4, **kw))
+    for kw in ROTARY_BAD:
+        refused(call(fields({**ROTARY, **kw}, more())))
+    for kw in (dict(w=0), dict(w=3 * X + 1), dict(wd=7), dict(x=0), dict(x=4 * X + 1), dict(ld=63), dict(hs=63), dict(dw=5 * X + 2), dict(xd=3), dict(x=2 * X), dict(dw=4 * X), dict(dw=X), dict(dw=2 * X),
+               dict(dw=3 * X)):
+        refused(call(fields(ROTARY, more(**kw))))
+    second = {**ROTARY, "x": 8 * X, "out": 9 * X}
+    for a, b in ((second, more(w=10 * X, x=2 * X, dw=11 * X)), ({**second, "out": 4 * X}, more(w=10 * X, x=12 * X, dw=11 * X)), (second, more(w=10 * X, x=12 * X, dw=5 * X))):
+        refused(call(fields(ROTARY, more()) + fields(a, b), n=2))
+
+
+def test_ffn_refusals(P):
+    good = dict(x=X, ldx=64, rows=8, d=64, wg=2 * X, wu=3 * X, ldw=64, f=128, act=0, h=4 * X, ldh=128)
+    bad = (dict(x=None), dict(wg=None), dict(wu=None), dict(h=None), dict(rows=0), dict(rows=-1), dict(rows=(1 << 20) + 1), dict(d=60, ldx=60), dict(d=0), dict(f=4), dict(f=132), dict(act=3), dict(act=-1),
+           dict(ldx=56), dict(ldx=68), dict(ldw=72 - 4), dict(ldh=120), dict(ldx=1 << 22), dict(x=X + 8), dict(wg=2 * X + 2), dict(h=4 * X + 8), dict(h=X), dict(h=2 * X), dict(h=3 * X))
+    for kw in bad:
+        a = {**good, **kw}
+        refused(P.lib.spec_k_ffn_gated(a["x"], a["ldx"], a["rows"], a["d"], a["wg"], a["wu"], a["ldw"], a["f"], a["act"], a["h"], a["ldh"], None))
+    good.update(dx=5 * X, lddx=64, dwg=6 * X, dwu=7 * X, lddw=64, s=8 * X, n=1 << 40)
+    for kw in bad[:-3] + (dict(dwg=None), dict(dwu=None), dict(dx=5 * X + 8), dict(lddx=60), dict(lddw=8), dict(s=None), dict(s=8 * X + 16), dict(n=100), dict(dx=X), dict(dx=4 * X), dict(dwg=2 * X),
+                     dict(dwu=6 * X), dict(dx=8 * X), dict(s=X), dict(s=7 * X)):
+        a = {**good, **kw}
+        refused(P.lib.spec_k_ffn_gated_grad(a["x"], a["ldx"], a["rows"], a["d"], a["wg"], a["wu"], a["ldw"], a["f"], a["act"], a["h"], a["ldh"], a["dx"], a["lddx"], a["dwg"], a["dwu"],
+                                            a["lddw"], a["s"], a["n"], None))
+
+
+def test_grad_clip_refusals(P):
+    def parts(*rows):
+        return struct.pack("@" + "QQqii" * len(rows), *itertools.chain.from_iterable(rows))
+    one = (X, 2 * X, 100, 0, 0)
+    sums, norm = 8 * X, 9 * X
+    for p, s, n in ((parts(one), None, 1), (parts(one), sums + 4, 1), (None, sums, 1), (parts(one), sums, -1), (parts((X, 0, -1, 0, 0)), sums, 1), (parts((0, 0, 5, 0, 0)), sums, 1),
+                    (parts((X + 2, 0, 5, 0, 0)), sums, 1), (parts((X, 0, 5, 2, 0)), sums, 1), (parts((sums, 0, 5, 0, 0)), sums, 1), (parts((X, 0, (1 << 40) + 1, 0, 0)), sums, 1)):
+        refused(P.lib.spec_k_grad_sums(n, p, s, None))
+
+    def clip(p, n=1, s=sums, limit=1.0, to=norm):
+        return P.lib.spec_k_grad_clip(n, p, s, limit, to, None)
+    for kw in (dict(n=-1), dict(s=None), dict(s=sums + 4), dict(limit=-1.0), dict(limit=float("nan")), dict(limit=float("inf")), dict(to=norm + 1), dict(to=sums)):
+        refused(clip(parts(one), **kw))
+    for p in (parts((X, 0, 5, 0, 0)), parts((X, 2 * X + 1, 5, 0, 0)), parts((X, 2 * X, 5, 0, 3)), parts((X, X, 5, 0, 1)), parts((X, sums, 5, 0, 0)), parts((X, norm, 5, 0, 0))):
+        refused(clip(p))
+    # outputs that overlap: the same tensor twice (in place too), neighbours, an output over another's gradient
+    for p in (parts(one, (3 * X, 2 * X, 100, 0, 0)), parts((X, X, 100, 0, 0), (X, X, 100, 0, 0)), parts(one, (3 * X, 2 * X + 396, 100, 0, 0)), parts(one, (2 * X + 200, 4 * X, 100, 0, 0)),
+              parts(one, (3 * X, X + 4, 10, 0, 0)), parts((X, X + 8, 100, 0, 0)), parts((X, 2 * X, 100, 0, 1), (3 * X, 2 * X + 196, 4, 0, 0))):
+        refused(clip(p, n=len(p) // 32))
+
+
+def test_oracle_gradients_against_differences():
+    rng = np.random.default_rng(0)
+
+    def check(value, args, grads, step=1e-6):
+        for i, g in enumerate(grads):
+            h = rng.standard_normal(args[i].shape)
+            hi, lo = (value(*[a + (s * h if j == i else 0) for j, a in enumerate(args)]) for s in (step, -step))
+            assert abs((hi - lo) / (2 * step) - (g * h).sum()) < 1e-6 * (np.abs(g * h).sum() + 1)
+    x, w, g = rng.standard_normal((3, 2, 12)), rng.standard_normal(12), rng.standard_normal((3, 2, 12))
+    pos, f = np.array([0, 5, 77]), np.array([1.0, 0.1, 0.01, 0.001])
+    for layout in ("half", "interleaved"):
+        check(lambda x, w: (O.headnorm_rotary(x, w, 1e-5, 1.0, pos, f, 1.2, 8, layout) * g).sum(), [x, w], O.headnorm_rotary_grad(g, x, w, 1e-5, 1.0, pos, f, 1.2, 8, layout))
+    x, wg, wu, dh = rng.standard_normal((5, 6)), rng.standard_normal((7, 6)), rng.standard_normal((7, 6)), rng.standard_normal((5, 7))
+    for act in ("silu", "gelu", "gelu_tanh"):
+        check(lambda *a: (O.ffn_gated(*a, act) * dh).sum(), [x, wg, wu], O.ffn_gated_grad(x, wg, wu, dh, act))
+    table, tok, dy = rng.standard_normal((4, 3)), np.array([1, -1, 3, 1, 9]), rng.standard_normal((5, 3))
+    check(lambda t: (O.embed(t, tok, 0.5) * dy).sum(), [table], [O.embed_grad(dy, tok, 4, 0.5)])
+    norm, scaled = O.grad_clip([x, wg], 0.5)
+    assert abs(np.sqrt(sum((s * s).sum() for s in scaled)) - 0.5) < 1e-5 and abs(norm ** 2 - (x * x).sum() - (wg * wg).sum()) < 1e-9
