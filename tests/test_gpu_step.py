@@ -558,3 +558,204 @@ def test_clip_sums_of_two_parts_add_up(P):
             close(g, v, np.abs(v) * (2.1 * U32 + 1.01 * unit(g.dtype)))
     kept = torch.empty(P.SPEC_GRAD_SUMS, dtype=torch.float64, device="cuda")
     assert float(P.spec_k_grad_clip([], P.spec_k_grad_sums([], sums=kept), 0.5)) == 0.0
+
+
+# ---- together -----------------------------------------------------------------------------------------
+
+def step_state(seed, rows=200, vocab=300, heads=4, hd=64, f=264):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+    d = heads * hd
+    s = dict(rows=rows, vocab=vocab, heads=heads, hd=hd, d=d, f=f)
+    s["table"], s["w"] = randn(vocab, d).bfloat16(), (1 + 0.2 * randn(hd)).bfloat16()
+    s["wg"], s["wu"] = ((randn(f, d) / d ** 0.5).bfloat16() for _ in range(2))
+    s["tok"], s["dh"] = torch.randint(-1, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32), (randn(rows, f) * 0.1).bfloat16()
+    return s
+
+
+def train_step(P, plan, s, limit=0.5):
+    """Lookup, norm and turning of the heads, feed-forward block, and back; every gradient, clipped into fp32."""
+    rows, heads, hd, d = s["rows"], s["heads"], s["hd"], s["d"]
+    e = P.spec_k_embed(s["table"], s["tok"], scale=0.7).view(rows, heads, hd)
+    x = P.spec_k_headnorm_rotary(plan, [e], 3, [s["w"]])[0].view(rows, d)
+    h = P.spec_k_ffn_gated(x, s["wg"], s["wu"])
+    dx, dwg, dwu = P.spec_k_ffn_gated_grad(x, s["wg"], s["wu"], s["dh"])
+    (de,), (dw,) = P.spec_k_headnorm_rotary_grad(plan, [dx.view(rows, heads, hd)], [e], 3, [s["w"]])
+    dt = P.spec_k_embed_grad(de.view(rows, d), s["tok"], s["vocab"], scale=0.7, out_dtype=torch.float32)
+    grads = [dt, dw, dwg, dwu]
+    outs = [torch.empty(t.shape, dtype=torch.float32, device="cuda") for t in grads]
+    norm = P.spec_k_grad_clip(grads, P.spec_k_grad_sums(grads), limit, outs=outs)
+    return [h, norm] + outs
+
+
+def test_a_training_step(P):
+    """Against the derivative in 64 bits of the whole step.  Along the way to a gradient lie at most nine roundings to bf16 (rows, x, dx, dg or du, the result ..), each of at most u16 of a value,
+    and every map between them is linear or nearly so at that size: in the Frobenius norm the gradients are at most 9 u16 and what the slopes of the activation and the norm add
+    (at most as much again) off; rows without a token, whose heads are zeros, are left out of the norm's gradient (their mean square is eps alone)."""
+    s = step_state(1)
+    plan = P.spec_rotary_plan(64, 1e4)
+    f, m = L.rope_frequencies(64, 1e4)
+    got = train_step(P, plan, s)
+    rows, heads, hd = s["rows"], s["heads"], s["hd"]
+    leaves = [s[k].double().requires_grad_() for k in ("table", "w", "wg", "wu")]
+    table, w, wg, wu = leaves
+    real = s["tok"] >= 0
+    e = torch.where(real[:, None], table[s["tok"].clamp(min=0).long()], 0.0).view(rows, heads, hd) * 0.7
+    z = e / torch.sqrt((e * e).mean(-1, keepdim=True) + 1e-6) * w
+    t = (3 + torch.arange(rows, device="cuda", dtype=torch.float64))[:, None, None] * torch.from_numpy(f).cuda()
+    c, n = torch.cos(t), torch.sin(t)
+    a, b = z[..., :32], z[..., 32:]
+    x = torch.cat([a * c - b * n, b * c + a * n], -1).view(rows, -1)
+    g, u = x @ wg.t(), x @ wu.t()
+    h = g * torch.sigmoid(g) * u
+    grads = torch.autograd.grad((h * s["dh"].double()).sum(), leaves)
+    norm = torch.sqrt(sum((q * q).sum() for q in grads))
+    bound = 18 * U16
+    assert float((got[0].double() - h.detach()).norm() / h.detach().norm()) <= bound
+    assert abs(float(got[1]) / float(norm) - 1) <= bound
+    for o, q in zip(got[2:], grads):
+        assert float((o.double() - q * (0.5 / norm)).norm() / (q * (0.5 / norm)).norm()) <= 2 * bound
+    total = float(torch.sqrt(sum((o.double() ** 2).sum() for o in got[2:])))
+    assert abs(total - 0.5) <= 0.5 * 8 * U32 + 1e-6
+
+
+def test_a_training_step_in_a_graph_and_on_another_stream(P):
+    plan = P.spec_rotary_plan(64, 1e4)
+    s = step_state(1)
+    others = [step_state(2 + i) for i in range(4)]
+    changing = ("table", "w", "wg", "wu", "tok", "dh")
+    want = [[t.clone() for t in train_step(P, plan, o)] for o in others]
+
+    def put(o):
+        for k in changing:
+            s[k].copy_(o[k])
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        put(others[0])
+        got = train_step(P, plan, s)
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want[0]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = train_step(P, plan, s)
+    for i in (1, 2, 0, 3, 3):
+        put(others[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
+        assert all(torch.equal(a, b) for a, b in zip(train_step(P, plan, s), want[i]))   # eager work between the replays
+        torch.cuda.synchronize()
+
+
+def test_two_training_steps_at_once(P):
+    plan = P.spec_rotary_plan(64, 1e4)
+    sides = [step_state(7), step_state(8, rows=5000, f=1032)]
+    want = [[t.clone() for t in train_step(P, plan, s)] for s in sides]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sides]
+    for _ in range(5):
+        got = []
+        for s, stream in zip(sides, streams):
+            with torch.cuda.stream(stream):
+                got.append(train_step(P, plan, s))
+        torch.cuda.synchronize()
+        for g, t in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(g, t))
+
+
+def test_scratch_of_the_callers(P):
+    """Kept for two calls, dirty; too little is refused."""
+    rows, vocab, d = 5000, 64, 40
+    dy, tok = rand(1, rows, d).cuda(), tokens(2, rows, vocab)
+    x, wg, wu, dh = ffn_case(5, 300, 512, 264)
+    plan = P.spec_rotary_plan(64, 1e4)
+    q = rand(3, 50, 4, 64).cuda()
+    w = rand(4, 64).cuda()
+    for n, call in ((P.spec_k_embed_grad_scratch_bytes(rows, vocab, d), lambda **kw: [P.spec_k_embed_grad(dy, tok, vocab, **kw)]),
+                    (P.spec_k_ffn_gated_grad_scratch_bytes(300, 512, 264), lambda **kw: list(P.spec_k_ffn_gated_grad(x, wg, wu, dh, **kw))),
+                    (P.spec_k_headnorm_rotary_grad_scratch_bytes(1, 64), lambda **kw: sum(P.spec_k_headnorm_rotary_grad(plan, [q], [q], 0, [w], **kw), []))):
+        want = call()
+        kept = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+        for _ in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(call(scratch=kept), want))
+        with pytest.raises(P.SpecError):
+            call(scratch=kept[:n - 256])
+
+
+def test_refusals_of_the_binding(P):
+    E, bf = P.SpecError, torch.bfloat16
+    t, tok = rand(1, 50, 16).cuda(), tokens(1, 9, 50)
+    dy = rand(2, 9, 16).cuda()
+    x, wg, wu, dh = ffn_case(5, 20, 64, 40)
+    plan = P.spec_rotary_plan(32, 1e4)
+    q, w = rand(3, 9, 4, 64).cuda(), rand(4, 64).cuda()
+    sums = P.spec_k_grad_sums([t])
+    far = torch.empty(2 ** 32 + 64, dtype=bf, device="cuda")
+    for call in (lambda: P.spec_k_embed(t.cpu(), tok), lambda: P.spec_k_embed(t, tok.cpu()), lambda: P.spec_k_embed(t, tok.long()), lambda: P.spec_k_embed(t.half(), tok), lambda: P.spec_k_embed(t.t(), tok),
+                 lambda: P.spec_k_embed(t, tok, out=torch.empty(8, 16, device="cuda")), lambda: P.spec_k_embed(t, tok, out=dy, out_dtype=bf), lambda: P.spec_k_embed(t, tok[:0]),
+                 lambda: P.spec_k_embed(t, tok, out=t[:9]), lambda: P.spec_k_embed(far.view(-1, 1), tok), lambda: P.spec_k_embed(t[:1].expand(50, 16), tok),
+                 lambda: P.spec_k_embed_grad(dy[:8], tok, 50), lambda: P.spec_k_embed_grad(dy, tok, 0), lambda: P.spec_k_embed_grad(dy, tok, 2 ** 32 + 50), lambda: P.spec_k_embed_grad(dy, tok, 50, accumulate=True),
+                 lambda: P.spec_k_embed_grad(dy, tok, 50, out=t[:49]), lambda: P.spec_k_embed_grad(dy[:1].expand(9, 16), tok, 50), lambda: P.spec_k_embed_grad(far.view(-1, 1), tok, 50),
+                 lambda: P.spec_k_headnorm_rotary(plan, [q], 0, []), lambda: P.spec_k_headnorm_rotary(plan, [q], 0, [w[:63]]), lambda: P.spec_k_headnorm_rotary(plan, [q], 0, [w.half()]),
+                 lambda: P.spec_k_headnorm_rotary(plan, [q], 0, [w], eps=-1.0), lambda: P.spec_k_headnorm_rotary(plan, [q, q[:8]], 0, [w, w]), lambda: P.spec_k_headnorm_rotary(plan, [q.transpose(1, 2)], 0, [w]),
+                 lambda: P.spec_k_headnorm_rotary(plan, [q], 2 ** 31, [w]), lambda: P.spec_k_headnorm_rotary(plan, [q], tok[:8], [w]), lambda: P.spec_k_headnorm_rotary(plan, [q, q], 0, [w, w], outs=[q, q]),
+                 lambda: P.spec_k_headnorm_rotary(plan, [q.cpu()], 0, [w]), lambda: P.spec_k_headnorm_rotary(plan, [q[0]], 0, [w]), lambda: P.spec_k_headnorm_rotary(plan, [q[:, :1].expand(9, 4, 64)], 0, [w]),
+                 lambda: P.spec_k_headnorm_rotary_grad(plan, [q], [None], 0, [w]), lambda: P.spec_k_headnorm_rotary_grad(plan, [q], [q[:8]], 0, [w]), lambda: P.spec_k_headnorm_rotary_grad(plan, [q], [q], 0, [w], outs=[q[:8]]),
+                 lambda: P.spec_k_ffn_gated(x.float(), wg, wu), lambda: P.spec_k_ffn_gated(x, wg, wu, act="relu"), lambda: P.spec_k_ffn_gated(x[:, :60], wg[:, :60], wu[:, :60]),
+                 lambda: P.spec_k_ffn_gated(x[:, 4:60], wg[:, 4:60], wu[:, 4:60]), lambda: P.spec_k_ffn_gated(x, wg[:39], wu[:39]), lambda: P.spec_k_ffn_gated(x, wg, wu[:32]), lambda: P.spec_k_ffn_gated(x, wg.t(), wu.t()),
+                 lambda: P.spec_k_ffn_gated(x, wg, wu.repeat(1, 2)[:, :64]), lambda: P.spec_k_ffn_gated(x.cpu(), wg, wu), lambda: P.spec_k_ffn_gated(x, wg, wu, out=torch.empty(20, 40, device="cuda")),
+                 lambda: P.spec_k_ffn_gated(x[:1].expand(20, 64), wg, wu), lambda: P.spec_k_ffn_gated(x[:0], wg, wu),
+                 lambda: P.spec_k_ffn_gated_grad(x, wg, wu, dh[:19]), lambda: P.spec_k_ffn_gated_grad(x, wg, wu, dh.float()), lambda: P.spec_k_ffn_gated_grad(x, wg, wu, dh, want=(False, False)),
+                 lambda: P.spec_k_ffn_gated_grad(x, wg, wu, dh, outs=(x, None, None)), lambda: P.spec_k_ffn_gated_grad(x, wg, wu, dh, outs=(x.clone(), None, None), want=(False, True)),
+                 lambda: P.spec_k_ffn_gated_grad(x, wg, wu, dh, outs=(None, wg.clone(), wu.repeat(1, 2)[:, :64])),
+                 lambda: P.spec_k_grad_sums([]), lambda: P.spec_k_grad_sums([t.half()]), lambda: P.spec_k_grad_sums([t.t()]), lambda: P.spec_k_grad_sums([t, t.cpu()]), lambda: P.spec_k_grad_sums([t], sums=sums[:5]),
+                 lambda: P.spec_k_grad_clip([t], sums.float(), 1.0), lambda: P.spec_k_grad_clip([t], sums, -1.0), lambda: P.spec_k_grad_clip([t], sums, float("nan")), lambda: P.spec_k_grad_clip([t, t], sums, 1.0),
+                 lambda: P.spec_k_grad_clip([t], sums, 1.0, outs=[]), lambda: P.spec_k_grad_clip([t], sums, 1.0, outs=[dy]), lambda: P.spec_k_grad_clip([t, dy], sums, 1.0, outs=[torch.empty_like(t), t[:9]])):
+        with pytest.raises(E):
+            call()
+
+
+def test_more_elements_than_31_bits_count_of_a_step(P):
+    """Rows, columns and elements that lie beyond 2^31 elements, against the same at the front."""
+    rows = 1 << 20
+    dy = rand(1, 64, 2112).bfloat16().cuda().repeat(rows // 64, 1)       # 2^31.04
+    tok = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    tok[-64:] = tok[:64] = torch.arange(64, device="cuda", dtype=torch.int32)
+    got = P.spec_k_embed_grad(dy, tok, 70, out_dtype=torch.float32)
+    assert torch.equal(got[:64], 2 * dy[:64].float()) and (got[64:] == 0).all()
+    tok[:64] = torch.arange(1 << 20, (1 << 20) + 64, device="cuda", dtype=torch.int32)
+    got = P.spec_k_embed_grad(dy, tok, (1 << 20) + 64)                   # a table as large
+    assert torch.equal(got[-64:], dy[:64]) and torch.equal(got[:64], dy[:64]) and not got[64:-64].any()
+    assert torch.equal(P.spec_k_embed(got, tok[:64]), dy[:64])
+    del got, dy
+    x = rand(3, 64, 64, 128).bfloat16().cuda()
+    w = rand(4, 128).cuda()
+    pos = torch.arange(64, dtype=torch.int32, device="cuda").repeat(4200)
+    many = x.repeat(4200, 1, 1)                                          # 268800 rows
+    plan = P.spec_rotary_plan(128, 1e4)
+    y = P.spec_k_headnorm_rotary(plan, [many], pos, [w])[0]
+    assert torch.equal(y[-64:], y[:64]) and torch.equal(y[:64], P.spec_k_headnorm_rotary(plan, [x], 0, [w])[0])
+    (dx,), _ = P.spec_k_headnorm_rotary_grad(plan, [y], [many], pos, [w], outs=[y])
+    assert torch.equal(dx[-64:], dx[:64]) and not torch.equal(dx[1], dx[0])
+    del y, dx, many
+    x, wg, wu, dh = ffn_case(5, 64, 64, 4104)
+    n = (1 << 19) // 64                                                  # 2^31.003 elements of h
+    h = P.spec_k_ffn_gated(x.repeat(n, 1), wg, wu)
+    want, tol = ffn_want(x, wg, wu, "silu")[0]
+    within(h[:64], want, tol)
+    assert torch.equal(h[-64:], h[:64])
+    del h
+    dx, dwg, dwu = P.spec_k_ffn_gated_grad(x.repeat(n, 1), wg, wu, dh.repeat(n, 1))
+    back = ffn_want(x, wg, wu, "silu", dh)
+    within(dx[:64], *back[0])
+    assert torch.equal(dx[-64:], dx[:64])
+    for o, (want, tol) in zip((dwg, dwu), back[1:]):                     # every row n times: products of 64 rows as they are, sums of n of them
+        size = (n * 64 + 40) * U32 * (n * tol / U16)
+        within(o, n * want, n * tol + size)
+    del dx, dwg, dwu
+    g = rand(6, 1 << 10).cuda().repeat((1 << 21) + 7)
+    norm = P.spec_k_grad_clip([g], P.spec_k_grad_sums([g]), 1.0)
+    assert abs(float(norm) / (float(rand(6, 1 << 10).double().norm()) * ((1 << 21) + 7) ** 0.5) - 1) < 2 * U32 and torch.equal(g[-1024:], g[:1024])
