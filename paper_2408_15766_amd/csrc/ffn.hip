@@ -347,8 +347,8 @@ __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, in
 // tiles x / m_parts, + 8 / m_parts, .., and walks them four n tiles at a time, for each m tile those four (32 compute units then read 8 + 4 panels).
 constexpr int kGroup = 4, kXcdUnits = 32;
 struct TilePlace { int m, n, count; };                        // count: tiles of this XCD
-__device__ __forceinline__ TilePlace tile_place(const FfnArgs &a, int j) {
-  const int x = (int)blockIdx.x % 8, xm = x % a.m_parts, xn = x / a.m_parts, n_parts = 8 / a.m_parts;
+__device__ __forceinline__ TilePlace tile_place(const FfnArgs &a, int id, int j) {
+  const int x = id % 8, xm = x % a.m_parts, xn = x / a.m_parts, n_parts = 8 / a.m_parts;
   const int ms = (a.m_tiles * a.halves - xm + a.m_parts - 1) / a.m_parts, ns = (a.n_tiles - xn + n_parts - 1) / n_parts;
   TilePlace p{-1, -1, ms * ns};
   if (j >= p.count) return p;
@@ -358,9 +358,9 @@ __device__ __forceinline__ TilePlace tile_place(const FfnArgs &a, int j) {
   return p;
 }
 template <class L, bool MM, bool NM, int TO>
-__device__ __forceinline__ void tile_at(const FfnArgs &a, int mt, int nt, int rows, unsigned char *ms0, unsigned char *ms1, unsigned char *ns0, unsigned char *ns1, unsigned char *ns2) {
+__device__ __forceinline__ void tile_at(const FfnArgs &a, int mt, int nt, int rows, int split, unsigned char *ms0, unsigned char *ms1, unsigned char *ns0, unsigned char *ns1, unsigned char *ns2) {
   // rows: of the m tile, how far in the body begins
-  const int total = a.segs * ((a.k + kStageK - 1) / kStageK), split = blockIdx.y, half = mt / a.m_tiles;
+  const int total = a.segs * ((a.k + kStageK - 1) / kStageK), half = mt / a.m_tiles;
   const int s0 = (int)((int64_t)total * split / a.splits), s1 = (int)((int64_t)total * (split + 1) / a.splits);
   float *part = TO == kToParts ? a.part + ((int64_t)split * a.halves + half) * (int64_t)a.m * a.n : nullptr;
   tile_body<L, MM, NM, TO>(a, __builtin_amdgcn_readfirstlane(half), __builtin_amdgcn_readfirstlane((mt - half * a.m_tiles) * a.tile_m + rows),
@@ -370,8 +370,8 @@ __device__ __forceinline__ void tile_at(const FfnArgs &a, int mt, int nt, int ro
 template <class L, bool MM, bool NM, int TO>
 __global__ __launch_bounds__(L::kThreads, 2) void ffn_tile_kernel(FfnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char ms0[L::kMBytes], ms1[L::kMBytes], ns0[L::kNBytes], ns1[L::kNBytes], ns2[L::kNBytes];
-  const TilePlace p = tile_place(a, (int)blockIdx.x / 8);
-  if (p.m >= 0) tile_at<L, MM, NM, TO>(a, p.m, p.n, 0, ms0, ms1, ns0, ns1, ns2);
+  const TilePlace p = tile_place(a, blockIdx.x, (int)blockIdx.x / 8);
+  if (p.m >= 0) tile_at<L, MM, NM, TO>(a, p.m, p.n, 0, blockIdx.y, ms0, ms1, ns0, ns1, ns2);
 }
 using Big = Tile<2, 8, 4, 4>;                                 // 256 x 256
 using Mid = Tile<2, 4, 4, 4>;                                 // 128 x 256
@@ -381,13 +381,31 @@ __host__ __device__ inline int halved_tiles(int count) { return count % kXcdUnit
 template <bool MM, bool NM, int TO>
 __global__ __launch_bounds__(Big::kThreads, 2) void ffn_mixed_kernel(FfnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char ms0[Big::kMBytes], ms1[Big::kMBytes], ns0[Big::kNBytes], ns1[Big::kNBytes], ns2[Big::kNBytes];
-  const int j = (int)blockIdx.x / 8, count = tile_place(a, 0x7FFFFFFF).count, whole = count - halved_tiles(count);
-  const TilePlace p = tile_place(a, j < whole ? j : whole + (j - whole) / 2);
+  const int j = (int)blockIdx.x / 8, count = tile_place(a, blockIdx.x, 0x7FFFFFFF).count, whole = count - halved_tiles(count);
+  const TilePlace p = tile_place(a, blockIdx.x, j < whole ? j : whole + (j - whole) / 2);
   if (p.m < 0) return;
   const int left = a.m - (p.m % a.m_tiles) * Big::kM, rows = j < whole ? 0 : ((j - whole) & 1) * Mid::kM;   // of the tile; of those, where this workgroup begins
   if (rows >= left) return;
-  if (j < whole && left > Mid::kM) tile_at<Big, MM, NM, TO>(a, p.m, p.n, 0, ms0, ms1, ns0, ns1, ns2);
-  else tile_at<Mid, MM, NM, TO>(a, p.m, p.n, rows, ms0, ms1, ns0, ns1, ns2);
+  if (j < whole && left > Mid::kM) tile_at<Big, MM, NM, TO>(a, p.m, p.n, 0, blockIdx.y, ms0, ms1, ns0, ns1, ns2);
+  else tile_at<Mid, MM, NM, TO>(a, p.m, p.n, rows, blockIdx.y, ms0, ms1, ns0, ns1, ns2);
+}
+
+// dx and the weights' gradients of a small call in one launch, where neither fills the chip for long: the workgroups of dx, range of k by range, then those of the others.
+struct FfnBoth { FfnArgs dx, dw; int dx_each, dw_each; };     // ..each: workgroups of a range
+template <int TX, int TW>
+__global__ __launch_bounds__(Small::kThreads, 2) void ffn_both_kernel(FfnBoth b) {
+  using L = Small;
+  __shared__ __attribute__((aligned(1024))) unsigned char ms0[L::kMBytes], ms1[L::kMBytes], ns0[L::kNBytes], ns1[L::kNBytes], ns2[L::kNBytes];
+  const int id = blockIdx.x, first = b.dx_each * b.dx.splits;
+  if (id < first) {
+    const int split = id / b.dx_each;
+    const TilePlace p = tile_place(b.dx, id, (id - split * b.dx_each) / 8);
+    if (p.m >= 0) tile_at<L, false, true, TX>(b.dx, p.m, p.n, 0, split, ms0, ms1, ns0, ns1, ns2);
+  } else {
+    const int split = (id - first) / b.dw_each;
+    const TilePlace p = tile_place(b.dw, id, (id - first - split * b.dw_each) / 8);
+    if (p.m >= 0) tile_at<L, true, true, TW>(b.dw, p.m, p.n, 0, split, ms0, ms1, ns0, ns1, ns2);
+  }
 }
 
 // The ranges' sums, in ascending order: eight columns a thread
@@ -595,33 +613,42 @@ __global__ __launch_bounds__(256, 2) void ffn_some_kernel(FfnArgs a) {
 
 // ---- launches -----------------------------------------------------------------------------------------
 
-template <class L, bool MM, bool NM, int TO> hipError_t launch_tiles(FfnArgs a, hipStream_t st) {
+// Tiles of the fullest XCD where the m tiles are shared out in m_parts
+int64_t fullest(int64_t m_tiles, int64_t n_tiles, int m_parts) { return (m_tiles + m_parts - 1) / m_parts * ((n_tiles + 8 / m_parts - 1) / (8 / m_parts)); }
+// In two parts (m) by four (n), if that is no less even than all n tiles' eighths: of a training step at the 7B widths dx and the weights' gradients are 2 % sooner than with one by
+// eight and the same with four by two, the forward product is the same with each.
+int parts_of_m(int64_t m_tiles, int64_t n_tiles) { return fullest(m_tiles, n_tiles, 2) <= fullest(m_tiles, n_tiles, 1) ? 2 : 1; }
+
+template <class L, int TO> bool set_tiles(FfnArgs &a) {       // false: more tiles than a grid holds
   constexpr int kCols = TO == kToH || TO == kToDgu ? L::kN / 2 : L::kN;
   a.tile_m = L::kM;
   a.m_tiles = (a.m + L::kM - 1) / L::kM;
   a.n_tiles = (a.n + kCols - 1) / kCols;
-  const int mt = a.m_tiles * a.halves;
-  a.m_parts = mt > 1 ? 2 : 1;
-  // the fullest XCD's workgroups, the first one's
-  const int n_parts = 8 / a.m_parts;
-  const int64_t count = (int64_t)((mt + a.m_parts - 1) / a.m_parts) * ((a.n_tiles + n_parts - 1) / n_parts);
+  a.m_parts = parts_of_m(a.m_tiles * a.halves, a.n_tiles);
+  return fullest(a.m_tiles * a.halves, a.n_tiles, a.m_parts) <= 0x7FFFFFFF / L::kThreads / 8 - kXcdUnits;
+}
+template <class L, bool MM, bool NM, int TO> hipError_t launch_tiles(FfnArgs a, hipStream_t st) {
+  if (!set_tiles<L, TO>(a)) return hipErrorInvalidValue;
+  const int64_t count = fullest(a.m_tiles * a.halves, a.n_tiles, a.m_parts);
   constexpr bool kMixed = L::kM == 256;
-  const int64_t grid = 8 * (kMixed ? count + kXcdUnits / 2 : count);   // (an XCD may have fewer tiles and more halves)
-  if (grid > 0x7FFFFFFF / L::kThreads) return hipErrorInvalidValue;
-  if constexpr (kMixed) hipLaunchKernelGGL((ffn_mixed_kernel<MM, NM, TO>), dim3((unsigned)grid, a.splits), dim3(L::kThreads), 0, st, a);
-  else hipLaunchKernelGGL((ffn_tile_kernel<L, MM, NM, TO>), dim3((unsigned)grid, a.splits), dim3(L::kThreads), 0, st, a);
+  const dim3 grid((unsigned)(8 * (kMixed ? count + kXcdUnits / 2 : count)), a.splits);   // (an XCD may have fewer tiles and more halves)
+  if constexpr (kMixed) hipLaunchKernelGGL((ffn_mixed_kernel<MM, NM, TO>), grid, dim3(L::kThreads), 0, st, a);
+  else hipLaunchKernelGGL((ffn_tile_kernel<L, MM, NM, TO>), grid, dim3(L::kThreads), 0, st, a);
   return hipGetLastError();
 }
 
-// Which tile, and into how many ranges k is cut (1: not at all)
+// Which tile, and into how many ranges k is cut (1: not at all): as many as fill the chip once, with halves of the large tile or two workgroups of the small one to a compute unit.
+// Measured (us): dx of 1024 rows, 4096 x 11008 (64 large tiles, 344 stages) in 1, 2, 3, 4, 6 ranges 352, 207, 266, 220, 236, small tiles 277, 215, 234, 222, 237; of 512 rows, 4096 x 14336 (32
+// large tiles) 441, 233, 161, 142, 177, small (128) 346, 186, 162, 142, 156; of 777 rows, 1000 x 2728 (16, 56) 91, 54, 42, 36, 31, small 72, 43, 35, 30, 30, in eight 29.  Forward, large /
+// small: 512 rows of 4096 x 14336 (224 large tiles) 96 / 113, 777 of 1000 x 2728 (88) 19.6 / 20.9, 300 of 4096 x 4096 (64) 42.6 / 40.3, 200 of 8192 x 2000 (16) 74 / 62.
 struct FfnPlan { int tile, splits; };                         // tile 0: 256 x 256 and halves, 1: 128 x 128
-constexpr int kTileM[2] = {256, 128}, kTileN[2] = {256, 128};
 FfnPlan ffn_plan(int64_t m, int64_t n, int64_t k, int halves, int segs, bool gated) {
-  const int stages = segs * (int)((k + kStageK - 1) / kStageK);
-  auto tiles = [&](int t) { const int64_t cols = gated ? kTileN[t] / 2 : kTileN[t]; return ((m + kTileM[t] - 1) / kTileM[t]) * ((n + cols - 1) / cols) * halves; };
-  FfnPlan p{tiles(0) >= 64 ? 0 : 1, 1};
+  auto tiles_m = [&](int t) { const int size = t ? Small::kM : Big::kM; return (m + size - 1) / size * halves; };
+  auto tiles_n = [&](int t) { const int size = (t ? Small::kN : Big::kN) / (gated ? 2 : 1); return (n + size - 1) / size; };
+  FfnPlan p{tiles_m(0) * tiles_n(0) >= 64 ? 0 : 1, 1};
   if (gated) return p;
-  const int64_t ranges = p.tile == 0 ? 128 / tiles(0) : 512 / tiles(1), most = stages / 4 < 16 ? stages / 4 : 16;
+  const int64_t m_tiles = tiles_m(p.tile), n_tiles = tiles_n(p.tile), stages = segs * ((k + kStageK - 1) / kStageK);
+  const int64_t ranges = (p.tile == 0 ? kXcdUnits / 2 : 2 * kXcdUnits) / fullest(m_tiles, n_tiles, parts_of_m(m_tiles, n_tiles)), most = stages / 4 < 16 ? stages / 4 : 16;
   p.splits = (int)(ranges < most ? ranges : most);
   if (p.splits < 1) p.splits = 1;
   return p;
@@ -629,16 +656,38 @@ FfnPlan ffn_plan(int64_t m, int64_t n, int64_t k, int halves, int segs, bool gat
 template <bool MM, bool NM, int TO> hipError_t launch_planned(const FfnArgs &a, int tile, hipStream_t st) {
   return tile == 0 ? launch_tiles<Big, MM, NM, TO>(a, st) : launch_tiles<Small, MM, NM, TO>(a, st);
 }
+hipError_t launch_join(const FfnArgs &a, hipStream_t st) {
+  const int64_t pieces = (int64_t)a.m * (a.n / 8) * a.halves, groups = (pieces + 255) / 256;
+  hipLaunchKernelGGL(ffn_join_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, st, a.part, a.splits, a.halves, a.m, a.n, a.out[0], a.out[1], a.ldo);
+  return hipGetLastError();
+}
 // A product into out, through ranges' sums if k is cut
 template <bool MM, bool NM> hipError_t launch_product(FfnArgs a, hipStream_t st) {
   const FfnPlan p = ffn_plan(a.m, a.n, a.k, a.halves, a.segs, false);
   a.splits = p.splits;
   if (p.splits == 1) return launch_planned<MM, NM, kToOut>(a, p.tile, st);
   const hipError_t e = launch_planned<MM, NM, kToParts>(a, p.tile, st);
-  if (e != hipSuccess) return e;
-  const int64_t pieces = (int64_t)a.m * (a.n / 8) * a.halves, groups = (pieces + 255) / 256;
-  hipLaunchKernelGGL(ffn_join_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, st, a.part, a.splits, a.halves, a.m, a.n, a.out[0], a.out[1], a.ldo);
-  return hipGetLastError();
+  return e != hipSuccess ? e : launch_join(a, st);
+}
+// Both products in one launch, if dx takes small tiles and the others are at most two rounds of them
+bool both_pay(const FfnArgs &dx, const FfnArgs &dw) {
+  return ffn_plan(dx.m, dx.n, dx.k, dx.halves, dx.segs, false).tile == 1 && ((int64_t)(dw.m + Small::kM - 1) / Small::kM) * dw.halves * ((dw.n + Small::kN - 1) / Small::kN) <= 1024;
+}
+hipError_t launch_both(FfnBoth b, hipStream_t st) {
+  for (FfnArgs *a : {&b.dx, &b.dw}) {
+    const FfnPlan p = ffn_plan(a->m, a->n, a->k, a->halves, a->segs, false);
+    a->splits = p.splits;
+    if (!set_tiles<Small, kToOut>(*a)) return hipErrorInvalidValue;
+  }
+  b.dx_each = (int)(8 * fullest(b.dx.m_tiles, b.dx.n_tiles, b.dx.m_parts));
+  b.dw_each = (int)(8 * fullest(b.dw.m_tiles * b.dw.halves, b.dw.n_tiles, b.dw.m_parts));
+  const bool x = b.dx.splits > 1, w = b.dw.splits > 1;
+  const auto kernel = x ? (w ? ffn_both_kernel<kToParts, kToParts> : ffn_both_kernel<kToParts, kToOut>) : w ? ffn_both_kernel<kToOut, kToParts> : ffn_both_kernel<kToOut, kToOut>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(b.dx_each * b.dx.splits + b.dw_each * b.dw.splits)), dim3(Small::kThreads), 0, st, b);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && x) e = launch_join(b.dx, st);
+  if (e == hipSuccess && w) e = launch_join(b.dw, st);
+  return e;
 }
 uint64_t parts_bytes(int64_t m, int64_t n, int64_t k, int halves, int segs) {
   const FfnPlan p = ffn_plan(m, n, k, halves, segs, false);
@@ -648,10 +697,10 @@ uint64_t up256(uint64_t b) { return (b + 255) / 256 * 256; }
 
 }  // namespace
 
-// dg and du, and behind them room for the ranges' sums of one product at a time
+// dg and du, and behind them room for the ranges' sums
 uint64_t ffn_grad_scratch_bytes(int rows, int d, int f) {
   const uint64_t x = parts_bytes(rows, d, f, 1, 2), w = parts_bytes(f, d, rows, 2, 1);
-  return 2 * up256((uint64_t)rows * f * 2) + up256(x > w ? x : w);
+  return 2 * up256((uint64_t)rows * f * 2) + up256(x) + up256(w);
 }
 
 // Which of the three takes a forward call (us; few / some / tiles of 128 x 128): 16 rows of 4096 x 11008 37.8 / 45.6 / 58.2, 24 46.5 / 45.8 / 58.6, 60 74 / 48.9 / 61.4, 128 - / 62.2 / 65.8;
@@ -681,18 +730,16 @@ hipError_t launch_ffn_grad(const FfnCall &c, void *scratch, hipStream_t st) {
   a.dh = c.h; a.lddh = c.ldh; a.out[0] = dg; a.out[1] = du; a.ldo = c.f;
   hipError_t e = launch_planned<false, false, kToDgu>(a, ffn_plan(a.m, a.n, a.k, 1, 1, true).tile, st);
   if (e != hipSuccess) return e;
-  FfnArgs b{};
-  b.part = (float *)((char *)scratch + 2 * each);
-  if (c.dx) {
-    b.m = c.rows; b.n = c.d; b.k = c.f; b.segs = 2; b.halves = 1;
-    b.m_src[0] = dg; b.m_src[1] = du; b.ldm = c.f; b.n_src[0] = c.wg; b.n_src[1] = c.wu; b.ldn = c.ldw; b.out[0] = c.dx; b.ldo = c.lddx;
-    if ((e = launch_product<false, true>(b, st)) != hipSuccess) return e;
-  }
-  if (c.dwg) {
-    b.m = c.f; b.n = c.d; b.k = c.rows; b.segs = 1; b.halves = 2;
-    b.m_src[0] = dg; b.m_src[1] = du; b.ldm = c.f; b.n_src[0] = b.n_src[1] = c.x; b.ldn = c.ldx; b.out[0] = c.dwg; b.out[1] = c.dwu; b.ldo = c.lddw;
-    if ((e = launch_product<true, true>(b, st)) != hipSuccess) return e;
-  }
+  FfnBoth b{};
+  b.dx.part = (float *)((char *)scratch + 2 * each);
+  b.dw.part = (float *)((char *)b.dx.part + up256(parts_bytes(c.rows, c.d, c.f, 1, 2)));
+  b.dx.m = c.rows; b.dx.n = c.d; b.dx.k = c.f; b.dx.segs = 2; b.dx.halves = 1;
+  b.dx.m_src[0] = dg; b.dx.m_src[1] = du; b.dx.ldm = c.f; b.dx.n_src[0] = c.wg; b.dx.n_src[1] = c.wu; b.dx.ldn = c.ldw; b.dx.out[0] = c.dx; b.dx.ldo = c.lddx;
+  b.dw.m = c.f; b.dw.n = c.d; b.dw.k = c.rows; b.dw.segs = 1; b.dw.halves = 2;
+  b.dw.m_src[0] = dg; b.dw.m_src[1] = du; b.dw.ldm = c.f; b.dw.n_src[0] = b.dw.n_src[1] = c.x; b.dw.ldn = c.ldx; b.dw.out[0] = c.dwg; b.dw.out[1] = c.dwu; b.dw.ldo = c.lddw;
+  if (c.dx && c.dwg && both_pay(b.dx, b.dw)) return launch_both(b, st);
+  if (c.dx && (e = launch_product<false, true>(b.dx, st)) != hipSuccess) return e;
+  if (c.dwg && (e = launch_product<true, true>(b.dw, st)) != hipSuccess) return e;
   return hipSuccess;
 }
 
