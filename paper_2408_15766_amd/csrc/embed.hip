@@ -10,6 +10,8 @@
 #include "elements.h"
 #include "kernels.h"
 
+#include <type_traits>
+
 namespace spec {
 
 namespace {
@@ -18,12 +20,49 @@ constexpr int kTile = 4096, kRun = 32, kRuns = 1024;          // positions of a 
 constexpr int kLongLeast = 8192;                              // positions from which on the longer runs are summed (below, a walk meets 256 sums at most)
 constexpr int kEmbedThreads = 256;
 
-// Eight columns of a row at a time (VEC), or one.  A thread's columns do not change from row to row.
-template <bool VEC>
-__global__ __launch_bounds__(kEmbedThreads) void embed_kernel(const void *table, int64_t ldt, int vocab, int d, const int *tok, int rows, float scale, int dtype,
-                                                              int out_dtype, void *out, int64_t ldo) {
-  constexpr int W = VEC ? 8 : 1;
-  const int cols = (d + W - 1) / W, per = cols < kEmbedThreads ? kEmbedThreads / cols : 1;   // rows that the workgroup's threads share out
+// Eight columns of a row, at any alignment of their type (the memory takes unaligned accesses of 16 bytes; a column at a time took 130 us where they take 58: the gradient of a 60000 x 2001
+// table in bf16), or the n that are left at its end.
+typedef u32x4_t u32x4_any __attribute__((aligned(2)));
+typedef f32x4_t f32x4_any __attribute__((aligned(4)));
+struct Columns { float x[8]; };
+template <bool WHOLE> __device__ __forceinline__ Columns load_columns(const void *p, int64_t i, int n, bool bf16) {   // WHOLE: n >= 8 (asked at each load, every load waited for the one before)
+  Columns r;
+  if constexpr (WHOLE) {
+    Eight e;
+    if (bf16) e.v[0] = *(const u32x4_any *)((const bf16_t *)p + i);
+    else {
+      e.v[0] = __builtin_bit_cast(u32x4_t, (f32x4_t)*(const f32x4_any *)((const float *)p + i));
+      e.v[1] = __builtin_bit_cast(u32x4_t, (f32x4_t)*(const f32x4_any *)((const float *)p + i + 4));
+    }
+    widen8(e, bf16, r.x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; j++) r.x[j] = j < n ? load1(p, i + j, bf16) : 0.f;
+  }
+  return r;
+}
+__device__ __forceinline__ void store_columns(void *p, int64_t i, int n, bool bf16, const Columns &c) {
+  if (n >= 8) {
+    if (bf16) *(u32x4_any *)((bf16_t *)p + i) = u32x4_t{pack_bf16x2(c.x[0], c.x[1]), pack_bf16x2(c.x[2], c.x[3]), pack_bf16x2(c.x[4], c.x[5]), pack_bf16x2(c.x[6], c.x[7])};
+    else {
+      *(f32x4_any *)((float *)p + i) = f32x4_t{c.x[0], c.x[1], c.x[2], c.x[3]};
+      *(f32x4_any *)((float *)p + i + 4) = f32x4_t{c.x[4], c.x[5], c.x[6], c.x[7]};
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+      if (j < n) store1(p, i + j, bf16, c.x[j]);
+  }
+}
+__device__ __forceinline__ void add_columns(Columns &s, const Columns &v) {
+#pragma unroll
+  for (int j = 0; j < 8; j++) s.x[j] += v.x[j];
+}
+
+// A workgroup has a row, or as many short ones as its threads hold.
+__global__ __launch_bounds__(kEmbedThreads) void embed_kernel(const void *table, int64_t ldt, int vocab, int d, const int *tok, int rows, float scale, int dtype, int out_dtype,
+                                                              void *out, int64_t ldo) {
+  const int cols = (d + 7) / 8, per = cols < kEmbedThreads ? kEmbedThreads / cols : 1;
   const int mine = cols < kEmbedThreads ? threadIdx.x / cols : 0, c0 = cols < kEmbedThreads ? threadIdx.x % cols : threadIdx.x;
   if (mine >= per) return;
   const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * per + mine;
@@ -31,17 +70,14 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(const void *table,
   const int t = tok[row];
   const bool real = t >= 0 && t < vocab;
   for (int c = c0; c < cols; c += kEmbedThreads) {
-    if constexpr (VEC) {
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (real) {
-        widen8(load8(table, t * ldt + c * 8, dtype), dtype, x);
+    const int n = d - 8 * c;
+    Columns x = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+    if (real) {
+      x = n >= 8 ? load_columns<true>(table, t * ldt + c * 8, n, dtype) : load_columns<false>(table, t * ldt + c * 8, n, dtype);
 #pragma unroll
-        for (int j = 0; j < 8; j++) x[j] *= scale;
-      }
-      store8(out, row * ldo + c * 8, out_dtype, x);
-    } else {
-      store1(out, row * ldo + c, out_dtype, real ? scale * load1(table, t * ldt + c, dtype) : 0.f);
+      for (int j = 0; j < 8; j++) x.x[j] *= scale;
     }
+    store_columns(out, row * ldo + c * 8, n, out_dtype, x);
   }
 }
 
@@ -126,18 +162,6 @@ __global__ __launch_bounds__(kRankThreads) void embed_merge_kernel(const int *ti
 
 // ---- sums ---------------------------------------------------------------------------------------
 
-template <int W> struct Columns { float x[W]; };
-template <int W> __device__ __forceinline__ void add_columns(Columns<W> &s, const Columns<W> &v) {
-#pragma unroll
-  for (int j = 0; j < W; j++) s.x[j] += v.x[j];
-}
-template <int W> __device__ __forceinline__ Columns<W> row_columns(const void *p, int64_t i, bool bf16) {
-  Columns<W> r;
-  if constexpr (W == 8) widen8(load8(p, i, bf16), bf16, r.x);
-  else r.x[0] = load1(p, i, bf16);
-  return r;
-}
-
 // The number of keys below v, by one wavefront: 64 places are looked at at a time.  Every lane gets it.
 __device__ __forceinline__ int keys_below(const int *keys, int rows, int v) {
   const int lane = threadIdx.x & 63;
@@ -155,7 +179,7 @@ __device__ __forceinline__ int keys_below(const int *keys, int rows, int v) {
 
 // The first sorted position of every token (starts[vocab]: where padding begins; a workgroup has 256 tokens, whose share of the keys two of its wavefronts look up first), and the runs of 32.
 // BF16: dy's type (asked at each load, every load waited for the one before).
-template <int W, bool BF16>
+template <bool BF16>
 __global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(EmbedGradArgs a, const int *keys, const int *order, int *starts, int start_groups, float *runs) {
   __shared__ int range[2];
   if ((int)blockIdx.x < start_groups) {
@@ -178,12 +202,15 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(EmbedGradArgs
   const int run = blockIdx.x - start_groups;
   const int key = keys[run * kRun];
   if (key >= a.vocab || key != keys[run * kRun + kRun - 1]) return;
-  for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * W; c < a.d; c += gridDim.y * kEmbedThreads * W) {
-    Columns<W> s = row_columns<W>(a.dy, order[run * kRun] * a.ldy + c, BF16);
+  for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * 8; c < a.d; c += gridDim.y * kEmbedThreads * 8) {
+    auto sum = [&](auto whole) __attribute__((always_inline)) {
+      constexpr bool kWhole = decltype(whole)::value;
+      Columns s = load_columns<kWhole>(a.dy, order[run * kRun] * a.ldy + c, a.d - c, BF16);
 #pragma unroll 16
-    for (int i = 1; i < kRun; i++) add_columns<W>(s, row_columns<W>(a.dy, order[run * kRun + i] * a.ldy + c, BF16));
-    if constexpr (W == 8) store8(runs, (int64_t)run * a.d + c, 0, s.x);
-    else runs[(int64_t)run * a.d + c] = s.x[0];
+      for (int i = 1; i < kRun; i++) add_columns(s, load_columns<kWhole>(a.dy, order[run * kRun + i] * a.ldy + c, a.d - c, BF16));
+      store_columns(runs, (int64_t)run * a.d + c, a.d - c, false, s);
+    };
+    if (a.d - c >= 8) sum(std::true_type{}); else sum(std::false_type{});
   }
 }
 
@@ -202,7 +229,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_long_runs_kernel(const in
 
 // A few table rows to a workgroup (blockIdx.y: its share of the columns).
 constexpr int kTableRows = 8;
-template <int W, bool BF16>
+template <bool BF16>
 __global__ __launch_bounds__(kEmbedThreads) void embed_table_kernel(EmbedGradArgs a, const int *order, const int *starts, const float *runs, const float *long_runs) {
   const int v0 = blockIdx.x * kTableRows, vn = min(a.vocab - v0, kTableRows);
   int start[kTableRows + 1];                                  // (all asked for at once; most rows of a large vocabulary have no token, and their zeros go out first)
@@ -213,46 +240,43 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_table_kernel(EmbedGradArg
   for (int r = 0; r < kTableRows; r++) {
     if (start[r] != start[r + 1]) full |= 1u << r;
     else if (!a.accumulate && r < vn)
-      for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * W; c < a.d; c += gridDim.y * kEmbedThreads * W) {
-        const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        const int64_t at = (v0 + r) * a.ldt + c;
-        if constexpr (W == 8) store8(a.dtable, at, a.out_dtype, zero);
-        else store1(a.dtable, at, a.out_dtype, 0.f);
+      for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * 8; c < a.d; c += gridDim.y * kEmbedThreads * 8) {
+        const Columns zero = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+        store_columns(a.dtable, (v0 + r) * a.ldt + c, a.d - c, a.out_dtype, zero);
       }
   }
   for (; full != 0; full &= full - 1) {
     const int v = v0 + __builtin_ctz(full), s0 = starts[v], s1 = starts[v + 1];
-    for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * W; c < a.d; c += gridDim.y * kEmbedThreads * W) {
-      Columns<W> s;
-#pragma unroll
-      for (int j = 0; j < W; j++) s.x[j] = 0.f;
-      int i = s0;
-      auto single = [&](int to) {
+    for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * 8; c < a.d; c += gridDim.y * kEmbedThreads * 8) {
+      const int n = a.d - c;
+      auto sum = [&](auto whole_columns) __attribute__((always_inline)) {
+        constexpr bool kWhole = decltype(whole_columns)::value;
+        Columns s = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
+        int i = s0;
+        auto single = [&](int to) __attribute__((always_inline)) {
 #pragma unroll 4
-        for (; i < to; i++) add_columns<W>(s, row_columns<W>(a.dy, order[i] * a.ldy + c, BF16));
-      };
-      auto whole = [&](const float *p, int length, int to) {  // runs, from a multiple of their length on
+          for (; i < to; i++) add_columns(s, load_columns<kWhole>(a.dy, order[i] * a.ldy + c, n, BF16));
+        };
+        auto whole = [&](const float *p, int length, int to) __attribute__((always_inline)) {   // runs, from a multiple of their length on
 #pragma unroll 8
-        for (; i + length <= to; i += length) add_columns<W>(s, row_columns<W>(p, (int64_t)(i / length) * a.d + c, false));
-      };
-      single(min(s1, (i + kRun - 1) / kRun * kRun));
-      if (i + kRun <= s1) {
-        if (a.rows >= kLongLeast) {
-          whole(runs, kRun, min(s1, (i + kRuns - 1) / kRuns * kRuns));
-          whole(long_runs, kRuns, s1);
+          for (; i + length <= to; i += length) add_columns(s, load_columns<kWhole>(p, (int64_t)(i / length) * a.d + c, n, false));
+        };
+        single(min(s1, (i + kRun - 1) / kRun * kRun));
+        if (i + kRun <= s1) {
+          if (a.rows >= kLongLeast) {
+            whole(runs, kRun, min(s1, (i + kRuns - 1) / kRuns * kRuns));
+            whole(long_runs, kRuns, s1);
+          }
+          whole(runs, kRun, s1);
         }
-        whole(runs, kRun, s1);
-      }
-      single(s1);
-      const int64_t at = v * a.ldt + c;
+        single(s1);
+        const int64_t at = v * a.ldt + c;
 #pragma unroll
-      for (int j = 0; j < W; j++) s.x[j] *= a.scale;
-      if (a.accumulate) {
-        const Columns<W> was = row_columns<W>(a.dtable, at, a.out_dtype);
-        add_columns<W>(s, was);
-      }
-      if constexpr (W == 8) store8(a.dtable, at, a.out_dtype, s.x);
-      else store1(a.dtable, at, a.out_dtype, s.x[0]);
+        for (int j = 0; j < 8; j++) s.x[j] *= a.scale;
+        if (a.accumulate) add_columns(s, load_columns<kWhole>(a.dtable, at, n, a.out_dtype));
+        store_columns(a.dtable, at, n, a.out_dtype, s);
+      };
+      if (n >= 8) sum(std::true_type{}); else sum(std::false_type{});
     }
   }
 }
@@ -274,14 +298,12 @@ EmbedScratch embed_scratch(int rows, int vocab, int d) {
   return s;
 }
 
-bool eights(const void *p, int64_t ld, int bf16, int64_t rows) { return ((uintptr_t)p & 15) == 0 && (rows <= 1 || ld % (bf16 ? 8 : 4) == 0); }
-
-template <int W, bool BF16> hipError_t embed_sums(const EmbedGradArgs &a, const EmbedScratch &s, char *base, hipStream_t st) {
+template <bool BF16> hipError_t embed_sums(const EmbedGradArgs &a, const EmbedScratch &s, char *base, hipStream_t st) {
   int *keys = (int *)(base + s.keys), *order = (int *)(base + s.order), *starts = (int *)(base + s.starts);
   float *runs = (float *)(base + s.runs), *long_runs = (float *)(base + s.long_runs);
-  const int slices = (a.d + kEmbedThreads * W - 1) / (kEmbedThreads * W), start_groups = (a.vocab + kEmbedThreads) / kEmbedThreads;
+  const int slices = (a.d + kEmbedThreads * 8 - 1) / (kEmbedThreads * 8), start_groups = (a.vocab + kEmbedThreads) / kEmbedThreads;
   const int ys = slices > 64 ? 64 : slices;
-  hipLaunchKernelGGL((embed_runs_kernel<W, BF16>), dim3(start_groups + a.rows / kRun, ys), dim3(kEmbedThreads), 0, st, a, keys, order, starts, start_groups, runs);
+  hipLaunchKernelGGL(embed_runs_kernel<BF16>, dim3(start_groups + a.rows / kRun, ys), dim3(kEmbedThreads), 0, st, a, keys, order, starts, start_groups, runs);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.rows >= kLongLeast) {
@@ -289,7 +311,7 @@ template <int W, bool BF16> hipError_t embed_sums(const EmbedGradArgs &a, const 
     hipLaunchKernelGGL(embed_long_runs_kernel, dim3(a.rows / kRuns, wide > 64 ? 64 : wide), dim3(kEmbedThreads), 0, st, keys, a.vocab, a.d, runs, long_runs);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((embed_table_kernel<W, BF16>), dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
+  hipLaunchKernelGGL(embed_table_kernel<BF16>, dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
   return hipGetLastError();
 }
 
@@ -297,12 +319,10 @@ template <int W, bool BF16> hipError_t embed_sums(const EmbedGradArgs &a, const 
 
 hipError_t launch_embed(int dtype, const void *table, int64_t ldt, int vocab, int d, const int *tok, int rows, float scale, int out_dtype, void *out, int64_t ldo,
                         hipStream_t st) {
-  const bool vec = d % 8 == 0 && eights(table, ldt, dtype, vocab) && eights(out, ldo, out_dtype, rows);
-  const int cols = vec ? d / 8 : d, per = cols < kEmbedThreads ? kEmbedThreads / cols : 1;
+  const int cols = (d + 7) / 8, per = cols < kEmbedThreads ? kEmbedThreads / cols : 1;
   const int64_t groups = ((int64_t)rows + per - 1) / per, deep = (groups + (1 << 23) - 1) >> 23;   // (a grid's dimension holds less than 2^32 threads)
   const dim3 grid((unsigned)((groups + deep - 1) / deep), (unsigned)deep);
-  if (vec) hipLaunchKernelGGL(embed_kernel<true>, grid, dim3(kEmbedThreads), 0, st, table, ldt, vocab, d, tok, rows, scale, dtype, out_dtype, out, ldo);
-  else hipLaunchKernelGGL(embed_kernel<false>, grid, dim3(kEmbedThreads), 0, st, table, ldt, vocab, d, tok, rows, scale, dtype, out_dtype, out, ldo);
+  hipLaunchKernelGGL(embed_kernel, grid, dim3(kEmbedThreads), 0, st, table, ldt, vocab, d, tok, rows, scale, dtype, out_dtype, out, ldo);
   return hipGetLastError();
 }
 
@@ -321,9 +341,7 @@ hipError_t launch_embed_grad(EmbedGradArgs a, void *scratch, hipStream_t st) {
                        (int *)(base + s.keys), (int *)(base + s.order));
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  const bool vec = a.d % 8 == 0 && eights(a.dy, a.ldy, a.dtype, a.rows) && eights(a.dtable, a.ldt, a.out_dtype, a.vocab);
-  if (vec) return a.dtype ? embed_sums<8, true>(a, s, base, st) : embed_sums<8, false>(a, s, base, st);
-  return a.dtype ? embed_sums<1, true>(a, s, base, st) : embed_sums<1, false>(a, s, base, st);
+  return a.dtype ? embed_sums<true>(a, s, base, st) : embed_sums<false>(a, s, base, st);
 }
 
 }  // namespace spec

@@ -1,7 +1,7 @@
 // Norms of heads with the rotary embedding in the same pass, and their gradients (include/spec_step.h).
 //
-// A head is held by a group of lanes (2^n, at most 32, or a wavefront where dims are taken one at a time), each with the same dims of every head it meets: eight planes (16 dims), or eight dims
-// that do not turn.  So a weight is read once, the sums over a head are a few exchanges between neighbouring lanes, and a lane adds up its dims' share of the
+// A head is held by a group of 2^n lanes, each with the same dims of every head it meets: eight planes (16 dims) or eight dims that do not turn, four where eight do not fit the layout
+// (a head of 72), else up to four single ones (then a wavefront holds the head, and takes five times as long).  So a weight is read once, the sums over a head are a few exchanges between neighbouring lanes, and a lane adds up its dims' share of the
 // weights' gradient in registers over all its heads; the workgroup's shares meet in the LDS once, in a fixed order, the workgroups' in a second
 // launch.  The rows' (cos, sin) table is made in the LDS as for the rotary embedding alone.
 // Bound: memory (forward: each element once in, once out; gradients: dy and x once in, dx once out).
@@ -29,31 +29,37 @@ __device__ __forceinline__ float group_sum(float x, int group) {
   return x;
 }
 
-// The dims of a lane.  VEC: x[0 .. 7] are eight consecutive dims, x[8 .. 15] their planes' partners (half layout) or nothing.  Else up to four items a lane, item k: x[2 k] and,
+// The dims of a lane.  W = 8 or 4: x[0 .. W - 1] are W consecutive dims, x[W ..] their planes' partners (half layout) or nothing.  W = 1: up to four items a lane, item k: x[2 k] and,
 // if it is a plane, x[2 k + 1].
 enum { kIdle = 0, kPass = 1, kPairs = 2, kInterleaved = 3 };
-template <bool VEC> struct Dims { static constexpr int kItems = VEC ? 1 : 4, kElems = VEC ? 16 : 8; int kind[kItems], first[kItems], plane[kItems]; };
-template <bool VEC> __device__ __forceinline__ Dims<VEC> dims_of(int lane, int items, int group, int rot, bool interleaved) {
-  Dims<VEC> r;
-  constexpr int W = VEC ? 8 : 1;
-  const int half = rot / 2, turning = VEC && interleaved ? half / 4 : half / W;
+template <int W> struct Dims { static constexpr int kItems = W > 1 ? 1 : 4, kElems = W > 1 ? 2 * W : 8; int kind[kItems], first[kItems], plane[kItems]; };
+template <int W> __device__ __forceinline__ Dims<W> dims_of(int lane, int items, int group, int rot, bool interleaved) {
+  Dims<W> r;
+  const int half = rot / 2, planes = W > 1 && interleaved ? W / 2 : W, turning = half / planes;   // planes of a step, and steps that turn
 #pragma unroll
-  for (int k = 0; k < Dims<VEC>::kItems; k++) {
+  for (int k = 0; k < Dims<W>::kItems; k++) {
     const int it = lane + k * group;
     r.kind[k] = it >= items ? kIdle : it >= turning ? kPass : interleaved ? kInterleaved : kPairs;
-    r.plane[k] = VEC && interleaved ? 4 * it : W * it;
+    r.plane[k] = planes * it;
     r.first[k] = r.kind[k] == kPass ? rot + W * (it - turning) : interleaved ? 2 * r.plane[k] : r.plane[k];
   }
   return r;
 }
 // As they are in memory, then as numbers
-struct Raw { u32x4_t a, b, c, d; };                           // VEC: a and b (bf16: a), and the partners' c and d
-template <bool VEC> __device__ __forceinline__ Raw load_dims(const void *p, int64_t at, int bf16, const Dims<VEC> &m, int half) {
+struct Raw { u32x4_t a, b, c, d; };                           // W = 8: a and b (bf16: a), and the partners' c and d; W = 4: a, and c
+template <int W> __device__ __forceinline__ Eight load_w(const void *p, int64_t i, int bf16) {
+  if constexpr (W == 8) return load8(p, i, bf16);
+  Eight r;
+  if (bf16) { const u32x2_t v = *(const u32x2_t *)((const bf16_t *)p + i); r.v[0] = u32x4_t{v.x, v.y, 0u, 0u}; }
+  else r.v[0] = *(const u32x4_t *)((const float *)p + i);
+  return r;
+}
+template <int W> __device__ __forceinline__ Raw load_dims(const void *p, int64_t at, int bf16, const Dims<W> &m, int half) {
   const u32x4_t zero = {0u, 0u, 0u, 0u};
   Raw r{zero, zero, zero, zero};
-  if constexpr (VEC) {
-    if (m.kind[0] != kIdle) { const Eight e = load8(p, at + m.first[0], bf16); r.a = e.v[0]; if (!bf16) r.b = e.v[1]; }
-    if (m.kind[0] == kPairs) { const Eight e = load8(p, at + m.first[0] + half, bf16); r.c = e.v[0]; if (!bf16) r.d = e.v[1]; }
+  if constexpr (W > 1) {
+    if (m.kind[0] != kIdle) { const Eight e = load_w<W>(p, at + m.first[0], bf16); r.a = e.v[0]; if (W == 8 && !bf16) r.b = e.v[1]; }
+    if (m.kind[0] == kPairs) { const Eight e = load_w<W>(p, at + m.first[0] + half, bf16); r.c = e.v[0]; if (W == 8 && !bf16) r.d = e.v[1]; }
   } else {
     uint32_t x[8];
 #pragma unroll
@@ -67,25 +73,29 @@ template <bool VEC> __device__ __forceinline__ Raw load_dims(const void *p, int6
   }
   return r;
 }
-template <bool VEC> __device__ __forceinline__ void widen_dims(const Raw &r, int bf16, const Dims<VEC> &m, float (&x)[Dims<VEC>::kElems]) {
-  if constexpr (VEC) {
+template <int W> __device__ __forceinline__ void widen_dims(const Raw &r, int bf16, float (&x)[Dims<W>::kElems]) {
+  if constexpr (W > 1) {
     float a[8], b[8];
     widen8(Eight{{r.a, r.b}}, bf16, a);
     widen8(Eight{{r.c, r.d}}, bf16, b);
 #pragma unroll
-    for (int j = 0; j < 8; j++) { x[j] = a[j]; x[8 + j] = b[j]; }
+    for (int j = 0; j < W; j++) { x[j] = a[j]; x[W + j] = b[j]; }
   } else {
 #pragma unroll
     for (int j = 0; j < 4; j++) { x[j] = __uint_as_float(r.a[j]); x[4 + j] = __uint_as_float(r.b[j]); }
   }
 }
-template <bool VEC> __device__ __forceinline__ void store_dims(void *p, int64_t at, int bf16, const Dims<VEC> &m, int half, const float (&x)[Dims<VEC>::kElems]) {
-  if constexpr (VEC) {
-    float a[8], b[8];
-#pragma unroll
-    for (int j = 0; j < 8; j++) { a[j] = x[j]; b[j] = x[8 + j]; }
-    if (m.kind[0] != kIdle) store8(p, at + m.first[0], bf16, a);
-    if (m.kind[0] == kPairs) store8(p, at + m.first[0] + half, bf16, b);
+template <int W> __device__ __forceinline__ void store_w(void *p, int64_t i, int bf16, const float *x) {
+  if constexpr (W == 8) {
+    const float v[8] = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+    store8(p, i, bf16, v);
+  } else if (bf16) *(u32x2_t *)((bf16_t *)p + i) = u32x2_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+  else *(f32x4_t *)((float *)p + i) = f32x4_t{x[0], x[1], x[2], x[3]};
+}
+template <int W> __device__ __forceinline__ void store_dims(void *p, int64_t at, int bf16, const Dims<W> &m, int half, const float (&x)[Dims<W>::kElems]) {
+  if constexpr (W > 1) {
+    if (m.kind[0] != kIdle) store_w<W>(p, at + m.first[0], bf16, x);
+    if (m.kind[0] == kPairs) store_w<W>(p, at + m.first[0] + half, bf16, x + W);
   } else {
 #pragma unroll
     for (int k = 0; k < 4; k++) {
@@ -94,63 +104,56 @@ template <bool VEC> __device__ __forceinline__ void store_dims(void *p, int64_t 
     }
   }
 }
-// Turned by the row's table (back: by the opposite angles).  INTER is for eight dims at a time (two patterns behind one branch went to memory)
-template <bool VEC, bool INTER> __device__ __forceinline__ void turn_dims(float (&x)[Dims<VEC>::kElems], const Dims<VEC> &m, const float2 *cs, float back) {
-  if constexpr (VEC && !INTER) {
+// Turned by the row's table (back: by the opposite angles).  INTER is for several dims at a time (two patterns behind one branch went to memory)
+template <int W, bool INTER> __device__ __forceinline__ void turn_dims(float (&x)[Dims<W>::kElems], const Dims<W> &m, const float2 *cs, float back) {
+  auto turn = [&](float &a, float &b, int plane) __attribute__((always_inline)) {
+    const float2 c = make_float2(cs[plane].x, back * cs[plane].y);
+    const float u = rope_first(a, b, c), v = rope_second(a, b, c);
+    a = u; b = v;
+  };
+  if constexpr (W > 1 && !INTER) {
     if (m.kind[0] == kPairs) {
 #pragma unroll
-      for (int j = 0; j < 8; j++) {
-        const float2 c = make_float2(cs[m.plane[0] + j].x, back * cs[m.plane[0] + j].y);
-        const float u = rope_first(x[j], x[8 + j], c), v = rope_second(x[j], x[8 + j], c);
-        x[j] = u; x[8 + j] = v;
-      }
+      for (int j = 0; j < W; j++) turn(x[j], x[W + j], m.plane[0] + j);
     }
-  } else if constexpr (VEC) {
+  } else if constexpr (W > 1) {
     if (m.kind[0] == kInterleaved) {
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        const float2 c = make_float2(cs[m.plane[0] + j].x, back * cs[m.plane[0] + j].y);
-        const float u = rope_first(x[2 * j], x[2 * j + 1], c), v = rope_second(x[2 * j], x[2 * j + 1], c);
-        x[2 * j] = u; x[2 * j + 1] = v;
-      }
+      for (int j = 0; j < W / 2; j++) turn(x[2 * j], x[2 * j + 1], m.plane[0] + j);
     }
   } else {
 #pragma unroll
     for (int k = 0; k < 4; k++)
-      if (m.kind[k] >= kPairs) {
-        const float2 c = make_float2(cs[m.plane[k]].x, back * cs[m.plane[k]].y);
-        const float u = rope_first(x[2 * k], x[2 * k + 1], c), v = rope_second(x[2 * k], x[2 * k + 1], c);
-        x[2 * k] = u; x[2 * k + 1] = v;
-      }
+      if (m.kind[k] >= kPairs) turn(x[2 * k], x[2 * k + 1], m.plane[k]);
   }
 }
 
 // Runs of rows_each rows of a part, every groups-th of them.  TYPE: of x (and dy) in all parts, or kAny: asked at each access (then one waits for the other).
 enum { kFp32 = 0, kBf16 = 1, kAny = 2 };
-template <bool VEC, bool GRAD, bool INTER, int TYPE>
+template <int W, bool GRAD, bool INTER, int TYPE>
 __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
-  constexpr int E = Dims<VEC>::kElems;
+  constexpr int E = Dims<W>::kElems;
   __shared__ float2 table[kNormTable];
   __shared__ float shares[GRAD ? kNormWg * E : 1];            // of dw: [element of a lane][thread]
   const int n = (int)blockIdx.x >= a.first[2] ? 2 : (int)blockIdx.x >= a.first[1] ? 1 : 0, wg = blockIdx.x - a.first[n];
   const HeadnormPart p = a.part[n];
   const int group = a.group, slots = kNormWg / group, lane = threadIdx.x & (group - 1), slot = threadIdx.x / group;
   const int half = a.rot / 2, heads = p.p.heads, hd = a.hd;
-  const Dims<VEC> m = dims_of<VEC>(lane, a.items, group, a.rot, a.interleaved != 0);
+  const Dims<W> m = dims_of<W>(lane, a.items, group, a.rot, a.interleaved != 0);
   const bool normed = p.w != nullptr;
   const int y_type = TYPE == kAny ? p.p.dtype : TYPE, x_type = TYPE == kAny ? p.x_dtype : TYPE;
-  float w[E], dw[E];
+  float w[E], dw[E];                                          // 2 W of them, or four pairs
 #pragma unroll
   for (int j = 0; j < E; j++) w[j] = dw[j] = 0.f;
   if (normed) {
-    if (VEC && ((uintptr_t)p.w & 15) != 0) {                  // (aligned to its type only)
+    if (W > 1 && ((uintptr_t)p.w & 15) != 0) {                // (aligned to its type only)
 #pragma unroll
-      for (int j = 0; j < 8; j++) {
+      for (int j = 0; j < (W > 1 ? W : 0); j++) {
         if (m.kind[0] != kIdle) w[j] = load1(p.w, m.first[0] + j, p.w_dtype);
-        if (VEC && m.kind[0] == kPairs) w[E - 8 + j] = load1(p.w, m.first[0] + half + j, p.w_dtype);
+        if (m.kind[0] == kPairs) w[W + j] = load1(p.w, m.first[0] + half + j, p.w_dtype);
       }
     } else {
-      widen_dims<VEC>(load_dims<VEC>(p.w, 0, p.w_dtype, m, half), p.w_dtype, m, w);
+      widen_dims<W>(load_dims<W>(p.w, 0, p.w_dtype, m, half), W > 1 ? p.w_dtype : 0, w);
     }
 #pragma unroll
     for (int j = 0; j < E; j++) w[j] += p.offset;             // (of absent dims: meets zeros)
@@ -176,8 +179,8 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
     auto ask = [&](int i) {
       if (i >= total) return;                                 // (the last values again, never used)
       next = place_of(i);
-      ny = load_dims<VEC>(p.p.x, next.y, y_type, m, half);
-      if (GRAD && normed) nx = load_dims<VEC>(p.x, next.x, x_type, m, half);
+      ny = load_dims<W>(p.p.x, next.y, y_type, m, half);
+      if (GRAD && normed) nx = load_dims<W>(p.x, next.x, x_type, m, half);
     };
     ask(slot);
     __syncthreads();                                          // nobody reads the last rows' table any more
@@ -193,8 +196,8 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
       const bool mine = i < total;
       const Place now = next;
       float y[E], x[E];
-      widen_dims<VEC>(ny, y_type, m, y);
-      if (GRAD && normed) widen_dims<VEC>(nx, x_type, m, x);
+      widen_dims<W>(ny, y_type, y);
+      if (GRAD && normed) widen_dims<W>(nx, x_type, x);
       ask(i + slots);
       const float2 *cs = table + (mine ? now.row : 0) * half;
       if constexpr (!GRAD) {
@@ -206,9 +209,9 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
 #pragma unroll
           for (int j = 0; j < E; j++) y[j] = y[j] * r * w[j];
         }
-        if (p.p.turn) turn_dims<VEC, INTER>(y, m, cs, 1.f);
+        if (p.p.turn) turn_dims<W, INTER>(y, m, cs, 1.f);
       } else {
-        if (p.p.turn) turn_dims<VEC, INTER>(y, m, cs, -1.f);
+        if (p.p.turn) turn_dims<W, INTER>(y, m, cs, -1.f);
         if (normed) {
           float q = 0.f, s = 0.f;
 #pragma unroll
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
           }
         }
       }
-      if (mine) store_dims<VEC>(p.p.out, now.o, p.p.out_dtype, m, half, y);
+      if (mine) store_dims<W>(p.p.out, now.o, p.p.out_dtype, m, half, y);
     }
   }
   if constexpr (GRAD) {
@@ -234,10 +237,10 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
     float *out = a.scratch + ((int64_t)n * kGradGroups + wg) * hd;
     for (int i = threadIdx.x; i < group * E; i += kNormWg) {
       const int l = i / E, j = i - l * E;
-      const Dims<VEC> d = dims_of<VEC>(l, a.items, group, a.rot, a.interleaved != 0);
+      const Dims<W> d = dims_of<W>(l, a.items, group, a.rot, a.interleaved != 0);
       int dim = -1;
-      if constexpr (VEC) {
-        if (j < 8 ? d.kind[0] != kIdle : d.kind[0] == kPairs) dim = d.first[0] + (j < 8 ? j : half + j - 8);
+      if constexpr (W > 1) {
+        if (j < W ? d.kind[0] != kIdle : d.kind[0] == kPairs) dim = d.first[0] + (j < W ? j : half + j - W);
       } else {
 #pragma unroll
         for (int k = 0; k < 4; k++)
@@ -275,26 +278,34 @@ __global__ __launch_bounds__(256) void headnorm_dw_kernel(HeadnormArgs a) {
   p.dw[dim] = s;
 }
 
-bool eights(const void *p, int64_t ld, int64_t hs, int bf16) { const int64_t e = bf16 ? 8 : 4; return ((uintptr_t)p & 15) == 0 && ld % e == 0 && hs % e == 0; }
-
-template <bool GRAD, bool INTER> auto of_type(int type) {
-  return type == kFp32 ? headnorm_kernel<true, GRAD, INTER, kFp32> : type == kBf16 ? headnorm_kernel<true, GRAD, INTER, kBf16> : headnorm_kernel<true, GRAD, INTER, kAny>;
+// Every access of `w` dims is a multiple of its size from one
+bool whole(const void *p, int64_t ld, int64_t hs, int bf16, int w) {
+  const int64_t bytes = bf16 ? 2 * w : 16, e = bytes / (bf16 ? 2 : 4);
+  return ((uintptr_t)p & (bytes - 1)) == 0 && ld % e == 0 && hs % e == 0;
+}
+template <int W, bool GRAD, bool INTER> auto of_type(int type) {
+  return type == kFp32 ? headnorm_kernel<W, GRAD, INTER, kFp32> : type == kBf16 ? headnorm_kernel<W, GRAD, INTER, kBf16> : headnorm_kernel<W, GRAD, INTER, kAny>;
+}
+template <int W> auto of_layout(bool grad, bool inter, int type) {
+  return inter ? (grad ? of_type<W, true, true>(type) : of_type<W, false, true>(type)) : grad ? of_type<W, true, false>(type) : of_type<W, false, false>(type);
 }
 
 hipError_t launch(HeadnormArgs a, bool grad, hipStream_t st) {
-  // eight dims at a time where every access is a multiple of 16 bytes from a multiple of 16 bytes
-  bool vec = a.hd % 8 == 0 && a.rot % (a.interleaved ? 8 : 16) == 0;
-  int heads = 0;
-  for (int n = 0; n < a.n_parts; n++) {
-    const HeadnormPart &p = a.part[n];
-    vec = vec && eights(p.p.x, p.p.ldx, p.p.hsx, p.p.dtype) && eights(p.p.out, p.p.ldo, p.p.hso, p.p.out_dtype);
-    if (grad && p.w) vec = vec && eights(p.x, p.ld, p.hs, p.x_dtype);
-    heads += p.p.heads;
+  int w = 8, heads = 0;
+  for (; w >= 4; w /= 2) {
+    bool fits = a.hd % w == 0 && a.rot % (a.interleaved ? w : 2 * w) == 0;
+    for (int n = 0; n < a.n_parts && fits; n++) {
+      const HeadnormPart &p = a.part[n];
+      fits = whole(p.p.x, p.p.ldx, p.p.hsx, p.p.dtype, w) && whole(p.p.out, p.p.ldo, p.p.hso, p.p.out_dtype, w) && (!grad || !p.w || whole(p.x, p.ld, p.hs, p.x_dtype, w));
+    }
+    if (fits) break;
   }
+  if (w < 4) w = 1;
+  for (int n = 0; n < a.n_parts; n++) heads += a.part[n].p.heads;
   const int half = a.rot / 2;
-  a.items = vec ? (a.interleaved ? a.hd / 8 : half / 8 + (a.hd - a.rot) / 8) : half + a.hd - a.rot;
+  a.items = a.interleaved && w > 1 ? a.hd / w : half / w + (a.hd - a.rot) / w;
   a.group = 1;
-  while (a.group < (vec ? a.items : 64)) a.group *= 2;
+  while (a.group < (w > 1 ? a.items : 64)) a.group *= 2;
   const int slots = kNormWg / a.group, all = grad ? kGradGroups : kForwardGroups, most_rows = half > 0 ? kNormTable / half : 1024;
   a.first[0] = 0;
   for (int n = 0; n < 3; n++) {
@@ -313,8 +324,8 @@ hipError_t launch(HeadnormArgs a, bool grad, hipStream_t st) {
   int type = a.part[0].p.dtype;
   for (int n = 0; n < a.n_parts; n++)
     if (a.part[n].p.dtype != type || (grad && a.part[n].w && a.part[n].x_dtype != type)) type = kAny;
-  const auto kernel = !vec ? (grad ? headnorm_kernel<false, true, false, kAny> : headnorm_kernel<false, false, false, kAny>)
-                      : a.interleaved ? (grad ? of_type<true, true>(type) : of_type<false, true>(type)) : (grad ? of_type<true, false>(type) : of_type<false, false>(type));
+  const auto kernel = w == 8 ? of_layout<8>(grad, a.interleaved, type) : w == 4 ? of_layout<4>(grad, a.interleaved, type)
+                      : grad ? headnorm_kernel<1, true, false, kAny> : headnorm_kernel<1, false, false, kAny>;
   hipLaunchKernelGGL(kernel, grid, dim3(kNormWg), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !grad) return e;

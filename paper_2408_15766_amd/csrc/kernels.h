@@ -386,7 +386,6 @@ struct EmbedGradArgs {
   int rows, d, vocab, accumulate;
   float scale;
   void *dtable;  int64_t ldt;  int out_dtype;
-  int vec;                              // set by launch_embed_grad: eight columns at a time
 };
 uint64_t embed_grad_scratch_bytes(int rows, int vocab, int d);
 hipError_t launch_embed_grad(EmbedGradArgs a, void *scratch, hipStream_t st);
