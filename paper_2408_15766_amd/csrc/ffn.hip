@@ -43,6 +43,7 @@ template <bool SLOPE> __device__ __forceinline__ Act activation(int act, float g
 // Products of 16 x 16 x 32: from registers alone they run at 2.00 PFLOP/s on normally distributed data where those of 32 x 32 x 16, which move their sums twice as often,
 // run at 1.78 (what limits both is the power).
 constexpr int kStageK = 64;
+constexpr int kOnce = 2;                                      // loads marked nontemporal: of weights that nobody reads again (one row of 4096 x 11008 32.4 -> 30.1 us, of 8192 x 28672 159 -> 145)
 template <int TW_, int MB_, int WQ_, int NB_> struct Tile {   // wavefronts and 16-blocks of each along m and n
   static constexpr int TW = TW_, MB = MB_, WQ = WQ_, NB = NB_;
   static constexpr int kWaves = TW * WQ, kThreads = kWaves * 64, kM = TW * MB * 16, kN = WQ * NB * 16;
@@ -81,7 +82,7 @@ template <int LOADS, bool MAJOR, int COLS> struct Side {
     step = MAJOR ? (int64_t)kStageK * ld * 2 : kStageK * 2;
   }
   // copies i0 .. of stage s of the segment
-  __device__ __forceinline__ void copy(int s, unsigned char *to, int i0, int i1, bool two = false) const {
+  template <int KIND = 0> __device__ __forceinline__ void copy(int s, unsigned char *to, int i0, int i1, bool two = false) const {
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
       if (i < i0 || i >= i1) continue;
@@ -89,7 +90,7 @@ template <int LOADS, bool MAJOR, int COLS> struct Side {
       const char *at = (h ? base[1] : base[0]) + s * step;
       const int64_t left = (h ? end[1] : end[0]) - at;
       const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, left < 0x7FFFFFFF ? (int)left : 0x7FFFFFFF, 0x00027000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void *)(to + i * 1024), 16, (int)off[i], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void *)(to + i * 1024), 16, (int)off[i], 0, 0, KIND);
     }
   }
   __device__ __forceinline__ void clear(int left, int q0, unsigned char *mine) const {   // mine: this wavefront's share of the stage, from its copy q0 on
@@ -455,7 +456,7 @@ __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
       const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc((void *)((i < 2 ? w0 : w1) + s * (kStageK * 2)), 0, 0x7FFFFFFF, 0x00027000);
       uint32_t o = off[i & 1];
       if (k[i & 1] >= left) o -= k[i & 1] * 2;                // past k: the stage's first (not used)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void *)(ring + wave * kFewStage + i * 1024), 16, (int)o, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void *)(ring + wave * kFewStage + i * 1024), 16, (int)o, 0, 0, kOnce);
     }
   };
   const char *xrow[TB];
@@ -566,7 +567,7 @@ __global__ __launch_bounds__(256, 2) void ffn_some_kernel(FfnArgs a) {
   unsigned char *const ring[4] = {b0, b1, b2, b3};
   auto copy = [&](unsigned char *to, int s) __attribute__((always_inline)) {
     s = min(s, stages - 1);                                   // past the end: the last stage again (never read)
-    ns.copy(s, to + kRows * 128 + wave * NL * 1024, 0, NL);
+    ns.template copy<kOnce>(s, to + kRows * 128 + wave * NL * 1024, 0, NL);
     ms.copy(s, to + wave * ML * 1024, 0, ML);
   };
   f32x4_t acc[NB][MB];
