@@ -64,7 +64,7 @@ __device__ __forceinline__ int chunk_turn(int k) { return (k & 3) | ((k >> 1) & 
 // One side of a tile: LOADS copies of this wavefront per stage.  The buffer ends with the matrix: what lies behind it (rows past the last, k past the end in the last row) is not
 // accessed; rows and columns past the tile's are never used, and k past the end is cleared.
 template <int LOADS, bool MAJOR, int COLS> struct Side {
-  const char *base[2], *end[2];                               // of the segment: the tile's first row (column, if MAJOR), and the matrix's end; [1]: of the copies from the fourth on, if they have their own
+  const char *base, *end;                                     // of the segment: the tile's first row (column, if MAJOR), and the matrix's end
   uint32_t off[LOADS];                                        // of a lane
   int64_t step;                                               // bytes from one stage to the next
   // k within a stage of copy q's lane
@@ -84,13 +84,12 @@ template <int LOADS, bool MAJOR, int COLS> struct Side {
     step = MAJOR ? (int64_t)kStageK * ld * 2 : kStageK * 2;
   }
   // copies i0 .. of stage s of the segment
-  template <int KIND = 0> __device__ __forceinline__ void copy(int s, unsigned char *to, int i0, int i1, bool two = false) const {
+  template <int KIND = 0> __device__ __forceinline__ void copy(int s, unsigned char *to, int i0, int i1) const {
 #pragma unroll
     for (int i = 0; i < LOADS; i++) {
       if (i < i0 || i >= i1) continue;
-      const int h = two && i >= 4;
-      const char *at = (h ? base[1] : base[0]) + s * step;
-      const int64_t left = (h ? end[1] : end[0]) - at;
+      const char *at = base + s * step;
+      const int64_t left = end - at;
       const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, left < 0x7FFFFFFF ? (int)left : 0x7FFFFFFF, 0x00027000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void *)(to + i * 1024), 16, (int)off[i], 0, 0, KIND);
     }
@@ -216,26 +215,23 @@ __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, in
   // where a matrix of a segment begins for this tile, and where it ends
   auto m_base = [&](int seg) {
     const char *p = (const char *)((MM ? half : seg) ? a.m_src[1] : a.m_src[0]);
-    ms.base[0] = p + (MM ? (int64_t)m0 * 2 : (int64_t)m0 * ldm * 2);
-    ms.end[0] = p + ((int64_t)((MM ? a.k : a.m) - 1) * ldm + (MM ? a.m : a.k)) * 2;
+    ms.base = p + (MM ? (int64_t)m0 * 2 : (int64_t)m0 * ldm * 2);
+    ms.end = p + ((int64_t)((MM ? a.k : a.m) - 1) * ldm + (MM ? a.m : a.k)) * 2;
   };
   auto n_base = [&](int seg) {
     const char *p = (const char *)(seg ? a.n_src[1] : a.n_src[0]);
-    ns.base[0] = p + (NM ? (int64_t)n0 * 2 : (int64_t)n0 * ldn * 2);
-    ns.end[0] = p + ((int64_t)((NM ? a.k : a.n) - 1) * ldn + (NM ? a.n : a.k)) * 2;
+    ns.base = p + (NM ? (int64_t)n0 * 2 : (int64_t)n0 * ldn * 2);
+    ns.end = p + ((int64_t)((NM ? a.k : a.n) - 1) * ldn + (NM ? a.n : a.k)) * 2;
   };
   m_base(0);
-  if constexpr (kGated) {                                     // blocks of 32: gate, up, gate, .. of the same columns; a wavefront copies one, two, or half of one
-    static_assert(NL == 2 || NL == 4 || NL == 8, "whole shares of blocks");
+  if constexpr (kGated) {                                     // blocks of 32: gate, up, gate, .. of the same columns; a wavefront copies one
+    static_assert(NL == 4, "a block");
+    const int first = min(n0 + wave / 2 * 32, a.n - 1);
+    const char *p = (const char *)(wave & 1 ? a.n_src[1] : a.n_src[0]);
+    ns.base = p + (int64_t)first * ldn * 2;
+    ns.end = p + ((int64_t)(a.n - 1) * ldn + a.k) * 2;
 #pragma unroll
-    for (int h = 0; h < (NL + 3) / 4; h++) {
-      const int q0 = wave * NL + 4 * h, block = q0 / 4, first = min(n0 + block / 2 * 32, a.n - 1);
-      const char *p = (const char *)(block & 1 ? a.n_src[1] : a.n_src[0]);
-      ns.base[h] = p + (int64_t)first * ldn * 2;
-      ns.end[h] = p + ((int64_t)(a.n - 1) * ldn + a.k) * 2;
-#pragma unroll
-      for (int i = 4 * h; i < 4 * h + 4 && i < NL; i++) ns.place(i, q0 - block * 4 + i - 4 * h, lane, ldn);
-    }
+    for (int i = 0; i < NL; i++) ns.place(i, i, lane, ldn);
   } else {
 #pragma unroll
     for (int i = 0; i < NL; i++) ns.place(i, wave * NL + i, lane, ldn);
@@ -254,7 +250,7 @@ __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, in
   auto load_n = [&](unsigned char *buf, int s, int i0, int i1) __attribute__((always_inline)) {
     const At at = at_of(s);
     if constexpr (!kGated) { if (a.segs == 2) n_base(at.second); }
-    ns.copy(at.s, buf + wave * NL * 1024, i0, i1, kGated && NL == 8);
+    ns.copy(at.s, buf + wave * NL * 1024, i0, i1);
   };
   auto load_m = [&](unsigned char *buf, int s, int i0, int i1) __attribute__((always_inline)) {
     const At at = at_of(s);
@@ -280,7 +276,7 @@ __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, in
   // that is behind the stage's last read.
   u32x4_t fm[4], fn[2][NB];
   constexpr int kBarrier = MB - 4, kEach = (NB + 1) / 2;
-  static_assert(MB % 4 == 0, "a ring of four blocks");
+  static_assert(MB % 4 == 0 && MB >= NL, "a ring of four blocks, a copy of the n side behind each");
   auto step = [&](int now, bool last, unsigned char *mc, unsigned char *nc, unsigned char *mn, unsigned char *nn, auto copies, auto turn) __attribute__((always_inline)) {
     int mat = mat_, nat = nat_;
     asm volatile("" : "+v"(mat), "+v"(nat));                  // (else the addresses of all steps are kept in registers at once)
@@ -304,7 +300,7 @@ __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, in
     }
   };
   auto stage = [&](unsigned char *mc, unsigned char *nc, unsigned char *mn, unsigned char *nn, unsigned char *np, int s) __attribute__((always_inline)) {
-    step(0, false, mc, nc, mn, nn, [&](int t) __attribute__((always_inline)) { load_n(np, s + 2, min(t, NL), min(t + 1, NL)); if (t == MB - 1) load_n(np, s + 2, min(MB, NL), NL); },
+    step(0, false, mc, nc, mn, nn, [&](int t) __attribute__((always_inline)) { load_n(np, s + 2, min(t, NL), min(t + 1, NL)); },
          []() {});
     step(1, true, mc, nc, mn, nn, [&](int t) __attribute__((always_inline)) {
       constexpr int kHalf = (ML + 1) / 2;
@@ -434,10 +430,9 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(const float *part, int sp
 // of stages of their own in the LDS (16 gate and 16 up rows x 64 k, 4 KB): nobody waits for anybody until the quarters meet.  x comes out of the L2, straight
 // into registers, as many stages ahead.
 constexpr int kFewStage = 4096, kFewRows = 16;
-template <int TB>                                             // blocks of 16 rows of x
 __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char r0[4 * kFewStage], r1[4 * kFewStage], r2[4 * kFewStage];   // (arrays of their own: the compiler waits for the copies into what it reads)
-  __shared__ float sums[4][TB * 8][64];
+  __shared__ float sums[4][8][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
   const int n0 = blockIdx.x * 16, stages = (a.k + kStageK - 1) / kStageK;
   const int s0 = stages * wave / 4, s1 = stages * (wave + 1) / 4;
@@ -461,27 +456,20 @@ __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void *)(ring + wave * kFewStage + i * 1024), 16, (int)o, 0, 0, kOnce);
     }
   };
-  const char *xrow[TB];
-#pragma unroll
-  for (int t = 0; t < TB; t++) xrow[t] = (const char *)a.m_src[0] + (int64_t)min(16 * t + r, a.m - 1) * a.ldm * 2;
-  struct X { u32x4_t v[2][TB]; };
+  const char *xrow = (const char *)a.m_src[0] + (int64_t)min(r, a.m - 1) * a.ldm * 2;
+  struct X { u32x4_t v[2]; };
   auto load_x = [&](X &x, int s) __attribute__((always_inline)) {
     s = min(s, s1 - 1);
 #pragma unroll
     for (int j = 0; j < 2; j++) {
       const int kk = s * kStageK + j * 32 + q * 8;
-#pragma unroll
-      for (int t = 0; t < TB; t++) x.v[j][t] = *(const u32x4_t *)(xrow[t] + (kk < a.k ? kk : 0) * 2);
+      x.v[j] = *(const u32x4_t *)(xrow + (kk < a.k ? kk : 0) * 2);
     }
   };
-  f32x4_t acc[2][TB];
-#pragma unroll
-  for (int b = 0; b < 2; b++)
-#pragma unroll
-    for (int t = 0; t < TB; t++) acc[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
   const int at = wave * kFewStage + r * 128 + ((q ^ (r >> 1)) * 16);
   auto stage = [&](unsigned char *ring, X &x, int s) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(0x0F70 | ((8 + 4 * TB) & 15) | (((8 + 4 * TB) >> 4) << 14));   // this stage's copies and x are here, the next two's may be under way
+    __builtin_amdgcn_s_waitcnt(0x0F70 | 12);                 // this stage's copies and x are here, the next two's may be under way
     u32x4_t w[2][2];
 #pragma unroll
     for (int j = 0; j < 2; j++)
@@ -493,19 +481,13 @@ __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
       const u32x4_t zero = {0u, 0u, 0u, 0u};
 #pragma unroll
       for (int j = 0; j < 2; j++)
-        if (s * kStageK + j * 32 + q * 8 >= a.k) {
-          w[j][0] = w[j][1] = zero;
-#pragma unroll
-          for (int t = 0; t < TB; t++) x.v[j][t] = zero;
-        }
+        if (s * kStageK + j * 32 + q * 8 >= a.k) w[j][0] = w[j][1] = x.v[j] = zero;
     }
 #pragma unroll
     for (int j = 0; j < 2; j++)
 #pragma unroll
       for (int b = 0; b < 2; b++)
-#pragma unroll
-        for (int t = 0; t < TB; t++)
-          acc[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w[j][b]), __builtin_bit_cast(bf16x8_t, x.v[j][t]), acc[b][t], 0, 0, 0);
+        acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w[j][b]), __builtin_bit_cast(bf16x8_t, x.v[j]), acc[b], 0, 0, 0);
   };
   if (s0 < s1) {
     X x0, x1, x2;
@@ -521,35 +503,33 @@ __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
     }
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);                         // no copy into the LDS outlives the workgroup
-  // lane (r, q) holds row r of a block of x at the columns 4 q + v
+  // lane (r, q) holds row r of x at the columns 4 q + v
 #pragma unroll
   for (int b = 0; b < 2; b++)
 #pragma unroll
-    for (int t = 0; t < TB; t++)
-#pragma unroll
-      for (int v = 0; v < 4; v++) sums[wave][(b * TB + t) * 4 + v][lane] = acc[b][t][v];
+    for (int v = 0; v < 4; v++) sums[wave][b * 4 + v][lane] = acc[b][v];
   __syncthreads();
-  if (wave >= TB) return;
-  const int m = wave * 16 + r, n = n0 + 4 * q;
+  if (wave != 0) return;
+  const int n = n0 + 4 * q;
   float h[4];
 #pragma unroll
   for (int v = 0; v < 4; v++) {
     float s[2];
 #pragma unroll
     for (int b = 0; b < 2; b++) {
-      const int e = (b * TB + wave) * 4 + v;
+      const int e = b * 4 + v;
       s[b] = ((sums[0][e][lane] + sums[1][e][lane]) + sums[2][e][lane]) + sums[3][e][lane];
     }
     h[v] = s[0] * activation<false>(a.act, s[0]).p * s[1];
   }
-  if (m < a.m && n < a.n) *(u32x2_t *)((bf16_t *)a.out[0] + (int64_t)m * a.ldo + n) = u32x2_t{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+  if (r < a.m && n < a.n) *(u32x2_t *)((bf16_t *)a.out[0] + (int64_t)r * a.ldo + n) = u32x2_t{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
 }
 
 // ---- some rows ---------------------------------------------------------------------------------------
 // 17 to 128 rows: still bound by the weights' way from memory, but x has to come through the LDS too (read by every wavefront for itself it took twice the weights' way: 98 us
 // for 60 rows, 4096 x 14336).  A workgroup has all rows and 32 columns of h, so that there are workgroups enough to keep the memory busy (tiles of 64 columns: 66 us); four
 // wavefronts with a quarter of the rows each; a ring of four (three) stages of 64 k, two workgroups to a compute unit.
-template <int MB, int TO>                                     // MB: blocks of 16 rows of a wavefront
+template <int MB>                                             // blocks of 16 rows of a wavefront
 __global__ __launch_bounds__(256, 2) void ffn_some_kernel(FfnArgs a) {
   constexpr int kRows = MB * 64, NB = 4, ML = MB * 2, NL = 2, kRing = MB == 1 ? 4 : 3, kBytes = (kRows + 64) * 128;
   __shared__ __attribute__((aligned(1024))) unsigned char b0[kBytes], b1[kBytes], b2[kBytes], b3[kRing > 3 ? kBytes : 16];
@@ -559,13 +539,13 @@ __global__ __launch_bounds__(256, 2) void ffn_some_kernel(FfnArgs a) {
   Side<NL, false, 64> ns;
 #pragma unroll
   for (int i = 0; i < ML; i++) ms.place(i, wave * ML + i, lane, a.ldm);
-  ms.base[0] = (const char *)a.m_src[0];
-  ms.end[0] = ms.base[0] + ((int64_t)(a.m - 1) * a.ldm + a.k) * 2;
+  ms.base = (const char *)a.m_src[0];
+  ms.end = ms.base + ((int64_t)(a.m - 1) * a.ldm + a.k) * 2;
 #pragma unroll
   for (int i = 0; i < NL; i++) ns.place(i, (wave & 1) * NL + i, lane, a.ldn);   // wavefronts 0 and 1 copy the gate rows, 2 and 3 the up rows
   const char *w = (const char *)(wave >> 1 ? a.n_src[1] : a.n_src[0]);
-  ns.base[0] = w + (int64_t)n0 * a.ldn * 2;
-  ns.end[0] = w + ((int64_t)(a.n - 1) * a.ldn + a.k) * 2;
+  ns.base = w + (int64_t)n0 * a.ldn * 2;
+  ns.end = w + ((int64_t)(a.n - 1) * a.ldn + a.k) * 2;
   unsigned char *const ring[4] = {b0, b1, b2, b3};
   auto copy = [&](unsigned char *to, int s) __attribute__((always_inline)) {
     s = min(s, stages - 1);                                   // past the end: the last stage again (never read)
@@ -613,7 +593,7 @@ __global__ __launch_bounds__(256, 2) void ffn_some_kernel(FfnArgs a) {
     if constexpr (kRing > 3) { if (s + 3 < stages) stage(b3, b2, s + 3); }
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);                         // no copy into the LDS outlives the workgroup
-  finish<MB, NB, TO>(a, acc, wave * MB * 16, n0, 0, nullptr);
+  finish<MB, NB, kToH>(a, acc, wave * MB * 16, n0, 0, nullptr);
 }
 
 // ---- launches -----------------------------------------------------------------------------------------
@@ -719,11 +699,11 @@ hipError_t launch_ffn(const FfnCall &c, hipStream_t st) {
   a.m = c.rows; a.n = c.f; a.k = c.d; a.segs = a.halves = a.splits = 1; a.act = c.act;
   a.m_src[0] = c.x; a.ldm = c.ldx; a.n_src[0] = c.wg; a.n_src[1] = c.wu; a.ldn = c.ldw; a.out[0] = c.h; a.ldo = c.ldh;
   if (c.rows > kFewRows && some_pays(c.rows, c.f)) {
-    hipLaunchKernelGGL((c.rows <= 64 ? ffn_some_kernel<1, kToH> : ffn_some_kernel<2, kToH>), dim3((c.f + 31) / 32), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((c.rows <= 64 ? ffn_some_kernel<1> : ffn_some_kernel<2>), dim3((c.f + 31) / 32), dim3(256), 0, st, a);
     return hipGetLastError();
   }
   if (c.rows > kFewRows) return launch_planned<false, false, kToH>(a, ffn_plan(a.m, a.n, a.k, 1, 1, true).tile, st);
-  hipLaunchKernelGGL(ffn_few_kernel<1>, dim3((c.f + 15) / 16), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(ffn_few_kernel, dim3((c.f + 15) / 16), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
