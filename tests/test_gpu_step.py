@@ -471,6 +471,29 @@ def test_ffn_gated_large_and_small_gates(P):
             within(o, want, tol)
 
 
+def test_ffn_gated_gates_whose_cube_overflows(P):
+    """Gates of up to 2^120, whose square or cube is beyond fp32: the slope is still one or nothing.  (One product each, all powers of two: exact results but for the
+    small gates' activations, which are left out here.)"""
+    d = f = 64
+    x = torch.zeros(70, d, device="cuda", dtype=torch.bfloat16)
+    x[:, 0] = 2.0 ** (torch.arange(70, device="cuda") - 10).float()       # 2^-10 .. 2^59
+    x[35:, 0] *= -1
+    wg, wu = torch.zeros(f, d, device="cuda").bfloat16(), torch.zeros(f, d, device="cuda").bfloat16()
+    wg[:, 0] = (2.0 ** (torch.arange(f, device="cuda") - 3).float()).bfloat16()   # 2^-3 .. 2^60
+    x[:, 1], wu[:, 1] = 1, 2.0 ** -100
+    g = x[:, :1].double() * wg[:, 0].double()
+    dh = torch.where(g.abs() >= 2.0 ** 10, 1.0, 0.0).bfloat16()
+    step = (g > 0).double() * dh.double()
+    dg, du = step * 2.0 ** -100, step * g
+    for act in ("silu", "gelu", "gelu_tanh"):
+        h = P.spec_k_ffn_gated(x, wg, wu, act=act)
+        assert torch.equal(torch.where(dh > 0, h, 0).double(), du * 2.0 ** -100)
+        dx, dwg, dwu = P.spec_k_ffn_gated_grad(x, wg, wu, dh, act=act)
+        for got, want, most in ((dx, dg @ wg.double() + du @ wu.double(), dg @ wg.double().abs() + du @ wu.double().abs()), (dwg, dg.t() @ x.double(), dg.t() @ x.double().abs()),
+                                (dwu, du.t() @ x.double(), du.t() @ x.double().abs())):
+            within(got, want, U16 * want.abs() + 2 * 200 * U32 * most + 1e-38)
+
+
 def test_ffn_gated_gradients_against_differences(P):
     rows, d, f = 70, 64, 72
     x, wg, wu, dh = ffn_case(3, rows, d, f)
