@@ -93,7 +93,7 @@ int spec_k_headnorm_rotary_grad(const spec_rotary_plan *plan /* host */, int32_t
  *   SPEC_ACT_GELU_TANH  g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2
  * Sums and activations in fp32.  Row strides ldx, ldw, .. in elements; d, f and the strides are multiples of 8,
  * pointers of 16 bytes.  1 <= rows <= 2^20, d, f <= 2^20, rows * d, rows * f and d * f <= 2^36, strides <=
- * 2^21.  What lies between rows is left alone.  h overlaps no input.  Up to 64 rows the call reads the weights once
+ * 2^21.  What lies between rows is left alone.  h overlaps no input.  Up to 128 rows the call reads the weights once
  * and is bound by that (decoding with weights as they are trained); the order of a sum depends on the number of rows, so that a row's last bits may change
  * with it. */
 #define SPEC_ACT_SILU 0

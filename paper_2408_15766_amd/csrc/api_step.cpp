@@ -60,6 +60,7 @@ bool ffn_sizes_ok(int32_t rows, int32_t d, int32_t f) {
 bool ffn_matrix_ok(const void *p, int64_t ld, int64_t rows, int64_t cols) {   // rows so far apart that 256 of them fit 31 bits
   return p && aligned(p, 16) && ld >= 0 && ld <= (1 << 21) && (rows == 1 || (ld >= cols && ld % 8 == 0));
 }
+int64_t row_step(int64_t ld, int32_t rows, int32_t cols) { return rows == 1 ? cols : ld; }   // one row's stride may be anything; the kernels place rows that are not there by it
 
 // ---- clipping
 bool grad_ok(const spec_grad_part &p, bool clip) {
@@ -194,7 +195,7 @@ int spec_k_ffn_gated(const void *x, int64_t ldx, int32_t rows, int32_t d, const 
   if (!ffn_matrix_ok(x, ldx, rows, d) || !ffn_matrix_ok(w_gate, ldw, f, d) || !ffn_matrix_ok(w_up, ldw, f, d) || !ffn_matrix_ok(h, ldh, rows, f)) return SPEC_EINVAL;
   if (h == x || h == w_gate || h == w_up) return SPEC_EINVAL;
   FfnCall c{};
-  c.x = x; c.ldx = ldx; c.wg = w_gate; c.wu = w_up; c.ldw = ldw; c.rows = rows; c.d = d; c.f = f; c.act = act; c.h = h; c.ldh = ldh;
+  c.x = x; c.ldx = row_step(ldx, rows, d); c.wg = w_gate; c.wu = w_up; c.ldw = ldw; c.rows = rows; c.d = d; c.f = f; c.act = act; c.h = h; c.ldh = row_step(ldh, rows, f);
   return done(launch_ffn(c, (hipStream_t)stream));
 }
 
@@ -216,8 +217,8 @@ int spec_k_ffn_gated_grad(const void *x, int64_t ldx, int32_t rows, int32_t d, c
       if (out[o] == in[i] || (out[o] && i < o && out[o] == out[i])) return SPEC_EINVAL;
   }
   FfnCall c{};
-  c.x = x; c.ldx = ldx; c.wg = w_gate; c.wu = w_up; c.ldw = ldw; c.rows = rows; c.d = d; c.f = f; c.act = act; c.h = const_cast<void *>(dh); c.ldh = lddh;
-  c.dx = dx; c.lddx = lddx; c.dwg = dw_gate; c.dwu = dw_up; c.lddw = lddw;
+  c.x = x; c.ldx = row_step(ldx, rows, d); c.wg = w_gate; c.wu = w_up; c.ldw = ldw; c.rows = rows; c.d = d; c.f = f; c.act = act; c.h = const_cast<void *>(dh); c.ldh = row_step(lddh, rows, f);
+  c.dx = dx; c.lddx = row_step(lddx, rows, d); c.dwg = dw_gate; c.dwu = dw_up; c.lddw = lddw;
   return done(launch_ffn_grad(c, scratch, (hipStream_t)stream));
 }
 

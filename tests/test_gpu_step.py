@@ -494,6 +494,20 @@ def test_ffn_gated_gates_whose_cube_overflows(P):
             within(got, want, U16 * want.abs() + 2 * 200 * U32 * most + 1e-38)
 
 
+def test_ffn_gated_one_row_of_any_stride(P):
+    """With one row its stride has no meaning, whatever it is."""
+    d, f = 136, 72
+    x, wg, wu, dh = ffn_case(11, 1, d, f)
+    want, back = P.spec_k_ffn_gated(x, wg, wu), P.spec_k_ffn_gated_grad(x, wg, wu, dh)
+    st, scratch = torch.cuda.current_stream().cuda_stream, torch.empty(P.spec_k_ffn_gated_grad_scratch_bytes(1, d, f), dtype=torch.uint8, device="cuda")
+    for ld in (0, 3, 1 << 21):
+        h, outs = torch.empty_like(want), [torch.empty_like(t) for t in back]
+        assert P.lib.spec_k_ffn_gated(x.data_ptr(), ld, 1, d, wg.data_ptr(), wu.data_ptr(), d, f, 0, h.data_ptr(), ld, st) == 0
+        assert P.lib.spec_k_ffn_gated_grad(x.data_ptr(), ld, 1, d, wg.data_ptr(), wu.data_ptr(), d, f, 0, dh.data_ptr(), ld, outs[0].data_ptr(), ld, outs[1].data_ptr(), outs[2].data_ptr(), d,
+                                           scratch.data_ptr(), scratch.numel(), st) == 0
+        assert torch.equal(h, want) and all(torch.equal(a, b) for a, b in zip(outs, back))
+
+
 def test_ffn_gated_gradients_against_differences(P):
     rows, d, f = 70, 64, 72
     x, wg, wu, dh = ffn_case(3, rows, d, f)
