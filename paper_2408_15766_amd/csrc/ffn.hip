@@ -410,18 +410,21 @@ __global__ __launch_bounds__(Small::kThreads, 2) void ffn_both_kernel(FfnBoth b)
   }
 }
 
-// The ranges' sums, in ascending order: eight columns a thread
-__global__ __launch_bounds__(256) void ffn_join_kernel(const float *part, int splits, int halves, int m, int n, void *out0, void *out1, int64_t ldo) {
-  const int per = n / 8;
-  const int64_t all = (int64_t)m * per, set = (int64_t)m * n * halves;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all * halves; i += (int64_t)gridDim.x * 256) {
-    const int half = i >= all;
-    const int64_t at = half ? i - all : i, row = at / per;
+// The ranges' sums of one product, or of both of a small call (1024 rows, 512 x 1376: 36.0 us, with a launch each 37.5), in ascending order: eight columns a thread
+struct FfnJoin { const float *part; int splits, halves, m, n; void *out[2]; int64_t ldo; };
+__global__ __launch_bounds__(256) void ffn_join_kernel(FfnJoin first, FfnJoin second) {
+  const int64_t here = (int64_t)first.m * (first.n / 8) * first.halves, all = here + (int64_t)second.m * (second.n / 8) * second.halves;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const FfnJoin j = i < here ? first : second;
+    const int per = j.n / 8;
+    const int64_t each = (int64_t)j.m * per, set = (int64_t)j.m * j.n * j.halves, k = i < here ? i : i - here;
+    const int half = k >= each;
+    const int64_t at = half ? k - each : k, row = at / per;
     const int col = (int)(at - row * per) * 8;
-    const float *p = part + half * (int64_t)m * n + row * n + col;
+    const float *p = j.part + half * (int64_t)j.m * j.n + row * j.n + col;
     f32x4_t a = *(const f32x4_t *)p, b = *(const f32x4_t *)(p + 4);
-    for (int s = 1; s < splits; s++) { a += *(const f32x4_t *)(p + s * set); b += *(const f32x4_t *)(p + s * set + 4); }
-    *(u32x4_t *)((bf16_t *)(half ? out1 : out0) + row * ldo + col) =
+    for (int s = 1; s < j.splits; s++) { a += *(const f32x4_t *)(p + s * set); b += *(const f32x4_t *)(p + s * set + 4); }
+    *(u32x4_t *)((bf16_t *)(half ? j.out[1] : j.out[0]) + row * j.ldo + col) =
         u32x4_t{pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y), pack_bf16x2(b.z, b.w)};
   }
 }
@@ -628,13 +631,13 @@ template <class L, bool MM, bool NM, int TO> hipError_t launch_tiles(FfnArgs a, 
 // large tiles) 441, 233, 161, 142, 177, small (128) 346, 186, 162, 142, 156; of 777 rows, 1000 x 2728 (16, 56) 91, 54, 42, 36, 31, small 72, 43, 35, 30, 30, in eight 29.  Forward, large /
 // small: 512 rows of 4096 x 14336 (224 large tiles) 96 / 113, 777 of 1000 x 2728 (88) 19.6 / 20.9, 300 of 4096 x 4096 (64) 42.6 / 40.3, 200 of 8192 x 2000 (16) 74 / 62.
 struct FfnPlan { int tile, splits; };                         // tile 0: 256 x 256 and halves, 1: 128 x 128
-FfnPlan ffn_plan(int64_t m, int64_t n, int64_t k, int halves, int segs, bool gated) {
+FfnPlan ffn_plan(int64_t m, int64_t n, int64_t k, int halves, int segs, bool gated, bool both = false) {
   auto tiles_m = [&](int t) { const int size = t ? Small::kM : Big::kM; return (m + size - 1) / size * halves; };
   auto tiles_n = [&](int t) { const int size = (t ? Small::kN : Big::kN) / (gated ? 2 : 1); return (n + size - 1) / size; };
   FfnPlan p{tiles_m(0) * tiles_n(0) >= 64 ? 0 : 1, 1};
   if (gated) return p;
   const int64_t m_tiles = tiles_m(p.tile), n_tiles = tiles_n(p.tile), stages = segs * ((k + kStageK - 1) / kStageK);
-  const int64_t ranges = (p.tile == 0 ? kXcdUnits / 2 : 2 * kXcdUnits) / fullest(m_tiles, n_tiles, parts_of_m(m_tiles, n_tiles)), most = stages / 4 < 16 ? stages / 4 : 16;
+  const int64_t ranges = (p.tile == 0 ? kXcdUnits / 2 : both ? kXcdUnits * 3 / 4 : 2 * kXcdUnits) / fullest(m_tiles, n_tiles, parts_of_m(m_tiles, n_tiles)), most = stages / 4 < 16 ? stages / 4 : 16;
   p.splits = (int)(ranges < most ? ranges : most);
   if (p.splits < 1) p.splits = 1;
   return p;
@@ -642,28 +645,30 @@ FfnPlan ffn_plan(int64_t m, int64_t n, int64_t k, int halves, int segs, bool gat
 template <bool MM, bool NM, int TO> hipError_t launch_planned(const FfnArgs &a, int tile, hipStream_t st) {
   return tile == 0 ? launch_tiles<Big, MM, NM, TO>(a, st) : launch_tiles<Small, MM, NM, TO>(a, st);
 }
-hipError_t launch_join(const FfnArgs &a, hipStream_t st) {
-  const int64_t pieces = (int64_t)a.m * (a.n / 8) * a.halves, groups = (pieces + 255) / 256;
-  hipLaunchKernelGGL(ffn_join_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, st, a.part, a.splits, a.halves, a.m, a.n, a.out[0], a.out[1], a.ldo);
+FfnJoin join_of(const FfnArgs &a) { return FfnJoin{a.part, a.splits, a.halves, a.splits > 1 ? a.m : 0, a.n, {a.out[0], a.out[1]}, a.ldo}; }   // (no rows if k is not cut)
+hipError_t launch_join(const FfnJoin &a, const FfnJoin &b, hipStream_t st) {
+  const int64_t pieces = (int64_t)a.m * (a.n / 8) * a.halves + (int64_t)b.m * (b.n / 8) * b.halves, groups = (pieces + 255) / 256;
+  hipLaunchKernelGGL(ffn_join_kernel, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, st, a, b);
   return hipGetLastError();
 }
 // A product into out, through ranges' sums if k is cut
-template <bool MM, bool NM> hipError_t launch_product(FfnArgs a, hipStream_t st) {
-  const FfnPlan p = ffn_plan(a.m, a.n, a.k, a.halves, a.segs, false);
+template <bool MM, bool NM> hipError_t launch_product(FfnArgs a, bool both, hipStream_t st) {
+  const FfnPlan p = ffn_plan(a.m, a.n, a.k, a.halves, a.segs, false, both);
   a.splits = p.splits;
   if (p.splits == 1) return launch_planned<MM, NM, kToOut>(a, p.tile, st);
   const hipError_t e = launch_planned<MM, NM, kToParts>(a, p.tile, st);
-  return e != hipSuccess ? e : launch_join(a, st);
+  return e != hipSuccess ? e : launch_join(join_of(a), FfnJoin{}, st);
 }
-// Both products in one launch, if dx takes small tiles and the others are at most two rounds of them (gradients in all, one after the other / together: 777 rows, 1000 x 2728 79 / 68 us, 300 of
-// 4096 x 4096 139 / 121, 100 of 1024 x 2752 43 / 36, 4096 of 512 x 1376 91 / 89)
-bool both_pay(const FfnArgs &dx, const FfnArgs &dw) {
-  return ffn_plan(dx.m, dx.n, dx.k, dx.halves, dx.segs, false).tile == 1 && ((int64_t)(dw.m + Small::kM - 1) / Small::kM) * dw.halves * ((dw.n + Small::kN - 1) / Small::kN) <= 1024;
+// dx and the weights' gradients in one launch, if dx takes small tiles and the others are at most two rounds of them (gradients in all, one after the other / together: 777 rows, 1000 x 2728 79 / 68
+// us, 300 of 4096 x 4096 139 / 121, 100 of 1024 x 2752 43 / 36, 4096 of 512 x 1376 91 / 89).  Neither has the chip to itself then, and fewer ranges are written and read again: with ranges for
+// 64 / 32 / 24 / 16 workgroups an XCD 777 rows of 1000 x 2728 take 67.6, 61.7, 60.7, 68.4 us, 512 of 768 x 2048 51.8, 35.0, 36.1, 39.2, 300 of 1024 x 2752 45.0, 43.2, 38.9, 41.8, 4096 of 256 x
+// 688 56.7, 49.4, 44.5, 40.6.  (Calls for one of the two alone keep those ranges, so that a sum's order does not depend on what else is asked for.)
+bool both_pay(int64_t rows, int64_t d, int64_t f) {
+  return ffn_plan(rows, d, f, 1, 2, false).tile == 1 && (f + Small::kM - 1) / Small::kM * 2 * ((d + Small::kN - 1) / Small::kN) <= 1024;
 }
 hipError_t launch_both(FfnBoth b, hipStream_t st) {
   for (FfnArgs *a : {&b.dx, &b.dw}) {
-    const FfnPlan p = ffn_plan(a->m, a->n, a->k, a->halves, a->segs, false);
-    a->splits = p.splits;
+    a->splits = ffn_plan(a->m, a->n, a->k, a->halves, a->segs, false, true).splits;
     if (!set_tiles<Small, kToOut>(*a)) return hipErrorInvalidValue;
   }
   b.dx_each = (int)(8 * fullest(b.dx.m_tiles, b.dx.n_tiles, b.dx.m_parts));
@@ -671,13 +676,11 @@ hipError_t launch_both(FfnBoth b, hipStream_t st) {
   const bool x = b.dx.splits > 1, w = b.dw.splits > 1;
   const auto kernel = x ? (w ? ffn_both_kernel<kToParts, kToParts> : ffn_both_kernel<kToParts, kToOut>) : w ? ffn_both_kernel<kToOut, kToParts> : ffn_both_kernel<kToOut, kToOut>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(b.dx_each * b.dx.splits + b.dw_each * b.dw.splits)), dim3(Small::kThreads), 0, st, b);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && x) e = launch_join(b.dx, st);
-  if (e == hipSuccess && w) e = launch_join(b.dw, st);
-  return e;
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || !(x || w) ? e : launch_join(join_of(b.dx), join_of(b.dw), st);
 }
-uint64_t parts_bytes(int64_t m, int64_t n, int64_t k, int halves, int segs) {
-  const FfnPlan p = ffn_plan(m, n, k, halves, segs, false);
+uint64_t parts_bytes(int64_t m, int64_t n, int64_t k, int halves, int segs, bool both) {
+  const FfnPlan p = ffn_plan(m, n, k, halves, segs, false, both);
   return p.splits == 1 ? 0 : (uint64_t)p.splits * halves * m * n * 4;
 }
 uint64_t up256(uint64_t b) { return (b + 255) / 256 * 256; }
@@ -686,7 +689,8 @@ uint64_t up256(uint64_t b) { return (b + 255) / 256 * 256; }
 
 // dg and du, and behind them room for the ranges' sums
 uint64_t ffn_grad_scratch_bytes(int rows, int d, int f) {
-  const uint64_t x = parts_bytes(rows, d, f, 1, 2), w = parts_bytes(f, d, rows, 2, 1);
+  const bool both = both_pay(rows, d, f);
+  const uint64_t x = parts_bytes(rows, d, f, 1, 2, both), w = parts_bytes(f, d, rows, 2, 1, both);
   return 2 * up256((uint64_t)rows * f * 2) + up256(x) + up256(w);
 }
 
@@ -717,16 +721,17 @@ hipError_t launch_ffn_grad(const FfnCall &c, void *scratch, hipStream_t st) {
   a.dh = c.h; a.lddh = c.ldh; a.out[0] = dg; a.out[1] = du; a.ldo = c.f;
   hipError_t e = launch_planned<false, false, kToDgu>(a, ffn_plan(a.m, a.n, a.k, 1, 1, true).tile, st);
   if (e != hipSuccess) return e;
+  const bool both = both_pay(c.rows, c.d, c.f);
   FfnBoth b{};
   b.dx.part = (float *)((char *)scratch + 2 * each);
-  b.dw.part = (float *)((char *)b.dx.part + up256(parts_bytes(c.rows, c.d, c.f, 1, 2)));
+  b.dw.part = (float *)((char *)b.dx.part + up256(parts_bytes(c.rows, c.d, c.f, 1, 2, both)));
   b.dx.m = c.rows; b.dx.n = c.d; b.dx.k = c.f; b.dx.segs = 2; b.dx.halves = 1;
   b.dx.m_src[0] = dg; b.dx.m_src[1] = du; b.dx.ldm = c.f; b.dx.n_src[0] = c.wg; b.dx.n_src[1] = c.wu; b.dx.ldn = c.ldw; b.dx.out[0] = c.dx; b.dx.ldo = c.lddx;
   b.dw.m = c.f; b.dw.n = c.d; b.dw.k = c.rows; b.dw.segs = 1; b.dw.halves = 2;
   b.dw.m_src[0] = dg; b.dw.m_src[1] = du; b.dw.ldm = c.f; b.dw.n_src[0] = b.dw.n_src[1] = c.x; b.dw.ldn = c.ldx; b.dw.out[0] = c.dwg; b.dw.out[1] = c.dwu; b.dw.ldo = c.lddw;
-  if (c.dx && c.dwg && both_pay(b.dx, b.dw)) return launch_both(b, st);
-  if (c.dx && (e = launch_product<false, true>(b.dx, st)) != hipSuccess) return e;
-  if (c.dwg && (e = launch_product<true, true>(b.dw, st)) != hipSuccess) return e;
+  if (c.dx && c.dwg && both) return launch_both(b, st);
+  if (c.dx && (e = launch_product<false, true>(b.dx, both, st)) != hipSuccess) return e;
+  if (c.dwg && (e = launch_product<true, true>(b.dw, both, st)) != hipSuccess) return e;
   return hipSuccess;
 }
 
