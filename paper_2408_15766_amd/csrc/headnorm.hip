@@ -4,8 +4,8 @@
 // (a head of 72), else up to four single ones (then a wavefront holds the head, and takes five times as long).  So a weight is read once, the sums over a head are a few exchanges between neighbouring lanes, and a lane adds up its dims' share of the
 // weights' gradient in registers over all its heads; the workgroup's shares meet in the LDS once, in a fixed order, the workgroups' in a second
 // launch.  The rows' (cos, sin) table is made in the LDS as for the rotary embedding alone.
-// Bound: memory (forward: each element once in, once out; gradients: dy and x once in, dx once out).  Measured: gradients of 4096 rows of 32 + 32 heads of 128 in bf16 38 us (5.3 TB/s) and 5
-// for the second launch; 52 with a fixed number of rows a workgroup, whose table was made again for each.  Rows of a tree (60, 32 + 8 + 8 heads) 5.5 us, a launch and two trips to memory.
+// Bound: memory (forward: each element once in, once out; gradients: dy and x once in, dx once out).  Measured: gradients of 4096 rows of 32 + 32 heads of 128 in bf16 38 us (5.3 TB/s) and 4
+// for the second launch (5 with eight threads to a dim); 52 with a fixed number of rows a workgroup, whose table was made again for each.  Rows of a tree (60, 32 + 8 + 8 heads) 5.5 us, a launch and two trips to memory.
 #include "common.h"
 #include "elements.h"
 #include "kernels.h"
@@ -258,9 +258,10 @@ __global__ __launch_bounds__(kNormWg) void headnorm_kernel(HeadnormArgs a) {
   }
 }
 
-// The workgroups' shares of dw, in their order: a thread adds up every eighth, then eight threads meet.
-__global__ __launch_bounds__(256) void headnorm_dw_kernel(HeadnormArgs a) {
-  __shared__ float sh[256];
+// The workgroups' shares of dw: a thread adds up every kSlices-th in their order, then kSlices threads meet.
+constexpr int kSlices = 32;
+__global__ __launch_bounds__(32 * kSlices) void headnorm_dw_kernel(HeadnormArgs a) {
+  __shared__ float sh[32 * kSlices];
   const HeadnormPart p = a.part[blockIdx.y];
   if (p.dw == nullptr) return;
   const int dim = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5;
@@ -269,13 +270,13 @@ __global__ __launch_bounds__(256) void headnorm_dw_kernel(HeadnormArgs a) {
   float s = 0.f;
   if (dim < a.hd) {
 #pragma unroll 8
-    for (int g = slice; g < groups; g += 8) s += share[(int64_t)g * a.hd + dim];
+    for (int g = slice; g < groups; g += kSlices) s += share[(int64_t)g * a.hd + dim];
   }
   sh[threadIdx.x] = s;
   __syncthreads();
   if (slice != 0 || dim >= a.hd) return;
 #pragma unroll
-  for (int i = 1; i < 8; i++) s += sh[i * 32 + threadIdx.x];
+  for (int i = 1; i < kSlices; i++) s += sh[i * 32 + threadIdx.x];
   p.dw[dim] = s;
 }
 
@@ -333,7 +334,7 @@ hipError_t launch(HeadnormArgs a, bool grad, hipStream_t st) {
   bool any = false;
   for (int n = 0; n < a.n_parts; n++) any = any || a.part[n].dw != nullptr;
   if (!any) return hipSuccess;
-  hipLaunchKernelGGL(headnorm_dw_kernel, dim3((a.hd + 31) / 32, a.n_parts), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(headnorm_dw_kernel, dim3((a.hd + 31) / 32, a.n_parts), dim3(32 * kSlices), 0, st, a);
   return hipGetLastError();
 }
 
