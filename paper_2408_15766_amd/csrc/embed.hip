@@ -1,8 +1,8 @@
 // Rows of an embedding table, and the gradient of the table (include/spec_step.h).
 //
 // The gradient sums rows of dy by token.  The positions are sorted by (token, position), so that a table row's sum is a walk over neighbours and its order is
-// fixed: in tiles of kTile positions a position's place is the number of smaller ones (counted, kTile comparisons for each), and over several tiles
-// its place in its own plus those that binary searches find in the others.  Padding sorts behind the vocabulary and is never read.
+// fixed: in tiles of kTile positions a position's place is the number of smaller ones (counted, kTile comparisons for each); over several tiles four sorted runs at a time become one,
+// a position's place being that in its own run plus those that searches find in the other three.  Padding sorts behind the vocabulary and is never read.
 // Tokens that occur often (padding apart, the most frequent word is a tenth of a text) would keep one workgroup busy long after the others: aligned runs of 32
 // and of 1024 sorted positions that hold one token are summed first, by workgroups of their own, and the walk takes a run's sum where it meets one.
 // Bound: memory (dy once in, the table once out).  Measured: 16384 rows into 128256 x 4096 in bf16: places 9 us, joined 6, runs 9 and 5, table 183 (6.3 TB/s).  Of 2^20 rows the places take 280 us and
@@ -137,40 +137,46 @@ __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(const int *tok
   order[tile + place] = tile + me;
 }
 
-// Several tiles: the place of each among all
-__global__ __launch_bounds__(kRankThreads) void embed_merge_kernel(const int *tile_keys, const int *tile_order, int rows, int *keys, int *order) {
-  __shared__ int sh[kTile];
-  const int i = blockIdx.x * kRankThreads + threadIdx.x, mine = blockIdx.x * kRankThreads / kTile;
-  const int key = i < rows ? tile_keys[i] : 0;
-  int place = i - mine * kTile;
-  const int tiles = (rows + kTile - 1) / kTile;
-  constexpr int kEach = kTile / kRankThreads;
-  int ahead[kEach];                                           // the next tile's keys, asked for before this one's are searched
-  auto ask = [&](int t) {
+// Runs of `run` sorted positions, kWays at a time, to one each: the place of each among them.  A search looks at kProbes places at once, and the searches in all other runs go side by side:
+// a step is one trip to memory.
+constexpr int kWays = 4, kProbes = 3, kMergeThreads = 256;
+__global__ __launch_bounds__(kMergeThreads) void embed_merge_kernel(const int *from_keys, const int *from_order, int rows, int run, int *keys, int *order) {
+  const int i = blockIdx.x * kMergeThreads + threadIdx.x;
+  if (i >= rows) return;
+  const int key = from_keys[i], at = from_order[i];
+  const int base = blockIdx.x * kMergeThreads / run / kWays * kWays * run, mine = (blockIdx.x * kMergeThreads - base) / run;   // of the runs that meet
+  int lo[kWays - 1], open[kWays - 1], below[kWays - 1], place = i - mine * run;
 #pragma unroll
-    for (int e = 0; e < kEach; e++) {
-      const int j = t * kTile + e * kRankThreads + threadIdx.x;
-      ahead[e] = t < tiles && j < rows ? tile_keys[j] : 0;
-    }
-  };
-  ask(mine == 0 ? 1 : 0);
-  for (int t = 0; t < tiles; t++) {
-    if (t == mine) continue;
-    const int n = min(rows - t * kTile, kTile);
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kEach; e++) sh[e * kRankThreads + threadIdx.x] = ahead[e];
-    __syncthreads();
-    ask(t + 1 == mine ? t + 2 : t + 1);
-    const int below = key + (t < mine ? 1 : 0);               // how many of this tile come before: keys under `below`
-    int lo = 0, hi = n;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (sh[mid] < below) lo = mid + 1; else hi = mid;
-    }
-    place += lo;
+  for (int o = 0; o < kWays - 1; o++) {
+    const int other = o < mine ? o : o + 1;
+    lo[o] = min(rows, base + other * run);
+    open[o] = min(rows, base + (other + 1) * run) - lo[o];
+    below[o] = key + (other < mine ? 1 : 0);                  // equal keys of earlier runs come before
+    place -= lo[o];
   }
-  if (i < rows) { keys[place] = key; order[place] = tile_order[i]; }
+  auto probe = [](int n, int q) { return (int)((unsigned)(n * q) / (kProbes + 1)); };   // of n open places, q = 1 .. kProbes
+  for (int left = run; left > 0; left /= kProbes + 1) {       // keys[x] < below for x < lo, not for x >= lo + open; open <= left
+    int k[kWays - 1][kProbes];
+#pragma unroll
+    for (int o = 0; o < kWays - 1; o++)
+#pragma unroll
+      for (int q = 0; q < kProbes; q++) k[o][q] = from_keys[min(lo[o] + probe(open[o], q + 1), rows - 1)];
+#pragma unroll
+    for (int o = 0; o < kWays - 1; o++) {
+      const int n = open[o];
+      int from = 0, to = n;
+#pragma unroll
+      for (int q = 0; q < kProbes; q++) from = k[o][q] < below[o] ? min(probe(n, q + 1) + 1, n) : from;
+#pragma unroll
+      for (int q = kProbes - 1; q >= 0; q--) to = k[o][q] < below[o] ? to : min(probe(n, q + 1), n);
+      lo[o] += from;
+      open[o] = to - from;
+    }
+  }
+#pragma unroll
+  for (int o = 0; o < kWays - 1; o++) place += lo[o];
+  keys[place] = key;
+  order[place] = at;
 }
 
 // ---- sums ---------------------------------------------------------------------------------------
@@ -342,16 +348,16 @@ uint64_t embed_grad_scratch_bytes(int rows, int vocab, int d) { return embed_scr
 hipError_t launch_embed_grad(EmbedGradArgs a, void *scratch, hipStream_t st) {
   const EmbedScratch s = embed_scratch(a.rows, a.vocab, a.d);
   char *base = (char *)scratch;
-  const bool tiled = a.rows > kTile;
-  int *keys = (int *)(base + (tiled ? s.tile_keys : s.keys)), *order = (int *)(base + (tiled ? s.tile_order : s.order));
-  hipLaunchKernelGGL(embed_rank_kernel, dim3((a.rows + kRankMine - 1) / kRankMine), dim3(kRankThreads), 0, st, a.tok, a.rows, a.vocab, keys, order);
+  int *keys[2] = {(int *)(base + s.keys), (int *)(base + s.tile_keys)}, *order[2] = {(int *)(base + s.order), (int *)(base + s.tile_order)};
+  int at = 0;                                                 // where the runs are: the last ones, in [0]
+  for (int64_t run = kTile; run < a.rows; run *= kWays) at ^= 1;
+  hipLaunchKernelGGL(embed_rank_kernel, dim3((a.rows + kRankMine - 1) / kRankMine), dim3(kRankThreads), 0, st, a.tok, a.rows, a.vocab, keys[at], order[at]);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (tiled) {
-    hipLaunchKernelGGL(embed_merge_kernel, dim3((a.rows + kRankThreads - 1) / kRankThreads), dim3(kRankThreads), 0, st, keys, order, a.rows,
-                       (int *)(base + s.keys), (int *)(base + s.order));
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  for (int64_t run = kTile; run < a.rows && e == hipSuccess; run *= kWays, at ^= 1) {
+    hipLaunchKernelGGL(embed_merge_kernel, dim3((a.rows + kMergeThreads - 1) / kMergeThreads), dim3(kMergeThreads), 0, st, keys[at], order[at], a.rows, (int)run, keys[at ^ 1], order[at ^ 1]);
+    e = hipGetLastError();
   }
+  if (e != hipSuccess) return e;
   return a.dtype ? embed_sums<true>(a, s, base, st) : embed_sums<false>(a, s, base, st);
 }
 

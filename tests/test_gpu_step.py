@@ -128,6 +128,17 @@ def test_embed_grad_order_does_not_depend_on_the_other_tokens_place(P):
     assert torch.equal(got[4], s) and (got[[0, 1, 2, 3, 5, 6, 7, 8]] == 0).all()
 
 
+@pytest.mark.parametrize("rows", [1023, 1025, 2048, 2049, 3073, 4095, 4097, 16383, 16385, 65537, 100001, (1 << 18) + 1])
+@pytest.mark.parametrize("vocab", [3, 700, 90000])
+def test_embed_grad_of_several_sorted_runs(P, rows, vocab):
+    """Positions that are sorted in parts: whole and ragged ones, keys that are equal across them, and padding."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    tok = torch.randint(-1, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    dy = torch.randint(-8, 9, (rows, 9), generator=g, device="cuda").float()                   # sums of integers: exact in any order
+    want = torch.zeros(vocab + 1, 9, dtype=torch.float64, device="cuda").index_add_(0, tok.long() % (vocab + 1), dy.double())[:vocab]
+    assert torch.equal(P.spec_k_embed_grad(dy, tok, vocab).double(), want)
+
+
 @pytest.mark.parametrize("out", ["bf16", "fp32"])
 def test_embed_grad_accumulates(P, out):
     rows, vocab, d = 500, 800, 72
