@@ -5,8 +5,8 @@
 // a position's place being that in its own run plus those that searches find in the other three.  Padding sorts behind the vocabulary and is never read.
 // Tokens that occur often (padding apart, the most frequent word is a tenth of a text) would keep one workgroup busy long after the others: aligned runs of 32
 // and of 1024 sorted positions that hold one token are summed first, by workgroups of their own, and the walk takes a run's sum where it meets one.
-// Bound: memory (dy once in, the table once out).  Measured: 16384 rows into 128256 x 4096 in bf16: places 9 us, joined 6, runs 9 and 5, table 183 (6.3 TB/s).  Of 2^20 rows the places take 280 us and
-// joining 256 tiles 850: more than the sums, where rows are short.
+// Bound: memory (dy once in, the table once out).  Measured: 16384 rows into 128256 x 4096 in bf16: places 9 us, joined 5, runs 5 and 5, table 183 (6.3 TB/s).  2^20 rows into 2000 x 64: places 266, joined
+// 4 times 30, of 475 in all.
 #include "common.h"
 #include "elements.h"
 #include "kernels.h"
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(const int *tok
 }
 
 // Runs of `run` sorted positions, kWays at a time, to one each: the place of each among them.  A search looks at kProbes places at once, and the searches in all other runs go side by side:
-// a step is one trip to memory.
+// a step is one trip to memory.  (16384 positions 4.8 us, one tile after the other through the LDS 6, the other three in the LDS at once 6.4; 2^20 120 against 850.)
 constexpr int kWays = 4, kProbes = 3, kMergeThreads = 256;
 __global__ __launch_bounds__(kMergeThreads) void embed_merge_kernel(const int *from_keys, const int *from_order, int rows, int run, int *keys, int *order) {
   const int i = blockIdx.x * kMergeThreads + threadIdx.x;
@@ -246,9 +246,9 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_long_runs_kernel(const in
   }
 }
 
-// A few table rows to a workgroup (blockIdx.y: its share of the columns).
+// A few table rows to a workgroup (blockIdx.y: its share of the columns).  SPLIT: they are short, its threads take 2, 4 or 8 at once.
 constexpr int kTableRows = 8;
-template <bool BF16>
+template <bool BF16, bool SPLIT>
 __global__ __launch_bounds__(kEmbedThreads) void embed_table_kernel(EmbedGradArgs a, const int *order, const int *starts, const float *runs, const float *long_runs) {
   const int v0 = blockIdx.x * kTableRows, vn = min(a.vocab - v0, kTableRows);
   int start[kTableRows + 1];                                  // (all asked for at once; most rows of a large vocabulary have no token, and their zeros go out first)
@@ -262,9 +262,9 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_table_kernel(EmbedGradArg
       for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * 8; c < a.d; c += gridDim.y * kEmbedThreads * 8)
         clear_columns(a.dtable, (v0 + r) * a.ldt + c, a.d - c, a.out_dtype);
   }
-  for (; full != 0; full &= full - 1) {
-    const int v = v0 + __builtin_ctz(full), s0 = starts[v], s1 = starts[v + 1];
-    for (int c = (blockIdx.y * kEmbedThreads + threadIdx.x) * 8; c < a.d; c += gridDim.y * kEmbedThreads * 8) {
+  auto walk = [&](int v, int c0) __attribute__((always_inline)) {
+    const int s0 = starts[v], s1 = starts[v + 1];
+    for (int c = c0; c < a.d; c += gridDim.y * kEmbedThreads * 8) {
       const int n = a.d - c;
       auto sum = [&](auto whole_columns) __attribute__((always_inline)) {
         constexpr bool kWhole = decltype(whole_columns)::value;
@@ -295,6 +295,13 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_table_kernel(EmbedGradArg
       };
       if (n >= 8) sum(std::true_type{}); else sum(std::false_type{});
     }
+  };
+  if constexpr (!SPLIT) {
+    for (; full != 0; full &= full - 1) walk(v0 + __builtin_ctz(full), (blockIdx.y * kEmbedThreads + threadIdx.x) * 8);
+  } else {                                                    // rows r, r + at_once, ..
+    const int cols = (a.d + 7) / 8, at_once = cols > kEmbedThreads / 4 ? 2 : cols > kEmbedThreads / 8 ? 4 : 8, mine = threadIdx.x / cols;
+    if (mine >= at_once) return;
+    for (full &= (at_once == 2 ? 0x55u : at_once == 4 ? 0x11u : 0x01u) << mine; full != 0; full &= full - 1) walk(v0 + __builtin_ctz(full), (threadIdx.x - mine * cols) * 8);
   }
 }
 
@@ -328,7 +335,10 @@ template <bool BF16> hipError_t embed_sums(const EmbedGradArgs &a, const EmbedSc
     hipLaunchKernelGGL(embed_long_runs_kernel, dim3(a.rows / kRuns, wide > 64 ? 64 : wide), dim3(kEmbedThreads), 0, st, keys, a.vocab, a.d, runs, long_runs);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(embed_table_kernel<BF16>, dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
+  // Rows at once pay where most have tokens (16384 rows into 1000 x 256 44 -> 28 us, 65536 into 2000 x 256 88 -> 53); one after the other they keep their places in scalar registers (8192 into
+  // 128256 x 512 46 us, at once 49).
+  const bool split = a.d <= kEmbedThreads * 4 && a.rows >= a.vocab / 4;
+  hipLaunchKernelGGL((split ? embed_table_kernel<BF16, true> : embed_table_kernel<BF16, false>), dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
   return hipGetLastError();
 }
 
