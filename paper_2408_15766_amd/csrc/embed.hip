@@ -5,7 +5,7 @@
 // a position's place being that in its own run plus those that searches find in the other three.  Padding sorts behind the vocabulary and is never read.
 // Tokens that occur often (padding apart, the most frequent word is a tenth of a text) would keep one workgroup busy long after the others: aligned runs of 32
 // and of 1024 sorted positions that hold one token are summed first, by workgroups of their own, and the walk takes a run's sum where it meets one.
-// Bound: memory (dy once in, the table once out).  Measured: 16384 rows into 128256 x 4096 in bf16: places 9 us, joined 5, runs 5 and 5, table 183 (6.3 TB/s).  2^20 rows into 2000 x 64: places 266, joined
+// Bound: memory (dy once in, the table once out).  Measured: 16384 rows into 128256 x 4096 in bf16: places 9 us, joined 5, runs 9 and 5, table 183 (6.3 TB/s).  2^20 rows into 2000 x 64: places 266, joined
 // 4 times 30, of 475 in all.
 #include "common.h"
 #include "elements.h"
