@@ -52,7 +52,8 @@ int spec_k_embed_grad(int32_t dtype, const void *dy, int64_t ldy, const int32_t 
  * plan.rot pass unturned).  w NULL: z = x, so that the call does what spec_k_rotary does.
  * Parts, strides, positions, sizes and aliasing as in spec_k_rotary; w in w_dtype,
  * aligned to it.  Squares, sums and products are fp32: heads with values
- * beyond 2^60 may come out as zeros.  eps >= 0 and finite; with eps = 0 a head of zeros gives NaN. */
+ * beyond 2^60 may come out as zeros.  eps >= 0 and finite; with eps = 0 a head of zeros gives NaN, one of values under 2^-60 may give
+ * infinities or NaN too. */
 typedef struct spec_headnorm_part {
   spec_rotary_part p;
   const void *w;
