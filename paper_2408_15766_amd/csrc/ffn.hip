@@ -29,11 +29,12 @@ template <bool SLOPE> __device__ __forceinline__ Act activation(int act, float g
     return r;
   }
   // p = 1 / (1 + e^-z), z = g or twice the argument of the tanh
-  const float z = act == kActSilu ? g : 1.5957691216057308f * fmaf(0.044715f * g, g * g, g);
+  constexpr double kTwice = 1.5957691216057308, kCube = 0.044715;   // 2 sqrt(2 / pi), and the share of the cube in the tanh's argument
+  const float z = act == kActSilu ? g : (float)kTwice * fmaf((float)kCube * g, g * g, g);
   r.p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
   if constexpr (SLOPE) {
     const float c = act == kActSilu ? g : fminf(fmaxf(g, -64.0f), 64.0f);   // (far out p (1 - p) is zero, and the cube of g would be infinite)
-    const float dz = act == kActSilu ? 1.0f : fmaf(0.21406881920f * c, c, 1.5957691216057308f);
+    const float dz = act == kActSilu ? 1.0f : fmaf((float)(3.0 * kCube * kTwice) * c, c, (float)kTwice);
     r.slope = fmaf(c * dz, r.p * (1.0f - r.p), r.p);
   }
   return r;

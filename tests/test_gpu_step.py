@@ -807,3 +807,88 @@ def test_more_elements_than_31_bits_count_of_a_step(P):
     g = rand(6, 1 << 10).cuda().repeat((1 << 21) + 7)
     norm = P.spec_k_grad_clip([g], P.spec_k_grad_sums([g]), 1.0)
     assert abs(float(norm) / (float(rand(6, 1 << 10).double().norm()) * ((1 << 21) + 7) ** 0.5) - 1) < 2 * U32 and torch.equal(g[-1024:], g[:1024])
+
+
+# ---- what the tests above leave open ------------------------------------------------------------------
+
+def activation_at(act, g):
+    """Per g, in 64 bits: act(g) and its slope, and how far the kernels' may be off before they are rounded to bf16.
+
+    silu and gelu_tanh: p = 1 / (1 + e^-z).  z is g, or c (g + 0.044715 g^3) with three roundings of the whole and three more of the cube's part; the exponential's argument has two, the hardware's
+    exponential and reciprocal are off by 2 u32 each, and the sum by one: e^-z is relatively E = 5 |z| u + 3 |cube| u + 2 u off (silu: 2 |z| u + 2 u), p by dp = p (1 - p) E + 3 p u.  The slope is
+    p + a p (1 - p) with a = g z'(g), five roundings: off by |1 + a (1 - 2 p)| dp, by 7 u of its second term (a's five, 1 - p, the product), and by its own rounding.
+    gelu: p = erfc(-g / sqrt 2) / 2, the argument with two roundings, erfc off by 16 units in the last place (32 u); the slope's second term has six and the exponential's argument three."""
+    g = np.asarray(g, np.float64)
+    value, slope = O.activation(act, g)
+    if act == "gelu":
+        phi = np.exp(-0.5 * g * g) / np.sqrt(2 * np.pi)
+        p = slope - g * phi
+        dp = 33 * U32 * p + 2 * U32 * np.abs(g) * phi
+        second = np.abs(g) * phi * (1.5 * g * g + 6) * U32
+        ds = dp + second
+    else:
+        c = 2 * np.sqrt(2 / np.pi)
+        cube = c * 0.044715 * g ** 3
+        z, dz, most = (g, np.ones_like(g), 2 * np.abs(g)) if act == "silu" else (c * g + cube, c + 3 * c * 0.044715 * g * g, 5 * np.abs(c * g + cube) + 3 * np.abs(cube))
+        p = 1.0 / (1.0 + np.exp(-z))
+        dp = p * (1 - p) * (most + 2) * U32 + 3 * p * U32
+        a = g * dz
+        ds = np.abs(1 + a * (1 - 2 * p)) * dp + 7 * U32 * np.abs(a) * p * (1 - p)
+    return value, slope, 1.01 * (np.abs(g) * dp + U32 * np.abs(value)), 1.01 * (ds + U32 * np.abs(slope))
+
+
+def gates_at_roundings(act, which):
+    """fp32 gates of whose value (which = 0) or slope (1) the rounding to bf16 tells a few u32 from each other: those a little over one and three times the allowed error before and behind the middle of two
+    bf16 numbers; for the slope also some thousand about the gate where it is nothing."""
+    grid = np.linspace(-6, 6, 60001)
+    y = activation_at(act, grid)[which]
+    f32 = torch.from_numpy(y).float()
+    cell = ((f32.view(torch.int32) + 0x8000) >> 16).numpy()              # changes where the rounded value does
+    at = np.nonzero((cell[1:] != cell[:-1]) & (np.abs(y[1:]) > 2.0 ** -8) & (np.abs(cell[1:] - cell[:-1]) == 1))[0]
+    upper = np.maximum(cell[at], cell[at + 1]).astype(np.int32)
+    middle = torch.from_numpy((upper << 16) - 0x8000).view(torch.float32).double().numpy()
+    lo, hi = grid[at], grid[at + 1]
+    for _ in range(60):
+        mid = 0.5 * (lo + hi)
+        low_side = (activation_at(act, mid)[which] - middle) * (activation_at(act, lo)[which] - middle) > 0
+        lo, hi = np.where(low_side, mid, lo), np.where(low_side, hi, mid)
+    error, step = activation_at(act, lo)[2 + which], 1e-6
+    incline = (activation_at(act, lo + step)[which] - activation_at(act, lo - step)[which]) / (2 * step)
+    some = np.abs(incline) > 0.05
+    gates = [lo[some] + m * (error / incline)[some] for m in (-3, -2, -1.4, -1.1, 1.1, 1.4, 2, 3)]
+    if which == 1:
+        zero = zero_between(lambda g: activation_at(act, g)[1], -1.5, -0.5)
+        gates.append(zero + np.linspace(-1e-3, 1e-3, 2001))
+    return np.concatenate(gates).astype(np.float32)
+
+
+def zero_between(f, lo, hi):
+    for _ in range(80):
+        mid = 0.5 * (lo + hi)
+        lo, hi = (mid, hi) if (f(mid) > 0) == (f(lo) > 0) else (lo, mid)
+    return lo
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_ffn_gated_activations_to_a_few_units(P, act):
+    """Single gates, each the exact sum of three bf16 numbers, beside an up sum of one: h is act(g) and (for a dh of one) dw_gate the slope, each rounded once from something within the kernel's few
+    roundings of it.  A constant that is 2e-5 off shows."""
+    for which in (0, 1):
+        gates = gates_at_roundings(act, which)
+        gates = np.concatenate([gates, np.zeros(-len(gates) % 8, np.float32)])
+        f = len(gates)
+        assert f > 2000
+        wg, left = torch.zeros(f, 8, dtype=torch.bfloat16, device="cuda"), torch.from_numpy(gates).cuda()
+        for k in range(3):
+            wg[:, k] = left.bfloat16()
+            left = left - wg[:, k].float()
+        assert not left.any()
+        wu = torch.zeros_like(wg)
+        wu[:, 0] = 1
+        one = torch.ones(1, 8, dtype=torch.bfloat16, device="cuda")
+        got = P.spec_k_ffn_gated(one, wg, wu, act=act)[0] if which == 0 else P.spec_k_ffn_gated_grad(one, wg, wu, torch.ones(1, f, dtype=torch.bfloat16, device="cuda"), act=act)[1][:, 0]
+        y, error = (activation_at(act, gates)[n] for n in (which, 2 + which))
+        error = error + U32 * np.abs(y)                                  # (the bounds go through fp32 on their way to bf16)
+        low, high = (torch.from_numpy(y + s * error).float().bfloat16().cuda() for s in (-1, 1))
+        bad = ~((low <= got) & (got <= high))
+        assert not bool(bad.any()), (which, int(bad.sum()), f, gates[bad.cpu().numpy()][:5], got[bad][:5], y[bad.cpu().numpy()][:5])
