@@ -124,6 +124,7 @@ int spec_k_ffn_gated_grad(const void *x, int64_t ldx, int32_t rows, int32_t d, c
  *                      (infinite from 2^128 on, which the factor is not; NULL: not wanted).  out may be g (in place, same dtype; nothing is written if the factor is 1); else it
  *                      overlaps no g and no other out.  A norm that is not finite does as the formula says: an infinite one makes finite gradients 0 and infinite
  *                      ones NaN, NaN makes all NaN.
+ * The sums and the norm overlap no g, no out and not each other.
  * The tensors are dense arrays of n elements, n >= 0 (0: skipped, pointers ignored), aligned to their type;
  * n_parts >= 0, any number; max_norm >= 0 and finite. */
 #define SPEC_GRAD_SUMS 1024

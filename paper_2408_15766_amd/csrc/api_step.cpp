@@ -70,6 +70,13 @@ bool grad_ok(const spec_grad_part &p, bool clip) {
   return !clip || (p.out && is_dtype(p.out_dtype) && aligned(p.out, size_of(p.out_dtype)) && (p.out != p.g || p.dtype == p.out_dtype));
 }
 
+// Whether the bytes at p and those at q meet
+bool meet(const void *p, uint64_t bytes, const void *q, uint64_t more) { return (uintptr_t)p < (uintptr_t)q + more && (uintptr_t)q < (uintptr_t)p + bytes; }
+bool grad_meets(const spec_grad_part &p, const void *q, uint64_t bytes, bool clip) {   // the gradient, or its output (clip), with the sums or the norm
+  return p.n > 0 && q && (meet(p.g, (uint64_t)p.n * size_of(p.dtype), q, bytes) || (clip && meet(p.out, (uint64_t)p.n * size_of(p.out_dtype), q, bytes)));
+}
+constexpr uint64_t kSumsBytes = SPEC_GRAD_SUMS * sizeof(double);
+
 // The tensors, as many as a launch takes at a time.  launch(args) is called once at least.
 template <typename Launch> int for_each_launch(int32_t n_parts, const spec_grad_part *parts, GradArgs &a, Launch launch) {
   int at = 0;
@@ -226,19 +233,19 @@ int spec_k_grad_sums(int32_t n_parts, const spec_grad_part *parts, double *sums,
   static_assert(SPEC_GRAD_SUMS == kGradSums, "header and kernel agree on the sums");
   if (n_parts < 0 || (n_parts > 0 && !parts) || !sums || !aligned(sums, 8)) return SPEC_EINVAL;
   for (int n = 0; n < n_parts; n++)
-    if (!grad_ok(parts[n], false) || (parts[n].n > 0 && parts[n].g == sums)) return SPEC_EINVAL;
+    if (!grad_ok(parts[n], false) || grad_meets(parts[n], sums, kSumsBytes, false)) return SPEC_EINVAL;
   GradArgs a{};
   a.sums = sums; a.first = 1;
   return for_each_launch(n_parts, parts, a, [&](const GradArgs &b) { return launch_grad_sums(b, (hipStream_t)stream); });
 }
 
 int spec_k_grad_clip(int32_t n_parts, const spec_grad_part *parts, const double *sums, double max_norm, float *norm, void *stream) {
-  if (n_parts < 0 || (n_parts > 0 && !parts) || !sums || !aligned(sums, 8) || !aligned(norm, 4) || (const void *)norm == (const void *)sums) return SPEC_EINVAL;
+  if (n_parts < 0 || (n_parts > 0 && !parts) || !sums || !aligned(sums, 8) || !aligned(norm, 4)) return SPEC_EINVAL;
+  if (norm && meet(norm, sizeof(float), sums, kSumsBytes)) return SPEC_EINVAL;
   if (!(max_norm >= 0.0) || !std::isfinite(max_norm)) return SPEC_EINVAL;
   for (int n = 0; n < n_parts; n++) {
     const spec_grad_part &p = parts[n];
-    if (!grad_ok(p, true)) return SPEC_EINVAL;
-    if (p.n > 0 && (p.out == sums || p.g == sums || (norm && (p.out == norm || p.g == norm)))) return SPEC_EINVAL;
+    if (!grad_ok(p, true) || grad_meets(p, sums, kSumsBytes, true) || grad_meets(p, norm, sizeof(float), true)) return SPEC_EINVAL;
   }
   try {
     if (!apart(n_parts, parts)) return SPEC_EINVAL;

@@ -151,3 +151,23 @@ def test_oracle_gradients_against_differences():
     check(lambda t: (O.embed(t, tok, 0.5) * dy).sum(), [table], [O.embed_grad(dy, tok, 4, 0.5)])
     norm, scaled = O.grad_clip([x, wg], 0.5)
     assert abs(np.sqrt(sum((s * s).sum() for s in scaled)) - 0.5) < 1e-5 and abs(norm ** 2 - (x * x).sum() - (wg * wg).sum()) < 1e-9
+
+
+def test_grad_sums_and_norm_lie_apart_from_the_gradients(P):
+    """The sums (8 KB) and the norm inside a gradient or an output, or reaching into one, not only at its start: workgroups read the sums while others write."""
+    def parts(*rows):
+        return struct.pack("@" + "QQqii" * len(rows), *itertools.chain.from_iterable(rows))
+    far, g, n = (X, 2 * X, 100, 0, 0), 1 << 22, 1 << 18                   # a tensor of 1 MB (fp32) at g
+    inside = g + 4 * n // 2
+    for sums in (inside, g + 4 * n - 8, g - 8192 + 8, g + 8):
+        refused(P.lib.spec_k_grad_sums(1, parts((g, 0, n, 0, 0)), sums, None))
+        refused(P.lib.spec_k_grad_sums(2, parts(far, (g, 0, n, 0, 0)), sums, None))
+        for p in ((g, g, n, 0, 0), (5 * X, g, n, 0, 0), (g, 9 * X, n, 0, 0), (5 * X, g, 2 * n, 1, 1)):
+            refused(P.lib.spec_k_grad_clip(2, parts(far, p), sums, 1.0, 8 * X, None))
+            refused(P.lib.spec_k_grad_clip(2, parts(far, p), sums, 1.0, None, None))
+    for norm in (inside, g + 4 * n - 4, g + 4):
+        for p in ((g, g, n, 0, 0), (5 * X, g, n, 0, 0), (g, 9 * X, n, 0, 0)):
+            refused(P.lib.spec_k_grad_clip(2, parts(far, p), 8 * X, 1.0, norm, None))
+    for norm in (8 * X + 4, 8 * X + 8188):                                # a norm inside the sums
+        refused(P.lib.spec_k_grad_clip(1, parts(far), 8 * X, 1.0, norm, None))
+        refused(P.lib.spec_k_grad_clip(0, None, 8 * X, 1.0, norm, None))
