@@ -114,6 +114,12 @@ int spec_k_ffn_gated_grad(const void *x, int64_t ldx, int32_t rows, int32_t d, c
                           const void *dh, int64_t lddh, void *dx, int64_t lddx, void *dw_gate, void *dw_up, int64_t lddw, void *scratch,
                           uint64_t scratch_bytes, void *stream);
 
+/* How calls of these sizes run (host only; for tests).  forward: 16, 64 or 65: the kernels of up to 16, 64 and 128 rows that read the weights once; 128 or 256: tiles of 128 x 128, or
+ * of 256 x 256 and halves of it.  The gradients: again (g and u formed again), dx and dw (both weights' gradients, asked for alone): tiles of 128 or 256; dx_ranges and dw_ranges: into how
+ * many ranges their k is cut; together != 0: a call for all of them forms dx and dw in one launch, of tiles of 128. */
+int spec_k_ffn_gated_plan(int32_t rows, int32_t d, int32_t f, int32_t *forward, int32_t *again, int32_t *dx, int32_t *dx_ranges, int32_t *dw, int32_t *dw_ranges,
+                          int32_t *together);
+
 /* ---- gradient clipping ------------------------------------------------------------
  * The norm of n tensors' elements together, n = sqrt(sum g^2), and the tensors scaled by
  * min(1, max_norm / (norm + 1e-6)), without a wait in between:

@@ -10,7 +10,7 @@ from .binding import (Engine, SpecError, Tree, lib, spec_accept, spec_committed,
 from .binding import (spec_k_attention8, spec_k_attention8_plan, spec_k_attention8_scratch_bytes, spec_k_gemm8, spec_k_gemm8_scratch_bytes, spec_k_kv8_load, spec_k_kv8_store,
                       spec_k_rotary, spec_kv8_alloc, spec_kv8_bytes, spec_pack_weight8, spec_packed8_bytes, spec_rotary_plan)
 from .binding_step import (SPEC_GRAD_SUMS, spec_k_embed, spec_k_embed_grad, spec_k_embed_grad_scratch_bytes, spec_k_ffn_gated, spec_k_ffn_gated_grad,
-                           spec_k_ffn_gated_grad_scratch_bytes, spec_k_grad_clip, spec_k_grad_sums, spec_k_headnorm_rotary,
+                           spec_k_ffn_gated_grad_scratch_bytes, spec_k_ffn_gated_plan, spec_k_grad_clip, spec_k_grad_sums, spec_k_headnorm_rotary,
                            spec_k_headnorm_rotary_grad, spec_k_headnorm_rotary_grad_scratch_bytes)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

@@ -31,6 +31,7 @@ lib.spec_k_ffn_gated_grad_scratch_bytes.restype = C.c_uint64
 lib.spec_k_ffn_gated_grad_scratch_bytes.argtypes = [C.c_int32] * 3
 lib.spec_k_ffn_gated_grad.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
                                       C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_uint64, C.c_void_p]
+lib.spec_k_ffn_gated_plan.argtypes = [C.c_int32] * 3 + [C.POINTER(C.c_int32)] * 7
 lib.spec_k_grad_sums.argtypes = [C.c_int32, C.c_char_p, C.c_void_p, C.c_void_p]
 lib.spec_k_grad_clip.argtypes = [C.c_int32, C.c_char_p, C.c_void_p, C.c_double, C.c_void_p, C.c_void_p]
 
@@ -313,6 +314,16 @@ def spec_k_ffn_gated_grad(x, w_gate, w_up, dh, act: str = "silu", outs: Optional
     if rc:
         raise SpecError(rc, f"{what}: {rows} rows, {d} by {f} (multiples of 8, 16-byte aligned), strides {ldx}, {ldw}, {lddh}, {lddx}, {lddw}, {room} bytes of scratch")
     return dx, dwg, dwu
+
+
+def spec_k_ffn_gated_plan(rows: int, d: int, f: int):
+    """How calls of these sizes run: (kernel of the forward call, tiles of g and u formed again, tiles of dx, ranges of its k, tiles of the weights' gradients, ranges of their k, whether a call for all
+    gradients forms dx and those in one launch)."""
+    out = [C.c_int32() for _ in range(7)]
+    rc = lib.spec_k_ffn_gated_plan(rows, d, f, *(C.byref(o) for o in out)) if _fit(rows, d, f) else SPEC_EINVAL
+    if rc:
+        raise SpecError(rc, f"spec_k_ffn_gated_plan: {rows} rows, {d} by {f}")
+    return tuple(o.value for o in out)
 
 
 # ---- gradient clipping ------------------------------------------------------------------------------

@@ -229,6 +229,14 @@ int spec_k_ffn_gated_grad(const void *x, int64_t ldx, int32_t rows, int32_t d, c
   return done(launch_ffn_grad(c, scratch, (hipStream_t)stream));
 }
 
+int spec_k_ffn_gated_plan(int32_t rows, int32_t d, int32_t f, int32_t *forward, int32_t *again, int32_t *dx, int32_t *dx_ranges, int32_t *dw, int32_t *dw_ranges,
+                          int32_t *together) {
+  if (!ffn_sizes_ok(rows, d, f) || !forward || !again || !dx || !dx_ranges || !dw || !dw_ranges || !together) return SPEC_EINVAL;
+  const FfnPlans p = ffn_plans(rows, d, f);
+  *forward = p.forward; *again = p.again; *dx = p.dx; *dx_ranges = p.dx_ranges; *dw = p.dw; *dw_ranges = p.dw_ranges; *together = p.together;
+  return SPEC_OK;
+}
+
 int spec_k_grad_sums(int32_t n_parts, const spec_grad_part *parts, double *sums, void *stream) {
   static_assert(SPEC_GRAD_SUMS == kGradSums, "header and kernel agree on the sums");
   if (n_parts < 0 || (n_parts > 0 && !parts) || !sums || !aligned(sums, 8)) return SPEC_EINVAL;

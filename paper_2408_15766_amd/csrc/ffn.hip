@@ -699,17 +699,27 @@ uint64_t ffn_grad_scratch_bytes(int rows, int d, int f) {
 // of 4096 x 14336 16 48.7 / 52.2 / 60.9, 60 98 / 55.0 / 64.0, 128 - / 66.2 / 68.1; of 1024 x 2752 16 6.1 / 9.7 / 14.1, 60 11.3 / 10.1 / 14.5.  Where the tiles fill the
 // chip by themselves they have less of x to read: 8192 x 28672 16 165 / 174 / 177, 32 208 / 177 / 177, 60 304 / 189 / 176, 128 - / 240 / 178.
 static bool some_pays(int rows, int f) { return rows <= 32 || (rows <= 128 && (f + 63) / 64 < 256); }
+static FfnKernel forward_kernel(int rows, int d, int f) {
+  if (rows <= kFewRows) return kFfnFew;
+  if (some_pays(rows, f)) return rows <= 64 ? kFfnSome64 : kFfnSome128;
+  return ffn_plan(rows, f, d, 1, 1, true).tile == 0 ? kFfnTiles256 : kFfnTiles128;
+}
+
+FfnPlans ffn_plans(int rows, int d, int f) {
+  const bool both = both_pay(rows, d, f);
+  const FfnPlan x = ffn_plan(rows, d, f, 1, 2, false, both), w = ffn_plan(f, d, rows, 2, 1, false, both);
+  auto tile = [](int t) { return t == 0 ? kFfnTiles256 : kFfnTiles128; };
+  return FfnPlans{forward_kernel(rows, d, f), tile(ffn_plan(rows, f, d, 1, 1, true).tile), tile(x.tile), x.splits, tile(w.tile), w.splits, both};
+}
 
 hipError_t launch_ffn(const FfnCall &c, hipStream_t st) {
   FfnArgs a{};
   a.m = c.rows; a.n = c.f; a.k = c.d; a.segs = a.halves = a.splits = 1; a.act = c.act;
   a.m_src[0] = c.x; a.ldm = c.ldx; a.n_src[0] = c.wg; a.n_src[1] = c.wu; a.ldn = c.ldw; a.out[0] = c.h; a.ldo = c.ldh;
-  if (c.rows > kFewRows && some_pays(c.rows, c.f)) {
-    hipLaunchKernelGGL((c.rows <= 64 ? ffn_some_kernel<1> : ffn_some_kernel<2>), dim3((c.f + 31) / 32), dim3(256), 0, st, a);
-    return hipGetLastError();
-  }
-  if (c.rows > kFewRows) return launch_planned<false, false, kToH>(a, ffn_plan(a.m, a.n, a.k, 1, 1, true).tile, st);
-  hipLaunchKernelGGL(ffn_few_kernel, dim3((c.f + 15) / 16), dim3(256), 0, st, a);
+  const FfnKernel kernel = forward_kernel(c.rows, c.d, c.f);
+  if (kernel == kFfnTiles128 || kernel == kFfnTiles256) return launch_planned<false, false, kToH>(a, kernel == kFfnTiles256 ? 0 : 1, st);
+  if (kernel == kFfnFew) hipLaunchKernelGGL(ffn_few_kernel, dim3((c.f + 15) / 16), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((kernel == kFfnSome64 ? ffn_some_kernel<1> : ffn_some_kernel<2>), dim3((c.f + 31) / 32), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -373,6 +373,9 @@ struct FfnArgs {                        // out[m][n] = sum over k of the two sid
   int m_tiles, n_tiles, splits;
   int tile_m, m_parts;                  // rows of an m tile; parts of the m tiles that XCDs share out
 };
+enum FfnKernel { kFfnFew = 16, kFfnSome64 = 64, kFfnSome128 = 65, kFfnTiles128 = 128, kFfnTiles256 = 256 };   // (spec_k_ffn_gated_plan's numbers)
+struct FfnPlans { FfnKernel forward, again, dx; int dx_ranges; FfnKernel dw; int dw_ranges; bool together; };
+FfnPlans ffn_plans(int rows, int d, int f);
 uint64_t ffn_grad_scratch_bytes(int rows, int d, int f);
 hipError_t launch_ffn(const FfnCall &c, hipStream_t st);
 hipError_t launch_ffn_grad(const FfnCall &c, void *scratch, hipStream_t st);

@@ -892,3 +892,18 @@ def test_ffn_gated_activations_to_a_few_units(P, act):
         low, high = (torch.from_numpy(y + s * error).float().bfloat16().cuda() for s in (-1, 1))
         bad = ~((low <= got) & (got <= high))
         assert not bool(bad.any()), (which, int(bad.sum()), f, gates[bad.cpu().numpy()][:5], got[bad][:5], y[bad.cpu().numpy()][:5])
+
+
+@pytest.mark.parametrize("rows,d,f", [(33, 72, 16392), (60, 136, 16392), (128, 72, 16456), (1000, 4088, 200), (1024, 4096, 264), (1025, 4088, 296), (515, 4088, 504), (601, 2040, 1016), (2048, 2048, 328),
+                                      (200, 1032, 2056), (130, 3000, 3000)])
+def test_ffn_gated_every_plan(P, rows, d, f):
+    """What the sizes above leave out (tests/test_step_host.py holds each of these to its plan): large tiles whose k is cut into ranges, for dx and for the weights' gradients, whole and ragged; forward calls of
+    33 to 128 rows whose columns fill the chip with one short tile; gradients of the weights that large tiles form alone and small ones beside dx, with the same bits."""
+    x, wg, wu, dh = ffn_case(rows + f, rows, d, f)
+    within(P.spec_k_ffn_gated(x, wg, wu), *ffn_want(x, wg, wu, "silu")[0])
+    got = P.spec_k_ffn_gated_grad(x, wg, wu, dh)
+    for o, (want, tol) in zip(got, ffn_want(x, wg, wu, "silu", dh)):
+        within(o, want, tol)
+    assert all(torch.equal(a, b) for a, b in zip(P.spec_k_ffn_gated_grad(x, wg, wu, dh), got))
+    assert torch.equal(P.spec_k_ffn_gated_grad(x, wg, wu, dh, want=(True, False))[0], got[0])
+    assert all(torch.equal(a, b) for a, b in zip(P.spec_k_ffn_gated_grad(x, wg, wu, dh, want=(False, True))[1:], got[1:]))

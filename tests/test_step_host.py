@@ -171,3 +171,26 @@ def test_grad_sums_and_norm_lie_apart_from_the_gradients(P):
     for norm in (8 * X + 4, 8 * X + 8188):                                # a norm inside the sums
         refused(P.lib.spec_k_grad_clip(1, parts(far), 8 * X, 1.0, norm, None))
         refused(P.lib.spec_k_grad_clip(0, None, 8 * X, 1.0, norm, None))
+
+
+# Sizes that the GPU tests run, and what takes them: (forward; again; dx, its ranges; the weights' gradients, their ranges; together).  A change of the plan has to find other sizes for what they no longer reach.
+FFN_PLANS = {(1, 4096, 136): (16, 128, 128, 1, 128, 1, 1), (16, 136, 40): (16, 128, 128, 1, 128, 1, 1), (17, 256, 128): (64, 128, 128, 1, 128, 1, 1), (60, 4096, 72): (64, 128, 128, 1, 128, 1, 1),
+             (100, 1000, 136): (65, 128, 128, 1, 128, 1, 1), (72, 4200, 4104): (65, 128, 128, 12, 256, 1, 0), (129, 136, 520): (128, 128, 128, 4, 128, 1, 1), (300, 200, 1000): (128, 128, 128, 8, 128, 1, 1),
+             (777, 1000, 344): (128, 128, 128, 3, 128, 3, 1), (2100, 72, 4200): (256, 256, 128, 2, 128, 1, 1), (8200, 40, 264): (256, 256, 128, 1, 128, 8, 1), (4200, 4104, 72): (128, 128, 256, 1, 128, 7, 0),
+             (130, 3000, 3000): (128, 128, 128, 10, 256, 1, 0), (200, 1032, 2056): (128, 128, 128, 8, 256, 1, 1),
+             # from here on test_ffn_gated_every_plan: one short tile of 256 columns' width, products of large tiles cut into ranges
+             (33, 72, 16392): (256, 256, 128, 16, 256, 1, 1), (60, 136, 16392): (256, 256, 128, 16, 256, 1, 1), (128, 72, 16456): (256, 256, 128, 16, 256, 1, 1),
+             (1000, 4088, 200): (128, 128, 256, 2, 128, 4, 0), (1024, 4096, 264): (128, 128, 256, 2, 256, 2, 0), (1025, 4088, 296): (128, 128, 256, 1, 256, 2, 0), (515, 4088, 504): (128, 128, 128, 1, 256, 2, 1),
+             (601, 2040, 1016): (128, 128, 128, 2, 256, 2, 1), (2048, 2048, 328): (128, 128, 256, 2, 128, 5, 0)}
+
+
+def test_ffn_gated_plan(P):
+    for size, plan in FFN_PLANS.items():
+        assert P.spec_k_ffn_gated_plan(*size) == plan
+        rows, d, f = size
+        parts = [0 if n == 1 else 4 * n * m for n, m in ((plan[3], rows * d), (plan[5], 2 * f * d))]
+        assert P.spec_k_ffn_gated_grad_scratch_bytes(*size) == sum(-(-b // 256) * 256 for b in (2 * rows * f, 2 * rows * f, *parts))
+    for bad in ((0, 64, 64), (64, 60, 64), (64, 64, 4), ((1 << 20) + 1, 64, 64), (1 << 20, 1 << 17, 8), (2 ** 32 + 8, 8, 8), (8, 2 ** 32 + 8, 8)):
+        with pytest.raises(P.SpecError):
+            P.spec_k_ffn_gated_plan(*bad)
+    assert P.lib.spec_k_ffn_gated_plan(8, 8, 8, None, None, None, None, None, None, None) == -1
