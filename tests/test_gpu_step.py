@@ -907,3 +907,28 @@ def test_ffn_gated_every_plan(P, rows, d, f):
     assert all(torch.equal(a, b) for a, b in zip(P.spec_k_ffn_gated_grad(x, wg, wu, dh), got))
     assert torch.equal(P.spec_k_ffn_gated_grad(x, wg, wu, dh, want=(True, False))[0], got[0])
     assert all(torch.equal(a, b) for a, b in zip(P.spec_k_ffn_gated_grad(x, wg, wu, dh, want=(False, True))[1:], got[1:]))
+
+
+def test_weights_gradients_beyond_31_bits(P):
+    """Gradients of weights whose only rows with a gradient lie beyond 2^31 elements: those rows' own, with their bounds (what is added for the others is zero)."""
+    x, wg, wu, dh = ffn_case(5, 64, 64, 4104)
+    rows = 1 << 19                                                       # 2^31.003 elements of dh, dg and du
+    back = ffn_want(x, wg, wu, "silu", dh)
+    late = torch.zeros(rows, 4104, dtype=torch.bfloat16, device="cuda")
+    late[-64:] = dh
+    dx, dwg, dwu = P.spec_k_ffn_gated_grad(x.repeat(rows // 64, 1), wg, wu, late)
+    for got, (want, tol) in zip((dx[-64:], dwg, dwu), back):
+        within(got, want, tol)
+    assert not dx[:-64].any()
+    del dx, dwg, dwu, late
+    x, dy, w = rand(3, 64, 64, 128).bfloat16().cuda(), rand(4, 64, 64, 128).bfloat16().cuda(), rand(5, 128).cuda()
+    rows = 64 * 4200                                                     # 2^31.04 elements
+    many, late = x.repeat(4200, 1, 1), torch.zeros(rows, 64, 128, dtype=torch.bfloat16, device="cuda")
+    late[-64:] = dy
+    plan = P.spec_rotary_plan(128, 1e4)
+    f, m = L.rope_frequencies(128, 1e4)
+    (dx,), (dw,) = P.spec_k_headnorm_rotary_grad(plan, [late], [many], 0, [w], outs=[late])
+    want, tol, want_w, tol_w = grad_bound(f64(dy), f64(x), f64(w), 1e-6, 0.0, np.arange(rows - 64, rows), f, m, 128, "half", torch.bfloat16)
+    close(dx[-64:], want, tol)
+    close(dw, want_w, tol_w)
+    assert not dx[:-64].any()
