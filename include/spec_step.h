@@ -38,7 +38,8 @@ int spec_k_embed(int32_t dtype, const void *table, int64_t ldt, int32_t vocab, i
  * for every v (zeros where there is none).  accumulate != 0: dtable[v] += that, and rows
  * without a token are neither read nor written.  Rows whose tok is not in 0 .. vocab-1 have no part in it, whatever they hold.
  * dy [rows, d] in dtype, row stride ldy; dtable [vocab, d] in out_dtype, row stride ldt;
- * sums in fp32 in an order that depends on tok alone.  1 <= rows <= 2^20, the rest as
+ * sums in fp32 in an order that depends on tok alone: up to 31 rows of a token in the order of their positions; more are added in groups that
+ * depend on the other tokens too, so that such a row's last bits may change with them.  1 <= rows <= 2^20, the rest as
  * above.  scratch: spec_k_embed_grad_scratch_bytes (host only; 0 for bad sizes), 256-byte
  * aligned; dtable overlaps none of the others. */
 uint64_t spec_k_embed_grad_scratch_bytes(int32_t rows, int32_t vocab, int32_t d);

@@ -932,3 +932,18 @@ def test_weights_gradients_beyond_31_bits(P):
     close(dx[-64:], want, tol)
     close(dw, want_w, tol_w)
     assert not dx[:-64].any()
+
+
+@pytest.mark.parametrize("rows,repeats", [(31, 1), (31, 4), (7, 100)])
+def test_embed_grad_walks_few_rows_of_a_token_in_their_order(P, rows, repeats):
+    """Up to 31 rows of a token are added one after the other in the order of their positions, whatever other tokens lie between, before and behind them: the bits of that walk in fp32.  (From 32 rows on, rows
+    that share an aligned run of 32 sorted positions are added first, so that the other tokens' number decides which those are.)"""
+    vocab = 3 * repeats
+    tok = torch.arange(vocab, dtype=torch.int32).repeat(rows)[torch.from_numpy(np.random.default_rng(repeats).permutation(vocab * rows))].cuda()
+    dy = rand(rows, vocab * rows, 8).cuda()
+    got = P.spec_k_embed_grad(dy, tok, vocab)
+    by_token = dy[torch.argsort(tok, stable=True)].view(vocab, rows, 8)
+    s = torch.zeros(vocab, 8, device="cuda")
+    for r in range(rows):
+        s = s + by_token[:, r]
+    assert torch.equal(got, s)
