@@ -947,3 +947,39 @@ def test_embed_grad_walks_few_rows_of_a_token_in_their_order(P, rows, repeats):
     for r in range(rows):
         s = s + by_token[:, r]
     assert torch.equal(got, s)
+
+
+@pytest.mark.parametrize("rows,f", [(200, 264), (60, 1032)])
+def test_a_training_step_link_by_link(P, rows, f):
+    """Every call of the step against 64 bits of what the call before it has left, within the bounds of a single call (the step as a whole has room for nine roundings on end)."""
+    s = step_state(4, rows=rows, f=f)
+    heads, hd, d, vocab, tok = s["heads"], s["hd"], s["d"], s["vocab"], s["tok"].cpu().numpy()
+    plan = P.spec_rotary_plan(hd, 1e4)
+    freq, m = L.rope_frequencies(hd, 1e4)
+    e = P.spec_k_embed(s["table"], s["tok"], scale=0.7)
+    want = O.embed(f64(s["table"]), tok, np.float32(0.7))
+    close(e, want, np.abs(want) * (U32 + 1.01 * U16) + 1e-40)
+    e = e.view(rows, heads, hd)
+    at = 3 + np.arange(rows)
+    x = P.spec_k_headnorm_rotary(plan, [e], 3, [s["w"]])[0]
+    close(x, *norm_bound(f64(e), f64(s["w"]), 1e-6, 0.0, at, freq, m, hd, "half", torch.bfloat16))
+    x = x.view(rows, d)
+    within(P.spec_k_ffn_gated(x, s["wg"], s["wu"]), *ffn_want(x, s["wg"], s["wu"], "silu")[0])
+    dx, dwg, dwu = P.spec_k_ffn_gated_grad(x, s["wg"], s["wu"], s["dh"])
+    for o, (want, tol) in zip((dx, dwg, dwu), ffn_want(x, s["wg"], s["wu"], "silu", s["dh"])):
+        within(o, want, tol)
+    dx = dx.view(rows, heads, hd)
+    (de,), (dw,) = P.spec_k_headnorm_rotary_grad(plan, [dx], [e], 3, [s["w"]])
+    want, tol, want_w, tol_w = grad_bound(f64(dx), f64(e), f64(s["w"]), 1e-6, 0.0, at, freq, m, hd, "half", torch.bfloat16)
+    close(de, want, tol)
+    close(dw, want_w, tol_w)
+    dt = check_embed_grad(P, de.view(rows, d), s["tok"], vocab, 0.7, torch.float32)
+    grads = [dt, dw, dwg, dwu]
+    check_clip(P, grads, 0.5, [torch.empty(t.shape, dtype=torch.float32, device="cuda") for t in grads])
+    assert all(torch.equal(a, b) for a, b in zip(train_step(P, plan, s)[2:], clipped(P, grads)))
+
+
+def clipped(P, grads):
+    outs = [torch.empty(t.shape, dtype=torch.float32, device="cuda") for t in grads]
+    P.spec_k_grad_clip(grads, P.spec_k_grad_sums(grads), 0.5, outs=outs)
+    return outs
