@@ -983,3 +983,70 @@ def clipped(P, grads):
     outs = [torch.empty(t.shape, dtype=torch.float32, device="cuda") for t in grads]
     P.spec_k_grad_clip(grads, P.spec_k_grad_sums(grads), 0.5, outs=outs)
     return outs
+
+
+def test_a_layer_with_norms_of_heads(P):
+    """The calls in a layer that has norms of q and k and a table of its own (plain products and attention between them, in fp32 and rounded to bf16), forward and back, against the derivative in 64 bits.
+    Between an input and a gradient lie at most 20 roundings to bf16 (ten tensors forward, ten back), each of at most u16 of a value, and the maps between them stretch no direction by more than twice at these
+    inputs' sizes: 40 u16 in the Frobenius norm, and as much again for the common norm that the gradients are divided by."""
+    g = torch.Generator(device="cuda").manual_seed(11)
+    rows, vocab, hq, hkv, hd, f, first = 96, 150, 4, 2, 64, 200, 5
+    d = hq * hd
+
+    def randn(*shape, scale=1.0):
+        return (torch.randn(*shape, generator=g, device="cuda") * scale).bfloat16()
+    table, w_qkv, w_o = randn(vocab, d), randn((hq + 2 * hkv) * hd, d, scale=d ** -0.5), randn(d, hq * hd, scale=d ** -0.5)
+    w_gate, w_up, w_down = randn(f, d, scale=d ** -0.5), randn(f, d, scale=d ** -0.5), randn(d, f, scale=f ** -0.5)
+    wq, wk = ((1 + 0.2 * torch.randn(hd, generator=g, device="cuda")).bfloat16() for _ in range(2))
+    tok, dy = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32), randn(rows, d)
+    plan = P.spec_rotary_plan(hd, 1e4)
+    unseen = torch.full((rows, rows), float("-inf"), device="cuda").triu(1)
+
+    def attention(q, k, v):
+        q, k, v = q.transpose(0, 1), *(t.repeat_interleave(hq // hkv, 1).transpose(0, 1) for t in (k, v))
+        p = torch.softmax(torch.matmul(q, k.transpose(1, 2).contiguous()) * hd ** -0.5 + unseen.to(q.dtype), -1)
+        return torch.matmul(p, v.contiguous()).transpose(0, 1).reshape(rows, d)
+
+    def mm(a, b):
+        return torch.mm(a.float(), b.float()).bfloat16()
+    e = P.spec_k_embed(table, tok)
+    q, k, v = (t.unflatten(1, (-1, hd)) for t in mm(e, w_qkv.t()).split([hq * hd, hkv * hd, hkv * hd], 1))
+    qo, ko, vo = P.spec_k_headnorm_rotary(plan, [q, k, v], first, [wq, wk, None], turned=[True, True, False])
+    heads = [t.float().requires_grad_() for t in (qo, ko, vo)]
+    att = attention(*heads)
+    x = e + mm(att.detach(), w_o.t())
+    h = P.spec_k_ffn_gated(x, w_gate, w_up, act="silu")
+    y = x + mm(h, w_down.t())
+    dw_down = mm(dy.t(), h)
+    dx, dw_gate, dw_up = P.spec_k_ffn_gated_grad(x, w_gate, w_up, mm(dy, w_down), act="silu")
+    dx = dx + dy
+    dw_o = mm(dx.t(), att.detach())
+    back = [t.bfloat16() for t in torch.autograd.grad(att, heads, mm(dx, w_o).float())]
+    (dq, dk, dv), (dwq, dwk, none) = P.spec_k_headnorm_rotary_grad(plan, back, [q, k, None], first, [wq, wk, None], turned=[True, True, False])
+    dqkv = torch.cat([t.flatten(1) for t in (dq, dk, dv)], 1)
+    de = dx + mm(dqkv, w_qkv)
+    dtable = P.spec_k_embed_grad(de, tok, vocab, out_dtype=torch.float32)
+    grads = [dtable, mm(dqkv.t(), e), dwq, dwk, dw_o, dw_gate, dw_up, dw_down]
+    norm = P.spec_k_grad_clip(grads, P.spec_k_grad_sums(grads), 0.5)
+    assert none is None
+
+    freq, _ = L.rope_frequencies(hd, 1e4)
+    leaves = [t.double().requires_grad_() for t in (table, w_qkv, wq, wk, w_o, w_gate, w_up, w_down)]
+    table, w_qkv, wq, wk, w_o, w_gate, w_up, w_down = leaves
+    angle = (first + torch.arange(rows, device="cuda", dtype=torch.float64))[:, None, None] * torch.from_numpy(freq).cuda()
+
+    def turned(z, w):
+        z = z / torch.sqrt((z * z).mean(-1, keepdim=True) + 1e-6) * w
+        a, b = z[..., :hd // 2], z[..., hd // 2:]
+        return torch.cat([a * torch.cos(angle) - b * torch.sin(angle), b * torch.cos(angle) + a * torch.sin(angle)], -1)
+    e = table[tok.long()]
+    q, k, v = (t.unflatten(1, (-1, hd)) for t in (e @ w_qkv.t()).split([hq * hd, hkv * hd, hkv * hd], 1))
+    x = e + attention(turned(q, wq), turned(k, wk), v) @ w_o.t()
+    gate = x @ w_gate.t()
+    want = x + (gate * torch.sigmoid(gate) * (x @ w_up.t())) @ w_down.t()
+    exact = torch.autograd.grad((want * dy.double()).sum(), leaves)
+    total = torch.sqrt(sum((t * t).sum() for t in exact))
+    assert float(((y.double() - want).norm() / want.norm()).detach()) <= 20 * U16 and abs(float(norm / total) - 1) <= 40 * U16
+    for got, t in zip(grads, exact):
+        t = t * (0.5 / total)
+        assert float((got.double() - t).norm() / t.norm()) <= 80 * U16
