@@ -1,9 +1,11 @@
 /*
- * libspec, operators of a training step around the kernels of spec_train.h (of use
- * at decoding time too, as said at each): the embedding lookup and the gradient of
- * its table, norms of the heads of q and k in the pass of their rotary embedding,
- * the gated half of a feed-forward block, and the clipping of all gradients
- * together.  Same conventions as spec_layer8.h: all data pointers are DEVICE
+ * libspec, operators of a training step that the kernels of spec_train.h leave to the
+ * caller (of use at decoding time too, as said at each): the gated half of a
+ * feed-forward block (its down projection is a plain product, and not here), the
+ * clipping of all gradients together, the embedding lookup with the gradient of its
+ * table (for models that train their own: a draft layer as spec.h has it shares the
+ * target's), and norms of the heads of q and k in the pass of their rotary embedding
+ * (for models that have such norms: the five of spec.h have none).  Same conventions as spec_layer8.h: all data pointers are DEVICE
  * pointers unless a comment says "host", calls enqueue on `stream` (a hipStream_t,
  * NULL = default stream, of the CURRENT device) and return without waiting; no call
  * allocates device memory or keeps anything for the next; SPEC_OK, or SPEC_EINVAL
@@ -69,7 +71,7 @@ int spec_k_headnorm_rotary(const spec_rotary_plan *plan /* host */, int32_t n_pa
  *     dw = sum over rows and heads of dz x r,
  * w NULL: dx = dz.  A part's p.x is dy in p.dtype, p.out is dx in p.out_dtype (p.x = p.out: in place, as
  * in spec_k_rotary); x, in x_dtype, is the call's input, head h of row r at r * ld + h * hs; it may
- * be NULL where w is.  dw: fp32 [hd], or NULL.  No dx overlaps any x.  scratch:
+ * be NULL where w is.  dw: fp32 [hd], or NULL; summed in fp32 in an order that depends on the sizes alone.  No dx overlaps any x.  scratch:
  * spec_k_headnorm_rotary_grad_scratch_bytes (host only), 256-byte aligned; it
  * may be NULL if no part has a dw. */
 typedef struct spec_headnorm_grad_part {

@@ -1,12 +1,14 @@
 // Rows of an embedding table, and the gradient of the table (include/spec_step.h).
 //
 // The gradient sums rows of dy by token.  The positions are sorted by (token, position), so that a table row's sum is a walk over neighbours and its order is
-// fixed: in tiles of kTile positions a position's place is the number of smaller ones (counted, kTile comparisons for each); over several tiles four sorted runs at a time become one,
-// a position's place being that in its own run plus those that searches find in the other three.  Padding sorts behind the vocabulary and is never read.
+// fixed: in tiles of kTile positions a position's place is the number of smaller ones (counted, kTile comparisons for each); over several
+// tiles four sorted runs at a time become one, a position's place being that in its own run plus those that searches find in the other
+// three.  Padding sorts behind the vocabulary and is never read.
 // Tokens that occur often (padding apart, the most frequent word is a tenth of a text) would keep one workgroup busy long after the others: aligned runs of 32
 // and of 1024 sorted positions that hold one token are summed first, by workgroups of their own, and the walk takes a run's sum where it meets one.
-// Bound: memory (dy once in, the table once out).  Measured: 16384 rows into 128256 x 4096 in bf16: places 9 us, joined 5, runs 9 and 5, table 183 (6.3 TB/s).  2^20 rows into 2000 x 64: places 266, joined
-// 4 times 30, of 475 in all.
+// Bound: memory (dy once in, the table once out).  Measured: 16384 rows into 128256 x 4096 in bf16: places 9 us, joined 5, runs 9 and 5,
+// table 184 (6.4 TB/s).  2^20 rows into 2000 x 64: places 266, joined 4 times 30, of 475 in all.  The lookup of 16384 rows of that table
+// 33.5 us in bf16 and 85 in fp32 (4.0 and 3.2 TB/s by the rows written alone).
 #include "common.h"
 #include "elements.h"
 #include "kernels.h"
@@ -21,12 +23,13 @@ constexpr int kTile = 4096, kRun = 32, kRuns = 1024;          // positions of a 
 constexpr int kLongLeast = 8192;                              // positions from which on the longer runs are summed (below, a walk meets 256 sums at most)
 constexpr int kEmbedThreads = 256;
 
-// Eight columns of a row, at any alignment of their type (the memory takes unaligned accesses of 16 bytes; a column at a time took 130 us where they take 58: the gradient of a 60000 x 2001
-// table in bf16), or the n that are left at its end.
+// Eight columns of a row, at any alignment of their type (the memory takes unaligned accesses of 16 bytes; a column at a time took 130 us
+// where they take 58: the gradient of a 60000 x 2001 table in bf16), or the n that are left at its end.
 typedef u32x4_t u32x4_any __attribute__((aligned(2)));
 typedef f32x4_t f32x4_any __attribute__((aligned(4)));
 struct Columns { float x[8]; };
-template <bool WHOLE> __device__ __forceinline__ Columns load_columns(const void *p, int64_t i, int n, bool bf16) {   // WHOLE: n >= 8 (asked at each load, every load waited for the one before)
+// WHOLE: n >= 8 (asked at each load, every load waited for the one before)
+template <bool WHOLE> __device__ __forceinline__ Columns load_columns(const void *p, int64_t i, int n, bool bf16) {
   Columns r;
   if constexpr (WHOLE) {
     Eight e;
@@ -137,8 +140,9 @@ __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(const int *tok
   order[tile + place] = tile + me;
 }
 
-// Runs of `run` sorted positions, kWays at a time, to one each: the place of each among them.  A search looks at kProbes places at once, and the searches in all other runs go side by side:
-// a step is one trip to memory.  (16384 positions 4.8 us, one tile after the other through the LDS 6, the other three in the LDS at once 6.4; 2^20 120 against 850.)
+// Runs of `run` sorted positions, kWays at a time, to one each: the place of each among them.  A search looks at kProbes places at once,
+// and the searches in all other runs go side by side: a step is one trip to memory.  (16384 positions 4.8 us, one tile after the other
+// through the LDS 6, the other three in the LDS at once 6.4; 2^20 120 against 850.)
 constexpr int kWays = 4, kProbes = 3, kMergeThreads = 256;
 __global__ __launch_bounds__(kMergeThreads) void embed_merge_kernel(const int *from_keys, const int *from_order, int rows, int run, int *keys, int *order) {
   const int i = blockIdx.x * kMergeThreads + threadIdx.x;
@@ -196,8 +200,8 @@ __device__ __forceinline__ int keys_below(const int *keys, int rows, int v) {
   return lo;
 }
 
-// The first sorted position of every token (starts[vocab]: where padding begins; a workgroup has 256 tokens, whose share of the keys two of its wavefronts look up first), and the runs of 32.
-// BF16: dy's type (asked at each load, every load waited for the one before).
+// The first sorted position of every token (starts[vocab]: where padding begins; a workgroup has 256 tokens, whose share of the keys two
+// of its wavefronts look up first), and the runs of 32.  BF16: dy's type (asked at each load, every load waited for the one before).
 template <bool BF16>
 __global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(EmbedGradArgs a, const int *keys, const int *order, int *starts, int start_groups, float *runs) {
   __shared__ int range[2];
@@ -335,10 +339,11 @@ template <bool BF16> hipError_t embed_sums(const EmbedGradArgs &a, const EmbedSc
     hipLaunchKernelGGL(embed_long_runs_kernel, dim3(a.rows / kRuns, wide > 64 ? 64 : wide), dim3(kEmbedThreads), 0, st, keys, a.vocab, a.d, runs, long_runs);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  // Rows at once pay where most have tokens (16384 rows into 1000 x 256 44 -> 28 us, 65536 into 2000 x 256 88 -> 53); one after the other they keep their places in scalar registers (8192 into
-  // 128256 x 512 46 us, at once 49).
+  // Rows at once pay where most have tokens (16384 rows into 1000 x 256 44 -> 28 us, 65536 into 2000 x 256 88 -> 53); one after the
+  // other they keep their places in scalar registers (8192 into 128256 x 512 46 us, at once 49).
   const bool split = a.d <= kEmbedThreads * 4 && a.rows >= a.vocab / 4;
-  hipLaunchKernelGGL((split ? embed_table_kernel<BF16, true> : embed_table_kernel<BF16, false>), dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
+  const auto table = split ? embed_table_kernel<BF16, true> : embed_table_kernel<BF16, false>;
+  hipLaunchKernelGGL(table, dim3((a.vocab + kTableRows - 1) / kTableRows, ys), dim3(kEmbedThreads), 0, st, a, order, starts, runs, long_runs);
   return hipGetLastError();
 }
 

@@ -1,14 +1,19 @@
 // The gated half of a feed-forward block, h = act(x Wg^T) * (x Wu^T), and its gradients (include/spec_step.h).
 //
-// Products of matrices as they lie in memory (weights change with every step of a training run, so that nothing is packed ahead): out[m][n] = sum over k of A(m, k) B(n, k),
-// either side with k along its rows (x, the weights of the forward products) or with k across them (both sides of the weights' gradients, the weights of dx).
+// Products of matrices as they lie in memory (weights change with every step of a training run, so that nothing is packed ahead):
+// out[m][n] = sum over k of A(m, k) B(n, k), either side with k along its rows (x, the weights of the forward products) or with k
+// across them (both sides of the weights' gradients, the weights of dx).
 //   forward    : m = rows of x, n = columns of h; a workgroup's n are gate and up rows of the same columns, so that a lane holds both sums of an element of h
-//   dg and du  : the same sums again, then dg = dh u act'(g), du = dh act(g), rounded to bf16 for the products that follow
+//   dg and du  : the same sums again, then dg = dh u act'(g), du = dh act(g), rounded to bf16 for the products that follow (the
+//                matrix instruction takes both sides in one type: the gradients are 2.35e-3 of their norm off where their own
+//                rounding alone is 1.66e-3; as sums of two bf16 each they would cost 20 instead of 12 rows * d * f operations)
 //   dx         : dg Wg + du Wu, k = the columns of dg and then those of du
 //   dWg, dWu   : dg^T x, du^T x, k = rows of x
-// Bound: the matrix cores, under the power they take, from some hundreds of rows on; below, the weights' way from memory.  Measured (4096 rows, 4096 x 11008): forward 523 us alone (1.41 PFLOP/s; matrix
-// cores 74 % busy at the 1.7 GHz that they leave), dg and du 572, dx 594 (58 % at 1.95), dWg and dWu 594 (62 % at 1.97).  With all copies out of the L2: 517, and 3 % less for the gradients' products; without the wait for the
-// m side's copies: the same.  One row 27.9 us (6.5 TB/s of weights).
+// Bound: the matrix cores, under the power they take, from some hundreds of rows on; below, the weights' way from memory.
+// Measured (4096 rows, 4096 x 11008): forward 545 us (1.36 PFLOP/s; matrix cores 74 % busy at the 1.7 GHz that they leave; 607 in
+// thirty launches on end, as the clock falls), dg and du 584, dx 630 (58 % at 1.95), dWg and dWu 606 (62 % at 1.97).  With all copies
+// out of the L2 1 % less for the forward call and 3 % for the gradients' products; without the wait for the m side's copies the same.
+// One row 28.0 us (6.4 TB/s of weights).
 #include "common.h"
 #include "kernels.h"
 
@@ -44,10 +49,11 @@ template <bool SLOPE> __device__ __forceinline__ Act activation(int act, float g
 // Stages of 64 k in the LDS, copied there straight from memory, 16 bytes a lane and 1 KB a wavefront's instruction.
 // K along the rows (MAJOR = false): a row's 128 bytes, their eight pieces permuted by row / 2 so that sixteen rows' reads of one piece touch all banks.  K across
 // (MAJOR = true): per k the tile's columns, their chunks of 16 permuted by k so that the eight k of half a transposing read touch all banks.
-// Products of 16 x 16 x 32: from registers alone they run at 2.00 PFLOP/s on normally distributed data where those of 32 x 32 x 16, which move their sums twice as often,
-// run at 1.78 (what limits both is the power).
+// Products of 16 x 16 x 32: from registers alone they run at 2.00 PFLOP/s on normally distributed data where those of 32 x 32 x 16,
+// which move their sums twice as often, run at 1.78 (what limits both is the power).
 constexpr int kStageK = 64;
-constexpr int kOnce = 2;                                      // loads marked nontemporal: of weights that nobody reads again (one row of 4096 x 11008 32.4 -> 30.1 us, of 8192 x 28672 159 -> 145)
+// Loads marked nontemporal: of weights that nobody reads again (one row of 4096 x 11008 32.4 -> 30.1 us, of 8192 x 28672 159 -> 145)
+constexpr int kOnce = 2;
 template <int TW_, int MB_, int WQ_, int NB_> struct Tile {   // wavefronts and 16-blocks of each along m and n
   static constexpr int TW = TW_, MB = MB_, WQ = WQ_, NB = NB_;
   static constexpr int kWaves = TW * WQ, kThreads = kWaves * 64, kM = TW * MB * 16, kN = WQ * NB * 16;
@@ -63,8 +69,8 @@ __device__ __forceinline__ void wg_barrier() {                 // (without a wai
 // Which 16 columns of a row of k (MAJOR) stand where: chunk ^ chunk_turn(k)
 __device__ __forceinline__ int chunk_turn(int k) { return (k & 3) | ((k >> 1) & 4); }
 
-// One side of a tile: LOADS copies of this wavefront per stage.  The buffer ends with the matrix: what lies behind it (rows past the last, k past the end in the last row) is not
-// accessed; rows and columns past the tile's are never used, and k past the end is cleared.
+// One side of a tile: LOADS copies of this wavefront per stage.  The buffer ends with the matrix: what lies behind it (rows past the
+// last, k past the end in the last row) is not accessed; rows and columns past the tile's are never used, and k past the end is cleared.
 template <int LOADS, bool MAJOR, int COLS> struct Side {
   const char *base, *end;                                     // of the segment: the tile's first row (column, if MAJOR), and the matrix's end
   uint32_t off[LOADS];                                        // of a lane
@@ -118,7 +124,8 @@ template <bool MAJOR, int COLS> __device__ __forceinline__ u32x4_t frag(const un
   return u32x4_t{a.x, a.y, b.x, b.y};
 }
 
-// Four bf16 of block a (columns 4 q ..) and of block b in each of the lanes 16 q + r, to eight consecutive columns a lane: those from 8 (q / 2) on of block a (q even) or b
+// Four bf16 of block a (columns 4 q ..) and of block b in each of the lanes 16 q + r, to eight consecutive columns a lane: those from
+// 8 (q / 2) on of block a (q even) or b
 __device__ __forceinline__ u32x4_t gather8(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
   const auto x = __builtin_amdgcn_permlane16_swap(a0, b0, false, false), y = __builtin_amdgcn_permlane16_swap(a1, b1, false, false);
   return u32x4_t{x[0], y[0], x[1], y[1]};
@@ -274,8 +281,8 @@ __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, in
     for (int t = 0; t < MB; t++) acc[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const int mat_ = frag_lane<MM, L::kM>(lane, th * MB), nat_ = frag_lane<NM, L::kN>(lane, wq * NB);
   // A step is the products of 32 k, block by block of m.  Behind block t's products block t + 3 (of this step or the next) is read, three blocks
-  // ahead of its turn; the next step's blocks of n are read behind the last products of this one.  `last`: the step ends its stage, and what follows is read from the next one, after the barrier
-  // that is behind the stage's last read.
+  // ahead of its turn; the next step's blocks of n are read behind the last products of this one.  `last`: the step ends its stage, and what
+  // follows is read from the next one, after the barrier that is behind the stage's last read.
   u32x4_t fm[4], fn[2][NB];
   constexpr int kBarrier = MB - 4, kEach = (NB + 1) / 2;
   static_assert(MB % 4 == 0 && MB >= NL, "a ring of four blocks, a copy of the n side behind each");
@@ -346,8 +353,9 @@ __device__ __forceinline__ void tile_body(const FfnArgs &a, int half, int m0, in
   finish<MB, NB, TO>(a, acc, m0 + th * MB * 16, n0 + wq * NB * (kGated ? 8 : 16), half, part);
 }
 
-// The tile of a workgroup.  Ids 8 apart run on one XCD.  The XCDs share the tiles out in m_parts x 8 / m_parts: XCD x has the m tiles x % m_parts, + m_parts, .. and the n
-// tiles x / m_parts, + 8 / m_parts, .., and walks them four n tiles at a time, for each m tile those four (32 compute units then read 8 + 4 panels).
+// The tile of a workgroup.  Ids 8 apart run on one XCD.  The XCDs share the tiles out in m_parts x 8 / m_parts: XCD x has the m tiles
+// x % m_parts, + m_parts, .. and the n tiles x / m_parts, + 8 / m_parts, .., and walks them four n tiles at a time, for each m tile those
+// four (32 compute units then read 8 + 4 panels).
 constexpr int kGroup = 4, kXcdUnits = 32;
 struct TilePlace { int m, n, count; };                        // count: tiles of this XCD
 __device__ __forceinline__ TilePlace tile_place(const FfnArgs &a, int id, int j) {
@@ -379,7 +387,8 @@ __global__ __launch_bounds__(L::kThreads, 2) void ffn_tile_kernel(FfnArgs a) {
 using Big = Tile<2, 8, 4, 4>;                                 // 256 x 256
 using Mid = Tile<2, 4, 4, 4>;                                 // 128 x 256
 using Small = Tile<2, 4, 2, 4>;                               // 128 x 128
-// Tiles of 256 x 256, and halves of 128 x 256 for what an XCD's compute units would be half empty with (up to 16 tiles behind the last whole round) and for ends of m of up to 128 rows.
+// Tiles of 256 x 256, and halves of 128 x 256 for what an XCD's compute units would be half empty with (up to 16 tiles behind the last
+// whole round) and for ends of m of up to 128 rows.
 __host__ __device__ inline int halved_tiles(int count) { return count % kXcdUnits <= kXcdUnits / 2 ? count % kXcdUnits : 0; }
 template <bool MM, bool NM, int TO>
 __global__ __launch_bounds__(Big::kThreads, 2) void ffn_mixed_kernel(FfnArgs a) {
@@ -393,7 +402,8 @@ __global__ __launch_bounds__(Big::kThreads, 2) void ffn_mixed_kernel(FfnArgs a) 
   else tile_at<Mid, MM, NM, TO>(a, p.m, p.n, rows, blockIdx.y, ms0, ms1, ns0, ns1, ns2);
 }
 
-// dx and the weights' gradients of a small call in one launch, where neither fills the chip for long: the workgroups of dx, range of k by range, then those of the others.
+// dx and the weights' gradients of a small call in one launch, where neither fills the chip for long: the workgroups of dx, range of k
+// by range, then those of the others.
 struct FfnBoth { FfnArgs dx, dw; int dx_each, dw_each; };     // ..each: workgroups of a range
 template <int TX, int TW>
 __global__ __launch_bounds__(Small::kThreads, 2) void ffn_both_kernel(FfnBoth b) {
@@ -436,7 +446,8 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(FfnJoin first, FfnJoin se
 // into registers, as many stages ahead.
 constexpr int kFewStage = 4096, kFewRows = 16;
 __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
-  __shared__ __attribute__((aligned(1024))) unsigned char r0[4 * kFewStage], r1[4 * kFewStage], r2[4 * kFewStage];   // (arrays of their own: the compiler waits for the copies into what it reads)
+  // (arrays of their own: the compiler waits for the copies into what it reads)
+  __shared__ __attribute__((aligned(1024))) unsigned char r0[4 * kFewStage], r1[4 * kFewStage], r2[4 * kFewStage];
   __shared__ float sums[4][8][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
   const int n0 = blockIdx.x * 16, stages = (a.k + kStageK - 1) / kStageK;
@@ -531,9 +542,10 @@ __global__ __launch_bounds__(256) void ffn_few_kernel(FfnArgs a) {
 }
 
 // ---- some rows ---------------------------------------------------------------------------------------
-// 17 to 128 rows: still bound by the weights' way from memory, but x has to come through the LDS too (read by every wavefront for itself it took twice the weights' way: 98 us
-// for 60 rows, 4096 x 14336).  A workgroup has all rows and 32 columns of h, so that there are workgroups enough to keep the memory busy (tiles of 64 columns: 66 us); four
-// wavefronts with a quarter of the rows each; a ring of four (three) stages of 64 k, two workgroups to a compute unit.
+// 17 to 128 rows: still bound by the weights' way from memory, but x has to come through the LDS too (read by every wavefront for itself
+// it took twice the weights' way: 98 us for 60 rows, 4096 x 14336).  A workgroup has all rows and 32 columns of h, so that there are
+// workgroups enough to keep the memory busy (tiles of 64 columns: 66 us); four wavefronts with a quarter of the rows each; a ring of
+// four (three) stages of 64 k, two workgroups to a compute unit.
 template <int MB>                                             // blocks of 16 rows of a wavefront
 __global__ __launch_bounds__(256, 2) void ffn_some_kernel(FfnArgs a) {
   constexpr int kRows = MB * 64, NB = 4, ML = MB * 2, NL = 2, kRing = MB == 1 ? 4 : 3, kBytes = (kRows + 64) * 128;
@@ -605,8 +617,8 @@ __global__ __launch_bounds__(256, 2) void ffn_some_kernel(FfnArgs a) {
 
 // Tiles of the fullest XCD where the m tiles are shared out in m_parts
 int64_t fullest(int64_t m_tiles, int64_t n_tiles, int m_parts) { return (m_tiles + m_parts - 1) / m_parts * ((n_tiles + 8 / m_parts - 1) / (8 / m_parts)); }
-// In two parts (m) by four (n), if that is no less even than all n tiles' eighths: of a training step at the 7B widths dx and the weights' gradients are 2 % sooner than with one by
-// eight and the same with four by two, the forward product is the same with each.
+// In two parts (m) by four (n), if that is no less even than all n tiles' eighths: of a training step at the 7B widths dx and the weights'
+// gradients are 2 % sooner than with one by eight and the same with four by two, the forward product is the same with each.
 int parts_of_m(int64_t m_tiles, int64_t n_tiles) { return fullest(m_tiles, n_tiles, 2) <= fullest(m_tiles, n_tiles, 1) ? 2 : 1; }
 
 template <class L, int TO> bool set_tiles(FfnArgs &a) {       // false: more tiles than a grid holds
@@ -627,10 +639,13 @@ template <class L, bool MM, bool NM, int TO> hipError_t launch_tiles(FfnArgs a, 
   return hipGetLastError();
 }
 
-// Which tile, and into how many ranges k is cut (1: not at all): as many as fill the chip once, with halves of the large tile or two workgroups of the small one to a compute unit.
-// Measured (us): dx of 1024 rows, 4096 x 11008 (64 large tiles, 344 stages) in 1, 2, 3, 4, 6 ranges 352, 207, 266, 220, 236, small tiles 277, 215, 234, 222, 237; of 512 rows, 4096 x 14336 (32
-// large tiles) 441, 233, 161, 142, 177, small (128) 346, 186, 162, 142, 156; of 777 rows, 1000 x 2728 (16, 56) 91, 54, 42, 36, 31, small 72, 43, 35, 30, 30, in eight 29.  Forward, large /
-// small: 512 rows of 4096 x 14336 (224 large tiles) 96 / 113, 777 of 1000 x 2728 (88) 19.6 / 20.9, 300 of 4096 x 4096 (64) 42.6 / 40.3, 200 of 8192 x 2000 (16) 74 / 62.
+// Which tile, and into how many ranges k is cut (1: not at all): as many as fill the chip once, with halves of the large tile or two
+// workgroups of the small one to a compute unit.  Measured (us):
+//   dx of 1024 rows, 4096 x 11008 (64 large tiles, 344 stages) in 1, 2, 3, 4, 6 ranges 352, 207, 266, 220, 236, small tiles 277, 215,
+//   234, 222, 237; of 512 rows, 4096 x 14336 (32 large tiles) 441, 233, 161, 142, 177, small (128) 346, 186, 162, 142, 156; of 777 rows,
+//   1000 x 2728 (16, 56) 91, 54, 42, 36, 31, small 72, 43, 35, 30, 30, in eight 29;
+//   forward, large / small: 512 rows of 4096 x 14336 (224 large tiles) 96 / 113, 777 of 1000 x 2728 (88) 19.6 / 20.9, 300 of
+//   4096 x 4096 (64) 42.6 / 40.3, 200 of 8192 x 2000 (16) 74 / 62.
 struct FfnPlan { int tile, splits; };                         // tile 0: 256 x 256 and halves, 1: 128 x 128
 FfnPlan ffn_plan(int64_t m, int64_t n, int64_t k, int halves, int segs, bool gated, bool both = false) {
   auto tiles_m = [&](int t) { const int size = t ? Small::kM : Big::kM; return (m + size - 1) / size * halves; };
@@ -638,7 +653,8 @@ FfnPlan ffn_plan(int64_t m, int64_t n, int64_t k, int halves, int segs, bool gat
   FfnPlan p{tiles_m(0) * tiles_n(0) >= 64 ? 0 : 1, 1};
   if (gated) return p;
   const int64_t m_tiles = tiles_m(p.tile), n_tiles = tiles_n(p.tile), stages = segs * ((k + kStageK - 1) / kStageK);
-  const int64_t ranges = (p.tile == 0 ? kXcdUnits / 2 : both ? kXcdUnits * 3 / 4 : 2 * kXcdUnits) / fullest(m_tiles, n_tiles, parts_of_m(m_tiles, n_tiles)), most = stages / 4 < 16 ? stages / 4 : 16;
+  const int64_t units = p.tile == 0 ? kXcdUnits / 2 : both ? kXcdUnits * 3 / 4 : 2 * kXcdUnits, most = stages / 4 < 16 ? stages / 4 : 16;
+  const int64_t ranges = units / fullest(m_tiles, n_tiles, parts_of_m(m_tiles, n_tiles));
   p.splits = (int)(ranges < most ? ranges : most);
   if (p.splits < 1) p.splits = 1;
   return p;
@@ -660,10 +676,12 @@ template <bool MM, bool NM> hipError_t launch_product(FfnArgs a, bool both, hipS
   const hipError_t e = launch_planned<MM, NM, kToParts>(a, p.tile, st);
   return e != hipSuccess ? e : launch_join(join_of(a), FfnJoin{}, st);
 }
-// dx and the weights' gradients in one launch, if dx takes small tiles and the others are at most two rounds of them (gradients in all, one after the other / together: 777 rows, 1000 x 2728 79 / 68
-// us, 300 of 4096 x 4096 139 / 121, 100 of 1024 x 2752 43 / 36, 4096 of 512 x 1376 91 / 89).  Neither has the chip to itself then, and fewer ranges are written and read again: with ranges for
-// 64 / 32 / 24 / 16 workgroups an XCD 777 rows of 1000 x 2728 take 67.6, 61.7, 60.7, 68.4 us, 512 of 768 x 2048 51.8, 35.0, 36.1, 39.2, 300 of 1024 x 2752 45.0, 43.2, 38.9, 41.8, 4096 of 256 x
-// 688 56.7, 49.4, 44.5, 40.6.  (Calls for one of the two alone keep those ranges, so that a sum's order does not depend on what else is asked for.)
+// dx and the weights' gradients in one launch, if dx takes small tiles and the others are at most two rounds of them (gradients in all,
+// one after the other / together: 777 rows, 1000 x 2728 79 / 68 us, 300 of 4096 x 4096 139 / 121, 100 of 1024 x 2752 43 / 36, 4096 of
+// 512 x 1376 91 / 89).  Neither has the chip to itself then, and fewer ranges are written and read again: with ranges for 64 / 32 / 24 /
+// 16 workgroups an XCD 777 rows of 1000 x 2728 take 67.6, 61.7, 60.7, 68.4 us, 512 of 768 x 2048 51.8, 35.0, 36.1, 39.2, 300 of
+// 1024 x 2752 45.0, 43.2, 38.9, 41.8, 4096 of 256 x 688 56.7, 49.4, 44.5, 40.6.  (Calls for one of the two alone keep those ranges, so
+// that a sum's order does not depend on what else is asked for.)
 bool both_pay(int64_t rows, int64_t d, int64_t f) {
   return ffn_plan(rows, d, f, 1, 2, false).tile == 1 && (f + Small::kM - 1) / Small::kM * 2 * ((d + Small::kN - 1) / Small::kN) <= 1024;
 }
@@ -695,9 +713,10 @@ uint64_t ffn_grad_scratch_bytes(int rows, int d, int f) {
   return 2 * up256((uint64_t)rows * f * 2) + up256(x) + up256(w);
 }
 
-// Which of the three takes a forward call (us; few / some / tiles of 128 x 128): 16 rows of 4096 x 11008 37.8 / 45.6 / 58.2, 24 46.5 / 45.8 / 58.6, 60 74 / 48.9 / 61.4, 128 - / 62.2 / 65.8;
-// of 4096 x 14336 16 48.7 / 52.2 / 60.9, 60 98 / 55.0 / 64.0, 128 - / 66.2 / 68.1; of 1024 x 2752 16 6.1 / 9.7 / 14.1, 60 11.3 / 10.1 / 14.5.  Where the tiles fill the
-// chip by themselves they have less of x to read: 8192 x 28672 16 165 / 174 / 177, 32 208 / 177 / 177, 60 304 / 189 / 176, 128 - / 240 / 178.
+// Which of the three takes a forward call (us; few / some / tiles of 128 x 128): 16 rows of 4096 x 11008 37.8 / 45.6 / 58.2, 24
+// 46.5 / 45.8 / 58.6, 60 74 / 48.9 / 61.4, 128 - / 62.2 / 65.8; of 4096 x 14336 16 48.7 / 52.2 / 60.9, 60 98 / 55.0 / 64.0, 128
+// - / 66.2 / 68.1; of 1024 x 2752 16 6.1 / 9.7 / 14.1, 60 11.3 / 10.1 / 14.5.  Where the tiles fill the chip by themselves they have
+// less of x to read: 8192 x 28672 16 165 / 174 / 177, 32 208 / 177 / 177, 60 304 / 189 / 176, 128 - / 240 / 178.
 static bool some_pays(int rows, int f) { return rows <= 32 || (rows <= 128 && (f + 63) / 64 < 256); }
 static FfnKernel forward_kernel(int rows, int d, int f) {
   if (rows <= kFewRows) return kFfnFew;

@@ -4,8 +4,9 @@
 // the L2) and scale.  A launch takes the addresses of up to kGradTensors tensors as arguments; they are cut into chunks of kGradChunk elements, counted from
 // the 16-byte boundary at or before the tensor's first element, that the workgroups take in turn.  Squares are exact in 64 bits and added up there, so that
 // the norm neither overflows nor depends on the number of elements.
-// Bound: memory.  Measured: 236 M elements, sums 114 us in bf16 (4.1 TB/s, while the outputs of the pass before are still on their way out of the last-level cache; 73 where they are not), 172 in fp32
-// (5.5 TB/s); clipped from bf16 into fp32 274 us (5.2 TB/s), in bf16 155 (6.1).  Half the loads in flight: sums 118, clipped 275.  Stores past the caches: clipped 328.
+// Bound: memory.  Measured: 236 M elements, sums 113 us in bf16 (4.2 TB/s, while the outputs of the pass before are still on their way
+// out of the last-level cache; 73 where they are not), 172 in fp32 (5.5 TB/s); clipped from bf16 into fp32 273 us (5.2 TB/s), in bf16 155
+// (6.1).  Half the loads in flight: sums 118, clipped 275.  Stores past the caches: clipped 328.
 #include "common.h"
 #include "elements.h"
 #include "kernels.h"
