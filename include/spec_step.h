@@ -5,7 +5,7 @@
  * clipping of all gradients together, the embedding lookup with the gradient of its
  * table (for models that train their own: a draft layer as spec.h has it shares the
  * target's), and norms of the heads of q and k in the pass of their rotary embedding
- * (for models that have such norms: the five of spec.h have none).  Same conventions as spec_layer8.h: all data pointers are DEVICE
+ * (for models that have such norms: those of spec.h have none).  Same conventions as spec_layer8.h: all data pointers are DEVICE
  * pointers unless a comment says "host", calls enqueue on `stream` (a hipStream_t,
  * NULL = default stream, of the CURRENT device) and return without waiting; no call
  * allocates device memory or keeps anything for the next; SPEC_OK, or SPEC_EINVAL
@@ -28,7 +28,7 @@ extern "C" {
 #endif
 
 /* ---- embedding ------------------------------------------------------------------
- * out[i] = scale * table[tok[i]], zeros where tok[i] is not in 0 .. vocab-1 (padding).
+ * out[i] = scale * table[tok[i]] (the product in fp32), zeros where tok[i] is not in 0 .. vocab-1 (padding).
  * table [vocab, d] in dtype with row stride ldt >= d, out [rows, d] in out_dtype with
  * row stride ldo >= d (what lies between rows is left alone).  1 <= rows <= 2^24, 1 <=
  * d <= 2^20, 1 <= vocab <= 2^24; pointers aligned to their type (fastest where they, the
@@ -129,7 +129,7 @@ int spec_k_ffn_gated_plan(int32_t rows, int32_t d, int32_t f, int32_t *forward, 
  *   spec_k_grad_sums : g -> sums, SPEC_GRAD_SUMS doubles that add up to norm^2 (squares
  *                      and sums are 64-bit: no gradient in fp32 overflows them).  Processes that each hold a part of the
  *                      gradients add their sums up, element by element, before the next call.
- *   spec_k_grad_clip : out = g * factor, the factor formed in 64 bits and held to 24; norm[0]: the norm in fp32
+ *   spec_k_grad_clip : out = g * factor (the product in fp32), the factor formed in 64 bits and held to 24; norm[0]: the norm in fp32
  *                      (infinite from 2^128 on, which the factor is not; NULL: not wanted).  out may be g (in place, same dtype; nothing is written if the factor is 1); else it
  *                      overlaps no g and no other out.  A norm that is not finite does as the formula says: an infinite one makes finite gradients 0 and infinite
  *                      ones NaN, NaN makes all NaN.
