@@ -5,9 +5,10 @@
  * clipping of all gradients together, the embedding lookup with the gradient of its
  * table (for models that train their own: a draft layer as spec.h has it shares the
  * target's), and norms of the heads of q and k in the pass of their rotary embedding
- * (for models that have such norms: those of spec.h have none).  Same conventions as spec_layer8.h: all data pointers are DEVICE
- * pointers unless a comment says "host", calls enqueue on `stream` (a hipStream_t,
- * NULL = default stream, of the CURRENT device) and return without waiting; no call
+ * (for models that have such norms: those of spec.h have none).  Same conventions as
+ * spec_layer8.h: all data pointers are DEVICE pointers unless a comment says "host",
+ * calls enqueue on `stream` (a hipStream_t, NULL = default stream, of the CURRENT
+ * device) and return without waiting; no call
  * allocates device memory or keeps anything for the next; SPEC_OK, or SPEC_EINVAL
  * (nothing has been launched), or SPEC_EHIP.  dtype is SPEC_DTYPE_FP32 or
  * SPEC_DTYPE_BF16.  Buffers, scratch among them, are borrowed until the kernels have
